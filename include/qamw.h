@@ -59,7 +59,7 @@ enum {
     QAMW_ERR_DEVICE = 4       /* HIP reported an error at launch                          */
 };
 
-enum { QAMW_DTYPE_F32 = 0, QAMW_DTYPE_BF16 = 1 };
+enum { QAMW_DTYPE_F32 = 0, QAMW_DTYPE_BF16 = 1, QAMW_DTYPE_I8 = 2 };   /* I8: where an entry point says so */
 
 enum { QAMW_MAX_BITS = 12, QAMW_MAX_BLOCK = 1024 };
 
@@ -422,6 +422,85 @@ typedef struct qamw_matmul_item {
 } qamw_matmul_item;
 int qamw_matmul_batch(const qamw_matmul_item *items, int n_items, int x_dtype, int m, const float *codebook,
                       int bits, int hadamard_block, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Layers as they are served: products in 8-bit integers, routed experts.
+ * Device entry points with the conventions above.  A call with m = 0 rows is valid and does nothing (qamw_route writes
+ * n_experts + 1 zeros).  Pointers need the alignment of their elements only; rows of whole 16 bytes on 16-byte boundaries
+ * (pointers, leading dimensions, d_in) are served by the fast kernels.  Index arrays are device data and are not read on the
+ * host: an entry out of range makes the rows concerned unspecified, and nothing outside the arrays given is read or written.
+ * ------------------------------------------------------------------------------------------ */
+enum {
+    QAMW_INT8_MAX_ROWS = 1 << 22,      /* rows of a call                                                          */
+    QAMW_INT8_MAX_D_IN = 131056,       /* columns: 2^14 each, sums stay within 32 bits                             */
+    QAMW_PRODUCT_MAX_D_OUT = 1 << 24,
+    QAMW_MAX_EXPERTS = 1024,
+    QAMW_MAX_CHOICES = 32
+};
+
+/* Rows to 8-bit integers with one scale each (a token's activations, or the weights of an output channel):
+ *   v_j = X_ij * col_scale_j;  a = max_j |v_j|;  scales[i] = a / 127;  codes_ij = v_j * (127 / a) rounded to the nearest
+ * integer, ties to even; fp32, every operation rounded once (IEEE divisions), so that codes are within -127 .. 127.
+ * a < 2^-110: scale 0 and codes 0.  A row with an infinity or a NaN: scale NaN and codes 0, which makes every product with
+ * the row NaN.
+ *   X  device, m rows of d elements (F32 or BF16), leading dimension ldx;  col_scale  device, d floats, or NULL (ones);
+ *   codes  device, m rows of d int8, leading dimension ldc;  scales  device, m floats.
+ * Errors: m outside [0, QAMW_INT8_MAX_ROWS], d < 1, NULL or misaligned pointers, dtype -> INVALID_ARG; ldx < d, ldc < d -> SHAPE. */
+int qamw_int8_quantize(const void *X, int dtype, int m, int d, int64_t ldx, const float *col_scale, int8_t *codes, int64_t ldc,
+                       float *scales, void *stream);
+
+/* Y = X W^T in 8-bit integers:  y_in = x_scales[i] * w_scales[n] * sum_j X_ij W_nj, the sum exact in 32-bit integers, then
+ * fp32(fp32(sum) * x_scale) * w_scale, each product rounded once.
+ *   X  x_dtype I8: codes, with x_scales (m floats).  x_dtype F32 or BF16: quantised by row in the call as by
+ *      qamw_int8_quantize (with col_scale, nullable), x_scales = NULL
+ *   W  device, rows of d_in int8, leading dimension ldw, with w_scales, one float a row.  gated = 0: d_out rows.
+ *      gated = 1: the d_out rows of a gate, then the d_out rows of an up projection, and Y = g / (1 + exp(-g)) * u
+ *   Y  device, m rows of d_out elements of y_dtype (F32 or BF16, rounded to nearest even), leading dimension ldy
+ *   workspace  qamw_int8_matmul_workspace_bytes() of device memory, 16-byte aligned; NULL with 0 bytes for codes
+ * Errors: sizes out of the ranges above, NULL or misaligned pointers, x_scales with floating X or col_scale with codes, a
+ * workspace too small -> INVALID_ARG; leading dimensions smaller than a row -> SHAPE; more tiles than a launch has ->
+ * UNSUPPORTED. */
+int qamw_int8_matmul_workspace_bytes(int x_dtype, int m, int d_in, size_t *bytes_out);
+int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const float *col_scale, int m, int64_t ldx, const int8_t *W,
+                     const float *w_scales, int64_t ldw, int d_out, int d_in, int gated, void *Y, int y_dtype, int64_t ldy,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* The experts' products: for every expert e and every place i in offsets[e] .. offsets[e + 1],
+ *   Y_i = X_r W_e^T  with r = rows[i] (rows NULL: r = i).
+ *   X  device, x_rows rows of d_in elements: BF16 (sums in fp32), or I8 with x_scales (x_rows floats; arithmetic as
+ *      qamw_int8_matmul);  rows  device, m int32, values below x_rows
+ *   W  device, n_experts matrices of X's element type, expert_stride elements apart, each d_out rows (gated: 2 d_out rows, as
+ *      above) with leading dimension ldw;  w_scales  device, I8 only: n_experts times d_out (gated: 2 d_out) floats
+ *   offsets  device, n_experts + 1 int32, ascending, within 0 .. m.  Rows of Y that no expert has are left as they are.
+ * Errors: as qamw_int8_matmul; without rows x_rows < m, with rows x_rows < 1 -> SHAPE. */
+int qamw_grouped_matmul(const void *X, int dtype, const float *x_scales, int x_rows, int64_t ldx, const int32_t *rows, const void *W,
+                        const float *w_scales, int64_t ldw, int64_t expert_stride, const int32_t *offsets, int n_experts, int m,
+                        int d_out, int d_in, int gated, void *Y, int y_dtype, int64_t ldy, void *stream);
+
+/* Logits to experts: every token's k largest logits (of equal ones the lowest expert first), and its rows sorted by expert.
+ *   logits   device, m rows of n_experts elements (F32 or BF16), leading dimension ld.  -inf and NaN are never chosen: a token
+ *            with fewer than k other logits has fewer choices, a token with none is routed nowhere
+ *   experts  [m][k] the choices, -1 where there is none
+ *   weights  [m][k] fp32: softmax over the choices (renormalise = 1) or over all of the token's logits (0); 0 for no choice.
+ *            Logits of +inf share the whole weight equally
+ *   offsets  [n_experts + 1]: expert e has the places offsets[e] .. offsets[e + 1] of the sorted order, in which a token comes
+ *            before the next one
+ *   rows     [m k]: the token of each place; -1 for the places from offsets[n_experts] on
+ *   positions [m][k]: the place of each choice, -1 where there is none
+ *   workspace  qamw_route_workspace_bytes() of device memory, 16-byte aligned
+ * Errors: m outside [0, QAMW_INT8_MAX_ROWS], n_experts outside [1, QAMW_MAX_EXPERTS], k outside [1, min(n_experts,
+ * QAMW_MAX_CHOICES)], NULL or misaligned pointers, workspace too small -> INVALID_ARG; ld < n_experts -> SHAPE. */
+int qamw_route_workspace_bytes(int m, int n_experts, int k, size_t *bytes_out);
+int qamw_route(const void *logits, int dtype, int m, int n_experts, int64_t ld, int k, int renormalise, int32_t *experts,
+               float *weights, int32_t *offsets, int32_t *rows, int32_t *positions, void *workspace, size_t workspace_bytes,
+               void *stream);
+
+/* The way back: out_t = sum_j weights[t][j] * Y[positions[t][j]], fp32, j ascending, one fused multiply-add each.  A position
+ * below 0 (or from y_rows on) adds nothing, whatever its weight.
+ *   Y  device, y_rows rows of d elements (F32 or BF16), leading dimension ldy;  out  m rows of d elements of out_dtype
+ * Errors: sizes, NULL or misaligned pointers -> INVALID_ARG; ldy < d, ldo < d -> SHAPE. */
+int qamw_combine(const void *Y, int dtype, int y_rows, int64_t ldy, const int32_t *positions, const float *weights, int m, int k, int d,
+                 void *out, int out_dtype, int64_t ldo, void *stream);
 
 /* Which implementation the device entry points use: 0 = automatic (fast kernels when the shape
  * allows, otherwise the general ones), 1 = always the general kernels, 2 = as 0 but the encoder's

@@ -1,0 +1,116 @@
+// Y = X W^T for 8-bit integers with scales or bf16, one matrix or one for each expert.
+#include "qamw_product_tile.hpp"
+
+namespace qamw {
+namespace {
+
+// ---- every shape, alignment and extent ------------------------------------------------------------------------------------
+//
+// A workgroup has 64 rows of W and 64 of X and steps over 64 bytes of both at a time.  Elements are loaded one by one with a test
+// each, with 64-bit addresses, and zeros stand where there is nothing: rows past the end, the last columns of an odd d_in.
+constexpr int PA_TILE = 64, PA_THREADS = 256, PA_PITCH = 64 + 16;   // bytes: 16 more, or 4 rows of a fragment share their banks
+
+template <bool I8, bool GATED, bool YBF16>
+__global__ __launch_bounds__(PA_THREADS) void k_product_any(ProductArgs a, int col_tiles) {
+    using M = Mfma<I8>;
+    __shared__ __align__(16) char lds[2][PA_TILE * PA_PITCH];
+    const int t = (int)(blockIdx.x / (uint32_t)col_tiles), ct = (int)(blockIdx.x % (uint32_t)col_tiles);
+    const RowTile rt = find_tile<PA_TILE>(a, t);
+    if (rt.n <= 0) return;
+    const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, wn = wave & 1, wm = wave >> 1;
+    // row r of the tile's 64 rows of W; gated: 16 of the gate, then the same 16 of the up projection
+    auto out_of = [&](int r) { return GATED ? ct * 32 + (r >> 5) * 16 + (r & 15) : ct * 64 + r; };
+    const char *W = a.W + (int64_t)rt.expert * a.expert_stride;
+    // what this thread loads: 16 bytes of one row of each operand
+    const int lr = tid >> 2, lc = (tid & 3) * 16;
+    const int out = out_of(lr);
+    const bool has_w = out < a.d_out, has_x = lr < rt.n;
+    const char *src_w = W + (has_w ? (int64_t)(GATED && ((lr >> 4) & 1) ? a.d_out + (int64_t)out : out) * a.ldw : 0);
+    int64_t x_row = has_x ? rt.row0 + lr : 0;
+    if (a.rows && has_x) x_row = min(max(a.rows[x_row], 0), a.x_rows - 1);
+    const char *src_x = a.X + x_row * a.ldx;
+
+    typename M::acc_t acc[2][2] = {};
+    const int64_t bytes = (int64_t)a.d_in * M::ELEM;
+    for (int64_t k0 = 0; k0 < bytes; k0 += 64) {
+        union Piece {
+            char c[16];
+            uint16_t h[8];
+            pr_i32x4_t v;
+        } w, x;
+        for (int i = 0; i < 16 / M::ELEM; ++i) {
+            const int64_t at = k0 + lc + i * M::ELEM;
+            const bool in = at < bytes;
+            if (I8) {
+                w.c[i] = in && has_w ? src_w[at] : 0;
+                x.c[i] = in && has_x ? src_x[at] : 0;
+            } else {
+                w.h[i] = in && has_w ? *reinterpret_cast<const uint16_t *>(src_w + at) : 0;
+                x.h[i] = in && has_x ? *reinterpret_cast<const uint16_t *>(src_x + at) : 0;
+            }
+        }
+        __syncthreads();
+        *reinterpret_cast<pr_i32x4_t *>(&lds[0][lr * PA_PITCH + lc]) = w.v;
+        *reinterpret_cast<pr_i32x4_t *>(&lds[1][lr * PA_PITCH + lc]) = x.v;
+        __syncthreads();
+        pr_i32x4_t fw[2], fx[2];
+        for (int i = 0; i < 2; ++i) {
+            fw[i] = *reinterpret_cast<const pr_i32x4_t *>(&lds[0][(wn * 32 + i * 16 + lane % 16) * PA_PITCH + lane / 16 * 16]);
+            fx[i] = *reinterpret_cast<const pr_i32x4_t *>(&lds[1][(wm * 32 + i * 16 + lane % 16) * PA_PITCH + lane / 16 * 16]);
+        }
+        for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 2; ++j) acc[i][j] = M::mul(fw[i], fx[j], acc[i][j]);
+    }
+
+    const float *ws = I8 ? a.w_scales + (int64_t)rt.expert * a.d_out * (GATED ? 2 : 1) : nullptr;
+    for (int j = 0; j < 2; ++j) {
+        const int r = wm * 32 + j * 16 + lane % 16;
+        if (r >= rt.n) continue;
+        const int64_t row = rt.row0 + r;
+        const float xs = I8 ? a.x_scales[a.rows ? min(max(a.rows[row], 0), a.x_rows - 1) : row] : 1.0f;
+        for (int i = 0; i < (GATED ? 1 : 2); ++i)
+            for (int q = 0; q < 4; ++q) {
+                const int o = out_of(wn * 32 + i * 16 + lane / 16 * 4 + q);
+                if (o >= a.d_out) continue;
+                float v = (float)acc[i][j][q];
+                if (I8) v = v * xs * ws[o];
+                if (GATED) {
+                    float u = (float)acc[1][j][q];
+                    if (I8) u = u * xs * ws[a.d_out + o];
+                    v = silu(v) * u;
+                }
+                store_y<YBF16>(a.Y, row * a.ldy + o, v);
+            }
+    }
+}
+
+ProductArgs args_of(const Product &p) {
+    const int64_t e = p.i8 ? 1 : 2;
+    return {static_cast<const char *>(p.X), static_cast<const char *>(p.W), p.x_scales, p.w_scales, p.rows, p.offsets, p.Y,
+            p.ldx * e, p.ldw * e, p.expert_stride * e, p.ldy, p.m, p.x_rows, p.n_experts, p.d_out, p.d_in};
+}
+
+template <bool I8> hipError_t launch_any(const Product &p) {
+    const ProductArgs a = args_of(p);
+    const int outs = p.gated ? 32 : 64;
+    const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, n = most_row_tiles(p, PA_TILE) * cols;
+    if (n > 0x7FFFFFFF) return hipErrorNotSupported;
+    const dim3 g((uint32_t)n);
+    if (p.gated) {
+        if (p.y_bf16) k_product_any<I8, true, true><<<g, PA_THREADS, 0, p.stream>>>(a, (int)cols);
+        else k_product_any<I8, true, false><<<g, PA_THREADS, 0, p.stream>>>(a, (int)cols);
+    } else {
+        if (p.y_bf16) k_product_any<I8, false, true><<<g, PA_THREADS, 0, p.stream>>>(a, (int)cols);
+        else k_product_any<I8, false, false><<<g, PA_THREADS, 0, p.stream>>>(a, (int)cols);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_product(const Product &p) {
+    if (p.m == 0) return hipSuccess;
+    return p.i8 ? launch_any<true>(p) : launch_any<false>(p);
+}
+
+}  // namespace qamw

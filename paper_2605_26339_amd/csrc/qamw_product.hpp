@@ -1,0 +1,45 @@
+// Products of served layers: Y = X W^T with W in 8-bit integers or bf16, one matrix or one for each expert.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "qamw_common.hpp"
+
+namespace qamw {
+
+// One call.  Without offsets: one group of m rows.  With offsets: rows offsets[e] .. offsets[e + 1] belong to expert e.
+struct Product {
+    const void *X = nullptr;             // int8 codes or bf16
+    const float *x_scales = nullptr;     // int8: one for each row of X
+    const int32_t *rows = nullptr;       // row of X for each row of the product, nullable
+    const void *W = nullptr;             // gated: the gate's d_out rows, then the up projection's
+    const float *w_scales = nullptr;     // int8: one for each row of W, expert after expert
+    const int32_t *offsets = nullptr;    // device, n_experts + 1, nullable
+    void *Y = nullptr;
+    int64_t ldx = 0, ldw = 0, expert_stride = 0, ldy = 0;
+    int m = 0, x_rows = 0, n_experts = 1, d_out = 0, d_in = 0;
+    bool i8 = false, gated = false, y_bf16 = false;
+    hipStream_t stream = nullptr;
+};
+
+hipError_t launch_product(const Product &p);
+hipError_t launch_int8_quantize(const void *X, int dtype, int64_t m, int d, int64_t ldx, const float *col_scale, int8_t *codes,
+                                int64_t ldc, float *scales, hipStream_t stream);
+
+// Routed experts.
+struct RouteProblem {
+    const void *logits = nullptr;
+    int dtype = 0, m = 0, n_experts = 0, k = 0;
+    int64_t ld = 0;
+    bool renormalise = false;
+    int32_t *experts = nullptr, *offsets = nullptr, *rows = nullptr, *positions = nullptr;
+    float *weights = nullptr;
+    uint32_t *counts = nullptr;          // scratch
+    hipStream_t stream = nullptr;
+};
+size_t route_workspace_bytes(int m, int n_experts, int k);
+hipError_t launch_route(const RouteProblem &p);
+hipError_t launch_combine(const void *Y, int dtype, int64_t y_rows, int64_t ldy, const int32_t *positions, const float *weights, int m,
+                          int k, int d, void *out, int out_dtype, int64_t ldo, hipStream_t stream);
+
+}  // namespace qamw

@@ -1,0 +1,97 @@
+// What the product kernels share: operand types, the tile that a workgroup has, and the last step.
+#pragma once
+#include "qamw_product.hpp"
+
+namespace qamw {
+
+typedef int pr_i32x4_t __attribute__((ext_vector_type(4)));
+typedef float pr_f32x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 pr_bf16x8_t __attribute__((ext_vector_type(8)));
+
+// 16 rows of W times 16 rows of X over 64 bytes of each: lane l holds bytes 16 (l / 16) .. + 16 of row l % 16 of both operands,
+// and gets W rows 4 (l / 16) .. + 4 of the column that is X row l % 16.  int8 and bf16 lay their bytes out alike.
+template <bool I8> struct Mfma;
+template <> struct Mfma<true> {
+    using acc_t = pr_i32x4_t;
+    using sum_t = int;
+    static constexpr int ELEM = 1;
+    static __device__ __forceinline__ acc_t mul(pr_i32x4_t w, pr_i32x4_t x, acc_t c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, c, 0, 0, 0);
+    }
+};
+template <> struct Mfma<false> {
+    using acc_t = pr_f32x4_t;
+    using sum_t = float;
+    static constexpr int ELEM = 2;
+    static __device__ __forceinline__ acc_t mul(pr_i32x4_t w, pr_i32x4_t x, acc_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8_t, w), __builtin_bit_cast(pr_bf16x8_t, x), c, 0, 0, 0);
+    }
+};
+
+// The device side of a Product.
+struct ProductArgs {
+    const char *X, *W;
+    const float *x_scales, *w_scales;
+    const int32_t *rows, *offsets;
+    void *Y;
+    int64_t ldx, ldw, expert_stride;     // in bytes
+    int64_t ldy;                         // in elements
+    int m, x_rows, n_experts, d_out, d_in;
+};
+
+// Rows row0 .. row0 + n of the product, which are expert `expert`'s; n = 0: nothing to do.
+struct RowTile {
+    int expert, row0, n;
+};
+
+// The t-th tile of at most BM rows, counted over the experts in order.  Every wave of a workgroup finds it by itself: a lane has an
+// expert, and a prefix sum over lanes says where its tiles begin.  Offsets are held within 0 .. m, so that no value of theirs
+// makes a tile of rows that are not there.
+template <int BM> __device__ __forceinline__ RowTile find_tile(const ProductArgs &a, int t) {
+    if (!a.offsets) {
+        const int64_t row0 = (int64_t)t * BM;
+        return {0, (int)row0, row0 < a.m ? (int)min((int64_t)BM, a.m - row0) : 0};
+    }
+    const int lane = threadIdx.x % WAVE;
+    int before = 0;
+    for (int e0 = 0; e0 < a.n_experts; e0 += WAVE) {
+        const int e = e0 + lane;
+        const bool is = e < a.n_experts;
+        const int lo = is ? min(max(a.offsets[e], 0), a.m) : 0;
+        const int hi = is ? min(max(a.offsets[e + 1], lo), a.m) : lo;
+        const int tiles = (hi - lo) / BM + ((hi - lo) % BM != 0);
+        int upto = tiles;
+        for (int d = 1; d < WAVE; d <<= 1) {
+            const int v = __shfl_up(upto, d);
+            if (lane >= d) upto += v;
+        }
+        const unsigned long long past = __ballot(before + upto > t);
+        if (past) {
+            const int l = __ffsll((long long)past) - 1;
+            const int first = before + __shfl(upto - tiles, l), start = __shfl(lo, l), end = __shfl(hi, l);
+            const int row0 = start + (t - first) * BM;
+            return {e0 + l, row0, min(BM, end - row0)};
+        }
+        before += __shfl(upto, WAVE - 1);
+    }
+    return {0, 0, 0};
+}
+
+// Most tiles that find_tile() can number.
+inline int64_t most_row_tiles(const Product &p, int bm) {
+    const int64_t m = p.m;
+    return p.offsets ? m / bm + (m < p.n_experts ? m : p.n_experts) : (m + bm - 1) / bm;
+}
+
+// g / (1 + exp(-g)) with the hardware's exponential and reciprocal: a few units in the last place of fp32, below a product's own
+// rounding, for a fifth of the instructions.  exp overflows to infinity, whose reciprocal is 0.
+__device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
+
+template <bool BF16> __device__ __forceinline__ void store_y(void *Y, int64_t at, float v) {
+    if (BF16)
+        reinterpret_cast<uint16_t *>(Y)[at] = (uint16_t)bf16_rne_bits(v);
+    else
+        reinterpret_cast<float *>(Y)[at] = v;
+}
+
+}  // namespace qamw

@@ -6,6 +6,7 @@ device entry points raise if the library is missing or HIP reports an error.
 """
 from __future__ import annotations
 
+import collections
 import ctypes as C
 import functools
 import os
@@ -15,7 +16,7 @@ import numpy as np
 from . import build as _build
 
 OK, ERR_INVALID_ARG, ERR_SHAPE, ERR_UNSUPPORTED, ERR_DEVICE = 0, 1, 2, 3, 4
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_I8 = 0, 1, 2
 
 EXPORTS = [
     "qamw_status_string", "qamw_packed_row_bytes", "qamw_paper_block_size", "qamw_bpw", "qamw_sign_mask",
@@ -25,6 +26,8 @@ EXPORTS = [
     "qamw_normalised_pairs", "qamw_lloyd_workspace_bytes", "qamw_lloyd_device",
     "qamw_search_grid_size", "qamw_search_grid_build", "qamw_encode_pruned", "qamw_calibrate_sigma_static", "qamw_decode_traffic_probe", "qamw_encode_batch", "qamw_calibrate_sigma_batch",
     "qamw_encode_workspace_bytes", "qamw_encode_ws", "qamw_encode_batch_ws", "qamw_encode_pruned_ws",
+    "qamw_int8_quantize", "qamw_int8_matmul_workspace_bytes", "qamw_int8_matmul", "qamw_grouped_matmul",
+    "qamw_route_workspace_bytes", "qamw_route", "qamw_combine",
 ]
 
 
@@ -114,6 +117,13 @@ def lib() -> C.CDLL:
         L.qamw_search_grid_build.argtypes = [vp, i32, vp, C.c_size_t, C.POINTER(i32), C.POINTER(u64)]
         L.qamw_encode_pruned.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
         L.qamw_encode_pruned_ws.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, i32, i32, vp, vp, C.c_size_t, vp, vp, vp, vp]
+        L.qamw_int8_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp, i64, vp, vp]
+        L.qamw_int8_matmul_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(C.c_size_t)]
+        L.qamw_int8_matmul.argtypes = [vp, i32, vp, vp, i32, i64, vp, vp, i64, i32, i32, i32, vp, i32, i64, vp, C.c_size_t, vp]
+        L.qamw_grouped_matmul.argtypes = [vp, i32, vp, i32, i64, vp, vp, vp, i64, i64, vp, i32, i32, i32, i32, i32, vp, i32, i64, vp]
+        L.qamw_route_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(C.c_size_t)]
+        L.qamw_route.argtypes = [vp, i32, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.qamw_combine.argtypes = [vp, i32, i32, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp]
         for name in EXPORTS:
             if name != "qamw_status_string":
                 getattr(L, name).restype = C.c_int
@@ -599,3 +609,181 @@ def calibrate_sigma_batch(items, block: int, workspace, stream=None):
     _check(lib().qamw_calibrate_sigma_batch(arr, len(arr), code, block, max_rows, _ptr(workspace),
                                             workspace.numel() * workspace.element_size(), _stream(stream)),
            "qamw_calibrate_sigma_batch")
+
+
+# ------------------------------------------------------------------ served layers: 8-bit products, routed experts
+def _operand_code(t, name):
+    import torch
+
+    if t.dtype == torch.int8:
+        return DTYPE_I8
+    if t.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    if t.dtype == torch.float32:
+        return DTYPE_F32
+    raise TypeError(f"{name} must be int8, float32 or bfloat16, got {t.dtype}")
+
+
+def _expect(t, name, dtype, shape):
+    """A contiguous tensor of one type and shape, or None."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _matrix(t, name, dim=2):
+    """Rows of adjacent elements.  Returns the leading dimension, which a tensor of one row or none may leave open."""
+    if t.dim() != dim or t.shape[-1] < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be {dim}-D with unit column stride")
+    return t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])
+
+
+def _same_device(first, *others):
+    _require_cuda(first, *others)
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("all tensors of a call are on one device")
+
+
+def _result(out, shape, dtype, device, stream):
+    if out is None:
+        return _empty(shape, dtype, device, stream)
+    if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
+        raise ValueError(f"out must be {dtype} of shape {tuple(shape)}, got {out.dtype} {tuple(out.shape)}")
+    return out
+
+
+def int8_quantize(X, col_scale=None, out=None, stream=None):
+    """Rows of X (fp32 or bf16 [m][d]) to 8-bit integers with one scale each: (codes int8 [m][d], scales fp32 [m]).
+    col_scale (fp32 [d]) multiplies the columns first.  For weights a row is an output channel, for activations a token."""
+    import torch
+
+    _same_device(X, col_scale)
+    ldx = _matrix(X, "X")
+    m, d = X.shape
+    _expect(col_scale, "col_scale", torch.float32, (d,))
+    if out is None:
+        out = _empty((m, d), torch.int8, X.device, stream), _empty((m,), torch.float32, X.device, stream)
+    codes, scales = out
+    _same_device(X, codes, scales)
+    if codes.dtype != torch.int8 or tuple(codes.shape) != (m, d):
+        raise ValueError("codes must be int8, of the shape of X")
+    _expect(scales, "scales", torch.float32, (m,))
+    ldc = _matrix(codes, "codes")
+    _check(lib().qamw_int8_quantize(_ptr(X), _dtype_code(X), m, d, ldx, _ptr(col_scale), _ptr(codes), ldc, _ptr(scales),
+                                    _stream(stream)), "qamw_int8_quantize")
+    return codes, scales
+
+
+@functools.lru_cache(maxsize=256, typed=True)
+def int8_matmul_workspace_bytes(x_dtype: int, m: int, d_in: int) -> int:
+    out = C.c_size_t()
+    _check(lib().qamw_int8_matmul_workspace_bytes(x_dtype, m, d_in, C.byref(out)), "qamw_int8_matmul_workspace_bytes")
+    return int(out.value)
+
+
+def int8_matmul(X, W, w_scales, x_scales=None, col_scale=None, gated=False, out=None, out_dtype=None, workspace=None, stream=None):
+    """Y = X W^T in 8-bit integers: W int8 [d_out][d_in] with w_scales [d_out]; X int8 [m][d_in] with x_scales [m], or fp32 or
+    bf16 [m][d_in], quantised by row in the call (col_scale [d_in] multiplies its columns first).
+    gated: W has the gate's rows, then the up projection's, [2 d_out][d_in], and Y = silu(gate) * up.
+    Returns [m][d_out] of out_dtype (bf16 where neither it nor out is given)."""
+    import torch
+
+    _same_device(X, W, w_scales, x_scales, col_scale, out, workspace)
+    ldx, ldw = _matrix(X, "X"), _matrix(W, "W")
+    (m, d_in), outs, code = X.shape, W.shape[0], _operand_code(X, "X")
+    if W.dtype != torch.int8 or W.shape[1] != d_in or outs < 1 or (gated and outs % 2):
+        raise ValueError(f"W must be int8 [{'2 d_out' if gated else 'd_out'}][{d_in}], got {W.dtype} {tuple(W.shape)}")
+    _expect(w_scales, "w_scales", torch.float32, (outs,))
+    _expect(x_scales, "x_scales", torch.float32, (m,))
+    _expect(col_scale, "col_scale", torch.float32, (d_in,))
+    d_out = outs // 2 if gated else outs
+    y = _result(out, (m, d_out), out_dtype or (torch.bfloat16 if out is None else out.dtype), X.device, stream)
+    ldy = _matrix(y, "out")
+    if workspace is None:
+        need = int8_matmul_workspace_bytes(code, m, d_in)
+        workspace = _empty(need, torch.uint8, X.device, stream) if need else None
+    _check(lib().qamw_int8_matmul(_ptr(X), code, _ptr(x_scales), _ptr(col_scale), m, ldx, _ptr(W), _ptr(w_scales), ldw, d_out, d_in,
+                                  int(bool(gated)), _ptr(y), _dtype_code(y), ldy, _ptr(workspace),
+                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
+           "qamw_int8_matmul")
+    return y
+
+
+def grouped_matmul(X, W, offsets, rows=None, x_scales=None, w_scales=None, gated=False, out=None, out_dtype=None, stream=None):
+    """The experts' products: places offsets[e] .. offsets[e + 1] (int32 [n_experts + 1], on the device) are expert e's, and
+    Y[i] = X[rows[i]] W[e]^T (rows int32 [m]; without it Y[i] = X[i] W[e]^T).  X and W [n_experts][d_out][d_in] are both bf16, or
+    both int8 with x_scales [rows of X] and w_scales [n_experts][d_out].  gated: W [n_experts][2 d_out][d_in] and
+    Y = silu(gate) * up.  Returns [m][d_out] of out_dtype (bf16 where neither it nor out is given); rows that no expert has
+    are left as they are."""
+    import torch
+
+    _same_device(X, W, offsets, rows, x_scales, w_scales, out)
+    ldx, ldw = _matrix(X, "X"), _matrix(W, "W", 3)
+    (x_rows, d_in), (n, outs) = X.shape, W.shape[:2]
+    if X.dtype not in (torch.int8, torch.bfloat16) or W.dtype != X.dtype:
+        raise TypeError(f"X and W must both be int8 or both be bfloat16, got {X.dtype} and {W.dtype}")
+    if W.shape[2] != d_in or n < 1 or outs < 1 or (gated and outs % 2):
+        raise ValueError(f"W must be [n_experts][{'2 d_out' if gated else 'd_out'}][{d_in}], got {tuple(W.shape)}")
+    m = x_rows if rows is None else rows.numel()
+    _expect(offsets, "offsets", torch.int32, (n + 1,))
+    _expect(rows, "rows", torch.int32, (m,))
+    _expect(x_scales, "x_scales", torch.float32, (x_rows,))
+    _expect(w_scales, "w_scales", torch.float32, (n, outs))
+    d_out = outs // 2 if gated else outs
+    y = _result(out, (m, d_out), out_dtype or (torch.bfloat16 if out is None else out.dtype), X.device, stream)
+    ldy = _matrix(y, "out")
+    _check(lib().qamw_grouped_matmul(_ptr(X), _operand_code(X, "X"), _ptr(x_scales), x_rows, ldx, _ptr(rows), _ptr(W), _ptr(w_scales),
+                                     ldw, W.stride(0), _ptr(offsets), n, m, d_out, d_in, int(bool(gated)), _ptr(y), _dtype_code(y), ldy,
+                                     _stream(stream)), "qamw_grouped_matmul")
+    return y
+
+
+Routing = collections.namedtuple("Routing", "experts weights offsets rows positions")
+
+
+@functools.lru_cache(maxsize=256, typed=True)
+def route_workspace_bytes(m: int, n_experts: int, k: int) -> int:
+    out = C.c_size_t()
+    _check(lib().qamw_route_workspace_bytes(m, n_experts, k, C.byref(out)), "qamw_route_workspace_bytes")
+    return int(out.value)
+
+
+def route(logits, k: int, renormalise=True, workspace=None, stream=None):
+    """Every token's k experts by its logits (fp32 or bf16 [m][n_experts]), their softmax weights (over the chosen, or over all
+    where renormalise is false) and the rows sorted by expert.  Returns a Routing: experts [m][k], weights [m][k],
+    offsets [n_experts + 1], rows [m k] and positions [m][k]; -1 where there is none (see qamw_route in include/qamw.h)."""
+    import torch
+
+    _same_device(logits, workspace)
+    ld = _matrix(logits, "logits")
+    m, n = logits.shape
+    need = route_workspace_bytes(m, n, k)
+    dev = logits.device
+    if workspace is None:
+        workspace = _empty(need, torch.uint8, dev, stream) if need else None
+    r = Routing(_empty((m, k), torch.int32, dev, stream), _empty((m, k), torch.float32, dev, stream),
+                _empty((n + 1,), torch.int32, dev, stream), _empty((m * k,), torch.int32, dev, stream),
+                _empty((m, k), torch.int32, dev, stream))
+    _check(lib().qamw_route(_ptr(logits), _dtype_code(logits), m, n, ld, k, int(bool(renormalise)), _ptr(r.experts), _ptr(r.weights),
+                            _ptr(r.offsets), _ptr(r.rows), _ptr(r.positions), _ptr(workspace),
+                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "qamw_route")
+    return r
+
+
+def combine(Y, positions, weights, out=None, out_dtype=None, stream=None):
+    """out[t] = sum_j weights[t][j] * Y[positions[t][j]]: the experts' outputs (fp32 or bf16 [rows][d]) back to their tokens, fp32
+    sums, a position of -1 adds nothing.  Returns [m][d] of out_dtype (Y's type where neither it nor out is given)."""
+    import torch
+
+    _same_device(Y, positions, weights, out)
+    ldy = _matrix(Y, "Y")
+    if positions.dim() != 2:
+        raise ValueError("positions must be 2-D")
+    m, k = positions.shape
+    _expect(positions, "positions", torch.int32, (m, k))
+    _expect(weights, "weights", torch.float32, (m, k))
+    y = _result(out, (m, Y.shape[1]), out_dtype or (Y.dtype if out is None else out.dtype), Y.device, stream)
+    ldo = _matrix(y, "out")
+    _check(lib().qamw_combine(_ptr(Y), _dtype_code(Y), Y.shape[0], ldy, _ptr(positions), _ptr(weights), m, k, Y.shape[1], _ptr(y),
+                              _dtype_code(y), ldo, _stream(stream)), "qamw_combine")
+    return y
