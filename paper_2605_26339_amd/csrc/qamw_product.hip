@@ -84,12 +84,6 @@ __global__ __launch_bounds__(PA_THREADS) void k_product_any(ProductArgs a, int c
     }
 }
 
-ProductArgs args_of(const Product &p) {
-    const int64_t e = p.i8 ? 1 : 2;
-    return {static_cast<const char *>(p.X), static_cast<const char *>(p.W), p.x_scales, p.w_scales, p.rows, p.offsets, p.Y,
-            p.ldx * e, p.ldw * e, p.expert_stride * e, p.ldy, p.m, p.x_rows, p.n_experts, p.d_out, p.d_in};
-}
-
 template <bool I8> hipError_t launch_any(const Product &p) {
     const ProductArgs a = args_of(p);
     const int outs = p.gated ? 32 : 64;
@@ -110,6 +104,7 @@ template <bool I8> hipError_t launch_any(const Product &p) {
 
 hipError_t launch_product(const Product &p) {
     if (p.m == 0) return hipSuccess;
+    if (product_wide_supported(p)) return launch_product_wide(p);
     return p.i8 ? launch_any<true>(p) : launch_any<false>(p);
 }
 

@@ -39,19 +39,24 @@ struct ProductArgs {
     int m, x_rows, n_experts, d_out, d_in;
 };
 
+inline ProductArgs args_of(const Product &p) {
+    const int64_t e = p.i8 ? 1 : 2;
+    return {static_cast<const char *>(p.X), static_cast<const char *>(p.W), p.x_scales, p.w_scales, p.rows, p.offsets, p.Y,
+            p.ldx * e, p.ldw * e, p.expert_stride * e, p.ldy, p.m, p.x_rows, p.n_experts, p.d_out, p.d_in};
+}
+
 // Rows row0 .. row0 + n of the product, which are expert `expert`'s; n = 0: nothing to do.
 struct RowTile {
     int expert, row0, n;
 };
 
-// The t-th tile of at most BM rows, counted over the experts in order.  Every wave of a workgroup finds it by itself: a lane has an
-// expert, and a prefix sum over lanes says where its tiles begin.  Offsets are held within 0 .. m, so that no value of theirs
-// makes a tile of rows that are not there.
-template <int BM> __device__ __forceinline__ RowTile find_tile(const ProductArgs &a, int t) {
-    if (!a.offsets) {
-        const int64_t row0 = (int64_t)t * BM;
-        return {0, (int)row0, row0 < a.m ? (int)min((int64_t)BM, a.m - row0) : 0};
-    }
+// The tiles of at most BM rows are counted over the experts in order; an expert has the row tiles first .. first + tiles.  Every wave
+// of a workgroup finds them by itself: a lane has an expert, and a prefix sum over lanes says where its tiles begin.  Offsets are
+// held within 0 .. m, so that no value of theirs makes a tile of rows that are not there.
+struct ExpertTiles {
+    int expert, first, tiles, start, end;      // rows start .. end
+};
+template <int BM, typename Visit> __device__ __forceinline__ int visit_tiles(const ProductArgs &a, Visit visit) {
     const int lane = threadIdx.x % WAVE;
     int before = 0;
     for (int e0 = 0; e0 < a.n_experts; e0 += WAVE) {
@@ -65,19 +70,38 @@ template <int BM> __device__ __forceinline__ RowTile find_tile(const ProductArgs
             const int v = __shfl_up(upto, d);
             if (lane >= d) upto += v;
         }
-        const unsigned long long past = __ballot(before + upto > t);
-        if (past) {
-            const int l = __ffsll((long long)past) - 1;
-            const int first = before + __shfl(upto - tiles, l), start = __shfl(lo, l), end = __shfl(hi, l);
-            const int row0 = start + (t - first) * BM;
-            return {e0 + l, row0, min(BM, end - row0)};
-        }
-        before += __shfl(upto, WAVE - 1);
+        if (visit(e0, before, lo, hi, tiles, upto)) return -1;
+        before += __builtin_amdgcn_readlane(upto, WAVE - 1);
     }
-    return {0, 0, 0};
+    return before;
+}
+// All row tiles there are.
+template <int BM> __device__ __forceinline__ int count_tiles(const ProductArgs &a) {
+    if (!a.offsets) return a.m / BM + (a.m % BM != 0);
+    return visit_tiles<BM>(a, [](int, int, int, int, int, int) { return false; });
+}
+// The expert that has row tile t; tiles = 0 if none has.
+template <int BM> __device__ __forceinline__ ExpertTiles find_expert(const ProductArgs &a, int t) {
+    if (!a.offsets) return {0, 0, a.m / BM + (a.m % BM != 0), 0, a.m};
+    ExpertTiles found = {0, 0, 0, 0, 0};
+    visit_tiles<BM>(a, [&](int e0, int before, int lo, int hi, int tiles, int upto) {
+        const unsigned long long past = __ballot(before + upto > t);
+        if (!past) return false;
+        const int l = __ffsll((long long)past) - 1;
+        found = {e0 + l, before + __builtin_amdgcn_readlane(upto - tiles, l), __builtin_amdgcn_readlane(tiles, l),
+                 __builtin_amdgcn_readlane(lo, l), __builtin_amdgcn_readlane(hi, l)};
+        return true;
+    });
+    return found;
+}
+template <int BM> __device__ __forceinline__ RowTile find_tile(const ProductArgs &a, int t) {
+    const ExpertTiles e = find_expert<BM>(a, t);
+    if (t - e.first >= e.tiles) return {0, 0, 0};
+    const int row0 = e.start + (t - e.first) * BM;
+    return {e.expert, row0, min(BM, e.end - row0)};
 }
 
-// Most tiles that find_tile() can number.
+// Most row tiles that there can be.
 inline int64_t most_row_tiles(const Product &p, int bm) {
     const int64_t m = p.m;
     return p.offsets ? m / bm + (m < p.n_experts ? m : p.n_experts) : (m + bm - 1) / bm;
@@ -86,6 +110,28 @@ inline int64_t most_row_tiles(const Product &p, int bm) {
 // g / (1 + exp(-g)) with the hardware's exponential and reciprocal: a few units in the last place of fp32, below a product's own
 // rounding, for a fifth of the instructions.  exp overflows to infinity, whose reciprocal is 0.
 __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
+
+// Four neighbours of a row of Y, or of the scales of W, wherever they lie: the memory instructions take any address.
+template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Unaligned {
+    T v[N];
+};
+
+template <bool BF16> __device__ __forceinline__ void store_y4(void *Y, int64_t at, const float (&v)[4], int n) {
+    if (n >= 4) {
+        if (BF16) {
+            const uint2 two = {bf16_rne_bits(v[0]) | bf16_rne_bits(v[1]) << 16, bf16_rne_bits(v[2]) | bf16_rne_bits(v[3]) << 16};
+            *reinterpret_cast<Unaligned<uint16_t, 4> *>(reinterpret_cast<uint16_t *>(Y) + at) = __builtin_bit_cast(Unaligned<uint16_t, 4>, two);
+        } else {
+            *reinterpret_cast<Unaligned<float, 4> *>(reinterpret_cast<float *>(Y) + at) = Unaligned<float, 4>{{v[0], v[1], v[2], v[3]}};
+        }
+        return;
+    }
+    for (int q = 0; q < 3; ++q)
+        if (q < n) {
+            if (BF16) reinterpret_cast<uint16_t *>(Y)[at + q] = (uint16_t)bf16_rne_bits(v[q]);
+            else reinterpret_cast<float *>(Y)[at + q] = v[q];
+        }
+}
 
 template <bool BF16> __device__ __forceinline__ void store_y(void *Y, int64_t at, float v) {
     if (BF16)
