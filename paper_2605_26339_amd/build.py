@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libqamw.so")
 
 SOURCES = ["qamw_host.cpp", "qamw_api.hip", "qamw_general.hip", "qamw_decode_fast.hip", "qamw_encode_fast.hip",
            "qamw_encode_mfma.hip", "qamw_encode_cells.hip", "qamw_encode_polar.hip", "qamw_encode_grid.hip", "qamw_calibrate_fast.hip",
-           "qamw_matmul.hip", "qamw_lloyd.hip", "qamw_serve_api.hip", "qamw_quantize.hip", "qamw_product.hip", "qamw_product_wide.hip", "qamw_route.hip"]
+           "qamw_matmul.hip", "qamw_lloyd.hip", "qamw_serve_api.hip", "qamw_quantize.hip", "qamw_product.hip", "qamw_product_wide.hip", "qamw_product_few.hip", "qamw_route.hip"]
 
 # -ffp-contract=off: the codec's fp32 steps are rounded one by one; fused multiply-adds appear only
 # where the source asks for them.  Packed fp32 instructions are disabled for the device pass.

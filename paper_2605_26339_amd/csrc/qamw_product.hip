@@ -104,7 +104,7 @@ template <bool I8> hipError_t launch_any(const Product &p) {
 
 hipError_t launch_product(const Product &p) {
     if (p.m == 0) return hipSuccess;
-    if (product_wide_supported(p)) return launch_product_wide(p);
+    if (product_wide_supported(p)) return p.m <= 64 * (p.offsets ? p.n_experts : 1) ? launch_product_few(p) : launch_product_wide(p);
     return p.i8 ? launch_any<true>(p) : launch_any<false>(p);
 }
 

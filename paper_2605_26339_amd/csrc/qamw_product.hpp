@@ -25,6 +25,10 @@ struct Product {
 hipError_t launch_product(const Product &p);
 bool product_wide_supported(const Product &p);
 hipError_t launch_product_wide(const Product &p);     // of products that are
+hipError_t launch_product_few(const Product &p);      // likewise
+// The product of rows that are quantised in the same launch; W as launch_product_few() needs it.
+bool product_from_floats_supported(const Product &p, const void *X, int dtype, int64_t ldx, const float *col_scale);
+hipError_t launch_product_from_floats(const Product &p, const void *X, int dtype, int64_t ldx, const float *col_scale);
 hipError_t launch_int8_quantize(const void *X, int dtype, int64_t m, int d, int64_t ldx, const float *col_scale, int8_t *codes,
                                 int64_t ldc, float *scales, hipStream_t stream);
 

@@ -107,6 +107,49 @@ inline int64_t most_row_tiles(const Product &p, int bm) {
     return p.offsets ? m / bm + (m < p.n_experts ? m : p.n_experts) : (m + bm - 1) / bm;
 }
 
+// The largest of a wave's values, in every lane: within 16 lanes by DPP, then over the four of them.
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));    // lane ^ 1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));    // lane ^ 2
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));   // the other four of eight
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, false));   // the other eight of sixteen
+    const uint32_t a = __builtin_amdgcn_readlane((int)v, 0), b = __builtin_amdgcn_readlane((int)v, 16);
+    const uint32_t c = __builtin_amdgcn_readlane((int)v, 32), d = __builtin_amdgcn_readlane((int)v, 48);
+    return max(max(a, b), max(c, d));
+}
+
+// Eight neighbours of a row as they are read, and as fp32.
+template <int DTYPE> struct Eight;
+template <> struct Eight<0> {
+    pr_i32x4_t a, b;
+    template <typename R> __device__ __forceinline__ void load(R from, uint32_t at) {       // a buffer, a byte offset
+        a = __builtin_bit_cast(pr_i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0));
+        b = __builtin_bit_cast(pr_i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 16, 0));
+    }
+    __device__ __forceinline__ float value(int i) const { return __int_as_float(i < 4 ? a[i & 3] : b[i & 3]); }
+};
+template <> struct Eight<1> {
+    pr_i32x4_t a;
+    template <typename R> __device__ __forceinline__ void load(R from, uint32_t at) {
+        a = __builtin_bit_cast(pr_i32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from, (int)at, 0, 0));
+    }
+    __device__ __forceinline__ float value(int i) const {
+        return __int_as_float(i & 1 ? (int)((uint32_t)a[i >> 1] & 0xFFFF0000u) : a[i >> 1] << 16);
+    }
+};
+
+// Steps of the quantisation to 8 bits: the scale and the factor from the largest |v| (its bits order finite values, infinity, NaNs).
+struct Quantiser {
+    float inv, scale;                     // inv = 0: all codes are 0
+    __device__ __forceinline__ explicit Quantiser(uint32_t most) {
+        const float a = __uint_as_float(most);
+        const bool finite = most < 0x7F800000u, some = finite && a >= 0x1p-110f;
+        inv = some ? 127.0f / a : 0.0f;
+        scale = some ? a / 127.0f : finite ? 0.0f : __uint_as_float(0x7FC00000u);
+    }
+    __device__ __forceinline__ uint32_t code(float v) const { return inv != 0.0f ? (uint32_t)(int)rintf(v * inv) & 255u : 0u; }
+};
+
 // g / (1 + exp(-g)) with the hardware's exponential and reciprocal: a few units in the last place of fp32, below a product's own
 // rounding, for a fifth of the instructions.  exp overflows to infinity, whose reciprocal is 0.
 __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }

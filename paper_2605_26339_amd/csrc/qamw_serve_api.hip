@@ -48,19 +48,6 @@ int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const fl
         return QAMW_ERR_INVALID_ARG;
     if (ldx < d_in || ldw < d_in || ldy < d_out) return QAMW_ERR_SHAPE;
     qamw::Product p;
-    p.X = X;
-    p.ldx = ldx;
-    p.x_scales = x_scales;
-    if (!codes) {
-        const int64_t ldc = (int64_t)round16((size_t)d_in);
-        float *scales = reinterpret_cast<float *>(static_cast<char *>(workspace) + (size_t)m * (size_t)ldc);
-        const hipError_t e = qamw::launch_int8_quantize(X, x_dtype, m, d_in, ldx, col_scale, static_cast<int8_t *>(workspace), ldc,
-                                                        scales, (hipStream_t)stream);
-        if (e != hipSuccess) return status_of(e);
-        p.X = workspace;
-        p.ldx = ldc;
-        p.x_scales = scales;
-    }
     p.W = W;
     p.ldw = ldw;
     p.w_scales = w_scales;
@@ -73,6 +60,23 @@ int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const fl
     p.gated = gated != 0;
     p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
     p.stream = (hipStream_t)stream;
+    if (codes) {
+        p.X = X;
+        p.ldx = ldx;
+        p.x_scales = x_scales;
+    } else {
+        const int64_t ldc = (int64_t)round16((size_t)d_in);
+        float *scales = reinterpret_cast<float *>(static_cast<char *>(workspace) + (size_t)m * (size_t)ldc);
+        p.X = workspace;
+        p.ldx = ldc;
+        p.x_scales = scales;
+        if (m == 0) return QAMW_OK;
+        if (qamw::product_wide_supported(p) && qamw::product_from_floats_supported(p, X, x_dtype, ldx, col_scale))
+            return status_of(qamw::launch_product_from_floats(p, X, x_dtype, ldx, col_scale));
+        const hipError_t e = qamw::launch_int8_quantize(X, x_dtype, m, d_in, ldx, col_scale, static_cast<int8_t *>(workspace), ldc,
+                                                        scales, (hipStream_t)stream);
+        if (e != hipSuccess) return status_of(e);
+    }
     return status_of(qamw::launch_product(p));
 }
 
