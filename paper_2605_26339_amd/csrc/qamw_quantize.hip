@@ -2,17 +2,79 @@
 //   v_j = x_j c_j;  a = max_j |v_j|;  scale = a / 127;  code_j = rne(v_j * (127 / a)), each step rounded once to fp32.
 // a < 2^-110 (127 / a nears the largest float): scale 0, codes 0.  An infinity or a NaN in the row: scale NaN, codes 0, so
 // that whatever is computed with the row is NaN.
-#include "qamw_product.hpp"
+#include "qamw_product_tile.hpp"
 
 namespace qamw {
 namespace {
 
-constexpr int QT = 256;          // threads of a workgroup, which has one row
-
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-    for (int d = 32; d; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
-    return v;
+// ---- rows of whole 16 bytes ------------------------------------------------------------------------------------------------
+//
+// TR threads have a row and hold its values, EIGHTS groups of 8 each, between the maximum and the codes: one read of X.  Groups past
+// the end of the row are loaded as zeros, from beyond the buffer's end.
+template <int DTYPE, int TR, int EIGHTS>
+__global__ __launch_bounds__(TR < 256 ? 256 : TR) void k_quantize(const char *X, int m, int d, int64_t ldx, const float *col_scale,
+                                                                  int8_t *codes, int64_t ldc, float *scales) {
+    constexpr int ROWS = TR < 256 ? 256 / TR : 1, SPAN = TR * 8;
+    __shared__ uint32_t part[TR / WAVE];
+    const int tid = threadIdx.x % TR;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + (ROWS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TR) : 0);
+    if (ROWS > 1 && row >= m) return;                      // whole waves; rows of one wave meet no barrier
+    const auto xb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(X + row * ldx * (DTYPE ? 2 : 4)), 0, d * (DTYPE ? 2 : 4), 0x00020000);
+    const auto cb = __builtin_amdgcn_make_buffer_rsrc(const_cast<float *>(col_scale), 0, col_scale ? d * 4 : 0, 0x00020000);
+    Eight<DTYPE> raw[EIGHTS];
+    Eight<0> col[EIGHTS];
+#pragma unroll
+    for (int i = 0; i < EIGHTS; ++i) raw[i].load(xb, (uint32_t)(i * SPAN + tid * 8) * (DTYPE ? 2 : 4));
+    if (col_scale)
+#pragma unroll
+        for (int i = 0; i < EIGHTS; ++i) col[i].load(cb, (uint32_t)(i * SPAN + tid * 8) * 4);
+    float v[EIGHTS][8];
+    uint32_t most = 0;           // of the bits of |v|: orders finite values, then infinity, then NaNs
+#pragma unroll
+    for (int i = 0; i < EIGHTS; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            v[i][k] = raw[i].value(k);
+            if (col_scale) v[i][k] *= col[i].value(k);
+            most = max(most, __float_as_uint(v[i][k]) & 0x7FFFFFFFu);
+        }
+    most = wave_max(most);
+    if (TR > WAVE) {
+        if (tid % WAVE == 0) part[tid / WAVE] = most;
+        __syncthreads();
+        most = wave_max(part[tid % (TR / WAVE)]);
+    }
+    const Quantiser z(most);
+    if (tid == 0) scales[row] = z.scale;
+#pragma unroll
+    for (int i = 0; i < EIGHTS; ++i) {
+        const int j = i * SPAN + tid * 8;
+        if (j >= d) continue;
+        uint32_t c[2] = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) c[k / 4] |= z.code(v[i][k]) << (k % 4 * 8);
+        *reinterpret_cast<uint2 *>(codes + row * ldc + j) = {c[0], c[1]};
+    }
 }
+
+template <int DTYPE>
+hipError_t launch_whole(const void *X, int64_t m, int d, int64_t ldx, const float *col_scale, int8_t *codes, int64_t ldc, float *scales,
+                        hipStream_t stream) {
+    const char *x = static_cast<const char *>(X);
+    const uint32_t n = (uint32_t)m;
+    if (d <= 512) k_quantize<DTYPE, 64, 1><<<(n + 3) / 4, 256, 0, stream>>>(x, n, d, ldx, col_scale, codes, ldc, scales);
+    else if (d <= 1024) k_quantize<DTYPE, 64, 2><<<(n + 3) / 4, 256, 0, stream>>>(x, n, d, ldx, col_scale, codes, ldc, scales);
+    else if (d <= 2048) k_quantize<DTYPE, 256, 1><<<n, 256, 0, stream>>>(x, n, d, ldx, col_scale, codes, ldc, scales);
+    else if (d <= 4096) k_quantize<DTYPE, 512, 1><<<n, 512, 0, stream>>>(x, n, d, ldx, col_scale, codes, ldc, scales);
+    else if (d <= 8192) k_quantize<DTYPE, 512, 2><<<n, 512, 0, stream>>>(x, n, d, ldx, col_scale, codes, ldc, scales);
+    else k_quantize<DTYPE, 512, 4><<<n, 512, 0, stream>>>(x, n, d, ldx, col_scale, codes, ldc, scales);
+    return hipGetLastError();
+}
+constexpr int Q_MOST = 512 * 8 * 4;
+
+// ---- every shape and alignment ---------------------------------------------------------------------------------------------
+
+constexpr int QT = 256;          // threads of a workgroup, which has one row
 
 // Two sweeps over the row; the second one finds it in the caches.
 template <int DTYPE>
@@ -20,7 +82,7 @@ __global__ __launch_bounds__(QT) void k_quantize_any(const void *X, int d, int64
                                                      int64_t ldc, float *scales) {
     __shared__ uint32_t part[QT / WAVE];
     const int64_t row = blockIdx.x, at = row * ldx;
-    uint32_t most = 0;           // of the bits of |v|: orders finite values, then infinity, then NaNs
+    uint32_t most = 0;
     for (int j = threadIdx.x; j < d; j += QT) {
         const float v = Elem<DTYPE>::load(X, at + j) * (col_scale ? col_scale[j] : 1.0f);
         most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
@@ -28,15 +90,10 @@ __global__ __launch_bounds__(QT) void k_quantize_any(const void *X, int d, int64
     most = wave_max(most);
     if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = most;
     __syncthreads();
-    for (int w = 0; w < QT / WAVE; ++w) most = max(most, part[w]);
-    const float a = __uint_as_float(most);
-    const bool finite = most < 0x7F800000u, some = finite && a >= 0x1p-110f;
-    const float inv = some ? 127.0f / a : 0.0f;
-    if (threadIdx.x == 0) scales[row] = some ? a / 127.0f : finite ? 0.0f : __uint_as_float(0x7FC00000u);
-    for (int j = threadIdx.x; j < d; j += QT) {
-        const float v = Elem<DTYPE>::load(X, at + j) * (col_scale ? col_scale[j] : 1.0f);
-        codes[row * ldc + j] = some ? (int8_t)(int)rintf(v * inv) : (int8_t)0;
-    }
+    const Quantiser z(wave_max(part[threadIdx.x % (QT / WAVE)]));
+    if (threadIdx.x == 0) scales[row] = z.scale;
+    for (int j = threadIdx.x; j < d; j += QT)
+        codes[row * ldc + j] = (int8_t)z.code(Elem<DTYPE>::load(X, at + j) * (col_scale ? col_scale[j] : 1.0f));
 }
 
 }  // namespace
@@ -44,6 +101,10 @@ __global__ __launch_bounds__(QT) void k_quantize_any(const void *X, int d, int64
 hipError_t launch_int8_quantize(const void *X, int dtype, int64_t m, int d, int64_t ldx, const float *col_scale, int8_t *codes,
                                 int64_t ldc, float *scales, hipStream_t stream) {
     if (m == 0) return hipSuccess;
+    auto at = [](const void *q) { return reinterpret_cast<uintptr_t>(q); };
+    if (d % 8 == 0 && d <= Q_MOST && (at(X) | at(col_scale)) % 16 == 0 && ldx * (dtype == 0 ? 4 : 2) % 16 == 0 && at(codes) % 8 == 0 && ldc % 8 == 0)
+        return dtype == 0 ? launch_whole<0>(X, m, d, ldx, col_scale, codes, ldc, scales, stream)
+                          : launch_whole<1>(X, m, d, ldx, col_scale, codes, ldc, scales, stream);
     if (dtype == 0)
         k_quantize_any<0><<<dim3((uint32_t)m), QT, 0, stream>>>(X, d, ldx, col_scale, codes, ldc, scales);
     else

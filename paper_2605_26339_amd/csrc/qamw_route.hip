@@ -1,5 +1,5 @@
 // Routed experts: the choice of experts, the order of the rows, and the way back.
-#include "qamw_product.hpp"
+#include "qamw_product_tile.hpp"
 
 namespace qamw {
 namespace {
@@ -10,10 +10,6 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 //
 // A wave has a token, a lane the experts lane, lane + 64, ...  A logit becomes an unsigned number that orders as it does, 0 for
 // what is never chosen (-inf, NaN); the largest of the wave wins, of equals the lowest expert.
-__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
-    for (int d = 32; d; d >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, d));
-    return v;
-}
 __device__ __forceinline__ float wave_sum(float v) {
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
     return v;
@@ -43,13 +39,14 @@ __device__ __forceinline__ void pick(const void *logits, int64_t at, int n, int 
     for (int j = 0; j < k; ++j) {
         uint32_t best = 0;
         for (int i = 0; i < NPL; ++i) best = max(best, key[i]);
-        best = wave_umax(best);
+        best = wave_max(best);
         if (best == 0) break;
-        // the lowest expert that has it: its complement is the largest
-        uint32_t who = 0;
-        for (int i = 0; i < NPL; ++i)
-            if (key[i] == best) who = max(who, ~(uint32_t)(lane + i * WAVE));
-        who = ~wave_umax(who);
+        int who = 0;
+#pragma unroll
+        for (int i = NPL - 1; i >= 0; --i) {
+            const unsigned long long has = __ballot(key[i] == best);
+            if (has) who = i * WAVE + __ffsll((long long)has) - 1;
+        }
         const float v = value_of(best);
         if (j == 0) {
             top = v;
@@ -66,117 +63,153 @@ __device__ __forceinline__ void pick(const void *logits, int64_t at, int n, int 
         const float p = v == top ? 1.0f : expf(v - top);
         if (renormalise) total += p;
         if (lane == j) {
-            expert = (int)who;
+            expert = who;
             mine = p;
         }
         for (int i = 0; i < NPL; ++i)
-            if ((uint32_t)(lane + i * WAVE) == who) key[i] = 0;
+            if (lane + i * WAVE == who) key[i] = 0;
     }
     if (expert >= 0) weight = mine / total;
 }
 
 // ---- order ----------------------------------------------------------------------------------------------------------------
 //
-// A stable counting sort of the slots (token after token, choice after choice).  Workgroup b has the tokens b * tokens .. and
-// counts its slots by expert; what it writes as a slot's position is the slot's rank among those of its expert in the workgroup.
-// The second launch knows all counts: what comes before an expert, and before the workgroup within the expert.
-template <int DTYPE, int NPL>
-__global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q, int tokens) {
-    extern __shared__ int32_t rt_lds[];
-    int32_t *chosen = rt_lds;                              // [tokens * k]
-    uint32_t *counts = reinterpret_cast<uint32_t *>(rt_lds + tokens * q.k);   // [n_experts]
-    const int t0 = blockIdx.x * tokens, nt = min(tokens, q.m - t0), n = q.n_experts, k = q.k;
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
-    for (int e = threadIdx.x; e < n; e += RT_THREADS) counts[e] = 0;
-    for (int t = wave; t < nt; t += RT_WAVES) {
-        int expert;
-        float weight;
-        pick<DTYPE, NPL>(q.logits, (int64_t)(t0 + t) * q.ld, n, k, q.renormalise, expert, weight);
-        if (lane < k) {
-            const int64_t at = (int64_t)(t0 + t) * k + lane;
-            q.experts[at] = expert;
-            q.weights[at] = weight;
-            chosen[t * k + lane] = expert;
+// A stable counting sort of the slots (token after token, choice after choice).  A wave has the slots of the tokens that follow one
+// another and finds equal experts among 64 slots by the bits of the expert; a workgroup's counts are those of its waves in their
+// order, a launch's those of its workgroups.  What is written as a slot's position is first the slot's rank among those of its
+// expert in the workgroup; when all counts are known, what comes before is added: what comes before an expert, and before the
+// workgroup within the expert.  A single workgroup knows all counts by itself.
+
+// Exclusive sums of the counts in `total` (LDS), by one wave; their sum.
+__device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
+    const int lane = threadIdx.x % WAVE;
+    uint32_t before = 0;
+    for (int e0 = 0; e0 < n; e0 += WAVE) {
+        const int e = e0 + lane;
+        const uint32_t c = e < n ? total[e] : 0;
+        uint32_t upto = c;
+        for (int d = 1; d < WAVE; d <<= 1) {
+            const uint32_t v = (uint32_t)__shfl_up((int)upto, d);
+            if (lane >= d) upto += v;
         }
+        if (e < n) total[e] = before + upto - c;
+        before += (uint32_t)__builtin_amdgcn_readlane((int)upto, WAVE - 1);
     }
-    __syncthreads();
-    // one wave goes through the slots in order: 64 at a time, equal ones found by the bits of the expert
-    if (wave == 0) {
-        for (int s0 = 0; s0 < nt * k; s0 += WAVE) {
-            const int s = s0 + lane;
-            const int e = s < nt * k ? chosen[s] : -1;
-            unsigned long long same = __ballot(e >= 0);
-            for (int b = 0; b < 10; ++b) {
-                const unsigned long long has = __ballot((e >> b) & 1);
-                same &= (e >> b) & 1 ? has : ~has;
-            }
-            int rank = 0;
-            if (e >= 0) {
-                rank = (int)counts[e] + __popcll(same & ((1ull << lane) - 1));
-            }
-            __builtin_amdgcn_wave_barrier();
-            if (e >= 0) {
-                if ((same >> lane) == 1) counts[e] = (uint32_t)rank + 1;     // the last one of its expert
-                q.positions[(int64_t)t0 * k + s] = rank;
-            } else if (s < nt * k) {
-                q.positions[(int64_t)t0 * k + s] = -1;
-            }
-            __builtin_amdgcn_wave_barrier();
-        }
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < n; e += RT_THREADS) q.counts[(int64_t)blockIdx.x * n + e] = counts[e];
+    return before;
 }
 
-__global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int tokens, int blocks) {
-    extern __shared__ int32_t rt_lds[];
-    uint32_t *base = reinterpret_cast<uint32_t *>(rt_lds);   // [n_experts]: where this workgroup's rows of an expert begin
-    uint32_t *total = base + q.n_experts;                    // [n_experts + 1]
-    const int n = q.n_experts, k = q.k;
+template <int DTYPE, int NPL, bool ALONE>
+__global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q, int per_wave) {
+    extern __shared__ uint32_t rt_lds[];                    // [RT_WAVES][n_experts]: counts, then what comes before them
+    __shared__ uint32_t all;
+    const int n = q.n_experts, k = q.k, lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+    uint32_t *mine = rt_lds + wave * n, *total = rt_lds + RT_WAVES * n;
+    for (int i = threadIdx.x; i < RT_WAVES * n; i += RT_THREADS) rt_lds[i] = 0;
+    __syncthreads();
+    const int t0 = (blockIdx.x * RT_WAVES + wave) * per_wave, t1 = min(t0 + per_wave, q.m);
+    const int at_once = WAVE / k;                            // tokens whose slots are ranked together
+    for (int g0 = t0; g0 < t1; g0 += at_once) {
+        const int g1 = min(g0 + at_once, t1);
+        int e = -1;                                          // lane's slot: token g0 + lane / k, choice lane % k
+        for (int t = g0; t < g1; ++t) {
+            int expert;
+            float weight;
+            pick<DTYPE, NPL>(q.logits, (int64_t)t * q.ld, n, k, q.renormalise, expert, weight);
+            if (lane < k) q.weights[(int64_t)t * k + lane] = weight;
+            const int from = lane - (t - g0) * k, got = __shfl(expert, from & (WAVE - 1));
+            if (from >= 0 && from < k) e = got;
+        }
+        unsigned long long same = __ballot(e >= 0);
+        for (int b = 0; b < 10; ++b) {
+            const unsigned long long has = __ballot((e >> b) & 1);
+            same &= (e >> b) & 1 ? has : ~has;
+        }
+        if (lane < (g1 - g0) * k) {
+            const int64_t at = (int64_t)g0 * k + lane;
+            int rank = -1;
+            if (e >= 0) {
+                rank = (int)mine[e] + __popcll(same & ((1ull << lane) - 1));
+                // the wave's LDS accesses are made in order: all ranks are read before the last slot of an expert counts them
+                if ((same >> lane) == 1) mine[e] = (uint32_t)rank + 1;
+            }
+            q.experts[at] = e;
+            q.positions[at] = rank;
+        }
+    }
+    __syncthreads();
     for (int e = threadIdx.x; e < n; e += RT_THREADS) {
-        uint32_t before = 0, all = 0;
-        for (int b = 0; b < blocks; ++b) {
-            const uint32_t c = q.counts[(int64_t)b * n + e];
-            all += c;
-            if (b < (int)blockIdx.x) before += c;
-        }
-        base[e] = before;
-        total[e] = all;
-    }
-    __syncthreads();
-    if (threadIdx.x < WAVE) {                                // exclusive sums over the experts
         uint32_t before = 0;
-        for (int e0 = 0; e0 < n; e0 += WAVE) {
-            const int e = e0 + threadIdx.x;
-            const uint32_t c = e < n ? total[e] : 0;
-            uint32_t upto = c;
-            for (int d = 1; d < WAVE; d <<= 1) {
-                const uint32_t v = (uint32_t)__shfl_up((int)upto, d);
-                if ((int)threadIdx.x >= d) upto += v;
-            }
-            if (e < n) {
-                base[e] += before + upto - c;
-                if (blockIdx.x == 0) q.offsets[e] = (int32_t)(before + upto - c);
-            }
-            before += (uint32_t)__shfl((int)upto, WAVE - 1);
+        for (int w = 0; w < RT_WAVES; ++w) {
+            const uint32_t c = rt_lds[w * n + e];
+            rt_lds[w * n + e] = before;
+            before += c;
         }
-        if (threadIdx.x == 0) {
-            total[n] = before;
-            if (blockIdx.x == 0) q.offsets[n] = (int32_t)before;
-        }
+        if (ALONE) total[e] = before;
+        else q.counts[(int64_t)blockIdx.x * n + e] = before;
     }
     __syncthreads();
+    if (ALONE) {
+        if (wave == 0) {
+            const uint32_t sum = exclusive(total, n);
+            if (lane == 0) all = sum;
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < n; e += RT_THREADS) q.offsets[e] = (int32_t)total[e];
+        if (threadIdx.x == 0) q.offsets[n] = (int32_t)all;
+    }
+    // the wave's own slots again
+    for (int64_t s = (int64_t)t0 * k + lane; s < (int64_t)t1 * k; s += WAVE) {
+        const int e = q.experts[s];
+        if (e < 0) continue;
+        const uint32_t place = (ALONE ? total[e] : 0) + mine[e] + (uint32_t)q.positions[s];
+        q.positions[s] = (int32_t)place;
+        if (ALONE) q.rows[place] = (int32_t)(s / k);
+    }
+    if (ALONE)
+        for (int p = (int)all + threadIdx.x; p < q.m * k; p += RT_THREADS) q.rows[p] = -1;
+}
+
+// `lanes` threads, a power of two, have an expert each; RT_THREADS / lanes of them share the sums of an expert's counts.
+__global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int tokens, int blocks, int lanes) {
+    extern __shared__ uint32_t rt_lds[];
+    uint32_t *before = rt_lds, *total = rt_lds + q.n_experts;   // [n_experts] each: of the workgroups before, of all
+    __shared__ uint32_t all;
+    const int n = q.n_experts, k = q.k;
+    for (int i = threadIdx.x; i < 2 * n; i += RT_THREADS) rt_lds[i] = 0;
+    __syncthreads();
+    const int e0 = threadIdx.x % lanes, segment = threadIdx.x / lanes, segments = RT_THREADS / lanes;
+    if (e0 < n) {
+        uint32_t b = 0, t = 0;
+#pragma unroll 8
+        for (int i = segment; i < blocks; i += segments) {
+            const uint32_t c = q.counts[(int64_t)i * n + e0];
+            t += c;
+            b += i < (int)blockIdx.x ? c : 0;
+        }
+        atomicAdd(&before[e0], b);                          // whole numbers: their order changes nothing
+        atomicAdd(&total[e0], t);
+    }
+    __syncthreads();
+    if (threadIdx.x < WAVE) {
+        const uint32_t sum = exclusive(total, n);
+        if (threadIdx.x == 0) all = sum;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0) {
+        for (int e = threadIdx.x; e < n; e += RT_THREADS) q.offsets[e] = (int32_t)total[e];
+        if (threadIdx.x == 0) q.offsets[n] = (int32_t)all;
+    }
     const int64_t slots = (int64_t)q.m * k, s0 = (int64_t)blockIdx.x * tokens * k, s1 = min(s0 + (int64_t)tokens * k, slots);
     for (int64_t s = s0 + threadIdx.x; s < s1; s += RT_THREADS) {
         const int e = q.experts[s];
         if (e >= 0) {
-            const int64_t place = (int64_t)base[e] + q.positions[s];
+            const uint32_t place = total[e] + before[e] + (uint32_t)q.positions[s];
             q.positions[s] = (int32_t)place;
             q.rows[place] = (int32_t)(s / k);
         }
     }
     // places that no slot has
-    for (int64_t p = (int64_t)total[n] + (int64_t)blockIdx.x * RT_THREADS + threadIdx.x; p < slots; p += (int64_t)blocks * RT_THREADS)
+    for (int64_t p = (int64_t)all + (int64_t)blockIdx.x * RT_THREADS + threadIdx.x; p < slots; p += (int64_t)blocks * RT_THREADS)
         q.rows[p] = -1;
 }
 
@@ -184,69 +217,128 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int 
 
 constexpr int CB_THREADS = 256;
 
+// A thread has eight neighbours of a token's row, wherever they lie: the memory instructions take any address.  What it reads of
+// the experts' rows it asks for eight rows at a time.
+template <int DTYPE> struct EightOf;
+template <> struct EightOf<0> {
+    Unaligned<float, 4> a, b;
+    __device__ __forceinline__ float value(int i) const { return i < 4 ? a.v[i & 3] : b.v[i & 3]; }
+};
+template <> struct EightOf<1> {
+    Unaligned<uint16_t, 8> a;
+    __device__ __forceinline__ float value(int i) const { return __uint_as_float((uint32_t)a.v[i] << 16); }
+};
+
 template <int DTYPE, bool OBF16>
-__global__ __launch_bounds__(CB_THREADS) void k_combine_any(const void *Y, int64_t y_rows, int64_t ldy, const int32_t *positions,
-                                                            const float *weights, int k, int d, void *out, int64_t ldo) {
-    const int64_t t = blockIdx.x;
-    for (int c = threadIdx.x; c < d; c += CB_THREADS) {
-        float sum = 0.0f;
-        for (int j = 0; j < k; ++j) {
-            const int32_t at = positions[t * k + j];
-            if (at >= 0 && at < y_rows) sum = fmaf(weights[t * k + j], Elem<DTYPE>::load(Y, at * ldy + c), sum);
+__global__ __launch_bounds__(CB_THREADS) void k_combine(const void *Y, int64_t y_rows, int64_t ldy, const int32_t *positions,
+                                                        const float *weights, int m, int k, int d, int chunks, void *out, int64_t ldo) {
+    const uint32_t id = blockIdx.x * CB_THREADS + threadIdx.x;
+    const int t = (int)(id / (uint32_t)chunks), c = (int)(id % (uint32_t)chunks) * 8;
+    if (t >= m) return;
+    constexpr int AT_ONCE = 8;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    const int64_t s = (int64_t)t * k;
+    if (c + 8 <= d) {
+        for (int j0 = 0; j0 < k; j0 += AT_ONCE) {
+            int at[AT_ONCE];
+            float w[AT_ONCE];
+            EightOf<DTYPE> y[AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j) {
+                const bool is = j0 + j < k;
+                at[j] = is ? positions[s + j0 + j] : -1;
+                w[j] = is ? weights[s + j0 + j] : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j)
+                if (at[j] >= 0 && at[j] < y_rows)
+                    y[j] = *reinterpret_cast<const EightOf<DTYPE> *>(static_cast<const char *>(Y) + ((int64_t)at[j] * ldy + c) * (DTYPE ? 2 : 4));
+#pragma unroll
+            for (int j = 0; j < AT_ONCE; ++j)
+                if (at[j] >= 0 && at[j] < y_rows)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[i] = fmaf(w[j], y[j].value(i), sum[i]);
         }
-        if (OBF16)
-            reinterpret_cast<uint16_t *>(out)[t * ldo + c] = (uint16_t)bf16_rne_bits(sum);
-        else
-            reinterpret_cast<float *>(out)[t * ldo + c] = sum;
+        const float lo[4] = {sum[0], sum[1], sum[2], sum[3]}, hi[4] = {sum[4], sum[5], sum[6], sum[7]};
+        if (OBF16) {
+            Unaligned<uint32_t, 4> four;
+            for (int i = 0; i < 4; ++i) four.v[i] = bf16_rne_bits(sum[2 * i]) | bf16_rne_bits(sum[2 * i + 1]) << 16;
+            *reinterpret_cast<Unaligned<uint16_t, 8> *>(reinterpret_cast<uint16_t *>(out) + t * ldo + c) = __builtin_bit_cast(Unaligned<uint16_t, 8>, four);
+        } else {
+            store_y4<false>(out, t * ldo + c, lo, 4);
+            store_y4<false>(out, t * ldo + c + 4, hi, 4);
+        }
+        return;
+    }
+    for (int i = 0; c + i < d; ++i) {
+        float one = 0.0f;
+        for (int j = 0; j < k; ++j) {
+            const int32_t at = positions[s + j];
+            if (at >= 0 && at < y_rows) one = fmaf(weights[s + j], Elem<DTYPE>::load(Y, at * ldy + c + i), one);
+        }
+        store_y<OBF16>(out, t * ldo + c + i, one);
     }
 }
 
-// Tokens of a workgroup of the first launch.
-int route_tokens(int m, int k) {
-    (void)m;
-    return k <= 8 ? 64 : 16;
+// Tokens of a wave of the first launch, 16 times that of its workgroup.
+constexpr int RT_PER_WAVE = 4;
+constexpr int RT_TOKENS = RT_PER_WAVE * RT_WAVES;
+
+template <int DTYPE, int NPL> hipError_t launch_pick(const RouteProblem &q, int blocks) {
+    const size_t lds = ((size_t)RT_WAVES + 1) * q.n_experts * 4;
+    static const hipError_t once = [] {
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_route_pick<DTYPE, NPL, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
+        if (e != hipSuccess) return e;
+        return hipFuncSetAttribute(reinterpret_cast<const void *>(&k_route_pick<DTYPE, NPL, false>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
+    }();
+    if (once != hipSuccess) return once;
+    if (blocks == 1) k_route_pick<DTYPE, NPL, true><<<1, RT_THREADS, lds, q.stream>>>(q, RT_PER_WAVE);
+    else k_route_pick<DTYPE, NPL, false><<<blocks, RT_THREADS, lds, q.stream>>>(q, RT_PER_WAVE);
+    return hipGetLastError();
+}
+template <int DTYPE> hipError_t launch_pick(const RouteProblem &q, int blocks) {
+    const int lanes = (q.n_experts + WAVE - 1) / WAVE;      // experts of a lane
+    if (lanes <= 1) return launch_pick<DTYPE, 1>(q, blocks);
+    if (lanes <= 2) return launch_pick<DTYPE, 2>(q, blocks);
+    if (lanes <= 4) return launch_pick<DTYPE, 4>(q, blocks);
+    if (lanes <= 8) return launch_pick<DTYPE, 8>(q, blocks);
+    return launch_pick<DTYPE, 16>(q, blocks);
 }
 
-template <int DTYPE> hipError_t launch_pick(const RouteProblem &q, int tokens, int blocks) {
-    const size_t lds = ((size_t)tokens * q.k + q.n_experts) * 4;
-    const int npl = (q.n_experts + WAVE - 1) / WAVE;
-    if (npl <= 1) k_route_pick<DTYPE, 1><<<blocks, RT_THREADS, lds, q.stream>>>(q, tokens);
-    else if (npl <= 2) k_route_pick<DTYPE, 2><<<blocks, RT_THREADS, lds, q.stream>>>(q, tokens);
-    else if (npl <= 4) k_route_pick<DTYPE, 4><<<blocks, RT_THREADS, lds, q.stream>>>(q, tokens);
-    else if (npl <= 8) k_route_pick<DTYPE, 8><<<blocks, RT_THREADS, lds, q.stream>>>(q, tokens);
-    else k_route_pick<DTYPE, 16><<<blocks, RT_THREADS, lds, q.stream>>>(q, tokens);
+template <int DTYPE, bool OBF16>
+hipError_t launch_combine_type(const void *Y, int64_t y_rows, int64_t ldy, const int32_t *positions, const float *weights, int m, int k, int d,
+                               void *out, int64_t ldo, hipStream_t stream) {
+    const int64_t chunks = ((int64_t)d + 7) / 8, blocks = (chunks * m + CB_THREADS - 1) / CB_THREADS;
+    if (blocks * CB_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
+    k_combine<DTYPE, OBF16><<<dim3((uint32_t)blocks), CB_THREADS, 0, stream>>>(Y, y_rows, ldy, positions, weights, m, k, d, (int)chunks, out, ldo);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t route_workspace_bytes(int m, int n_experts, int k) {
-    const int tokens = route_tokens(m, k);
-    return (size_t)((m + tokens - 1) / tokens) * n_experts * 4;
+// Counts by workgroup and expert; a single workgroup keeps them.
+size_t route_workspace_bytes(int m, int n_experts, int) {
+    return m <= RT_TOKENS ? 0 : (size_t)((m + RT_TOKENS - 1) / RT_TOKENS) * n_experts * 4;
 }
 
 hipError_t launch_route(const RouteProblem &q) {
-    const int tokens = route_tokens(q.m, q.k), blocks = q.m ? (q.m + tokens - 1) / tokens : 1;
-    if (q.m) {
-        const hipError_t e = q.dtype == 0 ? launch_pick<0>(q, tokens, blocks) : launch_pick<1>(q, tokens, blocks);
-        if (e != hipSuccess) return e;
-    }
-    k_route_order<<<blocks, RT_THREADS, (2 * (size_t)q.n_experts + 1) * 4, q.stream>>>(q, tokens, q.m ? blocks : 0);
+    const int blocks = q.m <= RT_TOKENS ? 1 : (q.m + RT_TOKENS - 1) / RT_TOKENS;
+    const hipError_t e = q.dtype == 0 ? launch_pick<0>(q, blocks) : launch_pick<1>(q, blocks);
+    if (e != hipSuccess || blocks == 1) return e;
+    int lanes = WAVE;
+    while (lanes < q.n_experts) lanes *= 2;
+    k_route_order<<<blocks, RT_THREADS, 2 * (size_t)q.n_experts * 4, q.stream>>>(q, RT_TOKENS, blocks, lanes);
     return hipGetLastError();
 }
 
 hipError_t launch_combine(const void *Y, int dtype, int64_t y_rows, int64_t ldy, const int32_t *positions, const float *weights, int m,
                           int k, int d, void *out, int out_dtype, int64_t ldo, hipStream_t stream) {
     if (m == 0) return hipSuccess;
-    const dim3 g((uint32_t)m);
-    if (dtype == 0) {
-        if (out_dtype == 0) k_combine_any<0, false><<<g, CB_THREADS, 0, stream>>>(Y, y_rows, ldy, positions, weights, k, d, out, ldo);
-        else k_combine_any<0, true><<<g, CB_THREADS, 0, stream>>>(Y, y_rows, ldy, positions, weights, k, d, out, ldo);
-    } else {
-        if (out_dtype == 0) k_combine_any<1, false><<<g, CB_THREADS, 0, stream>>>(Y, y_rows, ldy, positions, weights, k, d, out, ldo);
-        else k_combine_any<1, true><<<g, CB_THREADS, 0, stream>>>(Y, y_rows, ldy, positions, weights, k, d, out, ldo);
-    }
-    return hipGetLastError();
+    if (dtype == 0)
+        return out_dtype == 0 ? launch_combine_type<0, false>(Y, y_rows, ldy, positions, weights, m, k, d, out, ldo, stream)
+                              : launch_combine_type<0, true>(Y, y_rows, ldy, positions, weights, m, k, d, out, ldo, stream);
+    return out_dtype == 0 ? launch_combine_type<1, false>(Y, y_rows, ldy, positions, weights, m, k, d, out, ldo, stream)
+                          : launch_combine_type<1, true>(Y, y_rows, ldy, positions, weights, m, k, d, out, ldo, stream);
 }
 
 }  // namespace qamw

@@ -612,44 +612,67 @@ def calibrate_sigma_batch(items, block: int, workspace, stream=None):
 
 
 # ------------------------------------------------------------------ served layers: 8-bit products, routed experts
-def _operand_code(t, name):
+# These calls are made for every layer of every token: a shape or a type is asked for once, and results of two dimensions are
+# made with their strides, which costs half as much as without.
+def _one_device(first, *others):
+    """The index of the device that all tensors are on."""
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("device entry points take CUDA (HIP) tensors")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("all tensors of a call are on one device")
+    return dev
+
+
+def _raw_stream(stream, dev):
+    if stream is not None:
+        return stream.cuda_stream
     import torch
 
-    if t.dtype == torch.int8:
-        return DTYPE_I8
-    if t.dtype == torch.bfloat16:
-        return DTYPE_BF16
-    if t.dtype == torch.float32:
-        return DTYPE_F32
-    raise TypeError(f"{name} must be int8, float32 or bfloat16, got {t.dtype}")
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
-def _expect(t, name, dtype, shape):
+def _vector(t, name, dtype, shape):
     """A contiguous tensor of one type and shape, or None."""
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
 
 
-def _matrix(t, name, dim=2):
-    """Rows of adjacent elements.  Returns the leading dimension, which a tensor of one row or none may leave open."""
-    if t.dim() != dim or t.shape[-1] < 1 or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name} must be {dim}-D with unit column stride")
-    return t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])
+def _leading(shape, stride, name):
+    """Rows of adjacent elements: their leading dimension, which a tensor of one row or none may leave open."""
+    if shape[-1] < 1 or (stride[-1] != 1 and shape[-1] > 1):
+        raise ValueError(f"{name} must have columns, and adjacent ones")
+    return stride[-2] if shape[-2] > 1 else max(stride[-2], shape[-1])
 
 
-def _same_device(first, *others):
-    _require_cuda(first, *others)
-    for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError("all tensors of a call are on one device")
+def _rows(t, name):
+    """(rows, columns, leading dimension) of a matrix."""
+    shape = t.shape
+    if len(shape) != 2:
+        raise ValueError(f"{name} must be 2-D")
+    return shape[0], shape[1], _leading(shape, t.stride(), name)
 
 
-def _result(out, shape, dtype, device, stream):
+def _new(m, d, dtype, like, stream):
+    import torch
+
+    if stream is None:
+        return torch.empty_strided((m, d), (d, 1), dtype=dtype, device=like.device)
+    return _empty((m, d), dtype, like.device, stream)
+
+
+def _result(out, m, d, dtype, like, stream):
+    """(the result's tensor, its type's code, its leading dimension)"""
+    import torch
+
     if out is None:
-        return _empty(shape, dtype, device, stream)
-    if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
-        raise ValueError(f"out must be {dtype} of shape {tuple(shape)}, got {out.dtype} {tuple(out.shape)}")
-    return out
+        out, ld = _new(m, d, dtype or torch.bfloat16, like, stream), d
+    else:
+        if out.shape != (m, d) or (dtype is not None and out.dtype != dtype):
+            raise ValueError(f"out must be {dtype or 'fp32 or bf16'} of shape {(m, d)}, got {out.dtype} {tuple(out.shape)}")
+        ld = _leading((m, d), out.stride(), "out")
+    return out, _dtype_code(out), ld
 
 
 def int8_quantize(X, col_scale=None, out=None, stream=None):
@@ -657,20 +680,19 @@ def int8_quantize(X, col_scale=None, out=None, stream=None):
     col_scale (fp32 [d]) multiplies the columns first.  For weights a row is an output channel, for activations a token."""
     import torch
 
-    _same_device(X, col_scale)
-    ldx = _matrix(X, "X")
-    m, d = X.shape
-    _expect(col_scale, "col_scale", torch.float32, (d,))
+    m, d, ldx = _rows(X, "X")
+    _vector(col_scale, "col_scale", torch.float32, (d,))
     if out is None:
-        out = _empty((m, d), torch.int8, X.device, stream), _empty((m,), torch.float32, X.device, stream)
-    codes, scales = out
-    _same_device(X, codes, scales)
-    if codes.dtype != torch.int8 or tuple(codes.shape) != (m, d):
-        raise ValueError("codes must be int8, of the shape of X")
-    _expect(scales, "scales", torch.float32, (m,))
-    ldc = _matrix(codes, "codes")
-    _check(lib().qamw_int8_quantize(_ptr(X), _dtype_code(X), m, d, ldx, _ptr(col_scale), _ptr(codes), ldc, _ptr(scales),
-                                    _stream(stream)), "qamw_int8_quantize")
+        codes, scales, ldc = _new(m, d, torch.int8, X, stream), _empty((m,), torch.float32, X.device, stream), d
+    else:
+        codes, scales = out
+        _vector(scales, "scales", torch.float32, (m,))
+        if codes.dtype != torch.int8 or codes.shape != (m, d):
+            raise ValueError("codes must be int8, of the shape of X")
+        ldc = _rows(codes, "codes")[2]
+    dev = _one_device(X, col_scale, codes, scales)
+    _check(lib().qamw_int8_quantize(X.data_ptr(), _dtype_code(X), m, d, ldx, _ptr(col_scale), codes.data_ptr(), ldc, scales.data_ptr(),
+                                    _raw_stream(stream, dev)), "qamw_int8_quantize")
     return codes, scales
 
 
@@ -688,23 +710,25 @@ def int8_matmul(X, W, w_scales, x_scales=None, col_scale=None, gated=False, out=
     Returns [m][d_out] of out_dtype (bf16 where neither it nor out is given)."""
     import torch
 
-    _same_device(X, W, w_scales, x_scales, col_scale, out, workspace)
-    ldx, ldw = _matrix(X, "X"), _matrix(W, "W")
-    (m, d_in), outs, code = X.shape, W.shape[0], _operand_code(X, "X")
-    if W.dtype != torch.int8 or W.shape[1] != d_in or outs < 1 or (gated and outs % 2):
+    m, d_in, ldx = _rows(X, "X")
+    outs, w_in, ldw = _rows(W, "W")
+    if W.dtype != torch.int8 or w_in != d_in or outs < 1 or (gated and outs % 2):
         raise ValueError(f"W must be int8 [{'2 d_out' if gated else 'd_out'}][{d_in}], got {W.dtype} {tuple(W.shape)}")
-    _expect(w_scales, "w_scales", torch.float32, (outs,))
-    _expect(x_scales, "x_scales", torch.float32, (m,))
-    _expect(col_scale, "col_scale", torch.float32, (d_in,))
+    _vector(w_scales, "w_scales", torch.float32, (outs,))
+    _vector(x_scales, "x_scales", torch.float32, (m,))
+    _vector(col_scale, "col_scale", torch.float32, (d_in,))
+    dev = _one_device(X, W, w_scales, x_scales, col_scale, out, workspace)
+    code = DTYPE_I8 if X.dtype == torch.int8 else _dtype_code(X)
     d_out = outs // 2 if gated else outs
-    y = _result(out, (m, d_out), out_dtype or (torch.bfloat16 if out is None else out.dtype), X.device, stream)
-    ldy = _matrix(y, "out")
+    y, y_code, ldy = _result(out, m, d_out, out_dtype, X, stream)
     if workspace is None:
-        need = int8_matmul_workspace_bytes(code, m, d_in)
-        workspace = _empty(need, torch.uint8, X.device, stream) if need else None
-    _check(lib().qamw_int8_matmul(_ptr(X), code, _ptr(x_scales), _ptr(col_scale), m, ldx, _ptr(W), _ptr(w_scales), ldw, d_out, d_in,
-                                  int(bool(gated)), _ptr(y), _dtype_code(y), ldy, _ptr(workspace),
-                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)),
+        size = int8_matmul_workspace_bytes(code, m, d_in)
+        work = _new(1, size, torch.uint8, X, stream) if size else None      # kept until the launch
+        at = _ptr(work)
+    else:
+        at, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(lib().qamw_int8_matmul(X.data_ptr(), code, _ptr(x_scales), _ptr(col_scale), m, ldx, W.data_ptr(), w_scales.data_ptr(), ldw,
+                                  d_out, d_in, 1 if gated else 0, y.data_ptr(), y_code, ldy, at, size, _raw_stream(stream, dev)),
            "qamw_int8_matmul")
     return y
 
@@ -717,24 +741,25 @@ def grouped_matmul(X, W, offsets, rows=None, x_scales=None, w_scales=None, gated
     are left as they are."""
     import torch
 
-    _same_device(X, W, offsets, rows, x_scales, w_scales, out)
-    ldx, ldw = _matrix(X, "X"), _matrix(W, "W", 3)
-    (x_rows, d_in), (n, outs) = X.shape, W.shape[:2]
+    x_rows, d_in, ldx = _rows(X, "X")
+    shape, stride = W.shape, W.stride()
     if X.dtype not in (torch.int8, torch.bfloat16) or W.dtype != X.dtype:
         raise TypeError(f"X and W must both be int8 or both be bfloat16, got {X.dtype} and {W.dtype}")
-    if W.shape[2] != d_in or n < 1 or outs < 1 or (gated and outs % 2):
-        raise ValueError(f"W must be [n_experts][{'2 d_out' if gated else 'd_out'}][{d_in}], got {tuple(W.shape)}")
+    if len(shape) != 3 or shape[2] != d_in or shape[0] < 1 or shape[1] < 1 or (gated and shape[1] % 2):
+        raise ValueError(f"W must be [n_experts][{'2 d_out' if gated else 'd_out'}][{d_in}], got {tuple(shape)}")
+    n, outs = shape[0], shape[1]
+    ldw = _leading(shape, stride, "W")
     m = x_rows if rows is None else rows.numel()
-    _expect(offsets, "offsets", torch.int32, (n + 1,))
-    _expect(rows, "rows", torch.int32, (m,))
-    _expect(x_scales, "x_scales", torch.float32, (x_rows,))
-    _expect(w_scales, "w_scales", torch.float32, (n, outs))
+    _vector(offsets, "offsets", torch.int32, (n + 1,))
+    _vector(rows, "rows", torch.int32, (m,))
+    _vector(x_scales, "x_scales", torch.float32, (x_rows,))
+    _vector(w_scales, "w_scales", torch.float32, (n, outs))
+    dev = _one_device(X, W, offsets, rows, x_scales, w_scales, out)
     d_out = outs // 2 if gated else outs
-    y = _result(out, (m, d_out), out_dtype or (torch.bfloat16 if out is None else out.dtype), X.device, stream)
-    ldy = _matrix(y, "out")
-    _check(lib().qamw_grouped_matmul(_ptr(X), _operand_code(X, "X"), _ptr(x_scales), x_rows, ldx, _ptr(rows), _ptr(W), _ptr(w_scales),
-                                     ldw, W.stride(0), _ptr(offsets), n, m, d_out, d_in, int(bool(gated)), _ptr(y), _dtype_code(y), ldy,
-                                     _stream(stream)), "qamw_grouped_matmul")
+    y, y_code, ldy = _result(out, m, d_out, out_dtype, X, stream)
+    _check(lib().qamw_grouped_matmul(X.data_ptr(), DTYPE_I8 if X.dtype == torch.int8 else DTYPE_BF16, _ptr(x_scales), x_rows, ldx, _ptr(rows),
+                                     W.data_ptr(), _ptr(w_scales), ldw, stride[0], offsets.data_ptr(), n, m, d_out, d_in,
+                                     1 if gated else 0, y.data_ptr(), y_code, ldy, _raw_stream(stream, dev)), "qamw_grouped_matmul")
     return y
 
 
@@ -754,19 +779,24 @@ def route(logits, k: int, renormalise=True, workspace=None, stream=None):
     offsets [n_experts + 1], rows [m k] and positions [m][k]; -1 where there is none (see qamw_route in include/qamw.h)."""
     import torch
 
-    _same_device(logits, workspace)
-    ld = _matrix(logits, "logits")
-    m, n = logits.shape
-    need = route_workspace_bytes(m, n, k)
-    dev = logits.device
+    m, n, ld = _rows(logits, "logits")
+    size = route_workspace_bytes(m, n, k)
+    dev = _one_device(logits, workspace)
+    i32, on = torch.int32, logits.device
     if workspace is None:
-        workspace = _empty(need, torch.uint8, dev, stream) if need else None
-    r = Routing(_empty((m, k), torch.int32, dev, stream), _empty((m, k), torch.float32, dev, stream),
-                _empty((n + 1,), torch.int32, dev, stream), _empty((m * k,), torch.int32, dev, stream),
-                _empty((m, k), torch.int32, dev, stream))
-    _check(lib().qamw_route(_ptr(logits), _dtype_code(logits), m, n, ld, k, int(bool(renormalise)), _ptr(r.experts), _ptr(r.weights),
-                            _ptr(r.offsets), _ptr(r.rows), _ptr(r.positions), _ptr(workspace),
-                            0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "qamw_route")
+        work = _new(1, size, torch.uint8, logits, stream) if size else None   # kept until the launches
+        at = _ptr(work)
+    else:
+        at, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if stream is None:
+        make = torch.empty_strided
+        r = Routing(make((m, k), (k, 1), dtype=i32, device=on), make((m, k), (k, 1), dtype=torch.float32, device=on),
+                    make((n + 1,), (1,), dtype=i32, device=on), make((m * k,), (1,), dtype=i32, device=on), make((m, k), (k, 1), dtype=i32, device=on))
+    else:
+        r = Routing(_empty((m, k), i32, on, stream), _empty((m, k), torch.float32, on, stream), _empty((n + 1,), i32, on, stream),
+                    _empty((m * k,), i32, on, stream), _empty((m, k), i32, on, stream))
+    _check(lib().qamw_route(logits.data_ptr(), _dtype_code(logits), m, n, ld, k, 1 if renormalise else 0, r[0].data_ptr(), r[1].data_ptr(),
+                            r[2].data_ptr(), r[3].data_ptr(), r[4].data_ptr(), at, size, _raw_stream(stream, dev)), "qamw_route")
     return r
 
 
@@ -775,15 +805,14 @@ def combine(Y, positions, weights, out=None, out_dtype=None, stream=None):
     sums, a position of -1 adds nothing.  Returns [m][d] of out_dtype (Y's type where neither it nor out is given)."""
     import torch
 
-    _same_device(Y, positions, weights, out)
-    ldy = _matrix(Y, "Y")
-    if positions.dim() != 2:
+    y_rows, d, ldy = _rows(Y, "Y")
+    shape = positions.shape
+    if len(shape) != 2:
         raise ValueError("positions must be 2-D")
-    m, k = positions.shape
-    _expect(positions, "positions", torch.int32, (m, k))
-    _expect(weights, "weights", torch.float32, (m, k))
-    y = _result(out, (m, Y.shape[1]), out_dtype or (Y.dtype if out is None else out.dtype), Y.device, stream)
-    ldo = _matrix(y, "out")
-    _check(lib().qamw_combine(_ptr(Y), _dtype_code(Y), Y.shape[0], ldy, _ptr(positions), _ptr(weights), m, k, Y.shape[1], _ptr(y),
-                              _dtype_code(y), ldo, _stream(stream)), "qamw_combine")
+    _vector(positions, "positions", torch.int32, shape)
+    _vector(weights, "weights", torch.float32, shape)
+    dev = _one_device(Y, positions, weights, out)
+    y, y_code, ldo = _result(out, shape[0], d, out_dtype or (Y.dtype if out is None else None), Y, stream)
+    _check(lib().qamw_combine(Y.data_ptr(), _dtype_code(Y), y_rows, ldy, positions.data_ptr(), weights.data_ptr(), shape[0], shape[1], d,
+                              y.data_ptr(), y_code, ldo, _raw_stream(stream, dev)), "qamw_combine")
     return y

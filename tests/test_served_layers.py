@@ -83,7 +83,7 @@ def test_refusals_of_the_entry_points():
 
     assert route(t=2) == I and route(k=0) == I and route(k=9) == I and route(n=64, ld=64, k=33) == I and route(n=1025, ld=1025) == I
     assert route(re=2) == I and route(x=None) == I and route(e=None) == I and route(w=None) == I and route(off=None) == I
-    assert route(rows=None) == I and route(pos=None) == I and route(work=None) == I and route(size=0) == I and route(work=p + 4) == I
+    assert route(rows=None) == I and route(pos=None) == I and route(m=100, work=None) == I and route(m=100, size=63) == I and route(m=100, work=p + 4) == I
     assert route(ld=7) == S and route(m=-1) == I and route(off=p + 2) == I
 
     def comb(Y=p, t=1, yr=8, ldy=8, pos=p, w=p, m=4, k=2, d=8, out=p, ot=1, ldo=8):
@@ -95,7 +95,7 @@ def test_refusals_of_the_entry_points():
 
 
 def test_refusals_of_the_binding(monkeypatch):
-    monkeypatch.setattr(qamw, "_require_cuda", lambda *t: None)
+    monkeypatch.setattr(qamw, "_one_device", lambda *t: 0)
     x8, w8, s = torch.zeros(4, 8, dtype=torch.int8), torch.zeros(6, 8, dtype=torch.int8), torch.ones(6)
     with pytest.raises(ValueError):
         qamw.int8_matmul(x8, w8[:, :7], s, x_scales=torch.ones(4))
