@@ -3,8 +3,8 @@
 // A workgroup of eight waves has a tile of BN rows of W and BM of X and steps over 64 bytes of both at a time (a stage: 64
 // columns of int8, 32 of bf16).  16 rows of a stage are a fragment, 1 KB in LDS, filled by one buffer load of a wave that goes
 // to LDS directly and read by one 16-byte LDS read of a wave: the operand of a 16x16 matrix instruction.
-//   In LDS the four 16-byte pieces of a row are exchanged by (row / 4) mod 4, or sixteen lanes of a read would meet in a
-//   quarter of the banks; the loading lanes ask for their piece accordingly, from the same 64 bytes.
+//   In LDS the four 16-byte pieces of a row are exchanged by (row / 2) mod 4, or the lanes of a read would meet in half of
+//   the banks; the loading lanes ask for their piece accordingly, from the same 64 bytes.
 //   Four stages are in LDS: one is read, the next ones are on their way while two others' products run, which covers the latency of memory.
 //   The waves form two groups of four, one wave of each group on every SIMD.  While one group reads its fragments the other
 //   multiplies, then they change places; a barrier is all that they need to keep in step.
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     const int bytes = a.d_in * M::ELEM, stages = (bytes + PW_KB - 1) / PW_KB;
     const char *wp = a.W + (int64_t)et.expert * a.expert_stride;
     const char *xp = a.rows ? a.X : a.X + (int64_t)row0 * a.ldx;
-    const int lr = lane >> 2, piece = ((lane & 3) ^ (lane >> 4)) * 16;
+    const int lr = lane >> 2, piece = ((lane ^ (lane >> 3)) & 3) * 16;
     const bool past = (stages - 1) * PW_KB + piece >= bytes;                  // nothing there in the last stage
     uint32_t off_w[S::LW], off_x[S::LX];
 #pragma unroll
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     };
 
     const int wn = wave % S::WN, wm = wave / S::WN;
-    const uint32_t mine = (uint32_t)((lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 2) & 3)) * 16));
+    const uint32_t mine = (uint32_t)((lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 1) & 3)) * 16));
     const uint32_t read_w = lds0 + mine + wn * S::FN * PW_FRAG, read_x = lds0 + mine + (S::NW + wm * S::FM) * PW_FRAG;
     typename M::acc_t acc[S::FN][S::FM] = {};
     constexpr int L = S::LW + S::LX;
