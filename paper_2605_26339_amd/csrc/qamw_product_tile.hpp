@@ -154,6 +154,13 @@ struct Quantiser {
 // rounding, for a fifth of the instructions.  exp overflows to infinity, whose reciprocal is 0.
 __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
+// Two values rounded to bf16 (nearest, ties to even).
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{lo, hi}), b2));
+}
+
 // Four neighbours of a row of Y, or of the scales of W, wherever they lie: the memory instructions take any address.
 template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Unaligned {
     T v[N];
@@ -162,7 +169,7 @@ template <typename T, int N> struct __attribute__((packed, aligned(sizeof(T)))) 
 template <bool BF16> __device__ __forceinline__ void store_y4(void *Y, int64_t at, const float (&v)[4], int n) {
     if (n >= 4) {
         if (BF16) {
-            const uint2 two = {bf16_rne_bits(v[0]) | bf16_rne_bits(v[1]) << 16, bf16_rne_bits(v[2]) | bf16_rne_bits(v[3]) << 16};
+            const uint2 two = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
             *reinterpret_cast<Unaligned<uint16_t, 4> *>(reinterpret_cast<uint16_t *>(Y) + at) = __builtin_bit_cast(Unaligned<uint16_t, 4>, two);
         } else {
             *reinterpret_cast<Unaligned<float, 4> *>(reinterpret_cast<float *>(Y) + at) = Unaligned<float, 4>{{v[0], v[1], v[2], v[3]}};

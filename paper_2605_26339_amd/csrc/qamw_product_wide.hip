@@ -15,7 +15,7 @@
 namespace qamw {
 namespace {
 
-constexpr int PW_WAVES = 8, PW_THREADS = PW_WAVES * WAVE, PW_STAGES = 4, PW_FRAG = 1024, PW_KB = 64;
+constexpr int PW_WAVES = 8, PW_THREADS = PW_WAVES * WAVE, PW_STAGES = 4, PW_FRAG = 1024, PW_KB = 64, PW_CUS = 256, PW_TURN = 2048;
 constexpr uint32_t PW_NOWHERE = 0x80000000u;       // added to an offset: beyond the end of any buffer here
 
 // Tiles: WN x WM waves, each of FN fragments of W and FM of X.
@@ -27,38 +27,103 @@ template <int WN_, int FN_, int WM_, int FM_> struct Shape {
     static_assert(WN * WM == PW_WAVES && NW % PW_WAVES == 0, "");
 };
 
-// FN + FM fragments of one stage, complete when this returns.
-template <int FN, int FM>
-__device__ __forceinline__ void read_fragments(uint32_t at_w, uint32_t at_x, pr_i32x4_t (&w)[FN], pr_i32x4_t (&x)[FM]) {
-    static_assert(FM == 4, "");
+// FN + FM fragments of one stage are read, and LW + LX pieces of a stage to come are asked for while they come: the loads' issue
+// takes as long as the reads.  The fragments are complete when this returns.  `to`: where the first piece goes, the others 8 KB on each.
+typedef uint32_t pw_u32x4_t __attribute__((ext_vector_type(4)));
+template <int FN, int FM, int LW, int LX>
+__device__ __forceinline__ void read_and_request(uint32_t at_w, uint32_t at_x, pr_i32x4_t (&w)[FN], pr_i32x4_t (&x)[FM], const uint32_t (&off_w)[LW],
+                                                 const uint32_t (&off_x)[LX], pw_u32x4_t wr, pw_u32x4_t xr, uint32_t so, uint32_t to) {
+    static_assert(FM == 4 && LW == 2 && LX == (FN == 8 ? 2 : 1), "");
     if constexpr (FN == 8) {
         asm volatile(
-            "ds_read_b128 %8, %13\n\tds_read_b128 %9, %13 offset:1024\n\tds_read_b128 %10, %13 offset:2048\n\tds_read_b128 %11, %13 offset:3072\n\t"
-            "ds_read_b128 %0, %12\n\tds_read_b128 %1, %12 offset:1024\n\tds_read_b128 %2, %12 offset:2048\n\tds_read_b128 %3, %12 offset:3072\n\t"
-            "ds_read_b128 %4, %12 offset:4096\n\tds_read_b128 %5, %12 offset:5120\n\tds_read_b128 %6, %12 offset:6144\n\tds_read_b128 %7, %12 offset:7168\n\t"
+            "ds_read_b128 %8, %13\n\t"
+            "ds_read_b128 %9, %13 offset:1024\n\t"
+            "ds_read_b128 %10, %13 offset:2048\n\t"
+            "ds_read_b128 %11, %13 offset:3072\n\t"
+            "ds_read_b128 %0, %12\n\t"
+            "ds_read_b128 %1, %12 offset:1024\n\t"
+            "ds_read_b128 %2, %12 offset:2048\n\t"
+            "ds_read_b128 %3, %12 offset:3072\n\t"
+            "ds_read_b128 %4, %12 offset:4096\n\t"
+            "ds_read_b128 %5, %12 offset:5120\n\t"
+            "ds_read_b128 %6, %12 offset:6144\n\t"
+            "ds_read_b128 %7, %12 offset:7168\n\t"
+            "s_mov_b32 m0, %21\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %14, %18, %20 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x2000\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %15, %18, %20 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x2000\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %16, %19, %20 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x2000\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %17, %19, %20 offen lds\n\t"
             "s_waitcnt lgkmcnt(0)"
             : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7]), "=&v"(x[0]),
               "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-            : "v"(at_w), "v"(at_x)
-            : "memory");
+            : "v"(at_w), "v"(at_x), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "v"(off_x[1]), "s"(wr), "s"(xr), "s"(so), "s"(to)
+            : "memory", "scc");
     } else if constexpr (FN == 4) {
         asm volatile(
-            "ds_read_b128 %4, %9\n\tds_read_b128 %5, %9 offset:1024\n\tds_read_b128 %6, %9 offset:2048\n\tds_read_b128 %7, %9 offset:3072\n\t"
-            "ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:1024\n\tds_read_b128 %2, %8 offset:2048\n\tds_read_b128 %3, %8 offset:3072\n\t"
+            "ds_read_b128 %4, %9\n\t"
+            "ds_read_b128 %5, %9 offset:1024\n\t"
+            "ds_read_b128 %6, %9 offset:2048\n\t"
+            "ds_read_b128 %7, %9 offset:3072\n\t"
+            "ds_read_b128 %0, %8\n\t"
+            "ds_read_b128 %1, %8 offset:1024\n\t"
+            "ds_read_b128 %2, %8 offset:2048\n\t"
+            "ds_read_b128 %3, %8 offset:3072\n\t"
+            "s_mov_b32 m0, %16\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %10, %13, %15 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x2000\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %11, %13, %15 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x2000\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %12, %14, %15 offen lds\n\t"
             "s_waitcnt lgkmcnt(0)"
             : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-            : "v"(at_w), "v"(at_x)
-            : "memory");
+            : "v"(at_w), "v"(at_x), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "s"(wr), "s"(xr), "s"(so), "s"(to)
+            : "memory", "scc");
     } else {
         static_assert(FN == 2, "");
         asm volatile(
-            "ds_read_b128 %2, %7\n\tds_read_b128 %3, %7 offset:1024\n\tds_read_b128 %4, %7 offset:2048\n\tds_read_b128 %5, %7 offset:3072\n\t"
-            "ds_read_b128 %0, %6\n\tds_read_b128 %1, %6 offset:1024\n\t"
+            "ds_read_b128 %2, %7\n\t"
+            "ds_read_b128 %3, %7 offset:1024\n\t"
+            "ds_read_b128 %4, %7 offset:2048\n\t"
+            "ds_read_b128 %5, %7 offset:3072\n\t"
+            "ds_read_b128 %0, %6\n\t"
+            "ds_read_b128 %1, %6 offset:1024\n\t"
+            "s_mov_b32 m0, %14\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %8, %11, %13 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x2000\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %9, %11, %13 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x2000\n\t"
+            "s_nop 0\n\t"
+            "buffer_load_dwordx4 %10, %12, %13 offen lds\n\t"
             "s_waitcnt lgkmcnt(0)"
             : "=&v"(w[0]), "=&v"(w[1]), "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-            : "v"(at_w), "v"(at_x)
-            : "memory");
+            : "v"(at_w), "v"(at_x), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "s"(wr), "s"(xr), "s"(so), "s"(to)
+            : "memory", "scc");
     }
+}
+
+// The same pieces without the reads, and four bytes a lane.
+template <int LW, int LX>
+__device__ __forceinline__ void request(const uint32_t (&off_w)[LW], const uint32_t (&off_x)[LX], pw_u32x4_t wr, pw_u32x4_t xr, uint32_t so, uint32_t to) {
+#pragma unroll
+    for (int i = 0; i < LW + LX; ++i)
+        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(i < LW ? off_w[i < LW ? i : 0] : off_x[i < LW ? 0 : i - LW]),
+                     "s"(i < LW ? wr : xr), "s"(so), "s"(to + i * PW_WAVES * PW_FRAG)
+                     : "memory");
+}
+__device__ __forceinline__ void request_dword(uint32_t off, pw_u32x4_t from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(off), "s"(from), "s"(to) : "memory");
 }
 
 template <int N> __device__ __forceinline__ void wait_loads() {
@@ -69,83 +134,132 @@ __device__ __forceinline__ void meet() {
     asm volatile("s_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
+__device__ __forceinline__ pw_u32x4_t resource(const void *p, uint32_t records = 0x7FFFFFFF) {
+    return {(uint32_t)(uintptr_t)p, (uint32_t)((uintptr_t)p >> 32) & 0xFFFFu, records, 0x00020000u};
+}
+
+template <bool BF16> struct Store {
+    using type = float;
+};
+template <> struct Store<true> {
+    using type = uint16_t;
+};
+
+// A tile: where its rows are, and what this lane asks for of them.
+template <typename S> struct Tile {
+    int expert, row0, n, ct;                         // rows row0 .. row0 + n, the ct-th columns; n = 0: no tile
+    const char *w, *x;
+    uint32_t off_w[S::LW], off_x[S::LX], off_scale;
+};
 
 template <bool I8, bool GATED, bool YBF16, typename S>
-__global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, int col_tiles, int group) {
+__global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, int col_tiles, int group, int whole) {
     using M = Mfma<I8>;
     extern __shared__ __align__(16) char pw_lds[];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)pw_lds;
+    const uint32_t turn = lds0 + PW_STAGES * S::STAGE + wave * PW_TURN, scales0 = lds0 + PW_STAGES * S::STAGE + PW_WAVES * PW_TURN;
 
     // Workgroups go to the 8 XCDs in turn: an XCD gets tiles that follow one another, and these are ordered such that `group` row
     // tiles share their W while it is in the XCD's cache.
-    const int row_tiles = count_tiles<S::BM>(a);
-    const uint32_t all = (uint32_t)row_tiles * (uint32_t)col_tiles, share = (all + 7) / 8;
-    const uint32_t nth = blockIdx.x / 8;
-    const uint32_t t = (blockIdx.x % 8) * share + nth;
-    if (nth >= share || t >= all) return;
-    const ExpertTiles et = find_expert<S::BM>(a, (int)(t / (uint32_t)col_tiles));
-    if (et.tiles == 0) return;
-    const uint32_t v = t - (uint32_t)et.first * (uint32_t)col_tiles, per = (uint32_t)(group * col_tiles);
-    const int g0 = (int)(v / per) * group, rows_in = min(group, et.tiles - g0), in = (int)(v % per);
-    const int ct = in / rows_in, rt = g0 + in % rows_in;
-    const int row0 = et.start + rt * S::BM, n = min(S::BM, et.end - row0);
-
-    // fragment f, row r of the tile's W: the output it makes, and the row that it is (gated: 16 of the gate, then the same 16 of up)
-    auto out_of = [&](int f, int r) { return GATED ? ct * (S::BN / 2) + (f >> 1) * 16 + r : ct * S::BN + f * 16 + r; };
-    const int bytes = a.d_in * M::ELEM, stages = (bytes + PW_KB - 1) / PW_KB;
-    const char *wp = a.W + (int64_t)et.expert * a.expert_stride;
-    const char *xp = a.rows ? a.X : a.X + (int64_t)row0 * a.ldx;
+    const uint32_t all = (uint32_t)count_tiles<S::BM>(a) * (uint32_t)col_tiles, share = (all + 7) / 8;
+    const uint32_t begin = blockIdx.x % 8 * share, end = min(begin + share, all), step = gridDim.x / 8;
+    // fragment f, row r of a tile's W: the output it makes (gated: 16 of the gate, then the same 16 of up)
+    auto out_of = [&](int ct, int f, int r) { return GATED ? ct * (S::BN / 2) + (f >> 1) * 16 + r : ct * S::BN + f * 16 + r; };
+    auto w_row = [&](int ct, int f, int r) { return (int64_t)(GATED && (f & 1) ? a.d_out : 0) + out_of(ct, f, r); };
+    const int bytes = a.d_in * M::ELEM, full = (bytes + PW_KB - 1) / PW_KB, stages = max(full, PW_STAGES - 1);
     const int lr = lane >> 2, piece = ((lane ^ (lane >> 3)) & 3) * 16;
-    const bool past = (stages - 1) * PW_KB + piece >= bytes;                  // nothing there in the last stage
-    uint32_t off_w[S::LW], off_x[S::LX];
+    const bool past = (full - 1) * PW_KB + piece >= bytes;                    // nothing there in the last stage
+
+    ExpertTiles et = {0, 0, 0, 0, 0};
+    auto tile_at = [&](uint32_t t) {
+        Tile<S> z;
+        z.n = 0;
+        z.w = z.x = nullptr;
+        z.expert = z.row0 = z.ct = 0;
+        z.off_scale = PW_NOWHERE;
+        for (int i = 0; i < S::LW; ++i) z.off_w[i] = PW_NOWHERE;
+        for (int i = 0; i < S::LX; ++i) z.off_x[i] = PW_NOWHERE;
+        if (t >= end) return z;
+        const int row_tile = (int)(t / (uint32_t)col_tiles);
+        if (row_tile < et.first || row_tile - et.first >= et.tiles) et = find_expert<S::BM>(a, row_tile);
+        if (et.tiles == 0) return z;
+        const uint32_t v = t - (uint32_t)et.first * (uint32_t)col_tiles, per = (uint32_t)(group * col_tiles);
+        const int g0 = (int)(v / per) * group, rows_in = min(group, et.tiles - g0), in = (int)(v % per);
+        z.expert = et.expert;
+        z.ct = in / rows_in;
+        z.row0 = et.start + (g0 + in % rows_in) * S::BM;
+        z.n = min(S::BM, et.end - z.row0);
+        z.w = a.W + (int64_t)et.expert * a.expert_stride;
+        z.x = a.rows ? a.X : a.X + (int64_t)z.row0 * a.ldx;
 #pragma unroll
-    for (int i = 0; i < S::LW; ++i) {
-        const int f = wave + i * PW_WAVES, o = out_of(f, lr);
-        const int64_t row = GATED && (f & 1) ? a.d_out + (int64_t)o : o;
-        off_w[i] = o < a.d_out ? (uint32_t)(row * a.ldw) + piece : PW_NOWHERE;
-    }
+        for (int i = 0; i < S::LW; ++i) {
+            const int f = wave + i * PW_WAVES;
+            z.off_w[i] = out_of(z.ct, f, lr) < a.d_out ? (uint32_t)(w_row(z.ct, f, lr) * a.ldw) + piece : PW_NOWHERE;
+        }
 #pragma unroll
-    for (int i = 0; i < S::LX; ++i) {
-        const int r = (wave + i * PW_WAVES) * 16 + lr;
-        const bool is = r < n;                                                // r < BM with it
-        int row = is ? r : 0;
-        if (a.rows && is) row = min(max(a.rows[row0 + r], 0), a.x_rows - 1);
-        off_x[i] = is ? (uint32_t)((int64_t)row * a.ldx) + piece : PW_NOWHERE;
-    }
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)pw_lds;
-    auto request = [&](int s) {
-        const int records = s < stages ? 0x7FFFFFFF : 0;
-        const auto wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(wp), 0, records, 0x00020000);
-        const auto xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(xp), 0, records, 0x00020000);
-        const uint32_t to = lds0 + (uint32_t)(s % PW_STAGES) * S::STAGE + wave * PW_FRAG, gone = s == stages - 1 && past ? PW_NOWHERE : 0;
-#pragma unroll
-        for (int i = 0; i < S::LW; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void *)(uintptr_t)(to + i * PW_WAVES * PW_FRAG), 16,
-                                                     (int)(off_w[i] | gone), s * PW_KB, 0, 0);
-#pragma unroll
-        for (int i = 0; i < S::LX; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (__attribute__((address_space(3))) void *)(uintptr_t)(to + (S::NW + i * PW_WAVES) * PW_FRAG), 16,
-                                                     (int)(off_x[i] | gone), s * PW_KB, 0, 0);
+        for (int i = 0; i < S::LX; ++i) {
+            const int r = (wave + i * PW_WAVES) * 16 + lr;
+            const bool is = r < z.n;                                          // r < BM with it
+            int row = is ? r : 0;
+            if (a.rows && is) row = min(max(a.rows[z.row0 + r], 0), a.x_rows - 1);
+            z.off_x[i] = is ? (uint32_t)((int64_t)row * a.ldx) + piece : PW_NOWHERE;
+        }
+        if (I8) {                                                             // one scale a thread: 256 of rows, 256 of outputs
+            const int r = threadIdx.x % 256;
+            if (threadIdx.x < 256) {
+                if (r < z.n) z.off_scale = 4 * (uint32_t)(a.rows ? min(max(a.rows[z.row0 + r], 0), a.x_rows - 1) : r);
+            } else if (out_of(z.ct, r >> 4, r & 15) < a.d_out) {
+                z.off_scale = 4 * (uint32_t)w_row(z.ct, r >> 4, r & 15);
+            }
+        }
+        return z;
+    };
+    auto request_scales = [&](const Tile<S> &z, uint32_t parity) {
+        if (!I8) return;
+        const float *from = wave < PW_WAVES / 2 ? a.x_scales + (a.rows ? 0 : z.row0) : a.w_scales + (int64_t)z.expert * a.d_out * (GATED ? 2 : 1);
+        request_dword(z.off_scale, resource(from), scales0 + parity * 2048 + wave * 256);
     };
 
     const int wn = wave % S::WN, wm = wave / S::WN;
     const uint32_t mine = (uint32_t)((lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 1) & 3)) * 16));
     const uint32_t read_w = lds0 + mine + wn * S::FN * PW_FRAG, read_x = lds0 + mine + (S::NW + wm * S::FM) * PW_FRAG;
-    typename M::acc_t acc[S::FN][S::FM] = {};
     constexpr int L = S::LW + S::LX;
+    constexpr int YB = YBF16 ? 2 : 4, OUTS = S::FN * 16 / (GATED ? 2 : 1), PASS = 128 / YB < OUTS ? 128 / YB : OUTS;   // outputs of a wave's row, of a pass
+    constexpr int PIECES = PASS * YB / 16, AT_ONCE = WAVE / PIECES, TIMES = AT_ONCE < 16 ? 16 / AT_ONCE : 1;   // 16-byte pieces of a pass' row, rows stored at once
+    constexpr int STORES = S::FM * (OUTS / PASS) * TIMES;
 
-    request(0);
-    request(1);
-    request(2);
-    wait_loads<2 * L>();
+    uint32_t t = begin + blockIdx.x / 8;
+    Tile<S> now = tile_at(t);
+    if (now.n == 0) return;
+    uint32_t at = 0, parity = 0;                                              // the stage that is read, the scales that are
+    auto after = [](uint32_t o) { return o == (PW_STAGES - 1) * S::STAGE ? 0u : o + (uint32_t)S::STAGE; };
+    request_scales(now, 0);
+    for (int s = 0; s < PW_STAGES - 1; ++s) {
+        uint32_t ow[S::LW], ox[S::LX];
+        const uint32_t gone = s >= full || (s == full - 1 && past) ? PW_NOWHERE : 0;
+        for (int i = 0; i < S::LW; ++i) ow[i] = now.off_w[i] | gone;
+        for (int i = 0; i < S::LX; ++i) ox[i] = now.off_x[i] | gone;
+        request<S::LW, S::LX>(ow, ox, resource(now.w), resource(now.x), s * PW_KB, lds0 + s * S::STAGE + wave * PW_FRAG);
+    }
+    wait_loads<(PW_STAGES - 2) * L>();
     meet();
     if (wave >= PW_WAVES / 2) meet();                                         // the second group is half a step behind
-    for (int s = 0; s < stages; ++s) {
+
+    typename M::acc_t acc[S::FN][S::FM];
+    // One stage: read it, ask for stage `s` of a tile over the one that both groups have read, multiply.  `stored`: the stores of the
+    // tile before may still be on their way, between the stages that are waited for and the newer ones.
+    auto stage = [&](const Tile<S> &z, int s, bool stored) {
         pr_i32x4_t fw[S::FN], fx[S::FM];
-        request(s + 3);                                                       // over the stage that both groups have read
-        const uint32_t at = (uint32_t)(s % PW_STAGES) * S::STAGE;
-        read_fragments<S::FN, S::FM>(read_w + at, read_x + at, fw, fx);
-        wait_loads<2 * L>();                                                  // stage s + 1 is there
+        uint32_t ow[S::LW], ox[S::LX];
+        const uint32_t gone = s >= full || (s == full - 1 && past) ? PW_NOWHERE : 0;
+        for (int i = 0; i < S::LW; ++i) ow[i] = z.off_w[i] | gone;
+        for (int i = 0; i < S::LX; ++i) ox[i] = z.off_x[i] | gone;
+        const uint32_t to = at == 0 ? (PW_STAGES - 1) * S::STAGE : at - S::STAGE;
+        read_and_request<S::FN, S::FM, S::LW, S::LX>(read_w + at, read_x + at, fw, fx, ow, ox, resource(z.w), resource(z.x), (uint32_t)s * PW_KB,
+                                                      lds0 + to + wave * PW_FRAG);
+        if (stored) wait_loads<(PW_STAGES - 2) * L + STORES>();               // the next stage is there
+        else wait_loads<(PW_STAGES - 2) * L>();
         meet();
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -154,57 +268,109 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
             for (int i = 0; i < S::FN; ++i) acc[i][j] = M::mul(fw[i], fx[j], acc[i][j]);
         __builtin_amdgcn_s_setprio(0);
         meet();
-    }
-    if (wave < PW_WAVES / 2) meet();
+        at = after(at);
+    };
 
-    const float *ws = I8 ? a.w_scales + (int64_t)et.expert * a.d_out * (GATED ? 2 : 1) : nullptr;
-    const int q0 = (lane >> 4) * 4;
-    float xs[S::FM];
+    bool stored = false;
+    for (;;) {
 #pragma unroll
-    for (int j = 0; j < S::FM; ++j) {
-        const int r = (wm * S::FM + j) * 16 + (lane & 15);
-        xs[j] = 1.0f;
-        if (I8 && r < n) xs[j] = a.x_scales[a.rows ? min(max(a.rows[row0 + r], 0), a.x_rows - 1) : row0 + r];
-    }
+        for (int i = 0; i < S::FN; ++i)
 #pragma unroll
-    for (int i = 0; i < S::FN; i += GATED ? 2 : 1) {
-        const int o = out_of(wn * S::FN + i, q0), there = a.d_out - o;        // of the four outputs from o
-        if (there <= 0) continue;
-        float sg[4] = {1, 1, 1, 1}, su[4] = {1, 1, 1, 1};
-        if (I8)
-            for (int q = 0; q < 4; ++q)
-                if (q < there) {
-                    sg[q] = ws[o + q];
-                    if (GATED) su[q] = ws[a.d_out + o + q];
-                }
+            for (int j = 0; j < S::FM; ++j) acc[i][j] = typename M::acc_t{};
+        for (int s = 0; s < stages - (PW_STAGES - 1); ++s) stage(now, s + PW_STAGES - 1, stored && s < PW_STAGES - 2);
+        // the last stages ask for the first ones of the next tile
+        t += step;
+        const Tile<S> next = tile_at(t);
+        request_scales(next, parity ^ 1);
+        for (int s = 0; s < PW_STAGES - 1; ++s) stage(next, s, false);
+
+        const int q0 = (lane >> 4) * 4;
+        // four outputs of fragment i (gated: and i + 1) in row j * 16 + lane % 16
+        auto four = [&](int i, int j, float (&y)[4]) {
+            const uint32_t sc = scales0 + parity * 2048;
+            float xs = 1.0f;
+            pr_f32x4_t sg = {1, 1, 1, 1}, su = {1, 1, 1, 1};
+            if (I8) {
+                xs = lds_read<float>(sc + ((wm * S::FM + j) * 16 + (lane & 15)) * 4);
+                sg = lds_read<pr_f32x4_t>(sc + 1024 + ((wn * S::FN + i) * 16 + q0) * 4);
+                if (GATED) su = lds_read<pr_f32x4_t>(sc + 1024 + ((wn * S::FN + i + 1) * 16 + q0) * 4);
+            }
 #pragma unroll
-        for (int j = 0; j < S::FM; ++j) {
-            const int r = (wm * S::FM + j) * 16 + (lane & 15);
-            if (r >= n) continue;
-            float y[4];
             for (int q = 0; q < 4; ++q) {
                 y[q] = (float)acc[i][j][q];
-                if (I8) y[q] = y[q] * xs[j] * sg[q];
+                if (I8) y[q] = y[q] * xs * sg[q];
                 if (GATED) {
                     float u = (float)acc[i + 1][j][q];
-                    if (I8) u = u * xs[j] * su[q];
+                    if (I8) u = u * xs * su[q];
                     y[q] = silu(y[q]) * u;
                 }
             }
-            store_y4<YBF16>(a.Y, (int64_t)(row0 + r) * a.ldy + o, y, there);
-        }
+        };
+        // 16 rows of PASS outputs at a time are turned in the wave's own 2 KB of LDS, so that 16 bytes a lane and whole lines are stored.  The
+        // eight 16-byte pieces of a row are exchanged by row mod 8.  Where Y's rows are whole pieces every wave makes the same number
+        // of stores: what is not there goes beyond the buffer's end.
+        constexpr int FRAGS = PASS / 16, STEP = GATED ? 2 : 1, EACH = 16 / YB;
+        const int col0 = out_of(now.ct, wn * S::FN, 0);
+        char *const yp = static_cast<char *>(a.Y) + (int64_t)now.row0 * a.ldy * YB;
+        const auto yr = __builtin_amdgcn_make_buffer_rsrc(yp, 0, 0x7FFFFFFF, 0x00020000);
+#pragma unroll
+        for (int j = 0; j < S::FM; ++j)
+#pragma unroll
+            for (int h = 0; h < OUTS / PASS; ++h) {
+#pragma unroll
+                for (int f = 0; f < FRAGS; ++f) {
+                    float y[4];
+                    four((h * FRAGS + f) * STEP, j, y);
+                    const int r = lane & 15, b = (f * 16 + q0) * YB;
+                    const uint32_t to = turn + r * 128 + (((b >> 4) ^ (r & 7)) << 4) + (b & 15);
+                    if constexpr (YBF16) lds_write<uint64_t>(to, (uint64_t)pack_bf16(y[2], y[3]) << 32 | pack_bf16(y[0], y[1]));
+                    else lds_write<pr_f32x4_t>(to, pr_f32x4_t{y[0], y[1], y[2], y[3]});
+                }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int k = 0; k < TIMES; ++k) {
+                    const int nth = k * AT_ONCE + lane / PIECES, r = nth & 15, p = lane % PIECES;
+                    const pr_i32x4_t v = lds_read<pr_i32x4_t>(turn + r * 128 + ((p ^ (r & 7)) << 4));
+                    const int row = (wm * S::FM + j) * 16 + r, col = col0 + h * PASS + p * EACH;
+                    const bool is = nth < 16 && row < now.n && col < a.d_out;
+                    if (whole) {
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(pw_u32x4_t, v), yr, (int)(is ? (uint32_t)(row * a.ldy + col) * YB : PW_NOWHERE), 0, 0);
+                    } else if (is) {
+                        using E = typename Store<YBF16>::type;
+                        E *to = reinterpret_cast<E *>(yp) + row * a.ldy + col;
+                        const auto e = __builtin_bit_cast(Unaligned<E, EACH>, v);
+                        if (col + EACH <= a.d_out) {
+                            *reinterpret_cast<Unaligned<E, EACH> *>(to) = e;
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < EACH - 1; ++i)
+                                if (col + i < a.d_out) to[i] = e.v[i];
+                        }
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+        if (next.n == 0) break;
+        now = next;
+        parity ^= 1;
+        stored = whole != 0;
     }
+    if (wave < PW_WAVES / 2) meet();
 }
 
 template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const Product &p) {
     const int outs = GATED ? S::BN / 2 : S::BN;
-    const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, tiles = most_row_tiles(p, S::BM) * cols, blocks = (tiles + 7) / 8 * 8;
-    if (blocks * PW_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
+    const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, tiles = most_row_tiles(p, S::BM) * cols;
+    if (tiles > 0x7FFFFFFF / 2) return hipErrorNotSupported;
+    const int64_t blocks = tiles < PW_CUS ? (tiles + 7) / 8 * 8 : PW_CUS;       // one a CU, which goes from tile to tile
+    const int64_t y_bytes = p.y_bf16 ? 2 : 4;
+    const bool whole = (reinterpret_cast<uintptr_t>(p.Y) & 15) == 0 && p.ldy * y_bytes % 16 == 0 && p.d_out * y_bytes % 16 == 0 &&
+                       p.ldy <= 0x7FFFFFFF / (S::BM * y_bytes);
     const auto kernel = &k_product_wide<I8, GATED, YBF16, S>;
-    constexpr int lds = PW_STAGES * S::STAGE;
+    constexpr int lds = PW_STAGES * S::STAGE + PW_WAVES * PW_TURN + 2 * 2048;
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (once != hipSuccess) return once;
-    kernel<<<dim3((uint32_t)blocks), PW_THREADS, lds, p.stream>>>(args_of(p), (int)cols, 8);
+    kernel<<<dim3((uint32_t)blocks), PW_THREADS, lds, p.stream>>>(args_of(p), (int)cols, 8, whole);
     return hipGetLastError();
 }
 
