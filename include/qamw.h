@@ -456,11 +456,12 @@ int qamw_int8_quantize(const void *X, int dtype, int m, int d, int64_t ldx, cons
  *   W  device, rows of d_in int8, leading dimension ldw, with w_scales, one float a row.  gated = 0: d_out rows.
  *      gated = 1: the d_out rows of a gate, then the d_out rows of an up projection, and Y = g / (1 + exp(-g)) * u
  *   Y  device, m rows of d_out elements of y_dtype (F32 or BF16, rounded to nearest even), leading dimension ldy
- *   workspace  qamw_int8_matmul_workspace_bytes() of device memory, 16-byte aligned; NULL with 0 bytes for codes
+ *   workspace  qamw_int8_matmul_workspace_bytes() of device memory, 16-byte aligned (the codes; and where there are too few
+ *      tiles for the chip, the sums of parts of the columns); NULL where that is 0
  * Errors: sizes out of the ranges above, NULL or misaligned pointers, x_scales with floating X or col_scale with codes, a
  * workspace too small -> INVALID_ARG; leading dimensions smaller than a row -> SHAPE; more tiles than a launch has ->
  * UNSUPPORTED. */
-int qamw_int8_matmul_workspace_bytes(int x_dtype, int m, int d_in, size_t *bytes_out);
+int qamw_int8_matmul_workspace_bytes(int x_dtype, int m, int d_out, int d_in, int gated, size_t *bytes_out);
 int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const float *col_scale, int m, int64_t ldx, const int8_t *W,
                      const float *w_scales, int64_t ldw, int d_out, int d_in, int gated, void *Y, int y_dtype, int64_t ldy,
                      void *workspace, size_t workspace_bytes, void *stream);

@@ -102,10 +102,76 @@ template <bool I8> hipError_t launch_any(const Product &p) {
 
 }  // namespace
 
+namespace {
+
+// ---- which kernel ----------------------------------------------------------------------------------------------------------
+//
+// The choice is by an estimate of the time, in us, of weights that come from memory.  The figures are fitted to measurements of
+// 33 to 2000 rows, 512 to 11008 outputs and 1024 to 13824 columns (within a fifth of them, a third at worst): what a launch costs, what a
+// stage and a tile's begin and end cost for each shape, and the bytes a us that a CU of the kernel for few rows gets, and memory.
+struct Plan {
+    bool few;
+    int tile_rows, parts;
+    double us;
+};
+constexpr double LAUNCH = 4.0, MEMORY = 4.7e6, PARTS_RATE = 5.5e6, FEW_RATE = 5.8e4;
+struct WideCost {
+    int rows;
+    double tile, stage;
+};
+constexpr WideCost WIDE[3] = {{64, 2.0, 0.52}, {128, 3.0, 0.57}, {256, 5.0, 0.70}};
+
+// groups: how many have rows, at most; row tiles are expected to be half a tile short.
+Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, bool gated, bool i8, bool may_part) {
+    const int64_t outs = d_out * (gated ? 2 : 1), bytes = d_in * (i8 ? 1 : 2);
+    const double each = (double)m / groups, weights = (double)groups * outs * bytes / MEMORY;
+    auto row_tiles = [&](int rows) {
+        if (!grouped) return (double)((m + rows - 1) / rows);
+        const double t = each / rows + 0.5;
+        return groups * (t < 1 ? 1 : t);
+    };
+    auto rounds = [](double blocks) { return blocks <= 256 ? 1.0 : blocks <= 1024 ? (double)(int64_t)((blocks + 255) / 256) : blocks / 256 + 0.5; };
+    Plan best = {true, 64, 1, 1e30};
+    auto offer = [&](bool few, int rows, int parts, double us) {
+        if (us < best.us) best = {few, rows, parts, us};
+    };
+    const int64_t units = (bytes + 127) / 128;
+    for (int rows = 16; rows <= 64; rows *= 2) {
+        const double tiles = row_tiles(rows) * ((d_out + 15) / 16);
+        const int split = few_split((int64_t)tiles, (int)units, 4);
+        const double slot = 2048.0 * ((gated ? 2 : 1) + rows / 16), work = rounds(tiles * split / 4) * units * 4 / split * slot / FEW_RATE;
+        offer(true, rows, 1, LAUNCH + (work > weights ? work : weights));
+    }
+    const double cols = (double)((outs + 255) / 256), stages = (double)((bytes + 63) / 64);
+    for (const WideCost &c : WIDE)
+        for (int parts : {1, 2, 3, 4, 6, 8}) {
+            if (parts > 1 && (!may_part || stages < parts * 8)) break;
+            const double work = rounds(row_tiles(c.rows) * cols * parts) * (c.tile + stages / parts * c.stage);
+            double us = LAUNCH + (work > weights ? work : weights);
+            if (parts > 1) us += 2.5 + 8.0 * parts * m * outs / PARTS_RATE;
+            offer(false, c.rows, parts, us);
+        }
+    return best;
+}
+Plan plan(const Product &p) {
+    const int64_t groups = !p.offsets ? 1 : p.m < p.n_experts ? p.m : p.n_experts;
+    return plan(p.m, groups, p.offsets != nullptr, p.d_out, p.d_in, p.gated, p.i8, p.scratch != nullptr);
+}
+
+}  // namespace
+
+// The sums of all parts: whole 16 bytes a row.
+size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated) {
+    if (m == 0) return 0;
+    const int parts = plan(m, 1, false, d_out, d_in, gated, true, true).parts;
+    return parts == 1 ? 0 : (size_t)parts * m * (((size_t)d_out * (gated ? 2 : 1) + 3) / 4 * 16);
+}
+
 hipError_t launch_product(const Product &p) {
     if (p.m == 0) return hipSuccess;
-    if (product_wide_supported(p)) return p.m <= 64 * (p.offsets ? p.n_experts : 1) ? launch_product_few(p) : launch_product_wide(p);
-    return p.i8 ? launch_any<true>(p) : launch_any<false>(p);
+    if (!product_wide_supported(p)) return p.i8 ? launch_any<true>(p) : launch_any<false>(p);
+    const Plan c = plan(p);
+    return c.few ? launch_product_few(p, c.tile_rows) : launch_product_wide(p, c.tile_rows, c.parts);
 }
 
 }  // namespace qamw

@@ -19,13 +19,22 @@ struct Product {
     int64_t ldx = 0, ldw = 0, expert_stride = 0, ldy = 0;
     int m = 0, x_rows = 0, n_experts = 1, d_out = 0, d_in = 0;
     bool i8 = false, gated = false, y_bf16 = false;
+    void *scratch = nullptr;             // product_scratch_bytes(), nullable: the product is not parted then
     hipStream_t stream = nullptr;
 };
 
 hipError_t launch_product(const Product &p);
+size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated);   // of an int8 product of one group
+// The kernels by what they are for.  wide and few: products that product_wide_supported(), tile_rows of 16 / 32 / 64 and 64 / 128 / 256.
 bool product_wide_supported(const Product &p);
-hipError_t launch_product_wide(const Product &p);     // of products that are
-hipError_t launch_product_few(const Product &p);      // likewise
+hipError_t launch_product_wide(const Product &p, int tile_rows, int parts);
+hipError_t launch_product_few(const Product &p, int tile_rows);
+// Waves that share a tile of outputs: enough for all of memory's bandwidth, about 8 on every CU, while a share has four units.
+inline int few_split(int64_t tiles, int units, int waves) {
+    int split = 1;
+    while (split < waves && tiles * split < 2048 && units >= split * 4) split *= 2;
+    return split;
+}
 // The product of rows that are quantised in the same launch; W as launch_product_few() needs it.
 bool product_from_floats_supported(const Product &p, const void *X, int dtype, int64_t ldx, const float *col_scale);
 hipError_t launch_product_from_floats(const Product &p, const void *X, int dtype, int64_t ldx, const float *col_scale);

@@ -17,9 +17,10 @@ constexpr uint32_t PF_NOWHERE = 0x80000000u;                    // added to an o
 // values by a thread.
 template <int T_, int FN_, int FROM_ = -1, int EIGHTS_ = 1> struct FewShape {
     static constexpr int T = T_, FN = FN_, FROM = FROM_, EIGHTS = EIGHTS_, XT = FROM >= 0 ? 0 : T;   // XT: fragments of X in the ring
-    static constexpr int RING = FROM >= 0 ? 4 : 2;                   // units on their way or being read
     static constexpr int SLOT = (FN + XT) * PF_SLOT;
-    static constexpr int WAVES = RING * SLOT * 8 <= 160 * 1024 ? 8 : 4;
+    // Workgroups of 4 waves, two or more on a CU, share the CUs more evenly than ones of 8; one that quantises has 8 for it.
+    static constexpr int WAVES = FROM >= 0 ? 8 : 4;
+    static constexpr int FIT = 80 * 1024 / (WAVES * SLOT), RING = FROM >= 0 || FIT > 4 ? 4 : FIT < 2 ? 2 : FIT;   // units on their way or being read
     static constexpr int THREADS = WAVES * WAVE, BM = T * 16;
     static constexpr int LDS = WAVES * RING * SLOT;
 };
@@ -34,7 +35,7 @@ struct FewArgs {
 
 // N fragments from `at` on, complete when this returns: rows are 128 bytes apart, `piece` is where the lane's 16 bytes are.
 template <int N> __device__ __forceinline__ void read_unit(uint32_t at, pr_i32x4_t (&v)[N]) {
-    static_assert(N == 1 || N == 2 || N == 3 || N == 4 || N == 5 || N == 6, "");
+    static_assert(N >= 1 && N <= 6, "");
     if constexpr (N == 1)
         asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v[0]) : "v"(at) : "memory");
     else if constexpr (N == 2)
@@ -68,7 +69,6 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     using M = Mfma<I8>;
     const ProductArgs &a = q.p;
     extern __shared__ __align__(16) char pf_lds[];
-    __shared__ uint32_t most_of[S::EIGHTS][S::WAVES];
     const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
     const int per = S::WAVES / q.split;                                        // tiles of columns of a workgroup
     const int groups = (q.col_tiles + per - 1) / per;
@@ -78,8 +78,8 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     const int bytes = a.d_in * M::ELEM, units = (bytes + PF_UNIT - 1) / PF_UNIT;
     const int u0 = (int)((int64_t)units * part / q.split), u1 = ct < q.col_tiles ? (int)((int64_t)units * (part + 1) / q.split) : u0;
 
-    // fragment f, row r of W: its output and row (gated: fragment 0 the gate, fragment 1 the same of up)
-    auto out_of = [&](int f, int r) { return GATED ? ct * 16 + r : (ct * S::FN + f) * 16 + r; };
+    // fragment f, row r of W: its output (gated: fragments in pairs, 16 of the gate and the same 16 of up)
+    auto out_of = [&](int f, int r) { return (GATED ? ct * (S::FN / 2) + f / 2 : ct * S::FN + f) * 16 + r; };
     const char *wp = a.W + (int64_t)rt.expert * a.expert_stride;
     const char *xp = a.rows ? a.X : a.X + (int64_t)rt.row0 * a.ldx;
     const int lr = lane >> 3, piece = ((lane & 7) ^ lr) * 16;
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int o = out_of(f, h * 8 + lr);
-            const int64_t row = GATED && f ? a.d_out + (int64_t)o : o;
+            const int64_t row = GATED && (f & 1) ? a.d_out + (int64_t)o : o;
             off_w[f][h] = o < a.d_out ? (uint32_t)(row * a.ldw) + piece : PF_NOWHERE;
         }
 #pragma unroll
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
         const float *from = a.w_scales + (int64_t)rt.expert * a.d_out * (GATED ? 2 : 1);
 #pragma unroll
         for (int f = 0; f < S::FN; ++f)
-            for (int k = 0; k < 4; ++k) ws[f][k] = from[min(out_of(f, q0 + k), a.d_out - 1) + (GATED && f ? a.d_out : 0)];
+            for (int k = 0; k < 4; ++k) ws[f][k] = from[min(out_of(f, q0 + k), a.d_out - 1) + (GATED && (f & 1) ? a.d_out : 0)];
         if (S::FROM < 0)
 #pragma unroll
             for (int t = 0; t < S::T; ++t) {
@@ -160,6 +160,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     // the rows of X as codes, a pitch of units * 128 + 16 bytes apart, behind the rings
     const uint32_t x_pitch = units * PF_UNIT + 16, x_at = lds0 + S::LDS;
     if constexpr (S::FROM >= 0) {
+        const uint32_t most_of = x_at + a.m * x_pitch;                        // [EIGHTS][WAVES], behind the codes
         float v[S::EIGHTS][8];
 #pragma unroll
         for (int i = 0; i < S::EIGHTS; ++i) {
@@ -171,7 +172,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
                 most = max(most, __float_as_uint(v[i][k]) & 0x7FFFFFFFu);
             }
             most = wave_max(most);
-            if (lane == 0) most_of[i][wave] = most;
+            if (lane == 0) lds_write<uint32_t>(most_of + (i * S::WAVES + wave) * 4, most);
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
             if (r >= a.m) continue;
             uint32_t most = 0;
             for (int s = 0; s < spans; ++s)
-                most = max(most, most_of[S::EIGHTS == 1 ? 0 : r * spans + s][lane % S::WAVES]);
+                most = max(most, lds_read<uint32_t>(most_of + ((S::EIGHTS == 1 ? 0 : r * spans + s) * S::WAVES + lane % S::WAVES) * 4));
             const Quantiser z(wave_max(most));
             if (fr == r) xs[0] = z.scale;
             if (j < units * PF_UNIT) {                                        // beyond d_in: zeros, which v holds there
@@ -250,8 +251,8 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
                 y[k] = (float)acc[f][t][k];
                 if (I8) y[k] = y[k] * xs[t] * ws[f][k];
                 if (GATED) {
-                    float u = (float)acc[S::FN - 1][t][k];
-                    if (I8) u = u * xs[t] * ws[S::FN - 1][k];
+                    float u = (float)acc[GATED ? f + 1 : f][t][k];
+                    if (I8) u = u * xs[t] * ws[GATED ? f + 1 : f][k];
                     y[k] = silu(y[k]) * u;
                 }
             }
@@ -262,13 +263,10 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
 
 template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const Product &p, const FewArgs &given, size_t more_lds) {
     FewArgs q = given;
-    const int outs = (GATED ? 1 : S::FN) * 16;
+    const int outs = (GATED ? S::FN / 2 : S::FN) * 16;
     const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, rows = most_row_tiles(p, S::BM);
-    // enough waves to ask for all of memory's bandwidth: about 8 on every CU, as far as a share still has two units
     const int units = (int)((p.d_in * (I8 ? 1 : 2) + PF_UNIT - 1) / PF_UNIT);
-    const int64_t tiles = (p.offsets && p.m < p.n_experts ? p.m : rows) * cols;
-    int split = 1;
-    while (split < S::WAVES && tiles * split < 2048 && units >= split * 4) split *= 2;
+    const int split = few_split((p.offsets && p.m < p.n_experts ? p.m : rows) * cols, units, S::WAVES);
     const int per = S::WAVES / split;
     const int64_t blocks = rows * ((cols + per - 1) / per);
     if (cols > 0x7FFFFFFF || blocks * S::THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
@@ -276,29 +274,29 @@ template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const P
     q.col_tiles = (int)cols;
     q.split = split;
     const auto kernel = &k_product_few<I8, GATED, YBF16, S>;
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - 256);
+    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
     if (once != hipSuccess) return once;
     kernel<<<dim3((uint32_t)blocks), S::THREADS, S::LDS + more_lds, p.stream>>>(q);
     return hipGetLastError();
 }
 
 template <bool I8, int T, int FROM, int EIGHTS> hipError_t launch_shape(const Product &p, const FewArgs &q, size_t more_lds) {
-    if (p.gated)
-        return p.y_bf16 ? launch<I8, true, true, FewShape<T, 2, FROM, EIGHTS>>(p, q, more_lds) : launch<I8, true, false, FewShape<T, 2, FROM, EIGHTS>>(p, q, more_lds);
-    return p.y_bf16 ? launch<I8, false, true, FewShape<T, 1, FROM, EIGHTS>>(p, q, more_lds) : launch<I8, false, false, FewShape<T, 1, FROM, EIGHTS>>(p, q, more_lds);
+    using Gated = FewShape<T, 2, FROM, EIGHTS>;
+    using Plain = FewShape<T, 1, FROM, EIGHTS>;
+    if (p.gated) return p.y_bf16 ? launch<I8, true, true, Gated>(p, q, more_lds) : launch<I8, true, false, Gated>(p, q, more_lds);
+    return p.y_bf16 ? launch<I8, false, true, Plain>(p, q, more_lds) : launch<I8, false, false, Plain>(p, q, more_lds);
 }
 
-template <bool I8> hipError_t launch_type(const Product &p) {
-    const int64_t rows = p.m / (p.offsets ? p.n_experts : 1);                  // of a group, on average
+template <bool I8> hipError_t launch_type(const Product &p, int tile_rows) {
     const FewArgs q = {};
-    if (rows <= (p.offsets ? 8 : 16)) return launch_shape<I8, 1, -1, 1>(p, q, 0);
-    if (rows <= (p.offsets ? 20 : 32)) return launch_shape<I8, 2, -1, 1>(p, q, 0);
+    if (tile_rows <= 16) return launch_shape<I8, 1, -1, 1>(p, q, 0);
+    if (tile_rows <= 32) return launch_shape<I8, 2, -1, 1>(p, q, 0);
     return launch_shape<I8, 4, -1, 1>(p, q, 0);
 }
 
 }  // namespace
 
-hipError_t launch_product_few(const Product &p) { return p.i8 ? launch_type<true>(p) : launch_type<false>(p); }
+hipError_t launch_product_few(const Product &p, int tile_rows) { return p.i8 ? launch_type<true>(p, tile_rows) : launch_type<false>(p, tile_rows); }
 
 // As many values as the threads of a workgroup hold, and rows that are read in whole 16 bytes, with offsets that 31 bits hold.
 constexpr int PF_MOST_EIGHTS = 4, PF_SPAN = 8 * 8 * WAVE;
@@ -318,7 +316,7 @@ hipError_t launch_product_from_floats(const Product &p, const void *X, int dtype
     q.xf = X;
     q.ldxf = ldx;
     q.col_scale = col_scale;
-    const size_t codes = (size_t)p.m * (((size_t)p.d_in + PF_UNIT - 1) / PF_UNIT * PF_UNIT + 16);
+    const size_t codes = (size_t)p.m * (((size_t)p.d_in + PF_UNIT - 1) / PF_UNIT * PF_UNIT + 16) + PF_MOST_EIGHTS * 8 * 4;   // and the waves' maxima
     return p.m == 1 && p.d_in <= PF_SPAN ? from_floats<1>(p, q, dtype, codes) : from_floats<PF_MOST_EIGHTS>(p, q, dtype, codes);
 }
 

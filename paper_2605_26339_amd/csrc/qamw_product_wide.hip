@@ -5,7 +5,7 @@
 // to LDS directly and read by one 16-byte LDS read of a wave: the operand of a 16x16 matrix instruction.
 //   In LDS the four 16-byte pieces of a row are exchanged by (row / 2) mod 4, or the lanes of a read would meet in half of
 //   the banks; the loading lanes ask for their piece accordingly, from the same 64 bytes.
-//   Four stages are in LDS: one is read, the next ones are on their way while two others' products run, which covers the latency of memory.
+//   Four or five stages are in LDS: one is read, the next ones are on their way.
 //   The waves form two groups of four, one wave of each group on every SIMD.  While one group reads its fragments the other
 //   multiplies, then they change places; a barrier is all that they need to keep in step.
 // What is not there (rows past the end, columns past d_in, stages past the last) is loaded as zeros: such a lane asks for an
@@ -15,15 +15,16 @@
 namespace qamw {
 namespace {
 
-constexpr int PW_WAVES = 8, PW_THREADS = PW_WAVES * WAVE, PW_STAGES = 4, PW_FRAG = 1024, PW_KB = 64, PW_CUS = 256, PW_TURN = 2048;
+constexpr int PW_WAVES = 8, PW_THREADS = PW_WAVES * WAVE, PW_FRAG = 1024, PW_KB = 64, PW_CUS = 256, PW_TURN = 2048;
 constexpr uint32_t PW_NOWHERE = 0x80000000u;       // added to an offset: beyond the end of any buffer here
 
-// Tiles: WN x WM waves, each of FN fragments of W and FM of X.
-template <int WN_, int FN_, int WM_, int FM_> struct Shape {
-    static constexpr int WN = WN_, FN = FN_, WM = WM_, FM = FM_, BN = WN * FN * 16, BM = WM * FM * 16;
+// Tiles: WN x WM waves, each of FN fragments of W and FM of X, and as many stages as LDS holds: where W comes from memory a stage
+// takes about 1.6 us to come.
+template <int WN_, int FN_, int WM_, int FM_, int STAGES_> struct Shape {
+    static constexpr int WN = WN_, FN = FN_, WM = WM_, FM = FM_, STAGES = STAGES_, BN = WN * FN * 16, BM = WM * FM * 16;
     static constexpr int NW = WN * FN, NX = WM * FM;                          // fragments of a stage
     static constexpr int LW = NW / PW_WAVES, LX = (NX + PW_WAVES - 1) / PW_WAVES;   // loads of a wave: fragments wave, wave + 8, ...
-    static constexpr int STAGE = (NW + (LX * PW_WAVES)) * PW_FRAG;            // where NX < 8, room for what some waves load for nothing
+    static constexpr int STAGE = (NW + LX * PW_WAVES) * PW_FRAG;              // where NX < 8, room for what some waves load for nothing
     static_assert(WN * WM == PW_WAVES && NW % PW_WAVES == 0, "");
 };
 
@@ -112,13 +113,13 @@ __device__ __forceinline__ void read_and_request(uint32_t at_w, uint32_t at_x, p
             : "memory", "scc");
     }
 }
-
 // The same pieces without the reads, and four bytes a lane.
 template <int LW, int LX>
 __device__ __forceinline__ void request(const uint32_t (&off_w)[LW], const uint32_t (&off_x)[LX], pw_u32x4_t wr, pw_u32x4_t xr, uint32_t so, uint32_t to) {
 #pragma unroll
     for (int i = 0; i < LW + LX; ++i)
-        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(i < LW ? off_w[i < LW ? i : 0] : off_x[i < LW ? 0 : i - LW]),
+        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(
+                         i < LW ? off_w[i < LW ? i : 0] : off_x[i < LW ? 0 : i - LW]),
                      "s"(i < LW ? wr : xr), "s"(so), "s"(to + i * PW_WAVES * PW_FRAG)
                      : "memory");
 }
@@ -147,40 +148,46 @@ template <> struct Store<true> {
 
 // A tile: where its rows are, and what this lane asks for of them.
 template <typename S> struct Tile {
-    int expert, row0, n, ct;                         // rows row0 .. row0 + n, the ct-th columns; n = 0: no tile
+    int expert, row0, n, ct;                         // rows row0 .. row0 + n, the ct-th outputs; n = 0: no tile
+    int part, full;                                  // the part of the columns, its stages
     const char *w, *x;
     uint32_t off_w[S::LW], off_x[S::LX], off_scale;
 };
 
-template <bool I8, bool GATED, bool YBF16, typename S>
-__global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, int col_tiles, int group, int whole) {
+// OUT: what is stored: 0 fp32, 1 bf16, 2 the sums of a part of the columns as they are (int32 or fp32), one array of `part_stride`
+// elements a part.
+template <bool I8, bool GATED, int OUT, typename S>
+__global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, int col_tiles, int group, int whole, int parts, int64_t part_stride) {
+    constexpr bool YBF16 = OUT == 1, SCALED = I8 && OUT != 2;
     using M = Mfma<I8>;
     extern __shared__ __align__(16) char pw_lds[];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)pw_lds;
-    const uint32_t turn = lds0 + PW_STAGES * S::STAGE + wave * PW_TURN, scales0 = lds0 + PW_STAGES * S::STAGE + PW_WAVES * PW_TURN;
+    const uint32_t turn = lds0 + S::STAGES * S::STAGE + wave * PW_TURN, scales0 = lds0 + S::STAGES * S::STAGE + PW_WAVES * PW_TURN;
 
     // Workgroups go to the 8 XCDs in turn: an XCD gets tiles that follow one another, and these are ordered such that `group` row
     // tiles share their W while it is in the XCD's cache.
-    const uint32_t all = (uint32_t)count_tiles<S::BM>(a) * (uint32_t)col_tiles, share = (all + 7) / 8;
+    const uint32_t one = (uint32_t)count_tiles<S::BM>(a) * (uint32_t)col_tiles, all = one * parts, share = (all + 7) / 8;
     const uint32_t begin = blockIdx.x % 8 * share, end = min(begin + share, all), step = gridDim.x / 8;
     // fragment f, row r of a tile's W: the output it makes (gated: 16 of the gate, then the same 16 of up)
     auto out_of = [&](int ct, int f, int r) { return GATED ? ct * (S::BN / 2) + (f >> 1) * 16 + r : ct * S::BN + f * 16 + r; };
     auto w_row = [&](int ct, int f, int r) { return (int64_t)(GATED && (f & 1) ? a.d_out : 0) + out_of(ct, f, r); };
-    const int bytes = a.d_in * M::ELEM, full = (bytes + PW_KB - 1) / PW_KB, stages = max(full, PW_STAGES - 1);
+    const int bytes = a.d_in * M::ELEM, every = (bytes + PW_KB - 1) / PW_KB;
     const int lr = lane >> 2, piece = ((lane ^ (lane >> 3)) & 3) * 16;
-    const bool past = (full - 1) * PW_KB + piece >= bytes;                    // nothing there in the last stage
+    const bool past = (every - 1) * PW_KB + piece >= bytes;                   // nothing there in the last stage of all
 
     ExpertTiles et = {0, 0, 0, 0, 0};
     auto tile_at = [&](uint32_t t) {
         Tile<S> z;
         z.n = 0;
         z.w = z.x = nullptr;
-        z.expert = z.row0 = z.ct = 0;
+        z.expert = z.row0 = z.ct = z.part = z.full = 0;
         z.off_scale = PW_NOWHERE;
         for (int i = 0; i < S::LW; ++i) z.off_w[i] = PW_NOWHERE;
         for (int i = 0; i < S::LX; ++i) z.off_x[i] = PW_NOWHERE;
         if (t >= end) return z;
+        z.part = (int)(t / one);
+        t -= z.part * one;
         const int row_tile = (int)(t / (uint32_t)col_tiles);
         if (row_tile < et.first || row_tile - et.first >= et.tiles) et = find_expert<S::BM>(a, row_tile);
         if (et.tiles == 0) return z;
@@ -190,8 +197,10 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         z.ct = in / rows_in;
         z.row0 = et.start + (g0 + in % rows_in) * S::BM;
         z.n = min(S::BM, et.end - z.row0);
-        z.w = a.W + (int64_t)et.expert * a.expert_stride;
-        z.x = a.rows ? a.X : a.X + (int64_t)z.row0 * a.ldx;
+        const int s0 = (int)((int64_t)every * z.part / parts);
+        z.full = (int)((int64_t)every * (z.part + 1) / parts) - s0;
+        z.w = a.W + (int64_t)et.expert * a.expert_stride + s0 * PW_KB;
+        z.x = (a.rows ? a.X : a.X + (int64_t)z.row0 * a.ldx) + s0 * PW_KB;
 #pragma unroll
         for (int i = 0; i < S::LW; ++i) {
             const int f = wave + i * PW_WAVES;
@@ -205,7 +214,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
             if (a.rows && is) row = min(max(a.rows[z.row0 + r], 0), a.x_rows - 1);
             z.off_x[i] = is ? (uint32_t)((int64_t)row * a.ldx) + piece : PW_NOWHERE;
         }
-        if (I8) {                                                             // one scale a thread: 256 of rows, 256 of outputs
+        if (SCALED) {                                                         // one scale a thread: 256 of rows, 256 of outputs
             const int r = threadIdx.x % 256;
             if (threadIdx.x < 256) {
                 if (r < z.n) z.off_scale = 4 * (uint32_t)(a.rows ? min(max(a.rows[z.row0 + r], 0), a.x_rows - 1) : r);
@@ -216,7 +225,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         return z;
     };
     auto request_scales = [&](const Tile<S> &z, uint32_t parity) {
-        if (!I8) return;
+        if (!SCALED) return;
         const float *from = wave < PW_WAVES / 2 ? a.x_scales + (a.rows ? 0 : z.row0) : a.w_scales + (int64_t)z.expert * a.d_out * (GATED ? 2 : 1);
         request_dword(z.off_scale, resource(from), scales0 + parity * 2048 + wave * 256);
     };
@@ -233,35 +242,37 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     Tile<S> now = tile_at(t);
     if (now.n == 0) return;
     uint32_t at = 0, parity = 0;                                              // the stage that is read, the scales that are
-    auto after = [](uint32_t o) { return o == (PW_STAGES - 1) * S::STAGE ? 0u : o + (uint32_t)S::STAGE; };
+    auto after = [](uint32_t o) { return o == (S::STAGES - 1) * S::STAGE ? 0u : o + (uint32_t)S::STAGE; };
+    auto nothing = [&](const Tile<S> &z, int s) { return s >= z.full || (s == z.full - 1 && z.part == parts - 1 && past) ? PW_NOWHERE : 0; };
     request_scales(now, 0);
-    for (int s = 0; s < PW_STAGES - 1; ++s) {
+    for (int s = 0; s < S::STAGES - 1; ++s) {
         uint32_t ow[S::LW], ox[S::LX];
-        const uint32_t gone = s >= full || (s == full - 1 && past) ? PW_NOWHERE : 0;
+        const uint32_t gone = nothing(now, s);
         for (int i = 0; i < S::LW; ++i) ow[i] = now.off_w[i] | gone;
         for (int i = 0; i < S::LX; ++i) ox[i] = now.off_x[i] | gone;
         request<S::LW, S::LX>(ow, ox, resource(now.w), resource(now.x), s * PW_KB, lds0 + s * S::STAGE + wave * PW_FRAG);
     }
-    wait_loads<(PW_STAGES - 2) * L>();
+    wait_loads<(S::STAGES - 2) * L>();
     meet();
     if (wave >= PW_WAVES / 2) meet();                                         // the second group is half a step behind
 
     typename M::acc_t acc[S::FN][S::FM];
     // One stage: read it, ask for stage `s` of a tile over the one that both groups have read, multiply.  `stored`: the stores of the
     // tile before may still be on their way, between the stages that are waited for and the newer ones.
-    auto stage = [&](const Tile<S> &z, int s, bool stored) {
+    auto stage = [&](const Tile<S> &z, int s, bool stored, bool busy) {
         pr_i32x4_t fw[S::FN], fx[S::FM];
         uint32_t ow[S::LW], ox[S::LX];
-        const uint32_t gone = s >= full || (s == full - 1 && past) ? PW_NOWHERE : 0;
+        const uint32_t gone = nothing(z, s);
         for (int i = 0; i < S::LW; ++i) ow[i] = z.off_w[i] | gone;
         for (int i = 0; i < S::LX; ++i) ox[i] = z.off_x[i] | gone;
-        const uint32_t to = at == 0 ? (PW_STAGES - 1) * S::STAGE : at - S::STAGE;
+        const uint32_t to = at == 0 ? (S::STAGES - 1) * S::STAGE : at - S::STAGE;
         read_and_request<S::FN, S::FM, S::LW, S::LX>(read_w + at, read_x + at, fw, fx, ow, ox, resource(z.w), resource(z.x), (uint32_t)s * PW_KB,
                                                       lds0 + to + wave * PW_FRAG);
-        if (stored) wait_loads<(PW_STAGES - 2) * L + STORES>();               // the next stage is there
-        else wait_loads<(PW_STAGES - 2) * L>();
+        if (stored) wait_loads<(S::STAGES - 2) * L + STORES>();               // the next stage is there
+        else wait_loads<(S::STAGES - 2) * L>();
         meet();
         __builtin_amdgcn_s_setprio(1);
+        if (busy)
 #pragma unroll
         for (int j = 0; j < S::FM; ++j)
 #pragma unroll
@@ -277,12 +288,13 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         for (int i = 0; i < S::FN; ++i)
 #pragma unroll
             for (int j = 0; j < S::FM; ++j) acc[i][j] = typename M::acc_t{};
-        for (int s = 0; s < stages - (PW_STAGES - 1); ++s) stage(now, s + PW_STAGES - 1, stored && s < PW_STAGES - 2);
+        const bool busy = wm * S::FM * 16 < now.n && out_of(now.ct, wn * S::FN, 0) < a.d_out;   // some of the wave's rows and outputs are there
+        for (int s = 0; s < now.full - (S::STAGES - 1); ++s) stage(now, s + S::STAGES - 1, stored && s < S::STAGES - 2, busy);
         // the last stages ask for the first ones of the next tile
         t += step;
         const Tile<S> next = tile_at(t);
         request_scales(next, parity ^ 1);
-        for (int s = 0; s < PW_STAGES - 1; ++s) stage(next, s, false);
+        for (int s = 0; s < S::STAGES - 1; ++s) stage(next, s, false, busy);
 
         const int q0 = (lane >> 4) * 4;
         // four outputs of fragment i (gated: and i + 1) in row j * 16 + lane % 16
@@ -290,7 +302,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
             const uint32_t sc = scales0 + parity * 2048;
             float xs = 1.0f;
             pr_f32x4_t sg = {1, 1, 1, 1}, su = {1, 1, 1, 1};
-            if (I8) {
+            if (SCALED) {
                 xs = lds_read<float>(sc + ((wm * S::FM + j) * 16 + (lane & 15)) * 4);
                 sg = lds_read<pr_f32x4_t>(sc + 1024 + ((wn * S::FN + i) * 16 + q0) * 4);
                 if (GATED) su = lds_read<pr_f32x4_t>(sc + 1024 + ((wn * S::FN + i + 1) * 16 + q0) * 4);
@@ -298,10 +310,10 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 y[q] = (float)acc[i][j][q];
-                if (I8) y[q] = y[q] * xs * sg[q];
+                if (SCALED) y[q] = y[q] * xs * sg[q];
                 if (GATED) {
                     float u = (float)acc[i + 1][j][q];
-                    if (I8) u = u * xs * su[q];
+                    if (SCALED) u = u * xs * su[q];
                     y[q] = silu(y[q]) * u;
                 }
             }
@@ -311,7 +323,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         // of stores: what is not there goes beyond the buffer's end.
         constexpr int FRAGS = PASS / 16, STEP = GATED ? 2 : 1, EACH = 16 / YB;
         const int col0 = out_of(now.ct, wn * S::FN, 0);
-        char *const yp = static_cast<char *>(a.Y) + (int64_t)now.row0 * a.ldy * YB;
+        char *const yp = static_cast<char *>(a.Y) + (now.part * part_stride + (int64_t)now.row0 * a.ldy) * YB;
         const auto yr = __builtin_amdgcn_make_buffer_rsrc(yp, 0, 0x7FFFFFFF, 0x00020000);
 #pragma unroll
         for (int j = 0; j < S::FM; ++j)
@@ -320,10 +332,11 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 #pragma unroll
                 for (int f = 0; f < FRAGS; ++f) {
                     float y[4];
-                    four((h * FRAGS + f) * STEP, j, y);
+                    if constexpr (OUT != 2) four((h * FRAGS + f) * STEP, j, y);
                     const int r = lane & 15, b = (f * 16 + q0) * YB;
                     const uint32_t to = turn + r * 128 + (((b >> 4) ^ (r & 7)) << 4) + (b & 15);
                     if constexpr (YBF16) lds_write<uint64_t>(to, (uint64_t)pack_bf16(y[2], y[3]) << 32 | pack_bf16(y[0], y[1]));
+                    else if constexpr (OUT == 2) lds_write<pr_i32x4_t>(to, __builtin_bit_cast(pr_i32x4_t, acc[h * FRAGS + f][j]));
                     else lds_write<pr_f32x4_t>(to, pr_f32x4_t{y[0], y[1], y[2], y[3]});
                 }
                 __builtin_amdgcn_wave_barrier();
@@ -358,36 +371,84 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     if (wave < PW_WAVES / 2) meet();
 }
 
-template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const Product &p) {
+// The sums of the parts, in their order, and what is done with them: four outputs a thread.
+constexpr int PS_THREADS = 256;
+template <bool GATED, bool YBF16>
+__global__ __launch_bounds__(PS_THREADS) void k_product_parts(ProductArgs a, const char *sums, int parts, int64_t part_stride, int64_t ld, int fours) {
+    const uint32_t id = blockIdx.x * PS_THREADS + threadIdx.x;
+    const int64_t row = id / (uint32_t)fours;
+    const int o = (int)(id % (uint32_t)fours) * 4;
+    if (row >= a.m) return;
+    const char *at = sums + (row * ld + o) * 4, *up = at + (int64_t)a.d_out * 4;
+    pr_i32x4_t g = {0, 0, 0, 0}, u = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        g += *reinterpret_cast<const pr_i32x4_t *>(at + p * part_stride * 4);
+        if (GATED) u += __builtin_bit_cast(pr_i32x4_t, *reinterpret_cast<const Unaligned<int, 4> *>(up + p * part_stride * 4));
+    }
+    const float xs = a.x_scales[row];
+    float y[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int i = min(o + q, a.d_out - 1);
+        y[q] = (float)g[q] * xs * a.w_scales[i];
+        if (GATED) y[q] = silu(y[q]) * ((float)u[q] * xs * a.w_scales[a.d_out + i]);
+    }
+    store_y4<YBF16>(a.Y, row * a.ldy + o, y, a.d_out - o);
+}
+
+template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Product &p, int parts, int64_t part_stride) {
     const int outs = GATED ? S::BN / 2 : S::BN;
-    const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, tiles = most_row_tiles(p, S::BM) * cols;
+    const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, tiles = most_row_tiles(p, S::BM) * cols * parts;
     if (tiles > 0x7FFFFFFF / 2) return hipErrorNotSupported;
     const int64_t blocks = tiles < PW_CUS ? (tiles + 7) / 8 * 8 : PW_CUS;       // one a CU, which goes from tile to tile
-    const int64_t y_bytes = p.y_bf16 ? 2 : 4;
-    const bool whole = (reinterpret_cast<uintptr_t>(p.Y) & 15) == 0 && p.ldy * y_bytes % 16 == 0 && p.d_out * y_bytes % 16 == 0 &&
+    const int64_t y_bytes = OUT == 1 ? 2 : 4;
+    const bool whole = (reinterpret_cast<uintptr_t>(p.Y) & 15) == 0 && p.ldy * y_bytes % 16 == 0 && (p.d_out * y_bytes % 16 == 0 || OUT == 2) &&
                        p.ldy <= 0x7FFFFFFF / (S::BM * y_bytes);
-    const auto kernel = &k_product_wide<I8, GATED, YBF16, S>;
-    constexpr int lds = PW_STAGES * S::STAGE + PW_WAVES * PW_TURN + 2 * 2048;
+    const auto kernel = &k_product_wide<I8, GATED, OUT, S>;
+    constexpr int lds = S::STAGES * S::STAGE + PW_WAVES * PW_TURN + 2 * 2048;
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (once != hipSuccess) return once;
-    kernel<<<dim3((uint32_t)blocks), PW_THREADS, lds, p.stream>>>(args_of(p), (int)cols, 8, whole);
+    kernel<<<dim3((uint32_t)blocks), PW_THREADS, lds, p.stream>>>(args_of(p), (int)cols, 8, whole, parts, part_stride);
     return hipGetLastError();
 }
 
 template <bool I8, typename S> hipError_t launch_shape(const Product &p) {
-    if (p.gated) return p.y_bf16 ? launch<I8, true, true, S>(p) : launch<I8, true, false, S>(p);
-    return p.y_bf16 ? launch<I8, false, true, S>(p) : launch<I8, false, false, S>(p);
+    if (p.gated) return p.y_bf16 ? launch<I8, true, 1, S>(p, 1, 0) : launch<I8, true, 0, S>(p, 1, 0);
+    return p.y_bf16 ? launch<I8, false, 1, S>(p, 1, 0) : launch<I8, false, 0, S>(p, 1, 0);
 }
 
-using Shape256 = Shape<2, 8, 4, 4>;
-using Shape128 = Shape<4, 4, 2, 4>;
-using Shape64 = Shape<8, 2, 1, 4>;
+// In `parts` parts of the columns, whose sums lie in p.scratch.
+template <typename S> hipError_t launch_parts(const Product &p, int parts) {
+    Product q = p;
+    q.d_out = p.d_out * (p.gated ? 2 : 1);
+    q.gated = false;
+    q.Y = p.scratch;
+    q.ldy = ((int64_t)q.d_out + 3) / 4 * 4;
+    const int64_t stride = q.ldy * p.m, fours = ((int64_t)p.d_out + 3) / 4, blocks = (fours * p.m + PS_THREADS - 1) / PS_THREADS;
+    if (blocks * PS_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
+    const hipError_t e = launch<true, false, 2, S>(q, parts, stride);
+    if (e != hipSuccess) return e;
+    const ProductArgs a = args_of(p);
+    const char *sums = static_cast<const char *>(p.scratch);
+    const dim3 g((uint32_t)blocks);
+    if (p.gated) {
+        if (p.y_bf16) k_product_parts<true, true><<<g, PS_THREADS, 0, p.stream>>>(a, sums, parts, stride, q.ldy, (int)fours);
+        else k_product_parts<true, false><<<g, PS_THREADS, 0, p.stream>>>(a, sums, parts, stride, q.ldy, (int)fours);
+    } else {
+        if (p.y_bf16) k_product_parts<false, true><<<g, PS_THREADS, 0, p.stream>>>(a, sums, parts, stride, q.ldy, (int)fours);
+        else k_product_parts<false, false><<<g, PS_THREADS, 0, p.stream>>>(a, sums, parts, stride, q.ldy, (int)fours);
+    }
+    return hipGetLastError();
+}
 
-template <bool I8> hipError_t launch_type(const Product &p) {
-    const int64_t rows = p.m / (p.offsets ? p.n_experts : 1);                  // of a group, on average
-    if (rows > 128) return launch_shape<I8, Shape256>(p);
-    if (rows > 64) return launch_shape<I8, Shape128>(p);
-    return launch_shape<I8, Shape64>(p);
+using Shape256 = Shape<2, 8, 4, 4, 4>;
+using Shape128 = Shape<4, 4, 2, 4, 5>;
+using Shape64 = Shape<8, 2, 1, 4, 5>;
+
+template <typename S> hipError_t launch_either(const Product &p, int parts) {
+    if (parts > 1) return launch_parts<S>(p, parts);
+    return p.i8 ? launch_shape<true, S>(p) : launch_shape<false, S>(p);
 }
 
 }  // namespace
@@ -403,6 +464,10 @@ bool product_wide_supported(const Product &p) {
     return p.ldw * e <= most / outs && p.ldx * e <= most / x_rows;
 }
 
-hipError_t launch_product_wide(const Product &p) { return p.i8 ? launch_type<true>(p) : launch_type<false>(p); }
+hipError_t launch_product_wide(const Product &p, int tile_rows, int parts) {
+    if (tile_rows <= 64) return launch_either<Shape64>(p, parts);
+    if (tile_rows <= 128) return launch_either<Shape128>(p, parts);
+    return launch_either<Shape256>(p, parts);
+}
 
 }  // namespace qamw

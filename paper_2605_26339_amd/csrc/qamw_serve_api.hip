@@ -25,11 +25,17 @@ int qamw_int8_quantize(const void *X, int dtype, int m, int d, int64_t ldx, cons
     return status_of(qamw::launch_int8_quantize(X, dtype, m, d, ldx, col_scale, codes, ldc, scales, (hipStream_t)stream));
 }
 
-int qamw_int8_matmul_workspace_bytes(int x_dtype, int m, int d_in, size_t *bytes_out) {
-    if (!bytes_out || m < 0 || m > QAMW_INT8_MAX_ROWS || d_in < 1 || d_in > QAMW_INT8_MAX_D_IN) return QAMW_ERR_INVALID_ARG;
+// In the workspace: the codes, rows of whole 16 bytes, their scales, then what the product needs.
+static size_t codes_bytes(int x_dtype, int m, int d_in) {
+    return x_dtype == QAMW_DTYPE_I8 ? 0 : (size_t)m * round16((size_t)d_in) + round16((size_t)m * 4);
+}
+
+int qamw_int8_matmul_workspace_bytes(int x_dtype, int m, int d_out, int d_in, int gated, size_t *bytes_out) {
+    if (!bytes_out || m < 0 || m > QAMW_INT8_MAX_ROWS || d_in < 1 || d_in > QAMW_INT8_MAX_D_IN || d_out < 1 ||
+        d_out > QAMW_PRODUCT_MAX_D_OUT || gated < 0 || gated > 1)
+        return QAMW_ERR_INVALID_ARG;
     if (!float_dtype(x_dtype) && x_dtype != QAMW_DTYPE_I8) return QAMW_ERR_INVALID_ARG;
-    // the codes, rows of whole 16 bytes, then their scales
-    *bytes_out = x_dtype == QAMW_DTYPE_I8 ? 0 : (size_t)m * round16((size_t)d_in) + round16((size_t)m * 4);
+    *bytes_out = codes_bytes(x_dtype, m, d_in) + qamw::product_scratch_bytes(m, d_out, d_in, gated != 0);
     return QAMW_OK;
 }
 
@@ -37,9 +43,9 @@ int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const fl
                      const float *w_scales, int64_t ldw, int d_out, int d_in, int gated, void *Y, int y_dtype, int64_t ldy,
                      void *workspace, size_t workspace_bytes, void *stream) {
     size_t need = 0;
-    const int rc = qamw_int8_matmul_workspace_bytes(x_dtype, m, d_in, &need);
+    const int rc = qamw_int8_matmul_workspace_bytes(x_dtype, m, d_out, d_in, gated, &need);
     if (rc != QAMW_OK) return rc;
-    if (d_out < 1 || d_out > QAMW_PRODUCT_MAX_D_OUT || !float_dtype(y_dtype) || gated < 0 || gated > 1) return QAMW_ERR_INVALID_ARG;
+    if (!float_dtype(y_dtype)) return QAMW_ERR_INVALID_ARG;
     const bool codes = x_dtype == QAMW_DTYPE_I8;
     if (m > 0 && (!X || !W || !w_scales || !Y || (codes && !x_scales) || (need && !workspace))) return QAMW_ERR_INVALID_ARG;
     if (codes ? col_scale != nullptr : x_scales != nullptr) return QAMW_ERR_INVALID_ARG;
@@ -60,6 +66,8 @@ int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const fl
     p.gated = gated != 0;
     p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
     p.stream = (hipStream_t)stream;
+    const size_t before = codes_bytes(x_dtype, m, d_in);
+    if (need > before) p.scratch = static_cast<char *>(workspace) + before;
     if (codes) {
         p.X = X;
         p.ldx = ldx;

@@ -118,7 +118,7 @@ def lib() -> C.CDLL:
         L.qamw_encode_pruned.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
         L.qamw_encode_pruned_ws.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, i32, i32, vp, vp, C.c_size_t, vp, vp, vp, vp]
         L.qamw_int8_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp, i64, vp, vp]
-        L.qamw_int8_matmul_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(C.c_size_t)]
+        L.qamw_int8_matmul_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, C.POINTER(C.c_size_t)]
         L.qamw_int8_matmul.argtypes = [vp, i32, vp, vp, i32, i64, vp, vp, i64, i32, i32, i32, vp, i32, i64, vp, C.c_size_t, vp]
         L.qamw_grouped_matmul.argtypes = [vp, i32, vp, i32, i64, vp, vp, vp, i64, i64, vp, i32, i32, i32, i32, i32, vp, i32, i64, vp]
         L.qamw_route_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(C.c_size_t)]
@@ -697,9 +697,9 @@ def int8_quantize(X, col_scale=None, out=None, stream=None):
 
 
 @functools.lru_cache(maxsize=256, typed=True)
-def int8_matmul_workspace_bytes(x_dtype: int, m: int, d_in: int) -> int:
+def int8_matmul_workspace_bytes(x_dtype: int, m: int, d_out: int, d_in: int, gated: bool = False) -> int:
     out = C.c_size_t()
-    _check(lib().qamw_int8_matmul_workspace_bytes(x_dtype, m, d_in, C.byref(out)), "qamw_int8_matmul_workspace_bytes")
+    _check(lib().qamw_int8_matmul_workspace_bytes(x_dtype, m, d_out, d_in, int(gated), C.byref(out)), "qamw_int8_matmul_workspace_bytes")
     return int(out.value)
 
 
@@ -722,7 +722,7 @@ def int8_matmul(X, W, w_scales, x_scales=None, col_scale=None, gated=False, out=
     d_out = outs // 2 if gated else outs
     y, y_code, ldy = _result(out, m, d_out, out_dtype, X, stream)
     if workspace is None:
-        size = int8_matmul_workspace_bytes(code, m, d_in)
+        size = int8_matmul_workspace_bytes(code, m, d_out, d_in, bool(gated))
         work = _new(1, size, torch.uint8, X, stream) if size else None      # kept until the launch
         at = _ptr(work)
     else:

@@ -46,11 +46,12 @@ def test_refusals_of_the_entry_points():
     assert quant(m=0, X=None, codes=None, scales=None) == qamw.OK
 
     need = C.c_size_t()
-    assert L.qamw_int8_matmul_workspace_bytes(0, 3, 17, C.byref(need)) == qamw.OK and need.value == 3 * 32 + 16
-    assert L.qamw_int8_matmul_workspace_bytes(2, 3, 17, C.byref(need)) == qamw.OK and need.value == 0
-    assert L.qamw_int8_matmul_workspace_bytes(3, 3, 17, C.byref(need)) == I
-    assert L.qamw_int8_matmul_workspace_bytes(0, 3, 131057, C.byref(need)) == I
-    assert L.qamw_int8_matmul_workspace_bytes(0, 3, 17, None) == I
+    size = lambda t, m, n, k, g=0: L.qamw_int8_matmul_workspace_bytes(t, m, n, k, g, C.byref(need))  # noqa: E731
+    assert size(0, 3, 8, 17) == qamw.OK and need.value == 3 * 32 + 16
+    assert size(2, 3, 8, 17) == qamw.OK and need.value == 0
+    assert size(2, 500, 2048, 13824) == qamw.OK and need.value > 0 and need.value % (500 * 2048 * 4) == 0   # the sums of parts
+    assert size(3, 3, 8, 17) == I and size(0, 3, 8, 131057) == I and size(0, 3, 0, 17) == I and size(0, 3, 8, 17, 2) == I
+    assert L.qamw_int8_matmul_workspace_bytes(0, 3, 8, 17, 0, None) == I
 
     def mm(X=p, xt=2, xs=p, cs=None, m=4, ldx=8, W=p, ws=p, ldw=8, d_out=8, d_in=8, gated=0, Y=p, yt=1, ldy=8, work=None, n=0):
         return L.qamw_int8_matmul(X, xt, xs, cs, m, ldx, W, ws, ldw, d_out, d_in, gated, Y, yt, ldy, work, n, None)
@@ -328,6 +329,34 @@ def test_int8_matmul_quantises_as_the_quantiser_does(m, d_out, d_in, x_dtype, sm
     if m:
         rc, rs = quantise_ref(f, c)
         assert torch.equal(y.cpu(), int8_ref(torch.from_numpy(rc), torch.from_numpy(rs), w, ws))
+
+
+@gpu
+@pytest.mark.parametrize("m,d_out,d_in", [(100, 2050, 13824), (500, 514, 13824), (129, 2049, 8192), (1000, 515, 4096)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_int8_matmul_in_parts(m, d_out, d_in, gated):
+    """Shapes whose columns are shared among workgroups: sums of parts, odd outputs, results in fp32 and bf16, a workspace of one's own."""
+    say(f"[int8] parts {m} x {d_out} x {d_in} gated {gated}")
+    g = _gen(m + d_in)
+    outs = d_out * (2 if gated else 1)
+    need = qamw.int8_matmul_workspace_bytes(qamw.DTYPE_I8, m, d_out, d_in, gated)
+    assert need > m * outs * 4
+    x, w, xs, ws = _codes(g, m, d_in), _codes(g, outs, d_in), torch.rand(m, generator=g) / (127 * math.sqrt(d_in)), (torch.rand(outs, generator=g) + 0.1) / 127
+    guarded = torch.full((need + 256,), 77, dtype=torch.uint8, device=DEV)
+    y = qamw.int8_matmul(x.to(DEV), w.to(DEV), ws.to(DEV), x_scales=xs.to(DEV), gated=gated, out_dtype=torch.float32, workspace=guarded[128:128 + need])
+    b = qamw.int8_matmul(x.to(DEV), w.to(DEV), ws.to(DEV), x_scales=xs.to(DEV), gated=gated)
+    assert (guarded[:128] == 77).all() and (guarded[128 + need:] == 77).all()
+    ref = int8_ref(x, xs, w, ws)
+    if gated:
+        want, slack = gate_ref(ref[:, :d_out], ref[:, d_out:], 0.0, 0.0)
+        check(y, want, slack, "fp32")
+    else:
+        assert torch.equal(y.cpu(), ref)
+    assert torch.equal(b.cpu(), y.cpu().bfloat16())
+    f = torch.randn(m, d_in, generator=g).bfloat16()              # codes and sums in one workspace
+    z = qamw.int8_matmul(f.to(DEV), w.to(DEV), ws.to(DEV), gated=gated, out_dtype=torch.float32)
+    c, s = qamw.int8_quantize(f.to(DEV))
+    assert torch.equal(z, qamw.int8_matmul(c, w.to(DEV), ws.to(DEV), x_scales=s, gated=gated, out_dtype=torch.float32))
 
 
 @gpu
