@@ -612,8 +612,8 @@ def calibrate_sigma_batch(items, block: int, workspace, stream=None):
 
 
 # ------------------------------------------------------------------ served layers: 8-bit products, routed experts
-# These calls are made for every layer of every token: a shape or a type is asked for once, and results of two dimensions are
-# made with their strides, which costs half as much as without.
+# These calls are made for every layer of every token: a shape or a type is asked for once, what is right is found so in one
+# expression, and results are made with their strides, which costs half as much as without.
 def _one_device(first, *others):
     """The index of the device that all tensors are on."""
     dev = first.get_device()
@@ -636,7 +636,7 @@ def _raw_stream(stream, dev):
 def _vector(t, name, dtype, shape):
     """A contiguous tensor of one type and shape, or None."""
     if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
 def _leading(shape, stride, name):
@@ -651,7 +651,9 @@ def _rows(t, name):
     shape = t.shape
     if len(shape) != 2:
         raise ValueError(f"{name} must be 2-D")
-    return shape[0], shape[1], _leading(shape, t.stride(), name)
+    m, d = shape
+    ld, step = t.stride()
+    return (m, d, ld) if step == 1 and m > 1 and d > 0 else (m, d, _leading(shape, (ld, step), name))
 
 
 def _new(m, d, dtype, like, stream):
@@ -667,12 +669,13 @@ def _result(out, m, d, dtype, like, stream):
     import torch
 
     if out is None:
-        out, ld = _new(m, d, dtype or torch.bfloat16, like, stream), d
-    else:
-        if out.shape != (m, d) or (dtype is not None and out.dtype != dtype):
-            raise ValueError(f"out must be {dtype or 'fp32 or bf16'} of shape {(m, d)}, got {out.dtype} {tuple(out.shape)}")
-        ld = _leading((m, d), out.stride(), "out")
-    return out, _dtype_code(out), ld
+        dtype = dtype or torch.bfloat16
+        if dtype != torch.bfloat16 and dtype != torch.float32:
+            raise TypeError(f"results are float32 or bfloat16, not {dtype}")
+        return _new(m, d, dtype, like, stream), DTYPE_BF16 if dtype == torch.bfloat16 else DTYPE_F32, d
+    if out.shape != (m, d) or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"out must be {dtype or 'fp32 or bf16'} of shape {(m, d)}, got {out.dtype} {tuple(out.shape)}")
+    return out, _dtype_code(out), _leading((m, d), out.stride(), "out")
 
 
 def int8_quantize(X, col_scale=None, out=None, stream=None):
@@ -788,10 +791,11 @@ def route(logits, k: int, renormalise=True, workspace=None, stream=None):
         at = _ptr(work)
     else:
         at, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    if stream is None:
-        make = torch.empty_strided
-        r = Routing(make((m, k), (k, 1), dtype=i32, device=on), make((m, k), (k, 1), dtype=torch.float32, device=on),
-                    make((n + 1,), (1,), dtype=i32, device=on), make((m * k,), (1,), dtype=i32, device=on), make((m, k), (k, 1), dtype=i32, device=on))
+    if stream is None:                                             # one allocation for all that is whole numbers
+        w = torch.empty_strided((m, k), (k, 1), dtype=torch.float32, device=on)
+        whole, part, slots = torch.empty_strided((3 * m * k + n + 1,), (1,), dtype=i32, device=on), torch.as_strided, m * k
+        r = Routing(part(whole, (m, k), (k, 1), 0), w, part(whole, (n + 1,), (1,), 3 * slots), part(whole, (slots,), (1,), 2 * slots),
+                    part(whole, (m, k), (k, 1), slots))
     else:
         r = Routing(_empty((m, k), i32, on, stream), _empty((m, k), torch.float32, on, stream), _empty((n + 1,), i32, on, stream),
                     _empty((m * k,), i32, on, stream), _empty((m, k), i32, on, stream))

@@ -312,7 +312,8 @@ def test_int8_matmul_strides(m, d_out, d_in, x_pad, w_pad, y_pad, skip, x_dtype)
 
 
 @gpu
-@pytest.mark.parametrize("m,d_out,d_in", [(1, 300, 512), (4, 300, 520), (13, 300, 5632), (50, 300, 1024), (300, 520, 768), (0, 20, 64)])
+@pytest.mark.parametrize("m,d_out,d_in", [(1, 300, 512), (4, 300, 520), (13, 300, 5632), (50, 300, 1024), (300, 520, 768), (0, 20, 64), (16, 33, 4096), (5, 2048, 8192), (9, 1000, 528),
+                                       (2, 50, 8192), (4, 70, 4096), (1, 40, 16384), (1, 40, 8208), (13, 4000, 4096), (16, 100, 8192)])
 @pytest.mark.parametrize("x_dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("smooth", [False, True])
 def test_int8_matmul_quantises_as_the_quantiser_does(m, d_out, d_in, x_dtype, smooth):
