@@ -8,10 +8,24 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 
 // ---- choice ---------------------------------------------------------------------------------------------------------------
 //
-// A wave has a token, a lane the experts lane, lane + 64, ...  A logit becomes an unsigned number that orders as it does, 0 for
-// what is never chosen (-inf, NaN); the largest of the wave wins, of equals the lowest expert.
-__device__ __forceinline__ float wave_sum(float v) {
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+// Sixteen lanes have a token, so that the largest of its logits is found by DPP within a row of lanes, for four tokens of a wave at a
+// time; a lane has PER experts that follow one another.  A logit becomes an unsigned number that orders as it does, 0 for what is
+// never chosen (-inf, NaN).  bf16 leaves room for the expert in the lower half, the lowest one as the largest number, so that one
+// maximum finds both; fp32 takes the lowest lane that has the maximum, and the lowest of its experts.
+constexpr int RT_LANES = 16, RT_GROUPS = WAVE / RT_LANES;
+
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));    // lane ^ 1
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));    // lane ^ 2
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xF, 0xF, false));   // the other four of eight
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140, 0xF, 0xF, false));   // the other eight of sixteen
+    return v;
+}
+__device__ __forceinline__ float row_sum(float v) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, false));
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false));
     return v;
 }
 __device__ __forceinline__ uint32_t key_of(float f) {
@@ -23,53 +37,72 @@ __device__ __forceinline__ uint32_t key_of(float f) {
 __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
+// exp(x - top), x <= top; infinities of one sign are equal
+__device__ __forceinline__ float share_of(float x, float top) { return x == top ? 1.0f : __expf(x - top); }
 
-// Lane j < k gets the j-th choice: its expert (-1: none) and weight.
-template <int DTYPE, int NPL>
-__device__ __forceinline__ void pick(const void *logits, int64_t at, int n, int k, bool renormalise, int &expert, float &weight) {
-    const int lane = threadIdx.x % WAVE;
-    uint32_t key[NPL];
-    for (int i = 0; i < NPL; ++i) {
-        const int e = lane + i * WAVE;
-        key[i] = e < n ? key_of(Elem<DTYPE>::load(logits, at + e)) : 0;
-    }
-    float total = 0.0f, top = 0.0f, mine = 0.0f;
-    expert = -1;
-    weight = 0.0f;
-    for (int j = 0; j < k; ++j) {
-        uint32_t best = 0;
-        for (int i = 0; i < NPL; ++i) best = max(best, key[i]);
-        best = wave_max(best);
-        if (best == 0) break;
-        int who = 0;
+// Lane j of a token's sixteen gets its choices j and j + 16: the experts (-1: none) and weights.  t >= m: none.
+template <int DTYPE, int PER>
+__device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&expert)[2], float (&weight)[2]) {
+    constexpr bool PACKED = DTYPE == 1;
+    const int lane = threadIdx.x % RT_LANES, n = q.n_experts, e0 = lane * PER;
+    using E = typename Elem<DTYPE>::type;
+    uint32_t key[PER];
+    Unaligned<E, PER> row;                                  // wherever it lies: the memory instructions take any address
+    const bool whole = t < q.m && e0 + PER <= n;
+    if (whole) row = *reinterpret_cast<const Unaligned<E, PER> *>(static_cast<const E *>(q.logits) + t * q.ld + e0);
 #pragma unroll
-        for (int i = NPL - 1; i >= 0; --i) {
-            const unsigned long long has = __ballot(key[i] == best);
-            if (has) who = i * WAVE + __ffsll((long long)has) - 1;
-        }
-        const float v = value_of(best);
+    for (int i = 0; i < PER; ++i) {
+        if (!whole) row.v[i] = t < q.m && e0 + i < n ? static_cast<const E *>(q.logits)[t * q.ld + e0 + i] : E(0);
+        const float f = DTYPE == 1 ? __uint_as_float((uint32_t)row.v[i] << 16) : (float)row.v[i];
+        key[i] = t < q.m && e0 + i < n ? key_of(f) : 0;
+        if (PACKED && key[i]) key[i] = (key[i] & 0xFFFF0000u) | (0xFFFFu - (uint32_t)(e0 + i));
+    }
+    // the value of a packed key: all its lower half is 1 for negative values
+    auto value = [](uint32_t k) { return value_of(PACKED ? (k & 0x80000000u ? k & 0xFFFF0000u : k | 0xFFFFu) : k); };
+    float total = 0.0f, top = 0.0f, mine[2] = {0.0f, 0.0f};
+    expert[0] = expert[1] = -1;
+    for (int j = 0; j < q.k; ++j) {
+        uint32_t own = key[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) own = max(own, key[i]);
+        const uint32_t best = row_max(own);
+        const bool some = best != 0;
+        if (!__any(some)) break;
+        const float v = value(best);
         if (j == 0) {
             top = v;
-            if (!renormalise) {
+            if (!q.renormalise) {
                 float sum = 0.0f;
-                for (int i = 0; i < NPL; ++i)
-                    if (key[i]) {
-                        const float x = value_of(key[i]);
-                        sum += x == top ? 1.0f : expf(x - top);
-                    }
-                total = wave_sum(sum);
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (key[i]) sum += share_of(value(key[i]), top);
+                total = row_sum(sum);
             }
         }
-        const float p = v == top ? 1.0f : expf(v - top);
-        if (renormalise) total += p;
-        if (lane == j) {
-            expert = who;
-            mine = p;
+        int who;
+        if (PACKED) {
+            who = (int)(0xFFFFu - (best & 0xFFFFu));
+#pragma unroll
+            for (int i = 0; i < PER; ++i) key[i] = key[i] == best ? 0 : key[i];
+        } else {
+            const uint32_t has = (uint32_t)(__ballot(own == best) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu;
+            const int winner = __ffs((int)has) - 1;
+            int at = 0;
+#pragma unroll
+            for (int i = PER - 1; i >= 0; --i) at = key[i] == best ? i : at;
+            who = __shfl(e0 + at, winner, RT_LANES);
+            at = lane == winner ? at : -1;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) key[i] = i == at ? 0 : key[i];
         }
-        for (int i = 0; i < NPL; ++i)
-            if (lane + i * WAVE == who) key[i] = 0;
+        const float p = some ? share_of(v, top) : 0.0f;
+        if (q.renormalise) total += p;
+        if (some && lane == j % RT_LANES) {
+            expert[j / RT_LANES] = who;
+            mine[j / RT_LANES] = p;
+        }
     }
-    if (expert >= 0) weight = mine / total;
+    for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 ? mine[h] / total : 0.0f;
 }
 
 // ---- order ----------------------------------------------------------------------------------------------------------------
@@ -98,42 +131,44 @@ __device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
     return before;
 }
 
-template <int DTYPE, int NPL, bool ALONE>
-__global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q, int per_wave) {
+template <int DTYPE, int PER, bool ALONE>
+__global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
     extern __shared__ uint32_t rt_lds[];                    // [RT_WAVES][n_experts]: counts, then what comes before them
     __shared__ uint32_t all;
     const int n = q.n_experts, k = q.k, lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
     uint32_t *mine = rt_lds + wave * n, *total = rt_lds + RT_WAVES * n;
     for (int i = threadIdx.x; i < RT_WAVES * n; i += RT_THREADS) rt_lds[i] = 0;
     __syncthreads();
-    const int t0 = (blockIdx.x * RT_WAVES + wave) * per_wave, t1 = min(t0 + per_wave, q.m);
-    const int at_once = WAVE / k;                            // tokens whose slots are ranked together
-    for (int g0 = t0; g0 < t1; g0 += at_once) {
-        const int g1 = min(g0 + at_once, t1);
-        int e = -1;                                          // lane's slot: token g0 + lane / k, choice lane % k
-        for (int t = g0; t < g1; ++t) {
-            int expert;
-            float weight;
-            pick<DTYPE, NPL>(q.logits, (int64_t)t * q.ld, n, k, q.renormalise, expert, weight);
-            if (lane < k) q.weights[(int64_t)t * k + lane] = weight;
-            const int from = lane - (t - g0) * k, got = __shfl(expert, from & (WAVE - 1));
-            if (from >= 0 && from < k) e = got;
-        }
-        unsigned long long same = __ballot(e >= 0);
-        for (int b = 0; b < 10; ++b) {
-            const unsigned long long has = __ballot((e >> b) & 1);
-            same &= (e >> b) & 1 ? has : ~has;
-        }
-        if (lane < (g1 - g0) * k) {
-            const int64_t at = (int64_t)g0 * k + lane;
-            int rank = -1;
-            if (e >= 0) {
-                rank = (int)mine[e] + __popcll(same & ((1ull << lane) - 1));
-                // the wave's LDS accesses are made in order: all ranks are read before the last slot of an expert counts them
-                if ((same >> lane) == 1) mine[e] = (uint32_t)rank + 1;
+    const int t0 = (blockIdx.x * RT_WAVES + wave) * RT_GROUPS, t1 = min(t0 + RT_GROUPS, q.m);
+    if (t0 < t1) {
+        int expert[2];
+        float weight[2];
+        pick<DTYPE, PER>(q, t0 + lane / RT_LANES, expert, weight);
+        const int at_once = k <= RT_LANES ? RT_GROUPS : 2;       // tokens whose slots are ranked together
+        for (int g0 = t0; g0 < t1; g0 += at_once) {
+            // lane's slot: token g0 + lane / k, choice lane % k
+            const int token = lane / k, choice = lane % k, from = ((g0 - t0 + token) % RT_GROUPS) * RT_LANES + choice % RT_LANES;
+            const bool is = token < at_once && g0 + token < t1;
+            const int lo = __shfl(expert[0], from), hi = __shfl(expert[1], from);
+            const float wlo = __shfl(weight[0], from), whi = __shfl(weight[1], from);
+            const int e = !is ? -1 : choice < RT_LANES ? lo : hi;
+            unsigned long long same = __ballot(e >= 0);
+            for (int b = 0; b < 10; ++b) {
+                const unsigned long long has = __ballot((e >> b) & 1);
+                same &= (e >> b) & 1 ? has : ~has;
             }
-            q.experts[at] = e;
-            q.positions[at] = rank;
+            if (is) {
+                const int64_t at = (int64_t)g0 * k + lane;
+                int rank = -1;
+                if (e >= 0) {
+                    rank = (int)mine[e] + __popcll(same & ((1ull << lane) - 1));
+                    // the wave's LDS accesses are made in order: all ranks are read before the last slot of an expert counts them
+                    if ((same >> lane) == 1) mine[e] = (uint32_t)rank + 1;
+                }
+                q.experts[at] = e;
+                q.weights[at] = choice < RT_LANES ? wlo : whi;
+                q.positions[at] = rank;
+            }
         }
     }
     __syncthreads();
@@ -280,29 +315,28 @@ __global__ __launch_bounds__(CB_THREADS) void k_combine(const void *Y, int64_t y
     }
 }
 
-// Tokens of a wave of the first launch, 16 times that of its workgroup.
-constexpr int RT_PER_WAVE = 4;
-constexpr int RT_TOKENS = RT_PER_WAVE * RT_WAVES;
+// Tokens of a workgroup of the first launch.
+constexpr int RT_TOKENS = RT_GROUPS * RT_WAVES;
 
-template <int DTYPE, int NPL> hipError_t launch_pick(const RouteProblem &q, int blocks) {
+template <int DTYPE, int PER> hipError_t launch_pick(const RouteProblem &q, int blocks) {
     const size_t lds = ((size_t)RT_WAVES + 1) * q.n_experts * 4;
     static const hipError_t once = [] {
-        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_route_pick<DTYPE, NPL, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
+        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
         if (e != hipSuccess) return e;
-        return hipFuncSetAttribute(reinterpret_cast<const void *>(&k_route_pick<DTYPE, NPL, false>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
+        return hipFuncSetAttribute(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, false>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
     }();
     if (once != hipSuccess) return once;
-    if (blocks == 1) k_route_pick<DTYPE, NPL, true><<<1, RT_THREADS, lds, q.stream>>>(q, RT_PER_WAVE);
-    else k_route_pick<DTYPE, NPL, false><<<blocks, RT_THREADS, lds, q.stream>>>(q, RT_PER_WAVE);
+    if (blocks == 1) k_route_pick<DTYPE, PER, true><<<1, RT_THREADS, lds, q.stream>>>(q);
+    else k_route_pick<DTYPE, PER, false><<<blocks, RT_THREADS, lds, q.stream>>>(q);
     return hipGetLastError();
 }
 template <int DTYPE> hipError_t launch_pick(const RouteProblem &q, int blocks) {
-    const int lanes = (q.n_experts + WAVE - 1) / WAVE;      // experts of a lane
-    if (lanes <= 1) return launch_pick<DTYPE, 1>(q, blocks);
-    if (lanes <= 2) return launch_pick<DTYPE, 2>(q, blocks);
-    if (lanes <= 4) return launch_pick<DTYPE, 4>(q, blocks);
-    if (lanes <= 8) return launch_pick<DTYPE, 8>(q, blocks);
-    return launch_pick<DTYPE, 16>(q, blocks);
+    if (q.n_experts <= 16) return launch_pick<DTYPE, 1>(q, blocks);
+    if (q.n_experts <= 64) return launch_pick<DTYPE, 4>(q, blocks);
+    if (q.n_experts <= 128) return launch_pick<DTYPE, 8>(q, blocks);
+    if (q.n_experts <= 256) return launch_pick<DTYPE, 16>(q, blocks);
+    if (q.n_experts <= 512) return launch_pick<DTYPE, 32>(q, blocks);
+    return launch_pick<DTYPE, 64>(q, blocks);
 }
 
 template <int DTYPE, bool OBF16>
