@@ -114,12 +114,12 @@ struct Plan {
     int tile_rows, parts;
     double us;
 };
-constexpr double LAUNCH = 4.0, MEMORY = 4.7e6, PARTS_RATE = 5.5e6, FEW_RATE = 5.8e4;
+constexpr double LAUNCH = 4.0, MEMORY = 4.7e6, PARTS_RATE = 6.2e6, FEW_RATE = 5.8e4;
 struct WideCost {
     int rows;
     double tile, stage;
 };
-constexpr WideCost WIDE[3] = {{64, 2.0, 0.52}, {128, 3.0, 0.57}, {256, 5.0, 0.70}};
+constexpr WideCost WIDE[3] = {{64, 2.5, 0.70}, {128, 4.4, 0.82}, {256, 7.7, 1.16}};
 
 // groups: how many have rows, at most; row tiles are expected to be half a tile short.
 Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, bool gated, bool i8, bool may_part) {
@@ -142,10 +142,10 @@ Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, 
         const double slot = 2048.0 * ((gated ? 2 : 1) + rows / 16), work = rounds(tiles * split / 4) * units * 4 / split * slot / FEW_RATE;
         offer(true, rows, 1, LAUNCH + (work > weights ? work : weights));
     }
-    const double cols = (double)((outs + 255) / 256), stages = (double)((bytes + 63) / 64);
+    const double cols = (double)((outs + 255) / 256), stages = (double)units;
     for (const WideCost &c : WIDE)
         for (int parts : {1, 2, 3, 4, 6, 8}) {
-            if (parts > 1 && (!may_part || stages < parts * 8)) break;
+            if (parts > 1 && (!may_part || stages < parts * 4)) break;
             const double work = rounds(row_tiles(c.rows) * cols * parts) * (c.tile + stages / parts * c.stage);
             double us = LAUNCH + (work > weights ? work : weights);
             if (parts > 1) us += 2.5 + 8.0 * parts * m * outs / PARTS_RATE;

@@ -1,11 +1,12 @@
 // Y = X W^T on the matrix cores for many rows: 8-bit integers with scales or bf16, one matrix or one for each expert.
 //
-// A workgroup of eight waves has a tile of BN rows of W and BM of X and steps over 64 bytes of both at a time (a stage: 64
-// columns of int8, 32 of bf16).  16 rows of a stage are a fragment, 1 KB in LDS, filled by one buffer load of a wave that goes
-// to LDS directly and read by one 16-byte LDS read of a wave: the operand of a 16x16 matrix instruction.
-//   In LDS the four 16-byte pieces of a row are exchanged by (row / 2) mod 4, or the lanes of a read would meet in half of
-//   the banks; the loading lanes ask for their piece accordingly, from the same 64 bytes.
-//   Four or five stages are in LDS: one is read, the next ones are on their way.
+// A workgroup of eight waves has a tile of BN rows of W and BM of X and steps over 128 bytes of both at a time (a stage: 128
+// columns of int8, 64 of bf16).  16 rows of a stage are a fragment, 2 KB in LDS, filled by two buffer loads of a wave that go
+// to LDS directly, eight whole lines each, and read by two 16-byte LDS reads of a wave: the operands of 16x16 matrix instructions.
+//   In LDS the eight 16-byte pieces of a row are exchanged by row mod 8, or the lanes of a read would meet in some of the
+//   banks; the loading lanes ask for their piece accordingly, from the same 128 bytes.
+//   A stage has two steps: X and half of each wave's W, then the other half of W with X in registers.  Two stages are in
+//   LDS; what a step has read is free for the stage after the next one, whose loads have a whole stage's time to come.
 //   The waves form two groups of four, one wave of each group on every SIMD.  While one group reads its fragments the other
 //   multiplies, then they change places; a barrier is all that they need to keep in step.
 // What is not there (rows past the end, columns past d_in, stages past the last) is loaded as zeros: such a lane asks for an
@@ -15,113 +16,115 @@
 namespace qamw {
 namespace {
 
-constexpr int PW_WAVES = 8, PW_THREADS = PW_WAVES * WAVE, PW_FRAG = 1024, PW_KB = 64, PW_CUS = 256, PW_TURN = 2048;
+constexpr int PW_WAVES = 8, PW_THREADS = PW_WAVES * WAVE, PW_FRAG = 2048, PW_KB = 128, PW_CUS = 256, PW_TURN = 2048;
 constexpr uint32_t PW_NOWHERE = 0x80000000u;       // added to an offset: beyond the end of any buffer here
 
-// Tiles: WN x WM waves, each of FN fragments of W and FM of X, and as many stages as LDS holds: where W comes from memory a stage
-// takes about 1.6 us to come.
-template <int WN_, int FN_, int WM_, int FM_, int STAGES_> struct Shape {
-    static constexpr int WN = WN_, FN = FN_, WM = WM_, FM = FM_, STAGES = STAGES_, BN = WN * FN * 16, BM = WM * FM * 16;
-    static constexpr int NW = WN * FN, NX = WM * FM;                          // fragments of a stage
-    static constexpr int LW = NW / PW_WAVES, LX = (NX + PW_WAVES - 1) / PW_WAVES;   // loads of a wave: fragments wave, wave + 8, ...
-    static constexpr int STAGE = (NW + LX * PW_WAVES) * PW_FRAG;              // where NX < 8, room for what some waves load for nothing
-    static_assert(WN * WM == PW_WAVES && NW % PW_WAVES == 0, "");
+// Tiles: WN x WM waves, each of FN fragments of W and FM of X.  A stage in LDS: the first halves of the waves' fragments of W, the second
+// halves, X.
+template <int WN_, int FN_, int WM_, int FM_> struct Shape {
+    static constexpr int WN = WN_, FN = FN_, WM = WM_, FM = FM_, BN = WN * FN * 16, BM = WM * FM * 16;
+    static constexpr int HN = FN / 2, NW = WN * FN, NX = WM * FM;             // fragments of a step, and of a stage
+    static constexpr int LW = NW / PW_WAVES, LX = NX * 2 / PW_WAVES;          // loads of a wave, 8 rows each: of half of W, of X
+    static constexpr int SECOND = NW / 2 * PW_FRAG, X = NW * PW_FRAG, STAGE = (NW + NX) * PW_FRAG;
+    static_assert(WN * WM == PW_WAVES && NW % PW_WAVES == 0 && NX * 2 % PW_WAVES == 0 && BN == 256 && BM <= 256, "");
 };
 
-// FN + FM fragments of one stage are read, and LW + LX pieces of a stage to come are asked for while they come: the loads' issue
-// takes as long as the reads.  The fragments are complete when this returns.  `to`: where the first piece goes, the others 8 KB on each.
 typedef uint32_t pw_u32x4_t __attribute__((ext_vector_type(4)));
-template <int FN, int FM, int LW, int LX>
-__device__ __forceinline__ void read_and_request(uint32_t at_w, uint32_t at_x, pr_i32x4_t (&w)[FN], pr_i32x4_t (&x)[FM], const uint32_t (&off_w)[LW],
-                                                 const uint32_t (&off_x)[LX], pw_u32x4_t wr, pw_u32x4_t xr, uint32_t so, uint32_t to) {
-    static_assert(FM == 4 && LW == 2 && LX == (FN == 8 ? 2 : 1), "");
-    if constexpr (FN == 8) {
+
+// The two steps of a stage: what they read, and the loads that they issue while that comes.  Complete when they return, but for the loads.
+// Both 64-byte halves of a row: their pieces are 64 bytes apart, exchanged by bit 6.  The loads go to LDS from `to` on, 8 KB apart.
+template <int HN, int FM, int LW>
+__device__ __forceinline__ void read_first(uint32_t at_w, uint32_t at_x, pr_i32x4_t (&w)[2][HN], pr_i32x4_t (&x)[2][FM], const uint32_t (&off_w)[LW],
+                                           pw_u32x4_t wr, uint32_t so, uint32_t to) {
+    static_assert(FM == 4 && LW == 2 && (HN == 4 || HN == 2 || HN == 1), "");
+    if constexpr (HN == 4) {
         asm volatile(
-            "ds_read_b128 %8, %13\n\t"
-            "ds_read_b128 %9, %13 offset:1024\n\t"
-            "ds_read_b128 %10, %13 offset:2048\n\t"
-            "ds_read_b128 %11, %13 offset:3072\n\t"
-            "ds_read_b128 %0, %12\n\t"
-            "ds_read_b128 %1, %12 offset:1024\n\t"
-            "ds_read_b128 %2, %12 offset:2048\n\t"
-            "ds_read_b128 %3, %12 offset:3072\n\t"
-            "ds_read_b128 %4, %12 offset:4096\n\t"
-            "ds_read_b128 %5, %12 offset:5120\n\t"
-            "ds_read_b128 %6, %12 offset:6144\n\t"
-            "ds_read_b128 %7, %12 offset:7168\n\t"
-            "s_mov_b32 m0, %21\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %14, %18, %20 offen lds\n\t"
-            "s_add_u32 m0, m0, 0x2000\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %15, %18, %20 offen lds\n\t"
-            "s_add_u32 m0, m0, 0x2000\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %16, %19, %20 offen lds\n\t"
-            "s_add_u32 m0, m0, 0x2000\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %17, %19, %20 offen lds\n\t"
-            "s_waitcnt lgkmcnt(0)"
-            : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(w[4]), "=&v"(w[5]), "=&v"(w[6]), "=&v"(w[7]), "=&v"(x[0]),
-              "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-            : "v"(at_w), "v"(at_x), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "v"(off_x[1]), "s"(wr), "s"(xr), "s"(so), "s"(to)
+            "ds_read_b128 %0, %18\n\tds_read_b128 %1, %18 offset:2048\n\tds_read_b128 %2, %18 offset:4096\n\t"
+            "ds_read_b128 %3, %18 offset:6144\n\tds_read_b128 %8, %16\n\tds_read_b128 %9, %16 offset:2048\n\t"
+            "ds_read_b128 %10, %16 offset:4096\n\tds_read_b128 %11, %16 offset:6144\n\tds_read_b128 %4, %19\n\t"
+            "ds_read_b128 %5, %19 offset:2048\n\tds_read_b128 %6, %19 offset:4096\n\t"
+            "ds_read_b128 %7, %19 offset:6144\n\tds_read_b128 %12, %17\n\tds_read_b128 %13, %17 offset:2048\n\t"
+            "ds_read_b128 %14, %17 offset:4096\n\tds_read_b128 %15, %17 offset:6144\n\ts_mov_b32 m0, %24\n\t"
+            "s_nop 0\n\tbuffer_load_dwordx4 %20, %22, %23 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %21, %22, %23 offen lds\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[0][3]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[1][2]),
+              "=&v"(x[1][3]), "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[0][2]), "=&v"(w[0][3]), "=&v"(w[1][0]), "=&v"(w[1][1]),
+              "=&v"(w[1][2]), "=&v"(w[1][3])
+            : "v"(at_w), "v"(at_w ^ 64u), "v"(at_x), "v"(at_x ^ 64u), "v"(off_w[0]), "v"(off_w[1]), "s"(wr), "s"(so), "s"(to)
             : "memory", "scc");
-    } else if constexpr (FN == 4) {
+    } else if constexpr (HN == 2) {
         asm volatile(
-            "ds_read_b128 %4, %9\n\t"
-            "ds_read_b128 %5, %9 offset:1024\n\t"
-            "ds_read_b128 %6, %9 offset:2048\n\t"
-            "ds_read_b128 %7, %9 offset:3072\n\t"
-            "ds_read_b128 %0, %8\n\t"
-            "ds_read_b128 %1, %8 offset:1024\n\t"
-            "ds_read_b128 %2, %8 offset:2048\n\t"
-            "ds_read_b128 %3, %8 offset:3072\n\t"
-            "s_mov_b32 m0, %16\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %10, %13, %15 offen lds\n\t"
-            "s_add_u32 m0, m0, 0x2000\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %11, %13, %15 offen lds\n\t"
-            "s_add_u32 m0, m0, 0x2000\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %12, %14, %15 offen lds\n\t"
+            "ds_read_b128 %0, %14\n\tds_read_b128 %1, %14 offset:2048\n\tds_read_b128 %2, %14 offset:4096\n\t"
+            "ds_read_b128 %3, %14 offset:6144\n\tds_read_b128 %8, %12\n\tds_read_b128 %9, %12 offset:2048\n\t"
+            "ds_read_b128 %4, %15\n\tds_read_b128 %5, %15 offset:2048\n\tds_read_b128 %6, %15 offset:4096\n\t"
+            "ds_read_b128 %7, %15 offset:6144\n\tds_read_b128 %10, %13\n\tds_read_b128 %11, %13 offset:2048\n\t"
+            "s_mov_b32 m0, %20\n\ts_nop 0\n\tbuffer_load_dwordx4 %16, %18, %19 offen lds\n\t"
+            "s_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\tbuffer_load_dwordx4 %17, %18, %19 offen lds\n\t"
             "s_waitcnt lgkmcnt(0)"
-            : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-            : "v"(at_w), "v"(at_x), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "s"(wr), "s"(xr), "s"(so), "s"(to)
+            : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[0][3]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[1][2]),
+              "=&v"(x[1][3]), "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[1][0]), "=&v"(w[1][1])
+            : "v"(at_w), "v"(at_w ^ 64u), "v"(at_x), "v"(at_x ^ 64u), "v"(off_w[0]), "v"(off_w[1]), "s"(wr), "s"(so), "s"(to)
             : "memory", "scc");
     } else {
-        static_assert(FN == 2, "");
         asm volatile(
-            "ds_read_b128 %2, %7\n\t"
-            "ds_read_b128 %3, %7 offset:1024\n\t"
-            "ds_read_b128 %4, %7 offset:2048\n\t"
-            "ds_read_b128 %5, %7 offset:3072\n\t"
-            "ds_read_b128 %0, %6\n\t"
-            "ds_read_b128 %1, %6 offset:1024\n\t"
-            "s_mov_b32 m0, %14\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %8, %11, %13 offen lds\n\t"
-            "s_add_u32 m0, m0, 0x2000\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %9, %11, %13 offen lds\n\t"
-            "s_add_u32 m0, m0, 0x2000\n\t"
-            "s_nop 0\n\t"
-            "buffer_load_dwordx4 %10, %12, %13 offen lds\n\t"
-            "s_waitcnt lgkmcnt(0)"
-            : "=&v"(w[0]), "=&v"(w[1]), "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
-            : "v"(at_w), "v"(at_x), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "s"(wr), "s"(xr), "s"(so), "s"(to)
+            "ds_read_b128 %0, %12\n\tds_read_b128 %1, %12 offset:2048\n\tds_read_b128 %2, %12 offset:4096\n\t"
+            "ds_read_b128 %3, %12 offset:6144\n\tds_read_b128 %8, %10\n\tds_read_b128 %4, %13\n\t"
+            "ds_read_b128 %5, %13 offset:2048\n\tds_read_b128 %6, %13 offset:4096\n\t"
+            "ds_read_b128 %7, %13 offset:6144\n\tds_read_b128 %9, %11\n\ts_mov_b32 m0, %18\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %14, %16, %17 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %15, %16, %17 offen lds\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[0][2]), "=&v"(x[0][3]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[1][2]),
+              "=&v"(x[1][3]), "=&v"(w[0][0]), "=&v"(w[1][0])
+            : "v"(at_w), "v"(at_w ^ 64u), "v"(at_x), "v"(at_x ^ 64u), "v"(off_w[0]), "v"(off_w[1]), "s"(wr), "s"(so), "s"(to)
             : "memory", "scc");
     }
 }
-// The same pieces without the reads, and four bytes a lane.
-template <int LW, int LX>
-__device__ __forceinline__ void request(const uint32_t (&off_w)[LW], const uint32_t (&off_x)[LX], pw_u32x4_t wr, pw_u32x4_t xr, uint32_t so, uint32_t to) {
-#pragma unroll
-    for (int i = 0; i < LW + LX; ++i)
-        asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(
-                         i < LW ? off_w[i < LW ? i : 0] : off_x[i < LW ? 0 : i - LW]),
-                     "s"(i < LW ? wr : xr), "s"(so), "s"(to + i * PW_WAVES * PW_FRAG)
-                     : "memory");
+template <int HN, int LW, int LX>
+__device__ __forceinline__ void read_second(uint32_t at_w, pr_i32x4_t (&w)[2][HN], const uint32_t (&off_w)[LW], const uint32_t (&off_x)[LX], pw_u32x4_t wr,
+                                            pw_u32x4_t xr, uint32_t so, uint32_t to_w, uint32_t to_x) {
+    static_assert(LW == 2 && LX == HN && (HN == 4 || HN == 2 || HN == 1), "");
+    if constexpr (LX == 4) {
+        asm volatile(
+            "ds_read_b128 %0, %8\n\tds_read_b128 %1, %8 offset:2048\n\tds_read_b128 %2, %8 offset:4096\n\t"
+            "ds_read_b128 %3, %8 offset:6144\n\tds_read_b128 %4, %9\n\tds_read_b128 %5, %9 offset:2048\n\t"
+            "ds_read_b128 %6, %9 offset:4096\n\tds_read_b128 %7, %9 offset:6144\n\ts_mov_b32 m0, %20\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %12, %17, %18 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %13, %17, %18 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %14, %17, %18 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %15, %17, %18 offen lds\n\ts_mov_b32 m0, %19\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %10, %16, %18 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %11, %16, %18 offen lds\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[0][2]), "=&v"(w[0][3]), "=&v"(w[1][0]), "=&v"(w[1][1]), "=&v"(w[1][2]),
+              "=&v"(w[1][3])
+            : "v"(at_w), "v"(at_w ^ 64u), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "v"(off_x[1]), "v"(off_x[2]), "v"(off_x[3]),
+              "s"(wr), "s"(xr), "s"(so), "s"(to_w), "s"(to_x)
+            : "memory", "scc");
+    } else if constexpr (LX == 2) {
+        asm volatile(
+            "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:2048\n\tds_read_b128 %2, %5\n\t"
+            "ds_read_b128 %3, %5 offset:2048\n\ts_mov_b32 m0, %14\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %8, %11, %12 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %9, %11, %12 offen lds\n\ts_mov_b32 m0, %13\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %6, %10, %12 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %7, %10, %12 offen lds\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(w[0][0]), "=&v"(w[0][1]), "=&v"(w[1][0]), "=&v"(w[1][1])
+            : "v"(at_w), "v"(at_w ^ 64u), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "v"(off_x[1]), "s"(wr), "s"(xr), "s"(so), "s"(to_w),
+              "s"(to_x)
+            : "memory", "scc");
+    } else {
+        asm volatile(
+            "ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_mov_b32 m0, %11\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %6, %8, %9 offen lds\n\ts_mov_b32 m0, %10\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %4, %7, %9 offen lds\n\ts_add_u32 m0, m0, 0x2000\n\ts_nop 0\n\t"
+            "buffer_load_dwordx4 %5, %7, %9 offen lds\n\ts_waitcnt lgkmcnt(0)"
+            : "=&v"(w[0][0]), "=&v"(w[1][0])
+            : "v"(at_w), "v"(at_w ^ 64u), "v"(off_w[0]), "v"(off_w[1]), "v"(off_x[0]), "s"(wr), "s"(xr), "s"(so), "s"(to_w), "s"(to_x)
+            : "memory", "scc");
+    }
+}
+// A load alone, of 16 bytes a lane or 4.
+__device__ __forceinline__ void request(uint32_t off, pw_u32x4_t from, uint32_t so, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(off), "s"(from), "s"(so), "s"(to) : "memory");
 }
 __device__ __forceinline__ void request_dword(uint32_t off, pw_u32x4_t from, uint32_t to) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(off), "s"(from), "s"(to) : "memory");
@@ -146,12 +149,18 @@ template <> struct Store<true> {
     using type = uint16_t;
 };
 
+template <int V> struct Half {
+    static constexpr int value = V;
+};
+using First = Half<0>;
+using Second = Half<1>;
+
 // A tile: where its rows are, and what this lane asks for of them.
 template <typename S> struct Tile {
     int expert, row0, n, ct;                         // rows row0 .. row0 + n, the ct-th outputs; n = 0: no tile
     int part, full;                                  // the part of the columns, its stages
     const char *w, *x;
-    uint32_t off_w[S::LW], off_x[S::LX], off_scale;
+    uint32_t off_w[2][S::LW], off_x[S::LX], off_scale;
 };
 
 // OUT: what is stored: 0 fp32, 1 bf16, 2 the sums of a part of the columns as they are (int32 or fp32), one array of `part_stride`
@@ -163,7 +172,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     extern __shared__ __align__(16) char pw_lds[];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)pw_lds;
-    const uint32_t turn = lds0 + S::STAGES * S::STAGE + wave * PW_TURN, scales0 = lds0 + S::STAGES * S::STAGE + PW_WAVES * PW_TURN;
+    const uint32_t turn = lds0 + 2 * S::STAGE + wave * PW_TURN, scales0 = lds0 + 2 * S::STAGE + PW_WAVES * PW_TURN;
 
     // Workgroups go to the 8 XCDs in turn: an XCD gets tiles that follow one another, and these are ordered such that `group` row
     // tiles share their W while it is in the XCD's cache.
@@ -173,7 +182,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     auto out_of = [&](int ct, int f, int r) { return GATED ? ct * (S::BN / 2) + (f >> 1) * 16 + r : ct * S::BN + f * 16 + r; };
     auto w_row = [&](int ct, int f, int r) { return (int64_t)(GATED && (f & 1) ? a.d_out : 0) + out_of(ct, f, r); };
     const int bytes = a.d_in * M::ELEM, every = (bytes + PW_KB - 1) / PW_KB;
-    const int lr = lane >> 2, piece = ((lane ^ (lane >> 3)) & 3) * 16;
+    const int lr = lane >> 3, piece = ((lane & 7) ^ lr) * 16;
     const bool past = (every - 1) * PW_KB + piece >= bytes;                   // nothing there in the last stage of all
 
     ExpertTiles et = {0, 0, 0, 0, 0};
@@ -183,7 +192,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         z.w = z.x = nullptr;
         z.expert = z.row0 = z.ct = z.part = z.full = 0;
         z.off_scale = PW_NOWHERE;
-        for (int i = 0; i < S::LW; ++i) z.off_w[i] = PW_NOWHERE;
+        for (int i = 0; i < S::LW; ++i) z.off_w[0][i] = z.off_w[1][i] = PW_NOWHERE;
         for (int i = 0; i < S::LX; ++i) z.off_x[i] = PW_NOWHERE;
         if (t >= end) return z;
         z.part = (int)(t / one);
@@ -202,13 +211,14 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         z.w = a.W + (int64_t)et.expert * a.expert_stride + s0 * PW_KB;
         z.x = (a.rows ? a.X : a.X + (int64_t)z.row0 * a.ldx) + s0 * PW_KB;
 #pragma unroll
-        for (int i = 0; i < S::LW; ++i) {
-            const int f = wave + i * PW_WAVES;
-            z.off_w[i] = out_of(z.ct, f, lr) < a.d_out ? (uint32_t)(w_row(z.ct, f, lr) * a.ldw) + piece : PW_NOWHERE;
+        for (int i = 0; i < 2 * S::LW; ++i) {
+            const int unit = wave + i % S::LW * PW_WAVES, in_half = unit / 2;  // 8 rows of a fragment of the first or the second halves
+            const int f = in_half / S::HN * S::FN + in_half % S::HN + i / S::LW * S::HN, r = unit % 2 * 8 + lr;
+            z.off_w[i / S::LW][i % S::LW] = out_of(z.ct, f, r) < a.d_out ? (uint32_t)(w_row(z.ct, f, r) * a.ldw) + piece : PW_NOWHERE;
         }
 #pragma unroll
         for (int i = 0; i < S::LX; ++i) {
-            const int r = (wave + i * PW_WAVES) * 16 + lr;
+            const int r = (wave + i * PW_WAVES) * 8 + lr;
             const bool is = r < z.n;                                          // r < BM with it
             int row = is ? r : 0;
             if (a.rows && is) row = min(max(a.rows[z.row0 + r], 0), a.x_rows - 1);
@@ -231,9 +241,9 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     };
 
     const int wn = wave % S::WN, wm = wave / S::WN;
-    const uint32_t mine = (uint32_t)((lane & 15) * 64 + (((lane >> 4) ^ ((lane >> 1) & 3)) * 16));
-    const uint32_t read_w = lds0 + mine + wn * S::FN * PW_FRAG, read_x = lds0 + mine + (S::NW + wm * S::FM) * PW_FRAG;
-    constexpr int L = S::LW + S::LX;
+    const uint32_t mine = (uint32_t)((lane & 15) * PW_KB + (((lane >> 4) ^ (lane & 7)) * 16));
+    const uint32_t read_w = lds0 + mine + wn * S::HN * PW_FRAG, read_x = lds0 + mine + S::X + wm * S::FM * PW_FRAG;
+    constexpr int L = 2 * S::LW + S::LX;
     constexpr int YB = YBF16 ? 2 : 4, OUTS = S::FN * 16 / (GATED ? 2 : 1), PASS = 128 / YB < OUTS ? 128 / YB : OUTS;   // outputs of a wave's row, of a pass
     constexpr int PIECES = PASS * YB / 16, AT_ONCE = WAVE / PIECES, TIMES = AT_ONCE < 16 ? 16 / AT_ONCE : 1;   // 16-byte pieces of a pass' row, rows stored at once
     constexpr int STORES = S::FM * (OUTS / PASS) * TIMES;
@@ -242,44 +252,69 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     Tile<S> now = tile_at(t);
     if (now.n == 0) return;
     uint32_t at = 0, parity = 0;                                              // the stage that is read, the scales that are
-    auto after = [](uint32_t o) { return o == (S::STAGES - 1) * S::STAGE ? 0u : o + (uint32_t)S::STAGE; };
+    // which lanes have nothing in stage s of a tile
     auto nothing = [&](const Tile<S> &z, int s) { return s >= z.full || (s == z.full - 1 && z.part == parts - 1 && past) ? PW_NOWHERE : 0; };
+    auto offsets = [&](auto &to, const auto &from, uint32_t gone) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(to) / sizeof(to[0])); ++i) to[i] = from[i] | gone;
+    };
     request_scales(now, 0);
-    for (int s = 0; s < S::STAGES - 1; ++s) {
-        uint32_t ow[S::LW], ox[S::LX];
-        const uint32_t gone = nothing(now, s);
-        for (int i = 0; i < S::LW; ++i) ow[i] = now.off_w[i] | gone;
-        for (int i = 0; i < S::LX; ++i) ox[i] = now.off_x[i] | gone;
-        request<S::LW, S::LX>(ow, ox, resource(now.w), resource(now.x), s * PW_KB, lds0 + s * S::STAGE + wave * PW_FRAG);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const uint32_t gone = nothing(now, s), to = lds0 + s * S::STAGE + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < S::LX; ++i) request(now.off_x[i] | gone, resource(now.x), s * PW_KB, to + S::X + i * 8192);
+#pragma unroll
+        for (int i = 0; i < S::LW; ++i) request(now.off_w[0][i] | gone, resource(now.w), s * PW_KB, to + i * 8192);
+        if (s == 0)
+#pragma unroll
+            for (int i = 0; i < S::LW; ++i) request(now.off_w[1][i] | gone, resource(now.w), 0, to + S::SECOND + i * 8192);
     }
-    wait_loads<(S::STAGES - 2) * L>();
+    wait_loads<L>();
     meet();
     if (wave >= PW_WAVES / 2) meet();                                         // the second group is half a step behind
 
     typename M::acc_t acc[S::FN][S::FM];
-    // One stage: read it, ask for stage `s` of a tile over the one that both groups have read, multiply.  `stored`: the stores of the
-    // tile before may still be on their way, between the stages that are waited for and the newer ones.
-    auto stage = [&](const Tile<S> &z, int s, bool stored, bool busy) {
-        pr_i32x4_t fw[S::FN], fx[S::FM];
-        uint32_t ow[S::LW], ox[S::LX];
-        const uint32_t gone = nothing(z, s);
-        for (int i = 0; i < S::LW; ++i) ow[i] = z.off_w[i] | gone;
-        for (int i = 0; i < S::LX; ++i) ox[i] = z.off_x[i] | gone;
-        const uint32_t to = at == 0 ? (S::STAGES - 1) * S::STAGE : at - S::STAGE;
-        read_and_request<S::FN, S::FM, S::LW, S::LX>(read_w + at, read_x + at, fw, fx, ow, ox, resource(z.w), resource(z.x), (uint32_t)s * PW_KB,
-                                                      lds0 + to + wave * PW_FRAG);
-        if (stored) wait_loads<(S::STAGES - 2) * L + STORES>();               // the next stage is there
-        else wait_loads<(S::STAGES - 2) * L>();
-        meet();
+    pr_i32x4_t fw[2][S::HN], fx[2][S::FM];                                    // [halves of a row]
+    auto multiply = [&](auto second, bool busy) {
+        constexpr int I0 = decltype(second)::value * S::HN;
         __builtin_amdgcn_s_setprio(1);
         if (busy)
 #pragma unroll
-        for (int j = 0; j < S::FM; ++j)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < S::FN; ++i) acc[i][j] = M::mul(fw[i], fx[j], acc[i][j]);
+                for (int j = 0; j < S::FM; ++j)
+#pragma unroll
+                    for (int i = 0; i < S::HN; ++i) acc[I0 + i][j] = M::mul(fw[h][i], fx[h][j], acc[I0 + i][j]);
         __builtin_amdgcn_s_setprio(0);
+    };
+    // A stage.  First step: X and half of W; the second half of W of stage s1 of tile z1, the next one, is asked for.  Second step: the
+    // second half of W; X and the first half of W of stage s2 of tile z2, the one after, are asked for.  Either goes over what
+    // both groups have read a step before, and is waited for a stage later.  `stored`: the stores of the tile before may still be on
+    // their way, between the loads that are waited for and the newer ones.
+    auto stage = [&](const Tile<S> &z1, int s1, const Tile<S> &z2, int s2, bool stored, bool busy) {
+        const uint32_t other = S::STAGE - at;
+        auto wait = [&] {
+            if (stored) wait_loads<L + STORES>();
+            else wait_loads<L>();
+        };
+        uint32_t ow[S::LW], ox[S::LX];
+        offsets(ow, z1.off_w[1], nothing(z1, s1));
+        read_first<S::HN, S::FM, S::LW>(read_w + at, read_x + at, fw, fx, ow, resource(z1.w), (uint32_t)s1 * PW_KB, lds0 + other + S::SECOND + wave * 1024);
+        wait();                                                               // the second half of this stage's W is there
         meet();
-        at = after(at);
+        multiply(First{}, busy);
+        meet();
+        const uint32_t gone = nothing(z2, s2);
+        offsets(ow, z2.off_w[0], gone);
+        offsets(ox, z2.off_x, gone);
+        read_second<S::HN, S::LW, S::LX>(read_w + at + S::SECOND, fw, ow, ox, resource(z2.w), resource(z2.x), (uint32_t)s2 * PW_KB,
+                                         lds0 + at + wave * 1024, lds0 + at + S::X + wave * 1024);
+        wait();                                                               // the rest of the next stage is there
+        meet();
+        multiply(Second{}, busy);
+        meet();
+        at = other;
     };
 
     bool stored = false;
@@ -289,12 +324,14 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 #pragma unroll
             for (int j = 0; j < S::FM; ++j) acc[i][j] = typename M::acc_t{};
         const bool busy = wm * S::FM * 16 < now.n && out_of(now.ct, wn * S::FN, 0) < a.d_out;   // some of the wave's rows and outputs are there
-        for (int s = 0; s < now.full - (S::STAGES - 1); ++s) stage(now, s + S::STAGES - 1, stored && s < S::STAGES - 2, busy);
-        // the last stages ask for the first ones of the next tile
+        const int stages = max(now.full, 2);
+        for (int s = 0; s < stages - 2; ++s) stage(now, s + 1, now, s + 2, stored && s == 0, busy);
+        // the last two stages ask for the first ones of the next tile
         t += step;
         const Tile<S> next = tile_at(t);
         request_scales(next, parity ^ 1);
-        for (int s = 0; s < S::STAGES - 1; ++s) stage(next, s, false, busy);
+        stage(now, stages - 1, next, 0, stored && stages == 2, busy);
+        stage(next, 0, next, 1, false, busy);
 
         const int q0 = (lane >> 4) * 4;
         // four outputs of fragment i (gated: and i + 1) in row j * 16 + lane % 16
@@ -406,7 +443,7 @@ template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Prod
     const bool whole = (reinterpret_cast<uintptr_t>(p.Y) & 15) == 0 && p.ldy * y_bytes % 16 == 0 && (p.d_out * y_bytes % 16 == 0 || OUT == 2) &&
                        p.ldy <= 0x7FFFFFFF / (S::BM * y_bytes);
     const auto kernel = &k_product_wide<I8, GATED, OUT, S>;
-    constexpr int lds = S::STAGES * S::STAGE + PW_WAVES * PW_TURN + 2 * 2048;
+    constexpr int lds = 2 * S::STAGE + PW_WAVES * PW_TURN + 2 * 2048;
     static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (once != hipSuccess) return once;
     kernel<<<dim3((uint32_t)blocks), PW_THREADS, lds, p.stream>>>(args_of(p), (int)cols, 8, whole, parts, part_stride);
@@ -442,9 +479,9 @@ template <typename S> hipError_t launch_parts(const Product &p, int parts) {
     return hipGetLastError();
 }
 
-using Shape256 = Shape<2, 8, 4, 4, 4>;
-using Shape128 = Shape<4, 4, 2, 4, 5>;
-using Shape64 = Shape<8, 2, 1, 4, 5>;
+using Shape256 = Shape<2, 8, 4, 4>;
+using Shape128 = Shape<4, 4, 2, 4>;
+using Shape64 = Shape<8, 2, 1, 4>;
 
 template <typename S> hipError_t launch_either(const Product &p, int parts) {
     if (parts > 1) return launch_parts<S>(p, parts);
