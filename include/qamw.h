@@ -457,7 +457,8 @@ int qamw_int8_quantize(const void *X, int dtype, int m, int d, int64_t ldx, cons
  *      gated = 1: the d_out rows of a gate, then the d_out rows of an up projection, and Y = g / (1 + exp(-g)) * u
  *   Y  device, m rows of d_out elements of y_dtype (F32 or BF16, rounded to nearest even), leading dimension ldy
  *   workspace  qamw_int8_matmul_workspace_bytes() of device memory, 16-byte aligned (the codes; and where there are too few
- *      tiles for the chip, the sums of parts of the columns); NULL where that is 0
+ *      tiles for the chip, the sums of parts of the columns); NULL where that is 0, and where the product's own launch quantises
+ *      the rows: m * ceil(d_in / 4096) <= 4, X, col_scale and W on 16-byte boundaries, their rows of whole 16 bytes, W below 2 GiB
  * Errors: sizes out of the ranges above, NULL or misaligned pointers, x_scales with floating X or col_scale with codes, a
  * workspace too small -> INVALID_ARG; leading dimensions smaller than a row -> SHAPE; more tiles than a launch has ->
  * UNSUPPORTED. */

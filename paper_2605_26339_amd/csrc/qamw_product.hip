@@ -160,11 +160,11 @@ Plan plan(const Product &p) {
 
 }  // namespace
 
-// The sums of all parts: whole 16 bytes a row.
+// The sums of all parts.
 size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated) {
     if (m == 0) return 0;
     const int parts = plan(m, 1, false, d_out, d_in, gated, true, true).parts;
-    return parts == 1 ? 0 : (size_t)parts * m * (((size_t)d_out * (gated ? 2 : 1) + 3) / 4 * 16);
+    return parts == 1 ? 0 : (size_t)parts * m * (size_t)parts_row(d_out, gated) * 4;
 }
 
 hipError_t launch_product(const Product &p) {

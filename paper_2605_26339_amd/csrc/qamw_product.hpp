@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "qamw_common.hpp"
 
 namespace qamw {
@@ -25,6 +27,23 @@ struct Product {
 
 hipError_t launch_product(const Product &p);
 size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated);   // of an int8 product of one group
+// Row of the sums of a part of the columns, in 32-bit words: whole 16 bytes; where the up projection's follow the gate's, four of them
+// are read together from anywhere.
+inline int64_t parts_row(int64_t d_out, bool gated) { return (d_out * (gated ? 2 : 1) + 3 + (gated ? 3 : 0)) / 4 * 4; }
+// More LDS than the 64 KB that a workgroup has without asking, asked for once on a device.
+struct MoreLds {
+    std::atomic<uint64_t> done{0};
+    hipError_t ask(const void *kernel, int bytes) {
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorNotSupported;
+        if (!(done.load(std::memory_order_acquire) & (1ull << dev))) {
+            const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+            if (e != hipSuccess) return e;
+            done.fetch_or(1ull << dev, std::memory_order_release);
+        }
+        return hipSuccess;
+    }
+};
 // The kernels by what they are for.  wide and few: products that product_wide_supported(), tile_rows of 16 / 32 / 64 and 64 / 128 / 256.
 bool product_wide_supported(const Product &p);
 hipError_t launch_product_wide(const Product &p, int tile_rows, int parts);

@@ -274,8 +274,9 @@ template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const P
     q.col_tiles = (int)cols;
     q.split = split;
     const auto kernel = &k_product_few<I8, GATED, YBF16, S>;
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (once != hipSuccess) return once;
+    static MoreLds more;
+    const hipError_t e = more.ask(reinterpret_cast<const void *>(kernel), 160 * 1024);
+    if (e != hipSuccess) return e;
     kernel<<<dim3((uint32_t)blocks), S::THREADS, S::LDS + more_lds, p.stream>>>(q);
     return hipGetLastError();
 }

@@ -444,8 +444,9 @@ template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Prod
                        p.ldy <= 0x7FFFFFFF / (S::BM * y_bytes);
     const auto kernel = &k_product_wide<I8, GATED, OUT, S>;
     constexpr int lds = 2 * S::STAGE + PW_WAVES * PW_TURN + 2 * 2048;
-    static const hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (once != hipSuccess) return once;
+    static MoreLds more;
+    const hipError_t e = more.ask(reinterpret_cast<const void *>(kernel), lds);
+    if (e != hipSuccess) return e;
     kernel<<<dim3((uint32_t)blocks), PW_THREADS, lds, p.stream>>>(args_of(p), (int)cols, 8, whole, parts, part_stride);
     return hipGetLastError();
 }
@@ -461,7 +462,7 @@ template <typename S> hipError_t launch_parts(const Product &p, int parts) {
     q.d_out = p.d_out * (p.gated ? 2 : 1);
     q.gated = false;
     q.Y = p.scratch;
-    q.ldy = ((int64_t)q.d_out + 3) / 4 * 4;
+    q.ldy = parts_row(p.d_out, p.gated);
     const int64_t stride = q.ldy * p.m, fours = ((int64_t)p.d_out + 3) / 4, blocks = (fours * p.m + PS_THREADS - 1) / PS_THREADS;
     if (blocks * PS_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
     const hipError_t e = launch<true, false, 2, S>(q, parts, stride);

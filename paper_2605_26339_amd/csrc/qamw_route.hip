@@ -320,12 +320,10 @@ constexpr int RT_TOKENS = RT_GROUPS * RT_WAVES;
 
 template <int DTYPE, int PER> hipError_t launch_pick(const RouteProblem &q, int blocks) {
     const size_t lds = ((size_t)RT_WAVES + 1) * q.n_experts * 4;
-    static const hipError_t once = [] {
-        hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
-        if (e != hipSuccess) return e;
-        return hipFuncSetAttribute(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, false>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024);
-    }();
-    if (once != hipSuccess) return once;
+    static MoreLds alone, together;
+    const hipError_t e = blocks == 1 ? alone.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, true>), 80 * 1024)
+                                     : together.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, false>), 80 * 1024);
+    if (e != hipSuccess) return e;
     if (blocks == 1) k_route_pick<DTYPE, PER, true><<<1, RT_THREADS, lds, q.stream>>>(q);
     else k_route_pick<DTYPE, PER, false><<<blocks, RT_THREADS, lds, q.stream>>>(q);
     return hipGetLastError();

@@ -47,12 +47,12 @@ int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const fl
     if (rc != QAMW_OK) return rc;
     if (!float_dtype(y_dtype)) return QAMW_ERR_INVALID_ARG;
     const bool codes = x_dtype == QAMW_DTYPE_I8;
-    if (m > 0 && (!X || !W || !w_scales || !Y || (codes && !x_scales) || (need && !workspace))) return QAMW_ERR_INVALID_ARG;
+    if (m > 0 && (!X || !W || !w_scales || !Y || (codes && !x_scales))) return QAMW_ERR_INVALID_ARG;
     if (codes ? col_scale != nullptr : x_scales != nullptr) return QAMW_ERR_INVALID_ARG;
-    if (workspace_bytes < need || (need && misaligned(workspace, 16))) return QAMW_ERR_INVALID_ARG;
     if (off_type(X, x_dtype) || off_type(Y, y_dtype) || misaligned(x_scales, 4) || misaligned(w_scales, 4) || misaligned(col_scale, 4))
         return QAMW_ERR_INVALID_ARG;
     if (ldx < d_in || ldw < d_in || ldy < d_out) return QAMW_ERR_SHAPE;
+    if (m == 0) return QAMW_OK;
     qamw::Product p;
     p.W = W;
     p.ldw = ldw;
@@ -66,22 +66,20 @@ int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const fl
     p.gated = gated != 0;
     p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
     p.stream = (hipStream_t)stream;
+    p.ldx = codes ? ldx : (int64_t)round16((size_t)d_in);
+    if (!codes && qamw::product_wide_supported(p) && qamw::product_from_floats_supported(p, X, x_dtype, ldx, col_scale))
+        return status_of(qamw::launch_product_from_floats(p, X, x_dtype, ldx, col_scale));
+    if (need && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return QAMW_ERR_INVALID_ARG;
     const size_t before = codes_bytes(x_dtype, m, d_in);
     if (need > before) p.scratch = static_cast<char *>(workspace) + before;
     if (codes) {
         p.X = X;
-        p.ldx = ldx;
         p.x_scales = x_scales;
     } else {
-        const int64_t ldc = (int64_t)round16((size_t)d_in);
-        float *scales = reinterpret_cast<float *>(static_cast<char *>(workspace) + (size_t)m * (size_t)ldc);
+        float *scales = reinterpret_cast<float *>(static_cast<char *>(workspace) + (size_t)m * (size_t)p.ldx);
         p.X = workspace;
-        p.ldx = ldc;
         p.x_scales = scales;
-        if (m == 0) return QAMW_OK;
-        if (qamw::product_wide_supported(p) && qamw::product_from_floats_supported(p, X, x_dtype, ldx, col_scale))
-            return status_of(qamw::launch_product_from_floats(p, X, x_dtype, ldx, col_scale));
-        const hipError_t e = qamw::launch_int8_quantize(X, x_dtype, m, d_in, ldx, col_scale, static_cast<int8_t *>(workspace), ldc,
+        const hipError_t e = qamw::launch_int8_quantize(X, x_dtype, m, d_in, ldx, col_scale, static_cast<int8_t *>(workspace), p.ldx,
                                                         scales, (hipStream_t)stream);
         if (e != hipSuccess) return status_of(e);
     }

@@ -724,13 +724,18 @@ def int8_matmul(X, W, w_scales, x_scales=None, col_scale=None, gated=False, out=
     code = DTYPE_I8 if X.dtype == torch.int8 else _dtype_code(X)
     d_out = outs // 2 if gated else outs
     y, y_code, ldy = _result(out, m, d_out, out_dtype, X, stream)
+    x_at, w_at, c_at = X.data_ptr(), W.data_ptr(), _ptr(col_scale)
     if workspace is None:
-        size = int8_matmul_workspace_bytes(code, m, d_out, d_in, bool(gated))
-        work = _new(1, size, torch.uint8, X, stream) if size else None      # kept until the launch
-        at = _ptr(work)
+        at = size = 0
+        # not where the product's own launch quantises the rows
+        if (code == DTYPE_I8 or m * -(-d_in // 4096) > 4 or (x_at | w_at | (c_at or 0) | d_in | ldw | ldx * X.element_size()) & 15
+                or ldw > 0x7FFFFE00 // outs or ldx > 1 << 24):
+            size = int8_matmul_workspace_bytes(code, m, d_out, d_in, bool(gated))
+            work = _new(1, size, torch.uint8, X, stream) if size else None  # kept until the launch
+            at = _ptr(work)
     else:
         at, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _check(lib().qamw_int8_matmul(X.data_ptr(), code, _ptr(x_scales), _ptr(col_scale), m, ldx, W.data_ptr(), w_scales.data_ptr(), ldw,
+    _check(lib().qamw_int8_matmul(x_at, code, _ptr(x_scales), c_at, m, ldx, w_at, w_scales.data_ptr(), ldw,
                                   d_out, d_in, 1 if gated else 0, y.data_ptr(), y_code, ldy, at, size, _raw_stream(stream, dev)),
            "qamw_int8_matmul")
     return y

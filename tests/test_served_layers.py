@@ -50,6 +50,7 @@ def test_refusals_of_the_entry_points():
     assert size(0, 3, 8, 17) == qamw.OK and need.value == 3 * 32 + 16
     assert size(2, 3, 8, 17) == qamw.OK and need.value == 0
     assert size(2, 500, 2048, 13824) == qamw.OK and need.value > 0 and need.value % (500 * 2048 * 4) == 0   # the sums of parts
+    assert size(2, 500, 2049, 13824, 1) == qamw.OK and need.value % (500 * 4104 * 4) == 0 and need.value > 0   # read by fours from column 2049 on: 4101 to the next four
     assert size(3, 3, 8, 17) == I and size(0, 3, 8, 131057) == I and size(0, 3, 0, 17) == I and size(0, 3, 8, 17, 2) == I
     assert L.qamw_int8_matmul_workspace_bytes(0, 3, 8, 17, 0, None) == I
 
@@ -330,6 +331,26 @@ def test_int8_matmul_quantises_as_the_quantiser_does(m, d_out, d_in, x_dtype, sm
     if m:
         rc, rs = quantise_ref(f, c)
         assert torch.equal(y.cpu(), int8_ref(torch.from_numpy(rc), torch.from_numpy(rs), w, ws))
+
+
+@gpu
+@pytest.mark.parametrize("m,d_in,shift", [(1, 4096, 0), (4, 512, 0), (1, 16384, 0), (5, 512, 0), (2, 8192, 0), (3, 8192, 0), (1, 4088, 0), (1, 4096, 4)])
+def test_int8_matmul_without_a_workspace(m, d_in, shift):
+    """Rows that the product's own launch quantises need none; all others are refused without it, and nothing is written."""
+    say(f"[int8] no workspace {m} x {d_in} shift {shift}")
+    g = _gen(m + d_in)
+    x = torch.randn(m * d_in + shift, generator=g).to(DEV)[shift // 4:][: m * d_in].view(m, d_in)
+    w, ws = _codes(g, 100, d_in).to(DEV), (torch.rand(100, generator=g) / 127).to(DEV)
+    y = torch.full((m, 100), 7.0, device=DEV)
+    rc = qamw.lib().qamw_int8_matmul(x.data_ptr(), 0, None, None, m, d_in, w.data_ptr(), ws.data_ptr(), d_in, 100, d_in, 0, y.data_ptr(), 0, 100, None, 0,
+                                     torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    if m * -(-d_in // 4096) <= 4 and d_in % 16 == 0 and shift == 0:
+        assert rc == qamw.OK and torch.equal(y, qamw.int8_matmul(x.clone(), w, ws, out_dtype=torch.float32, workspace=torch.empty(1 << 20, dtype=torch.uint8, device=DEV)))
+    else:
+        assert rc == qamw.ERR_INVALID_ARG and (y == 7.0).all()
+    c, s = qamw.int8_quantize(x)
+    assert torch.equal(qamw.int8_matmul(x, w, ws, out_dtype=torch.float32), qamw.int8_matmul(c, w, ws, x_scales=s, out_dtype=torch.float32))
 
 
 @gpu
