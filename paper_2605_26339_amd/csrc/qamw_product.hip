@@ -6,14 +6,16 @@ namespace {
 
 // ---- every shape, alignment and extent ------------------------------------------------------------------------------------
 //
-// A workgroup has 64 rows of W and 64 of X and steps over 64 bytes of both at a time.  Elements are loaded one by one with a test
-// each, with 64-bit addresses, and zeros stand where there is nothing: rows past the end, the last columns of an odd d_in.
-constexpr int PA_TILE = 64, PA_THREADS = 256, PA_PITCH = 64 + 16;   // bytes: 16 more, or 4 rows of a fragment share their banks
+// A workgroup has 64 rows of W and 64 of X and steps over 128 bytes of both at a time, two steps in LDS and the next one on its way to
+// registers.  Loads are 16 bytes wherever they begin, which the memory instructions allow, with 64-bit addresses; zeros stand
+// where there is nothing: rows past the end, and columns past the last one, up to which a row's last piece is loaded by elements.
+constexpr int PA_TILE = 64, PA_THREADS = 256, PA_K = 128, PA_PITCH = PA_K + 16;   // bytes: 16 more, or rows of a fragment share their banks
 
 template <bool I8, bool GATED, bool YBF16>
 __global__ __launch_bounds__(PA_THREADS) void k_product_any(ProductArgs a, int col_tiles) {
     using M = Mfma<I8>;
-    __shared__ __align__(16) char lds[2][PA_TILE * PA_PITCH];
+    using Piece = Unaligned<typename M::elem_t, 16 / M::ELEM>;
+    __shared__ __align__(16) char lds[2][2][PA_TILE * PA_PITCH];
     const int t = (int)(blockIdx.x / (uint32_t)col_tiles), ct = (int)(blockIdx.x % (uint32_t)col_tiles);
     const RowTile rt = find_tile<PA_TILE>(a, t);
     if (rt.n <= 0) return;
@@ -21,8 +23,8 @@ __global__ __launch_bounds__(PA_THREADS) void k_product_any(ProductArgs a, int c
     // row r of the tile's 64 rows of W; gated: 16 of the gate, then the same 16 of the up projection
     auto out_of = [&](int r) { return GATED ? ct * 32 + (r >> 5) * 16 + (r & 15) : ct * 64 + r; };
     const char *W = a.W + (int64_t)rt.expert * a.expert_stride;
-    // what this thread loads: 16 bytes of one row of each operand
-    const int lr = tid >> 2, lc = (tid & 3) * 16;
+    // what this thread loads: 32 bytes of one row of each operand
+    const int lr = tid >> 2, lc = (tid & 3) * 32;
     const int out = out_of(lr);
     const bool has_w = out < a.d_out, has_x = lr < rt.n;
     const char *src_w = W + (has_w ? (int64_t)(GATED && ((lr >> 4) & 1) ? a.d_out + (int64_t)out : out) * a.ldw : 0);
@@ -30,36 +32,42 @@ __global__ __launch_bounds__(PA_THREADS) void k_product_any(ProductArgs a, int c
     if (a.rows && has_x) x_row = min(max(a.rows[x_row], 0), a.x_rows - 1);
     const char *src_x = a.X + x_row * a.ldx;
 
-    typename M::acc_t acc[2][2] = {};
     const int64_t bytes = (int64_t)a.d_in * M::ELEM;
-    for (int64_t k0 = 0; k0 < bytes; k0 += 64) {
-        union Piece {
-            char c[16];
-            uint16_t h[8];
-            pr_i32x4_t v;
-        } w, x;
-        for (int i = 0; i < 16 / M::ELEM; ++i) {
-            const int64_t at = k0 + lc + i * M::ELEM;
-            const bool in = at < bytes;
-            if (I8) {
-                w.c[i] = in && has_w ? src_w[at] : 0;
-                x.c[i] = in && has_x ? src_x[at] : 0;
-            } else {
-                w.h[i] = in && has_w ? *reinterpret_cast<const uint16_t *>(src_w + at) : 0;
-                x.h[i] = in && has_x ? *reinterpret_cast<const uint16_t *>(src_x + at) : 0;
-            }
-        }
-        __syncthreads();
-        *reinterpret_cast<pr_i32x4_t *>(&lds[0][lr * PA_PITCH + lc]) = w.v;
-        *reinterpret_cast<pr_i32x4_t *>(&lds[1][lr * PA_PITCH + lc]) = x.v;
-        __syncthreads();
-        pr_i32x4_t fw[2], fx[2];
+    Piece w[2], x[2];
+    auto load = [&](const char *src, bool has, int64_t at, Piece &to) {
+        to = {};
+        if (!has) return;
+        if (at + 16 <= bytes) to = *reinterpret_cast<const Piece *>(src + at);
+        else
+            for (int i = 0; i < 16 / M::ELEM; ++i)
+                if (at + i * M::ELEM < bytes) to.v[i] = *reinterpret_cast<const typename M::elem_t *>(src + at + i * M::ELEM);
+    };
+    auto request = [&](int64_t k0) {
         for (int i = 0; i < 2; ++i) {
-            fw[i] = *reinterpret_cast<const pr_i32x4_t *>(&lds[0][(wn * 32 + i * 16 + lane % 16) * PA_PITCH + lane / 16 * 16]);
-            fx[i] = *reinterpret_cast<const pr_i32x4_t *>(&lds[1][(wm * 32 + i * 16 + lane % 16) * PA_PITCH + lane / 16 * 16]);
+            load(src_w, has_w, k0 + lc + i * 16, w[i]);
+            load(src_x, has_x, k0 + lc + i * 16, x[i]);
         }
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2; ++j) acc[i][j] = M::mul(fw[i], fx[j], acc[i][j]);
+    };
+    request(0);
+    typename M::acc_t acc[2][2] = {};
+    int half = 0;
+    for (int64_t k0 = 0; k0 < bytes; k0 += PA_K, half ^= 1) {
+        char(&to)[2][PA_TILE * PA_PITCH] = lds[half];
+        for (int i = 0; i < 2; ++i) {
+            *reinterpret_cast<pr_i32x4_t *>(&to[0][lr * PA_PITCH + lc + i * 16]) = __builtin_bit_cast(pr_i32x4_t, w[i]);
+            *reinterpret_cast<pr_i32x4_t *>(&to[1][lr * PA_PITCH + lc + i * 16]) = __builtin_bit_cast(pr_i32x4_t, x[i]);
+        }
+        __syncthreads();           // of the step before, all have read the other half when they come here again
+        request(k0 + PA_K);
+        for (int h = 0; h < PA_K; h += 64) {
+            pr_i32x4_t fw[2], fx[2];
+            for (int i = 0; i < 2; ++i) {
+                fw[i] = *reinterpret_cast<const pr_i32x4_t *>(&to[0][(wn * 32 + i * 16 + lane % 16) * PA_PITCH + h + lane / 16 * 16]);
+                fx[i] = *reinterpret_cast<const pr_i32x4_t *>(&to[1][(wm * 32 + i * 16 + lane % 16) * PA_PITCH + h + lane / 16 * 16]);
+            }
+            for (int i = 0; i < 2; ++i)
+                for (int j = 0; j < 2; ++j) acc[i][j] = M::mul(fw[i], fx[j], acc[i][j]);
+        }
     }
 
     const float *ws = I8 ? a.w_scales + (int64_t)rt.expert * a.d_out * (GATED ? 2 : 1) : nullptr;

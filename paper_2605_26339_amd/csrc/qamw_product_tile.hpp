@@ -13,7 +13,7 @@ typedef __bf16 pr_bf16x8_t __attribute__((ext_vector_type(8)));
 template <bool I8> struct Mfma;
 template <> struct Mfma<true> {
     using acc_t = pr_i32x4_t;
-    using sum_t = int;
+    using elem_t = int8_t;
     static constexpr int ELEM = 1;
     static __device__ __forceinline__ acc_t mul(pr_i32x4_t w, pr_i32x4_t x, acc_t c) {
         return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, c, 0, 0, 0);
@@ -21,7 +21,7 @@ template <> struct Mfma<true> {
 };
 template <> struct Mfma<false> {
     using acc_t = pr_f32x4_t;
-    using sum_t = float;
+    using elem_t = uint16_t;
     static constexpr int ELEM = 2;
     static __device__ __forceinline__ acc_t mul(pr_i32x4_t w, pr_i32x4_t x, acc_t c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8_t, w), __builtin_bit_cast(pr_bf16x8_t, x), c, 0, 0, 0);
