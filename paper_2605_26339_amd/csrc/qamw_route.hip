@@ -10,8 +10,9 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 //
 // Sixteen lanes have a token, so that the largest of its logits is found by DPP within a row of lanes, for four tokens of a wave at a
 // time; a lane has PER experts that follow one another.  A logit becomes an unsigned number that orders as it does, 0 for what is
-// never chosen (-inf, NaN).  bf16 leaves room for the expert in the lower half, the lowest one as the largest number, so that one
-// maximum finds both; fp32 takes the lowest lane that has the maximum, and the lowest of its experts.
+// never chosen (-inf, NaN).  bf16 leaves room for the expert below it, the lowest one as the largest number, so that one maximum
+// finds both, and the next one is the largest that is smaller: of numbers below 2^31 it has the largest difference to the last one as
+// an unsigned number.  fp32 takes the lowest lane that has the maximum, and the lowest of its experts, and strikes it out.
 constexpr int RT_LANES = 16, RT_GROUPS = WAVE / RT_LANES;
 
 __device__ __forceinline__ uint32_t row_max(uint32_t v) {
@@ -55,18 +56,21 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
         if (!whole) row.v[i] = t < q.m && e0 + i < n ? static_cast<const E *>(q.logits)[t * q.ld + e0 + i] : E(0);
         const float f = DTYPE == 1 ? __uint_as_float((uint32_t)row.v[i] << 16) : (float)row.v[i];
         key[i] = t < q.m && e0 + i < n ? key_of(f) : 0;
-        if (PACKED && key[i]) key[i] = (key[i] & 0xFFFF0000u) | (0xFFFFu - (uint32_t)(e0 + i));
+        if (PACKED && key[i]) key[i] = (key[i] >> 16) << 10 | (1023u - (uint32_t)(e0 + i));
     }
-    // the value of a packed key: all its lower half is 1 for negative values
-    auto value = [](uint32_t k) { return value_of(PACKED ? (k & 0x80000000u ? k & 0xFFFF0000u : k | 0xFFFFu) : k); };
+    // of a packed key all that a negative value lacks are ones
+    auto value = [](uint32_t k) { return value_of(PACKED ? (k >> 10 << 16) | (k & 0x2000000u ? 0u : 0xFFFFu) : k); };
     float total = 0.0f, top = 0.0f, mine[2] = {0.0f, 0.0f};
     expert[0] = expert[1] = -1;
+    uint32_t best = 0;
+    bool some = true;
     for (int j = 0; j < q.k; ++j) {
-        uint32_t own = key[0];
+        const uint32_t last = PACKED ? best : 0;
+        uint32_t own = key[0] - last;
 #pragma unroll
-        for (int i = 1; i < PER; ++i) own = max(own, key[i]);
-        const uint32_t best = row_max(own);
-        const bool some = best != 0;
+        for (int i = 1; i < PER; ++i) own = max(own, key[i] - last);
+        best = last + row_max(own);
+        some = some && best != 0;                           // a token that has run out of experts stays so
         if (!__any(some)) break;
         const float v = value(best);
         if (j == 0) {
@@ -81,9 +85,7 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
         }
         int who;
         if (PACKED) {
-            who = (int)(0xFFFFu - (best & 0xFFFFu));
-#pragma unroll
-            for (int i = 0; i < PER; ++i) key[i] = key[i] == best ? 0 : key[i];
+            who = (int)(1023u - (best & 1023u));
         } else {
             const uint32_t has = (uint32_t)(__ballot(own == best) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu;
             const int winner = __ffs((int)has) - 1;
@@ -140,18 +142,23 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
     for (int i = threadIdx.x; i < RT_WAVES * n; i += RT_THREADS) rt_lds[i] = 0;
     __syncthreads();
     const int t0 = (blockIdx.x * RT_WAVES + wave) * RT_GROUPS, t1 = min(t0 + RT_GROUPS, q.m);
+    // lane's slots, of the tokens that are ranked together: token g0 + lane / k, choice lane % k
+    const int at_once = k <= RT_LANES ? RT_GROUPS : 2, token = lane / k, choice = lane % k;
+    int slot_expert[2] = {-1, -1}, slot_rank[2] = {-1, -1};
     if (t0 < t1) {
         int expert[2];
         float weight[2];
         pick<DTYPE, PER>(q, t0 + lane / RT_LANES, expert, weight);
-        const int at_once = k <= RT_LANES ? RT_GROUPS : 2;       // tokens whose slots are ranked together
-        for (int g0 = t0; g0 < t1; g0 += at_once) {
-            // lane's slot: token g0 + lane / k, choice lane % k
-            const int token = lane / k, choice = lane % k, from = ((g0 - t0 + token) % RT_GROUPS) * RT_LANES + choice % RT_LANES;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int g0 = t0 + h * at_once;
+            if (g0 >= t0 + RT_GROUPS || g0 >= t1) break;
+            const int from = ((h * at_once + token) % RT_GROUPS) * RT_LANES + choice % RT_LANES;
             const bool is = token < at_once && g0 + token < t1;
             const int lo = __shfl(expert[0], from), hi = __shfl(expert[1], from);
             const float wlo = __shfl(weight[0], from), whi = __shfl(weight[1], from);
             const int e = !is ? -1 : choice < RT_LANES ? lo : hi;
+            asm volatile("" ::: "memory");                   // the counts of the tokens before are other lanes' work: read no earlier than here
             unsigned long long same = __ballot(e >= 0);
             for (int b = 0; b < 10; ++b) {
                 const unsigned long long has = __ballot((e >> b) & 1);
@@ -159,15 +166,16 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
             }
             if (is) {
                 const int64_t at = (int64_t)g0 * k + lane;
-                int rank = -1;
                 if (e >= 0) {
-                    rank = (int)mine[e] + __popcll(same & ((1ull << lane) - 1));
+                    const int rank = (int)mine[e] + __popcll(same & ((1ull << lane) - 1));
                     // the wave's LDS accesses are made in order: all ranks are read before the last slot of an expert counts them
                     if ((same >> lane) == 1) mine[e] = (uint32_t)rank + 1;
-                }
+                    slot_rank[h] = rank;
+                    slot_expert[h] = e;
+                } else
+                    q.positions[at] = -1;
                 q.experts[at] = e;
                 q.weights[at] = choice < RT_LANES ? wlo : whi;
-                q.positions[at] = rank;
             }
         }
     }
@@ -192,13 +200,13 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
         for (int e = threadIdx.x; e < n; e += RT_THREADS) q.offsets[e] = (int32_t)total[e];
         if (threadIdx.x == 0) q.offsets[n] = (int32_t)all;
     }
-    // the wave's own slots again
-    for (int64_t s = (int64_t)t0 * k + lane; s < (int64_t)t1 * k; s += WAVE) {
-        const int e = q.experts[s];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int e = slot_expert[h];
         if (e < 0) continue;
-        const uint32_t place = (ALONE ? total[e] : 0) + mine[e] + (uint32_t)q.positions[s];
-        q.positions[s] = (int32_t)place;
-        if (ALONE) q.rows[place] = (int32_t)(s / k);
+        const uint32_t place = (ALONE ? total[e] : 0) + mine[e] + (uint32_t)slot_rank[h];
+        q.positions[(int64_t)(t0 + h * at_once) * k + lane] = (int32_t)place;
+        if (ALONE) q.rows[place] = t0 + h * at_once + token;
     }
     if (ALONE)
         for (int p = (int)all + threadIdx.x; p < q.m * k; p += RT_THREADS) q.rows[p] = -1;
