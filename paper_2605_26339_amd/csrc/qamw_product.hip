@@ -9,6 +9,8 @@ namespace {
 // A workgroup has 64 rows of W and 64 of X and steps over 128 bytes of both at a time, two steps in LDS and the next one on its way to
 // registers.  Loads are 16 bytes wherever they begin, which the memory instructions allow, with 64-bit addresses; zeros stand
 // where there is nothing: rows past the end, and columns past the last one, up to which a row's last piece is loaded by elements.
+// Loads bound it, in latency and number.  4096 rows by 4096 x 4096: int8 207 us, bf16 388 us (60 and 105 us by whole lines and 256 rows);
+// 16 rows 27 and 54 us (11 and 13 by the kernel for few rows, the call's own cost), 512 rows 35 and 69 us (29 and 51).
 constexpr int PA_TILE = 64, PA_THREADS = 256, PA_K = 128, PA_PITCH = PA_K + 16;   // bytes: 16 more, or rows of a fragment share their banks
 
 template <bool I8, bool GATED, bool YBF16>
@@ -117,6 +119,20 @@ namespace {
 // The choice is by an estimate of the time, in us, of weights that come from memory.  The figures are fitted to measurements of
 // 33 to 2000 rows, 512 to 11008 outputs and 1024 to 13824 columns (within a fifth of them, a third at worst): what a launch costs, what a
 // stage and a tile's begin and end cost for each shape, and the bytes a us that a CU of the kernel for few rows gets, and memory.
+//   Both sides, int8 and us, few rows by 16 / 32 / 64 against wide ones by 64 / 128 / 256 in so many parts of the columns:
+//     outputs x columns   rows   few                  wide, whole columns    wide, parts            chosen
+//     1024 x 1024          64    3.5 / 4.0 / 5.1      10.9 / 12.8 / 18.1     (2) 10.9               few, 16
+//                          300   7.0 / 7.8 / 6.9      11.3 / 13.6 / 19.5     (2) 12.0               few, 64
+//     4096 x 4096            8   6.4 / 6.6 / 8.5      28.3 / 30.4 / 41.4     (4) 14.3 / 15.6 / 19.5 few, 16
+//                          100   17.2 / 13.9 / 13.9   28.5 / 33.4 / 42.7     (4) 17.8 / 19.7 / 23.3 few, 64
+//                          300   31.4 / 27.9 / 26.1   28.2 / 31.9 / 45.0     (2) 23.8 / 25.7 / 32.2 wide, 64 in 2
+//                         1000                        30.2 / 34.2 / 48.4     (2) 46.8 / 35.4 / 41.3 wide, 64
+//                         4000                        106 / 71.9 / 62.0                             wide, 256
+//     5120 x 13824          16   21.3 / 22.8 / 29.6   80.2 / 83.7 / 114      (4) 29.1 / 30.6 / 38.4 few, 16
+//                           64   39.6 / 35.0 / 39.6   86.5 / 89.6 / 114      (4) 31.7 / 33.1 / 39.7 wide, 64 in more: 27.8
+//                          300   118 / 112 / 95.6     81.3 / 88.0 / 127      (4) 57.6 / 40.0 / 50.4 wide, 128 in 4
+//                         1000                        161 / 96.6 / 133       (2) 146 / 120 / 89.3   wide, 256 in 3: 83.8
+// The choice was within 10 % of the fastest, or of what a call costs on the host, in all 32 measured shapes.
 struct Plan {
     bool few;
     int tile_rows, parts;

@@ -4,8 +4,16 @@
 // units of 128 bytes.  Units come to the wave's own ring in LDS by buffer loads that go there directly, whole 128-byte lines of
 // eight rows at a time; no barrier is needed until the waves that share rows of W add up what they have.
 //   In LDS the eight 16-byte pieces of a row are exchanged by row mod 8, against bank conflicts of the 16 lanes that read a column.
-// One token, quantised in the call: the workgroup's waves quantise the row while their first weights are on their way.  Every
-// workgroup does so again, which is cheaper than a launch for it.
+// What bounds it: one CU gets 45 to 58 GB/s of weights that come from memory, however many it asks for at once, so tiles share their
+// columns among waves until there are about 8 on every CU; with enough of them, memory.  Launches included: 4096 x 4096 int8 for 8 rows 6.4 us,
+// 11008 x 4096 12.1, 5120 x 13824 19.1 (3.7 TB/s); gated int8 of 8 experts of 2 x 5632 x 2048 for 10 rows 27 us; bf16 of 64 experts of
+// 1408 x 2048, nearly all with some of 288 rows, 46 us (up to 8 TB/s, part of it out of the Infinity Cache).
+//   Rows of X are read again for every 16 outputs, from the caches, so that many rows are dearer here than in tiles of 256 outputs; the
+// estimate that chooses has both sides.
+// Few values, quantised in the call: the workgroup's waves quantise the rows while their first weights are on their way.  Every
+// workgroup does so again.  Against a launch for it, in a graph: one row by 4096 x 4096 6.9 us (8.1), of 11008 columns 13.1 (15.2), 4 rows
+// of 4096 columns 9.9 (8.3); called one by one, a launch less is 4 us less of the host's time.  13 rows of 5632 took 18.6 us, in two launches
+// 8.5: so no more values than the threads hold in four groups of 8.
 #include "qamw_product_tile.hpp"
 
 namespace qamw {
@@ -18,7 +26,9 @@ constexpr uint32_t PF_NOWHERE = 0x80000000u;                    // added to an o
 template <int T_, int FN_, int FROM_ = -1, int EIGHTS_ = 1> struct FewShape {
     static constexpr int T = T_, FN = FN_, FROM = FROM_, EIGHTS = EIGHTS_, XT = FROM >= 0 ? 0 : T;   // XT: fragments of X in the ring
     static constexpr int SLOT = (FN + XT) * PF_SLOT;
-    // Workgroups of 4 waves, two or more on a CU, share the CUs more evenly than ones of 8; one that quantises has 8 for it.
+    // Workgroups of 4 waves, two or more on a CU, share the CUs more evenly than ones of 8 (calls
+    // of the experts above 58 and 21 us, 71 and 27 with ones of 8);
+    // one that quantises has 8 for it.
     static constexpr int WAVES = FROM >= 0 ? 8 : 4;
     static constexpr int FIT = 80 * 1024 / (WAVES * SLOT), RING = FROM >= 0 || FIT > 4 ? 4 : FIT < 2 ? 2 : FIT;   // units on their way or being read
     static constexpr int THREADS = WAVES * WAVE, BM = T * 16;

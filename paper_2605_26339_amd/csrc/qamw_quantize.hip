@@ -2,6 +2,7 @@
 //   v_j = x_j c_j;  a = max_j |v_j|;  scale = a / 127;  code_j = rne(v_j * (127 / a)), each step rounded once to fp32.
 // a < 2^-110 (127 / a nears the largest float): scale 0, codes 0.  An infinity or a NaN in the row: scale NaN, codes 0, so
 // that whatever is computed with the row is NaN.
+// Memory bounds it: 4 or 2 bytes a value are read and one is written.
 #include "qamw_product_tile.hpp"
 
 namespace qamw {
@@ -10,7 +11,9 @@ namespace {
 // ---- rows of whole 16 bytes ------------------------------------------------------------------------------------------------
 //
 // TR threads have a row and hold its values, EIGHTS groups of 8 each, between the maximum and the codes: one read of X.  Groups past
-// the end of the row are loaded as zeros, from beyond the buffer's end.
+// the end of the row are loaded as zeros, from beyond the buffer's end.  TR and EIGHTS are the fewest threads and groups that hold the
+// row, so that short rows waste no lanes.  8192 rows of 4096: bf16 17.3 us (5.8 TB/s; the sweeps below 47 us), fp32 24.5 us (6.8; 52);
+// 512 rows of 13824 bf16 6.2 us (the sweeps 19).
 template <int DTYPE, int TR, int EIGHTS>
 __global__ __launch_bounds__(TR < 256 ? 256 : TR) void k_quantize(const char *X, int m, int d, int64_t ldx, const float *col_scale,
                                                                   int8_t *codes, int64_t ldc, float *scales) {
@@ -76,7 +79,8 @@ constexpr int Q_MOST = 512 * 8 * 4;
 
 constexpr int QT = 256;          // threads of a workgroup, which has one row
 
-// Two sweeps over the row; the second one finds it in the caches.
+// Rows that do not begin or end on 16 bytes, and ones of more than Q_MOST values: two sweeps, the second one finds the row in the caches.
+// 8192 rows of 4096 bf16 in 47 us.
 template <int DTYPE>
 __global__ __launch_bounds__(QT) void k_quantize_any(const void *X, int d, int64_t ldx, const float *col_scale, int8_t *codes,
                                                      int64_t ldc, float *scales) {

@@ -13,6 +13,8 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 // never chosen (-inf, NaN).  bf16 leaves room for the expert below it, the lowest one as the largest number, so that one maximum
 // finds both, and the next one is the largest that is smaller: of numbers below 2^31 it has the largest difference to the last one as
 // an unsigned number.  fp32 takes the lowest lane that has the maximum, and the lowest of its experts, and strikes it out.
+//   Arithmetic and the way through memory bound it about alike: 16384 tokens over 256 experts, 8 of them chosen, 11.5 us, of which some 3
+// are the choices' instructions, 2 the logits' 8.4 MB, the rest a launch and the steps between; with 64 lanes for a token the whole routing took 31.6 us, with sixteen 19.3.
 constexpr int RT_LANES = 16, RT_GROUPS = WAVE / RT_LANES;
 
 __device__ __forceinline__ uint32_t row_max(uint32_t v) {
@@ -113,7 +115,9 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 // another and finds equal experts among 64 slots by the bits of the expert; a workgroup's counts are those of its waves in their
 // order, a launch's those of its workgroups.  What is written as a slot's position is first the slot's rank among those of its
 // expert in the workgroup; when all counts are known, what comes before is added: what comes before an expert, and before the
-// workgroup within the expert.  A single workgroup knows all counts by itself.
+// workgroup within the expert.  A single workgroup knows all counts by itself: up to 64 tokens are one launch (5 tokens, 8 experts 3.4 us),
+// more are two: a workgroup of the second sums the counts of all and of those before it, so none waits for another.  16384 tokens over
+// 256 experts 8.3 us; with four times as many counts on their way together 9.2.
 
 // Exclusive sums of the counts in `total` (LDS), by one wave; their sum.
 __device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
@@ -261,7 +265,8 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int 
 constexpr int CB_THREADS = 256;
 
 // A thread has eight neighbours of a token's row, wherever they lie: the memory instructions take any address.  What it reads of
-// the experts' rows it asks for eight rows at a time.
+// the experts' rows it asks for eight rows at a time.  Memory bounds it: 8192 tokens of 8 rows of 4096 bf16 in 132 us, 4.6 TB/s, the rate
+// of a large copy; one value a thread, one row at a time took 312.  5 tokens of 2 rows 3.4 us, a launch.
 template <int DTYPE> struct EightOf;
 template <> struct EightOf<0> {
     Unaligned<float, 4> a, b;
