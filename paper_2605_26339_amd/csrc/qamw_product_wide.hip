@@ -416,20 +416,21 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 }
 
 // The sums of the parts, in their order, and what is done with them: four outputs a thread.  Memory bounds it: 4 bytes a part and output
-// are read.  509 rows of 5120 outputs in 4 parts 10.3 us, 4.5 TB/s with what is written.
+// are read, and all parts' are asked for together, which is why their number is known here: 509 rows of 5120 outputs in 3 parts 7.1 us, 5.2 TB/s
+// with what is written (10.4 with a loop over any number).
 //   Parts pay where the tiles of whole columns leave CUs without one: 300 rows by 5120 x 13824 take 40.0 us in 4 parts of tiles of 128
 // rows, sums included, and 88 in one.  int8 only: its sums are whole numbers, and in any order the same.
 constexpr int PS_THREADS = 256;
-template <bool GATED, bool YBF16>
-__global__ __launch_bounds__(PS_THREADS) void k_product_parts(ProductArgs a, const char *sums, int parts, int64_t part_stride, int64_t ld, int fours) {
+template <bool GATED, bool YBF16, int PARTS>
+__global__ __launch_bounds__(PS_THREADS) void k_product_parts(ProductArgs a, const char *sums, int64_t part_stride, int64_t ld, int fours) {
     const uint32_t id = blockIdx.x * PS_THREADS + threadIdx.x;
     const int64_t row = id / (uint32_t)fours;
     const int o = (int)(id % (uint32_t)fours) * 4;
     if (row >= a.m) return;
     const char *at = sums + (row * ld + o) * 4, *up = at + (int64_t)a.d_out * 4;
     pr_i32x4_t g = {0, 0, 0, 0}, u = {0, 0, 0, 0};
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
         g += *reinterpret_cast<const pr_i32x4_t *>(at + p * part_stride * 4);
         if (GATED) u += __builtin_bit_cast(pr_i32x4_t, *reinterpret_cast<const Unaligned<int, 4> *>(up + p * part_stride * 4));
     }
@@ -466,26 +467,38 @@ template <bool I8, typename S> hipError_t launch_shape(const Product &p) {
     return p.y_bf16 ? launch<I8, false, 1, S>(p, 1, 0) : launch<I8, false, 0, S>(p, 1, 0);
 }
 
-// In `parts` parts of the columns, whose sums lie in p.scratch.
+template <int PARTS> void launch_sums(const Product &p, int64_t stride, int64_t ld) {
+    const int64_t fours = ((int64_t)p.d_out + 3) / 4;
+    const dim3 g((uint32_t)((fours * p.m + PS_THREADS - 1) / PS_THREADS));
+    const ProductArgs a = args_of(p);
+    const char *sums = static_cast<const char *>(p.scratch);
+    if (p.gated) {
+        if (p.y_bf16) k_product_parts<true, true, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
+        else k_product_parts<true, false, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
+    } else {
+        if (p.y_bf16) k_product_parts<false, true, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
+        else k_product_parts<false, false, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
+    }
+}
+
+// In `parts` parts of the columns (2, 3, 4, 6 or 8), whose sums lie in p.scratch.
 template <typename S> hipError_t launch_parts(const Product &p, int parts) {
     Product q = p;
     q.d_out = p.d_out * (p.gated ? 2 : 1);
     q.gated = false;
     q.Y = p.scratch;
     q.ldy = parts_row(p.d_out, p.gated);
-    const int64_t stride = q.ldy * p.m, fours = ((int64_t)p.d_out + 3) / 4, blocks = (fours * p.m + PS_THREADS - 1) / PS_THREADS;
-    if (blocks * PS_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
+    const int64_t stride = q.ldy * p.m;
+    if (((int64_t)p.d_out + 3) / 4 * p.m + PS_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
     const hipError_t e = launch<true, false, 2, S>(q, parts, stride);
     if (e != hipSuccess) return e;
-    const ProductArgs a = args_of(p);
-    const char *sums = static_cast<const char *>(p.scratch);
-    const dim3 g((uint32_t)blocks);
-    if (p.gated) {
-        if (p.y_bf16) k_product_parts<true, true><<<g, PS_THREADS, 0, p.stream>>>(a, sums, parts, stride, q.ldy, (int)fours);
-        else k_product_parts<true, false><<<g, PS_THREADS, 0, p.stream>>>(a, sums, parts, stride, q.ldy, (int)fours);
-    } else {
-        if (p.y_bf16) k_product_parts<false, true><<<g, PS_THREADS, 0, p.stream>>>(a, sums, parts, stride, q.ldy, (int)fours);
-        else k_product_parts<false, false><<<g, PS_THREADS, 0, p.stream>>>(a, sums, parts, stride, q.ldy, (int)fours);
+    switch (parts) {
+    case 2: launch_sums<2>(p, stride, q.ldy); break;
+    case 3: launch_sums<3>(p, stride, q.ldy); break;
+    case 4: launch_sums<4>(p, stride, q.ldy); break;
+    case 6: launch_sums<6>(p, stride, q.ldy); break;
+    case 8: launch_sums<8>(p, stride, q.ldy); break;
+    default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
 }
