@@ -265,16 +265,27 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int 
 constexpr int CB_THREADS = 256;
 
 // A thread has eight neighbours of a token's row, wherever they lie: the memory instructions take any address.  What it reads of
-// the experts' rows it asks for eight rows at a time.  Memory bounds it: 8192 tokens of 8 rows of 4096 bf16 in 132 us, 4.6 TB/s, the rate
-// of a large copy; one value a thread, one row at a time took 312.  5 tokens of 2 rows 3.4 us, a launch.
+// the experts' rows it asks for eight rows at a time.  Memory bounds it: 8192 tokens of 8 rows of 4096 bf16 in 104 us, 5.8 TB/s; one value a
+// thread, one row at a time took 312.  5 tokens of 2 rows 3.4 us, a launch.
+// Rows that are read once, and a layer's are many: what passes them by is kept in the caches instead (132 us with ordinary loads).
+typedef uint32_t cb_u32x4_t __attribute__((ext_vector_type(4)));
 template <int DTYPE> struct EightOf;
 template <> struct EightOf<0> {
-    Unaligned<float, 4> a, b;
-    __device__ __forceinline__ float value(int i) const { return i < 4 ? a.v[i & 3] : b.v[i & 3]; }
+    cb_u32x4_t a, b;
+    __device__ __forceinline__ void load(const void *from) {
+        typedef cb_u32x4_t Anywhere __attribute__((aligned(4)));
+        a = __builtin_nontemporal_load(static_cast<const Anywhere *>(from));
+        b = __builtin_nontemporal_load(static_cast<const Anywhere *>(from) + 1);
+    }
+    __device__ __forceinline__ float value(int i) const { return __uint_as_float(i < 4 ? a[i & 3] : b[i & 3]); }
 };
 template <> struct EightOf<1> {
-    Unaligned<uint16_t, 8> a;
-    __device__ __forceinline__ float value(int i) const { return __uint_as_float((uint32_t)a.v[i] << 16); }
+    cb_u32x4_t a;
+    __device__ __forceinline__ void load(const void *from) {
+        typedef cb_u32x4_t Anywhere __attribute__((aligned(2)));
+        a = __builtin_nontemporal_load(static_cast<const Anywhere *>(from));
+    }
+    __device__ __forceinline__ float value(int i) const { return __uint_as_float(i & 1 ? a[i / 2] & 0xFFFF0000u : a[i / 2] << 16); }
 };
 
 template <int DTYPE, bool OBF16>
@@ -300,7 +311,7 @@ __global__ __launch_bounds__(CB_THREADS) void k_combine(const void *Y, int64_t y
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j)
                 if (at[j] >= 0 && at[j] < y_rows)
-                    y[j] = *reinterpret_cast<const EightOf<DTYPE> *>(static_cast<const char *>(Y) + ((int64_t)at[j] * ldy + c) * (DTYPE ? 2 : 4));
+                    y[j].load(static_cast<const char *>(Y) + ((int64_t)at[j] * ldy + c) * (DTYPE ? 2 : 4));
 #pragma unroll
             for (int j = 0; j < AT_ONCE; ++j)
                 if (at[j] >= 0 && at[j] < y_rows)
