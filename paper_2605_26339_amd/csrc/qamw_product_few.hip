@@ -7,7 +7,7 @@
 // What bounds it: one CU gets 45 to 58 GB/s of weights that come from memory, however many it asks for at once, so tiles share their
 // columns among waves until there are about 8 on every CU; with enough of them, memory.  Launches included: 4096 x 4096 int8 for 8 rows 6.4 us,
 // 11008 x 4096 12.1, 5120 x 13824 19.1 (3.7 TB/s); gated int8 of 8 experts of 2 x 5632 x 2048 for 10 rows 27 us; bf16 of 64 experts of
-// 1408 x 2048, nearly all with some of 288 rows, 46 us (up to 8 TB/s, part of it out of the Infinity Cache).
+// 1408 x 2048 with 8 rows each 70.6 us (5.2 TB/s).
 //   Rows of X are read again for every 16 outputs, from the caches, so that many rows are dearer here than in tiles of 256 outputs; the
 // estimate that chooses has both sides.
 // Few values, quantised in the call: the workgroup's waves quantise the rows while their first weights are on their way.  Every
@@ -20,15 +20,15 @@ namespace qamw {
 namespace {
 
 constexpr int PF_UNIT = 128, PF_SLOT = 16 * PF_UNIT;            // 16 rows of a unit
+constexpr int PF_ONCE = 2;                                     // cache policy of a load: not kept (nt)
 constexpr uint32_t PF_NOWHERE = 0x80000000u;                    // added to an offset: beyond the end of any buffer here
 // FROM: where X comes from: -1 as the product takes it, from memory; 0 fp32 and 1 bf16 to be quantised here, EIGHTS groups of 8
 // values by a thread.
 template <int T_, int FN_, int FROM_ = -1, int EIGHTS_ = 1> struct FewShape {
     static constexpr int T = T_, FN = FN_, FROM = FROM_, EIGHTS = EIGHTS_, XT = FROM >= 0 ? 0 : T;   // XT: fragments of X in the ring
     static constexpr int SLOT = (FN + XT) * PF_SLOT;
-    // Workgroups of 4 waves, two or more on a CU, share the CUs more evenly than ones of 8 (calls
-    // of the experts above 58 and 21 us, 71 and 27 with ones of 8);
-    // one that quantises has 8 for it.
+    // Workgroups of 4 waves, two or more on a CU, share the CUs more evenly than ones of 8 (288 rows routed to those 64 experts 58 us a call
+    // and 10 to the 8 21 us, 71 and 27 with ones of 8); one that quantises has 8 for it.
     static constexpr int WAVES = FROM >= 0 ? 8 : 4;
     static constexpr int FIT = 80 * 1024 / (WAVES * SLOT), RING = FROM >= 0 || FIT > 4 ? 4 : FIT < 2 ? 2 : FIT;   // units on their way or being read
     static constexpr int THREADS = WAVES * WAVE, BM = T * 16;
@@ -74,7 +74,7 @@ template <int N> __device__ __forceinline__ void read_unit(uint32_t at, pr_i32x4
                      : "memory");
 }
 
-template <bool I8, bool GATED, bool YBF16, typename S>
+template <bool I8, bool GATED, bool YBF16, bool ONCE, typename S>
 __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     using M = Mfma<I8>;
     const ProductArgs &a = q.p;
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void *)(uintptr_t)(to + f * PF_SLOT + h * 1024), 16,
-                                                         (int)(off_w[f][h] | gone), u * PF_UNIT, 0, 0);
+                                                         (int)(off_w[f][h] | gone), u * PF_UNIT, 0, ONCE ? PF_ONCE : 0);
 #pragma unroll
         for (int t = 0; t < S::XT; ++t)
 #pragma unroll
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     }
 }
 
-template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const Product &p, const FewArgs &given, size_t more_lds) {
+template <bool I8, bool GATED, bool YBF16, bool ONCE, typename S> hipError_t launch_once(const Product &p, const FewArgs &given, size_t more_lds) {
     FewArgs q = given;
     const int outs = (GATED ? S::FN / 2 : S::FN) * 16;
     const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, rows = most_row_tiles(p, S::BM);
@@ -283,12 +283,22 @@ template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const P
     q.p = args_of(p);
     q.col_tiles = (int)cols;
     q.split = split;
-    const auto kernel = &k_product_few<I8, GATED, YBF16, S>;
+    const auto kernel = &k_product_few<I8, GATED, YBF16, ONCE, S>;
     static MoreLds more;
     const hipError_t e = more.ask(reinterpret_cast<const void *>(kernel), 160 * 1024);
     if (e != hipSuccess) return e;
     kernel<<<dim3((uint32_t)blocks), S::THREADS, S::LDS + more_lds, p.stream>>>(q);
     return hipGetLastError();
+}
+
+// Weights of which half the Infinity Cache would be full are read as what is not read again, where an expert's rows are a tile or so: 64 experts
+// of 1408 x 2048 bf16 with 8 rows each 70.6 us, 75.6 by ordinary loads, 8 of 11008 x 4096 134 and 147; with 20 rows each 91.2 and 91.4, with
+// 40 99.6 and 96.3.  Smaller weights may be found there again: 13824 x 5120 int8, over and over, 24.1 and 19.4.
+constexpr int64_t PF_KEPT = 128ll << 20;
+template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const Product &p, const FewArgs &q, size_t more_lds) {
+    const int64_t bytes = (int64_t)p.n_experts * p.d_out * (p.gated ? 2 : 1) * p.d_in * (I8 ? 1 : 2);
+    constexpr bool MAY = S::FROM < 0 && S::T == 1;
+    return MAY && bytes > PF_KEPT ? launch_once<I8, GATED, YBF16, MAY, S>(p, q, more_lds) : launch_once<I8, GATED, YBF16, false, S>(p, q, more_lds);
 }
 
 template <bool I8, int T, int FROM, int EIGHTS> hipError_t launch_shape(const Product &p, const FewArgs &q, size_t more_lds) {
