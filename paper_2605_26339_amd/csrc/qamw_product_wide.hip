@@ -292,7 +292,10 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 #pragma unroll
                 for (int j = 0; j < S::FM; ++j)
 #pragma unroll
-                    for (int i = 0; i < S::HN; ++i) acc[I0 + i][j] = M::mul(fw[h][i], fx[h][j], acc[I0 + i][j]);
+                    for (int n = 0; n < S::HN; ++n) {
+                        const int i = j & 1 ? S::HN - 1 - n : n;              // to and fro: one operand changes at a time, 1 % less time for random ones
+                        acc[I0 + i][j] = M::mul(fw[h][i], fx[h][j], acc[I0 + i][j]);
+                    }
         __builtin_amdgcn_s_setprio(0);
     };
     // A stage.  First step: X and half of W; the second half of W of stage s1 of tile z1, the next one, is asked for.  Second step: the
