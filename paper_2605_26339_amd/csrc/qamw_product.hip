@@ -1,4 +1,6 @@
 // Y = X W^T for 8-bit integers with scales or bf16, one matrix or one for each expert.
+#include <cmath>
+
 #include "qamw_product_tile.hpp"
 
 namespace qamw {
@@ -116,63 +118,82 @@ namespace {
 
 // ---- which kernel ----------------------------------------------------------------------------------------------------------
 //
-// The choice is by an estimate of the time, in us, of weights that come from memory.  The figures are fitted to measurements of
-// 33 to 2000 rows, 512 to 11008 outputs and 1024 to 13824 columns (within a fifth of them, a third at worst): what a launch costs, what a
-// stage and a tile's begin and end cost for each shape, and the bytes a us that a CU of the kernel for few rows gets, and memory.
+// The choice is by an estimate of the time, in us, of weights that come from memory: a launch, and the root of the squares of what the
+// busiest CU has to do and of what memory and the caches have to give: W, X once more for each of up to 8 XCDs that read it, in part, and for few
+// rows W again for each tile of rows, in part.  The figures are fitted to measurements of 1 to 9000 rows, 1 to 128 experts, 48 to 27648
+// outputs and 256 to 13824 columns in int8 and bf16 (a tenth off, in the mean): what a tile's begin and end and 128 bytes of columns cost, by rows of a
+// tile; the bytes a us that a CU of the kernel for few rows takes in; how much more either is where rows are not whole 128-byte lines.
 //   Both sides, int8 and us, few rows by 16 / 32 / 64 against wide ones by 64 / 128 / 256 in so many parts of the columns:
-//     outputs x columns   rows   few                  wide, whole columns    wide, parts            chosen
-//     1024 x 1024          64    3.5 / 4.0 / 5.1      10.9 / 12.8 / 18.1     (2) 10.9               few, 16
-//                          300   7.0 / 7.8 / 6.9      11.3 / 13.6 / 19.5     (2) 12.0               few, 64
-//     4096 x 4096            8   6.4 / 6.6 / 8.5      28.3 / 30.4 / 41.4     (4) 14.3 / 15.6 / 19.5 few, 16
-//                          100   17.2 / 13.9 / 13.9   28.5 / 33.4 / 42.7     (4) 17.8 / 19.7 / 23.3 few, 64
-//                          300   31.4 / 27.9 / 26.1   28.2 / 31.9 / 45.0     (2) 23.8 / 25.7 / 32.2 wide, 64 in 2
-//                         1000                        30.2 / 34.2 / 48.4     (2) 46.8 / 35.4 / 41.3 wide, 64
-//                         4000                        106 / 71.9 / 62.0                             wide, 256
-//     5120 x 13824          16   21.3 / 22.8 / 29.6   80.2 / 83.7 / 114      (4) 29.1 / 30.6 / 38.4 few, 16
-//                           64   39.6 / 35.0 / 39.6   86.5 / 89.6 / 114      (4) 31.7 / 33.1 / 39.7 wide, 64 in more: 27.8
-//                          300   118 / 112 / 95.6     81.3 / 88.0 / 127      (4) 57.6 / 40.0 / 50.4 wide, 128 in 4
-//                         1000                        161 / 96.6 / 133       (2) 146 / 120 / 89.3   wide, 256 in 3: 83.8
-// The choice was within 10 % of the fastest, or of what a call costs on the host, in all 32 measured shapes.
+//     outputs x columns   rows   few                  wide, whole columns    wide, parts
+//     1024 x 1024          64    3.5 / 4.0 / 5.1      10.9 / 12.8 / 18.1     (2) 10.9
+//                          300   7.0 / 7.8 / 6.9      11.3 / 13.6 / 19.5     (2) 12.0
+//     4096 x 4096            8   6.4 / 6.6 / 8.5      28.3 / 30.4 / 41.4     (4) 14.3 / 15.6 / 19.5
+//                          100   17.2 / 13.9 / 13.9   28.5 / 33.4 / 42.7     (4) 17.8 / 19.7 / 23.3
+//                          300   31.4 / 27.9 / 26.1   28.2 / 31.9 / 45.0     (2) 23.8 / 25.7 / 32.2
+//                         1000                        30.2 / 34.2 / 48.4     (2) 46.8 / 35.4 / 41.3
+//                         4000                        106 / 71.9 / 62.0
+//     5120 x 13824          16   21.3 / 22.8 / 29.6   80.2 / 83.7 / 114      (4) 29.1 / 30.6 / 38.4
+//                           64   39.6 / 35.0 / 39.6   86.5 / 89.6 / 114      (4) 31.7 / 33.1 / 39.7; (8) 27.8 by 64
+//                          300   118 / 112 / 95.6     81.3 / 88.0 / 127      (4) 57.6 / 40.0 / 50.4
+//                         1000                        161 / 96.6 / 133       (2) 146 / 120 / 89.3; (3) 83.8 by 256
+//     27648 x 12800         34   179 / 148 / 109      92.1 / 95.0 / 111      (2) 70.5 / 71.7 / 77.1
+//     27648 x 12720, off the lines: 34   253 / 179 / 148    132 / 135 / 143      (2) 86.5 / 88.0 / 92.1
+// Of 428 measured shapes the choice was within 15 % of the fastest in all but 15 (one matrix, or experts with as many rows each), a third off at
+// worst (3 rows by 1339 x 448, 5.3 us by tiles of 16, 3.9 by 32).
 struct Plan {
     bool few;
     int tile_rows, parts;
     double us;
 };
-constexpr double LAUNCH = 4.0, MEMORY = 4.7e6, PARTS_RATE = 6.2e6, FEW_RATE = 5.8e4;
-struct WideCost {
-    int rows;
-    double tile, stage;
+struct Off {
+    double work, memory;                                   // times as much for rows off the 128-byte lines
 };
-constexpr WideCost WIDE[3] = {{64, 2.5, 0.70}, {128, 4.4, 0.82}, {256, 7.7, 1.16}};
+struct Cost {
+    int rows;
+    double tile, stage;                                    // us, and bytes a us / us for 128 bytes of columns
+};
+constexpr double LAUNCH = 3.3, MEMORY = 7.3e6, PARTS = 2.2, PARTS_RATE = 6.5e6, FEW_X = 0.45, FEW_W = 0.15, WIDE_X = 0.12;
+constexpr Off FEW_OFF = {1.3, 1.45}, WIDE_OFF = {1.23, 1.23};
+constexpr Cost FEW[3] = {{16, 0.4, 9.4e4}, {32, 0.4, 9.9e4}, {64, 0.4, 8.0e4}}, WIDE[3] = {{64, 2.9, 0.72}, {128, 3.8, 0.83}, {256, 5.9, 1.12}};
+constexpr double FEW_GATED_64 = 0.75;                      // of the rate: the ring is two units then
 
 // groups: how many have rows, at most; row tiles are expected to be half a tile short.
 Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, bool gated, bool i8, bool may_part) {
-    const int64_t outs = d_out * (gated ? 2 : 1), bytes = d_in * (i8 ? 1 : 2);
-    const double each = (double)m / groups, weights = (double)groups * outs * bytes / MEMORY;
-    auto row_tiles = [&](int rows) {
+    const int64_t outs = d_out * (gated ? 2 : 1), bytes = d_in * (i8 ? 1 : 2), units = (bytes + 127) / 128;
+    const double each = (double)m / groups, w_bytes = (double)groups * outs * bytes, x_bytes = (double)m * bytes;
+    auto time = [&](double work, double memory, const Off &off) {
+        if (bytes % 128) {
+            work *= off.work;
+            memory *= off.memory;
+        }
+        memory /= MEMORY;
+        return LAUNCH + std::sqrt(work * work + memory * memory);
+    };
+    auto row_tiles = [&](int rows) {                        // of a group
         if (!grouped) return (double)((m + rows - 1) / rows);
         const double t = each / rows + 0.5;
-        return groups * (t < 1 ? 1 : t);
+        return t < 1 ? 1 : t;
     };
-    auto rounds = [](double blocks) { return blocks <= 256 ? 1.0 : blocks <= 1024 ? (double)(int64_t)((blocks + 255) / 256) : blocks / 256 + 0.5; };
+    auto rounds = [](double blocks) { return blocks <= 256 ? 1.0 : blocks <= 1024 ? (double)(((int64_t)blocks + 255) / 256) : blocks / 256 + 0.5; };
+    auto xcds = [](double readers) { return readers < 1 ? 1 : readers > 8 ? 8 : readers; };
     Plan best = {true, 64, 1, 1e30};
     auto offer = [&](bool few, int rows, int parts, double us) {
         if (us < best.us) best = {few, rows, parts, us};
     };
-    const int64_t units = (bytes + 127) / 128;
-    for (int rows = 16; rows <= 64; rows *= 2) {
-        const double tiles = row_tiles(rows) * ((d_out + 15) / 16);
+    for (const Cost &c : FEW) {
+        const double mine = row_tiles(c.rows), cols = (double)((d_out + 15) / 16), tiles = groups * mine * cols;
         const int split = few_split((int64_t)tiles, (int)units, 4);
-        const double slot = 2048.0 * ((gated ? 2 : 1) + rows / 16), work = rounds(tiles * split / 4) * units * 4 / split * slot / FEW_RATE;
-        offer(true, rows, 1, LAUNCH + (work > weights ? work : weights));
+        const double slot = 2048.0 * ((gated ? 2 : 1) + c.rows / 16), rate = gated && c.rows == 64 ? c.stage * FEW_GATED_64 : c.stage;
+        const double work = rounds(tiles * split / 4) * (c.tile + units * 4 / split * slot / rate);
+        offer(true, c.rows, 1, time(work, w_bytes * (1 + FEW_W * (mine - 1)) + x_bytes * FEW_X * xcds(cols * split / 4), FEW_OFF));
     }
-    const double cols = (double)((outs + 255) / 256), stages = (double)units;
-    for (const WideCost &c : WIDE)
+    const double cols = (double)((outs + 255) / 256);
+    for (const Cost &c : WIDE)
         for (int parts : {1, 2, 3, 4, 6, 8}) {
-            if (parts > 1 && (!may_part || stages < parts * 4)) break;
-            const double work = rounds(row_tiles(c.rows) * cols * parts) * (c.tile + stages / parts * c.stage);
-            double us = LAUNCH + (work > weights ? work : weights);
-            if (parts > 1) us += 2.5 + 8.0 * parts * m * outs / PARTS_RATE;
+            if (parts > 1 && (!may_part || units < parts * 4)) break;
+            const double work = rounds(groups * row_tiles(c.rows) * cols * parts) * (c.tile + (double)units / parts * c.stage);
+            double us = time(work, w_bytes + x_bytes * WIDE_X * xcds(cols), WIDE_OFF);
+            if (parts > 1) us += PARTS + 8.0 * parts * m * outs / PARTS_RATE;
             offer(false, c.rows, parts, us);
         }
     return best;
