@@ -68,7 +68,7 @@ struct RouteProblem {
     bool renormalise = false;
     int32_t *experts = nullptr, *offsets = nullptr, *rows = nullptr, *positions = nullptr;
     float *weights = nullptr;
-    uint32_t *counts = nullptr;          // scratch
+    uint8_t *counts = nullptr;           // scratch
     hipStream_t stream = nullptr;
 };
 size_t route_workspace_bytes(int m, int n_experts, int k);

@@ -16,6 +16,10 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 //   Arithmetic and the way through memory bound it about alike: 16384 tokens over 256 experts, 8 of them chosen, 11.5 us, of which some 3
 // are the choices' instructions, 2 the logits' 8.4 MB, the rest a launch and the steps between; with 64 lanes for a token the whole routing took 31.6 us, with sixteen 19.3.
 constexpr int RT_LANES = 16, RT_GROUPS = WAVE / RT_LANES;
+// Tokens of a workgroup of the first launch, and so the most that it can count for an expert: 8 bits hold it.  A workgroup's counts lie in
+// sectors of 32 bytes of their own, so that no two write to one.
+constexpr int RT_TOKENS = RT_GROUPS * RT_WAVES;
+__host__ __device__ constexpr int counts_row(int n_experts) { return (n_experts + 31) / 32 * 32; }
 
 __device__ __forceinline__ uint32_t row_max(uint32_t v) {
     v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));    // lane ^ 1
@@ -116,8 +120,8 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 // order, a launch's those of its workgroups.  What is written as a slot's position is first the slot's rank among those of its
 // expert in the workgroup; when all counts are known, what comes before is added: what comes before an expert, and before the
 // workgroup within the expert.  A single workgroup knows all counts by itself: up to 64 tokens are one launch (5 tokens, 8 experts 3.4 us),
-// more are two: a workgroup of the second sums the counts of all and of those before it, so none waits for another.  16384 tokens over
-// 256 experts 8.3 us; with four times as many counts on their way together 9.2.
+// more are two: a workgroup of the second sums the counts of all and of those before it, so none waits for another.  What it reads of
+// them bounds that: 16384 tokens over 256 experts 6.1 us with counts of 8 bits, four experts' to a load, 8.5 with ones of 32 bits.
 
 // Exclusive sums of the counts in `total` (LDS), by one wave; their sum.
 __device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
@@ -192,7 +196,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
             before += c;
         }
         if (ALONE) total[e] = before;
-        else q.counts[(int64_t)blockIdx.x * n + e] = before;
+        else q.counts[(int64_t)blockIdx.x * counts_row(n) + e] = (uint8_t)before;
     }
     __syncthreads();
     if (ALONE) {
@@ -216,7 +220,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
         for (int p = (int)all + threadIdx.x; p < q.m * k; p += RT_THREADS) q.rows[p] = -1;
 }
 
-// `lanes` threads, a power of two, have an expert each; RT_THREADS / lanes of them share the sums of an expert's counts.
+// `lanes` threads, a power of two, have four experts each; RT_THREADS / lanes of them share the sums of the experts' counts.
 __global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int tokens, int blocks, int lanes) {
     extern __shared__ uint32_t rt_lds[];
     uint32_t *before = rt_lds, *total = rt_lds + q.n_experts;   // [n_experts] each: of the workgroups before, of all
@@ -224,17 +228,28 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int 
     const int n = q.n_experts, k = q.k;
     for (int i = threadIdx.x; i < 2 * n; i += RT_THREADS) rt_lds[i] = 0;
     __syncthreads();
-    const int e0 = threadIdx.x % lanes, segment = threadIdx.x / lanes, segments = RT_THREADS / lanes;
+    const int e0 = threadIdx.x % lanes * 4, segment = threadIdx.x / lanes, segments = RT_THREADS / lanes, row = counts_row(n);
     if (e0 < n) {
-        uint32_t b = 0, t = 0;
+        constexpr int MOST = 0xFFFF / RT_TOKENS;            // counts that 16 bits hold the sum of
+        for (int i0 = segment; i0 < blocks; i0 += segments * MOST) {
+            uint32_t b[2] = {0, 0}, t[2] = {0, 0};          // experts e0 and e0 + 2, e0 + 1 and e0 + 3
+            const int i1 = min((int64_t)blocks, i0 + (int64_t)segments * MOST);
 #pragma unroll 8
-        for (int i = segment; i < blocks; i += segments) {
-            const uint32_t c = q.counts[(int64_t)i * n + e0];
-            t += c;
-            b += i < (int)blockIdx.x ? c : 0;
+            for (int i = i0; i < i1; i += segments) {
+                const uint32_t c = *reinterpret_cast<const uint32_t *>(q.counts + (int64_t)i * row + e0), even = c & 0xFF00FF, odd = c >> 8 & 0xFF00FF;
+                const bool is = i < (int)blockIdx.x;
+                t[0] += even;
+                t[1] += odd;
+                b[0] += is ? even : 0;
+                b[1] += is ? odd : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (e0 + j < n) {                           // whole numbers: their order changes nothing
+                    atomicAdd(&before[e0 + j], b[j & 1] >> (j / 2 * 16) & 0xFFFF);
+                    atomicAdd(&total[e0 + j], t[j & 1] >> (j / 2 * 16) & 0xFFFF);
+                }
         }
-        atomicAdd(&before[e0], b);                          // whole numbers: their order changes nothing
-        atomicAdd(&total[e0], t);
     }
     __syncthreads();
     if (threadIdx.x < WAVE) {
@@ -339,9 +354,6 @@ __global__ __launch_bounds__(CB_THREADS) void k_combine(const void *Y, int64_t y
     }
 }
 
-// Tokens of a workgroup of the first launch.
-constexpr int RT_TOKENS = RT_GROUPS * RT_WAVES;
-
 template <int DTYPE, int PER> hipError_t launch_pick(const RouteProblem &q, int blocks) {
     const size_t lds = ((size_t)RT_WAVES + 1) * q.n_experts * 4;
     static MoreLds alone, together;
@@ -374,7 +386,7 @@ hipError_t launch_combine_type(const void *Y, int64_t y_rows, int64_t ldy, const
 
 // Counts by workgroup and expert; a single workgroup keeps them.
 size_t route_workspace_bytes(int m, int n_experts, int) {
-    return m <= RT_TOKENS ? 0 : (size_t)((m + RT_TOKENS - 1) / RT_TOKENS) * n_experts * 4;
+    return m <= RT_TOKENS ? 0 : (size_t)((m + RT_TOKENS - 1) / RT_TOKENS) * counts_row(n_experts);
 }
 
 hipError_t launch_route(const RouteProblem &q) {
@@ -382,7 +394,7 @@ hipError_t launch_route(const RouteProblem &q) {
     const hipError_t e = q.dtype == 0 ? launch_pick<0>(q, blocks) : launch_pick<1>(q, blocks);
     if (e != hipSuccess || blocks == 1) return e;
     int lanes = WAVE;
-    while (lanes < q.n_experts) lanes *= 2;
+    while (lanes * 4 < q.n_experts) lanes *= 2;
     k_route_order<<<blocks, RT_THREADS, 2 * (size_t)q.n_experts * 4, q.stream>>>(q, RT_TOKENS, blocks, lanes);
     return hipGetLastError();
 }

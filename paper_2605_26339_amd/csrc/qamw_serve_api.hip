@@ -165,7 +165,7 @@ int qamw_route(const void *logits, int dtype, int m, int n_experts, int64_t ld, 
     q.offsets = offsets;
     q.rows = rows;
     q.positions = positions;
-    q.counts = static_cast<uint32_t *>(workspace);
+    q.counts = static_cast<uint8_t *>(workspace);
     q.stream = (hipStream_t)stream;
     return status_of(qamw::launch_route(q));
 }

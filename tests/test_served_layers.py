@@ -626,6 +626,27 @@ def test_route(m, n, k, dtype, renormalise):
 
 
 @gpu
+@pytest.mark.parametrize("m,n,k", [(1100003, 4, 2), (70001, 9, 9), (5000, 1021, 3)])
+def test_route_of_many_tokens(m, n, k):
+    """More workgroups than one sum of 16 bits holds the counts of, experts that all tokens like, rows of counts with an odd end."""
+    say(f"[route] many {m} x {n}, {k}")
+    x = torch.randn(m, n, generator=_gen(m)).bfloat16()
+    x[:, 1] += 6.0
+    x[100:3000] = -torch.inf
+    r = qamw.route(x.to(DEV), k)
+    flat = r.experts.reshape(-1).long()
+    assert torch.equal(r.experts[:, 0].cpu()[3000:].long(), x[3000:].float().max(1).indices)
+    assert (flat[100 * k:3000 * k] == -1).all() and (flat[:100 * k] >= 0).all() and (flat[3000 * k:] >= 0).all()
+    order = torch.sort(torch.where(flat < 0, n, flat), stable=True).indices[:int((flat >= 0).sum())]
+    counts = torch.bincount(flat[flat >= 0], minlength=n)
+    assert torch.equal(r.offsets.long(), torch.cat([counts.new_zeros(1), counts.cumsum(0)]))
+    assert torch.equal(r.rows[:len(order)].long(), order // k) and (r.rows[len(order):] == -1).all()
+    positions = torch.full_like(flat, -1)
+    positions[order] = torch.arange(len(order), device=DEV)
+    assert torch.equal(r.positions.reshape(-1).long(), positions)
+
+
+@gpu
 @pytest.mark.parametrize("m,k,d,pad,skip", [(0, 2, 8, 0, 0), (1, 1, 1, 0, 0), (5, 2, 4096, 0, 0), (7, 3, 100, 0, 0), (64, 8, 839, 0, 0), (33, 6, 2048, 8, 8), (20, 32, 70, 1, 1), (300, 2, 5120, 0, 0), (9, 5, 13825, 0, 0)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("out_dtype", [torch.float32, torch.bfloat16])
