@@ -9,12 +9,12 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 // ---- choice ---------------------------------------------------------------------------------------------------------------
 //
 // Sixteen lanes have a token, so that the largest of its logits is found by DPP within a row of lanes, for four tokens of a wave at a
-// time; a lane has PER experts that follow one another.  A logit becomes an unsigned number that orders as it does, 0 for what is
-// never chosen (-inf, NaN).  bf16 leaves room for the expert below it, the lowest one as the largest number, so that one maximum
-// finds both, and the next one is the largest that is smaller: of numbers below 2^31 it has the largest difference to the last one as
-// an unsigned number.  fp32 takes the lowest lane that has the maximum, and the lowest of its experts, and strikes it out.
-//   Arithmetic and the way through memory bound it about alike: 16384 tokens over 256 experts, 8 of them chosen, 11.5 us, of which some 3
-// are the choices' instructions, 2 the logits' 8.4 MB, the rest a launch and the steps between; with 64 lanes for a token the whole routing took 31.6 us, with sixteen 19.3.
+// time; a lane has PER experts that follow one another.  A logit becomes an unsigned number that orders as it does.
+// bf16 leaves room for the expert below it, the lowest one as the largest number, so that one maximum finds both, and the next one is the
+// largest that is smaller: of numbers below 2^31 it has the largest difference to the last one as an unsigned number.  fp32 takes the lowest lane that has the maximum, and the lowest of its experts, and strikes it out.
+//   Arithmetic bounds it, and the way through memory next: 16384 tokens over 256 experts, 8 of them chosen, 10.2 us, of which some 5 are
+// instructions, 2 the logits' 8.4 MB, the rest a launch and the steps between (12.4 where a choice was struck out, and values were made of numbers
+// again for the sum).  With 64 lanes for a token the whole routing took 31.6 us, with sixteen 16.4.
 constexpr int RT_LANES = 16, RT_GROUPS = WAVE / RT_LANES;
 // Tokens of a workgroup of the first launch, and so the most that it can count for an expert: 8 bits hold it.  A workgroup's counts lie in
 // sectors of 32 bytes of their own, so that no two write to one.
@@ -35,17 +35,18 @@ __device__ __forceinline__ float row_sum(float v) {
     v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false));
     return v;
 }
+// NaN as -inf, -0 as 0; -inf and what lies below it are never chosen
+__device__ __forceinline__ float clean(float f) { return fmaxf(f + 0.0f, -__builtin_inff()); }
+constexpr uint32_t RT_LEAST = 0x00800000u;                  // the key of the lowest finite value
 __device__ __forceinline__ uint32_t key_of(float f) {
-    if (!(f > -__builtin_inff())) return 0;
-    f += 0.0f;                                             // -0 is 0
     const uint32_t u = __float_as_uint(f);
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
-// exp(x - top), x <= top; infinities of one sign are equal
-__device__ __forceinline__ float share_of(float x, float top) { return x == top ? 1.0f : __expf(x - top); }
+// exp(x - top), x <= top; infinities of one sign are equal: their difference is no number, and 0 the smaller of the two
+__device__ __forceinline__ float share_of(float x, float top) { return __expf(fminf(x - top, 0.0f)); }
 
 // Lane j of a token's sixteen gets its choices j and j + 16: the experts (-1: none) and weights.  t >= m: none.
 template <int DTYPE, int PER>
@@ -57,13 +58,20 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
     Unaligned<E, PER> row;                                  // wherever it lies: the memory instructions take any address
     const bool whole = t < q.m && e0 + PER <= n;
     if (whole) row = *reinterpret_cast<const Unaligned<E, PER> *>(static_cast<const E *>(q.logits) + t * q.ld + e0);
+    else
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (DTYPE == 1) row.v[i] = (E)0xFF80u;          // -inf
+            else row.v[i] = (E)-__builtin_inff();
+            if (t < q.m && e0 + i < n) row.v[i] = static_cast<const E *>(q.logits)[t * q.ld + e0 + i];
+        }
+    auto logit = [&](int i) { return clean(DTYPE == 1 ? __uint_as_float((uint32_t)row.v[i] << 16) : (float)row.v[i]); };
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        if (!whole) row.v[i] = t < q.m && e0 + i < n ? static_cast<const E *>(q.logits)[t * q.ld + e0 + i] : E(0);
-        const float f = DTYPE == 1 ? __uint_as_float((uint32_t)row.v[i] << 16) : (float)row.v[i];
-        key[i] = t < q.m && e0 + i < n ? key_of(f) : 0;
-        if (PACKED && key[i]) key[i] = (key[i] >> 16) << 10 | (1023u - (uint32_t)(e0 + i));
+        key[i] = key_of(logit(i));
+        if (PACKED) key[i] = (key[i] >> 16 << 10 | (1023u - (uint32_t)e0)) - i;   // e0 + i <= 1023: no borrow
     }
+    constexpr uint32_t LEAST = PACKED ? RT_LEAST >> 16 << 10 : RT_LEAST;
     // of a packed key all that a negative value lacks are ones
     auto value = [](uint32_t k) { return value_of(PACKED ? (k >> 10 << 16) | (k & 0x2000000u ? 0u : 0xFFFFu) : k); };
     float total = 0.0f, top = 0.0f, mine[2] = {0.0f, 0.0f};
@@ -76,7 +84,7 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 #pragma unroll
         for (int i = 1; i < PER; ++i) own = max(own, key[i] - last);
         best = last + row_max(own);
-        some = some && best != 0;                           // a token that has run out of experts stays so
+        some = some && best >= LEAST;                       // a token that has run out of experts stays so
         if (!__any(some)) break;
         const float v = value(best);
         if (j == 0) {
@@ -84,8 +92,7 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
             if (!q.renormalise) {
                 float sum = 0.0f;
 #pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (key[i]) sum += share_of(value(key[i]), top);
+                for (int i = 0; i < PER; ++i) sum += share_of(PER > 32 ? value(key[i]) : logit(i), top);   // no registers for both
                 total = row_sum(sum);
             }
         }
