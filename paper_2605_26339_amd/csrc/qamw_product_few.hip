@@ -293,12 +293,14 @@ template <bool I8, bool GATED, bool YBF16, bool ONCE, typename S> hipError_t lau
 
 // Weights of which half the Infinity Cache would be full are read as what is not read again, where an expert's rows are a tile or so: 64 experts
 // of 1408 x 2048 bf16 with 8 rows each 70.6 us, 75.6 by ordinary loads, 8 of 11008 x 4096 134 and 147; with 20 rows each 91.2 and 91.4, with
-// 40 99.6 and 96.3.  Smaller weights may be found there again: 13824 x 5120 int8, over and over, 24.1 and 19.4.
+// 40 99.6 and 96.3.  Not where rows are off the 128-byte lines, whose other part the next unit asks for: 64 of 1408 x 2064 92.9 and 85.9, 8 of
+// 11008 x 4112 197 and 180.  Smaller weights may be found there again: 13824 x 5120 int8, over and over, 24.1 and 19.4.
 constexpr int64_t PF_KEPT = 128ll << 20;
 template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const Product &p, const FewArgs &q, size_t more_lds) {
     const int64_t bytes = (int64_t)p.n_experts * p.d_out * (p.gated ? 2 : 1) * p.d_in * (I8 ? 1 : 2);
     constexpr bool MAY = S::FROM < 0 && S::T == 1;
-    return MAY && bytes > PF_KEPT ? launch_once<I8, GATED, YBF16, MAY, S>(p, q, more_lds) : launch_once<I8, GATED, YBF16, false, S>(p, q, more_lds);
+    const bool on_lines = (p.ldw * (I8 ? 1 : 2) % 128 | p.expert_stride * (I8 ? 1 : 2) % 128 | (int64_t)(reinterpret_cast<uintptr_t>(p.W) % 128)) == 0;
+    return MAY && on_lines && bytes > PF_KEPT ? launch_once<I8, GATED, YBF16, MAY, S>(p, q, more_lds) : launch_once<I8, GATED, YBF16, false, S>(p, q, more_lds);
 }
 
 template <bool I8, int T, int FROM, int EIGHTS> hipError_t launch_shape(const Product &p, const FewArgs &q, size_t more_lds) {
