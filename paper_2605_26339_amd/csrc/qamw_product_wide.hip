@@ -336,11 +336,13 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         const bool busy = wm * S::FM * 16 < now.n && out_of(now.ct, wn * S::FN, 0) < a.d_out;   // some of the wave's rows and outputs are there
         const int stages = max(now.full, 2);
         for (int s = 0; s < stages - 2; ++s) stage(now, s + 1, now, s + 2, stored && s == 0, busy);
-        // the last two stages ask for the first ones of the next tile
+        // The last two stages ask for the first ones of the next tile.  Its scales go where those of the tile before this one were, which the second
+        // group reads up to the first barrier of this tile's own: they are asked for after a stage of this tile, however few it has.  The last
+        // stage's waits leave nothing older than its own loads on the way, so that they are there when the next tile needs them.
         t += step;
         const Tile<S> next = tile_at(t);
-        request_scales(next, parity ^ 1);
         stage(now, stages - 1, next, 0, stored && stages == 2, busy);
+        request_scales(next, parity ^ 1);
         stage(next, 0, next, 1, false, busy);
 
         const int q0 = (lane >> 4) * 4;
