@@ -479,6 +479,12 @@ int qamw_grouped_matmul(const void *X, int dtype, const float *x_scales, int x_r
                         const float *w_scales, int64_t ldw, int64_t expert_stride, const int32_t *offsets, int n_experts, int m,
                         int d_out, int d_in, int gated, void *Y, int y_dtype, int64_t ldy, void *stream);
 
+/* Which kernel a product takes whose operands are whole 16 bytes (a question for tests and measurements: it launches nothing).
+ * n_experts = 0: qamw_int8_matmul of codes (I8), with its workspace; otherwise qamw_grouped_matmul (BF16 or I8) of m rows.
+ *   plan_out  [0] 0: the kernel for few rows, 1: the one for many; [1] rows of its tiles; [2] parts of the columns
+ * Errors: m < 1, sizes out of the ranges above, BF16 without experts -> INVALID_ARG. */
+int qamw_product_plan(int dtype, int m, int n_experts, int d_out, int d_in, int gated, int plan_out[3]);
+
 /* Logits to experts: every token's k largest logits (of equal ones the lowest expert first), and its rows sorted by expert.
  *   logits   device, m rows of n_experts elements (F32 or BF16), leading dimension ld.  -inf and NaN are never chosen: a token
  *            with fewer than k other logits has fewer choices, a token with none is routed nowhere
@@ -511,10 +517,13 @@ int qamw_combine(const void *Y, int dtype, int y_rows, int64_t ldy, const int32_
  * 2 = the central cells in LDS whatever the size.  qamw_matmul / qamw_matmul_batch with one or two
  * activation rows: 0 = chosen by the size of the launch, 1 = activations rotated by a launch of their
  * own, 2 = rotated inside the product kernel; the results are the same, bit for bit.
+ * qamw_int8_matmul of codes / qamw_grouped_matmul: 0, 1 and 2 = chosen by an estimate of the time (qamw_product_plan),
+ * 64, 128 and 256 = the kernel for many rows by tiles of so many, where the operands are whole 16 bytes: in int8 the
+ * same bits, in bf16 sums in another order.  All other entry points take 64, 128 and 256 as 0.
  * This is the library's ONE piece of process-wide state: an atomic integer, safe to set from any thread, but it
  * affects every call of every thread made afterwards -- a switch for tests and measurements, not for production code
- * (all settings give the same results).  Returns the previous value (also for a value out of range, which changes
- * nothing). */
+ * (all settings give the same results, but for the order of those bf16 sums).  Returns the previous value (also
+ * for a value out of range, which changes nothing). */
 int qamw_set_kernel_path(int path);
 
 #ifdef __cplusplus

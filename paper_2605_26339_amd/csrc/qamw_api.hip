@@ -5,10 +5,16 @@
 
 #include "qamw.h"
 #include "qamw_internal.hpp"
+#include "qamw_product.hpp"
 
 namespace {
 
 std::atomic<int> g_kernel_path{0};
+// The codec's entry points: what concerns products alone leaves them as they are.
+int codec_path() {
+    const int path = g_kernel_path.load();
+    return path <= 2 ? path : 0;
+}
 
 // The packed stream is read and written in 32-bit words (its rows are multiples of 4 bytes).
 bool misaligned4(const void *q) { return (reinterpret_cast<uintptr_t>(q) & 3) != 0; }
@@ -44,7 +50,7 @@ qamw::Problem make_problem(int d_out, int d_in, const float *chan_scale, const i
 
 hipError_t launch_norms(const void *W, int dtype, int64_t ldw, int n_rows, const qamw::Problem &p, float *norms) {
     hipError_t e = hipSuccess;
-    if (g_kernel_path.load() != 1 && qamw::launch_row_norms_fast(W, dtype, ldw, n_rows, p, norms, &e)) return e;
+    if (codec_path() != 1 && qamw::launch_row_norms_fast(W, dtype, ldw, n_rows, p, norms, &e)) return e;
     return qamw::launch_row_norms(W, dtype, ldw, n_rows, p, norms);
 }
 
@@ -57,7 +63,7 @@ int decode_any(const uint8_t *packed, const float *row_norms, int d_out, int d_i
     if (ldo < d_in) return QAMW_ERR_SHAPE;
     qamw::Problem p = make_problem(d_out, d_in, chan_scale, signs, pair_sigma, codebook, bits, block, stream);
     hipError_t e;
-    if (g_kernel_path.load() != 1 && qamw::fast_decode_supported(p))
+    if (codec_path() != 1 && qamw::fast_decode_supported(p))
         e = qamw::launch_decode_fast(packed, row_norms, p, out, ldo, bf16);
     else
         e = qamw::launch_decode_general(packed, row_norms, p, out, ldo, bf16);
@@ -66,10 +72,15 @@ int decode_any(const uint8_t *packed, const float *row_norms, int d_out, int d_i
 
 }  // namespace
 
+int qamw::product_tile_rows() {
+    const int path = g_kernel_path.load();
+    return path > 2 ? path : 0;
+}
+
 extern "C" {
 
 int qamw_set_kernel_path(int path) {
-    if (path < 0 || path > 2) return g_kernel_path.load();
+    if ((path < 0 || path > 2) && path != 64 && path != 128 && path != 256) return g_kernel_path.load();
     return g_kernel_path.exchange(path);
 }
 
@@ -91,7 +102,7 @@ static int calibrate_impl(const void *W, int dtype, int d_out, int d_in, int64_t
     float *row_norms = static_cast<float *>(workspace);
     double *partial = reinterpret_cast<double *>(static_cast<char *>(workspace) + align_up((size_t)n * sizeof(float), 256));
     hipError_t e;
-    if (g_kernel_path.load() != 1 && qamw::fast_calibrate_supported(W, dtype, ldw, p)) {
+    if (codec_path() != 1 && qamw::fast_calibrate_supported(W, dtype, ldw, p)) {
         e = qamw::launch_calibrate_fast(W, dtype, ldw, n, p, partial, sigma_out);      // computes the rows' norms itself
     } else {
         if (launch_norms(W, dtype, ldw, n, p, row_norms) != hipSuccess) return QAMW_ERR_DEVICE;
@@ -129,7 +140,7 @@ int qamw_calibrate_sigma_batch(const qamw_calibrate_item *items, int n_items, in
     qamw::CalItem its[QAMW_MAX_BATCH];
     char *ws = static_cast<char *>(workspace);
     size_t used = 0;
-    bool fast = g_kernel_path.load() != 1;
+    bool fast = codec_path() != 1;
     for (int i = 0; i < n_items; ++i) {
         const qamw_calibrate_item &q = items[i];
         int rc = calibrate_check(q.W, dtype, q.d_out, q.d_in, q.ldw, hadamard_block, max_rows, q.sigma_out);
@@ -229,7 +240,7 @@ static int encode_impl(const void *W, int dtype, int d_out, int d_in, int64_t ld
     p.full_scans = full_scans;
     // The fast kernels compute the row norms themselves (W is fetched once); rows too long for that, and the general
     // kernels, get them from a launch of their own first.
-    const int path = g_kernel_path.load();
+    const int path = codec_path();
     const bool fused = path != 1 && qamw::fused_norms_supported(p);
     if (!fused && launch_norms(W, dtype, ldw, d_out, p, row_norms_out) != hipSuccess) return QAMW_ERR_DEVICE;
     hipError_t e = hipErrorNotSupported;                        // "not supported" = nothing launched yet
@@ -275,7 +286,7 @@ static int encode_batch_impl(const qamw_encode_item *items, int n_items, int dty
         fused = fused && qamw::fused_norms_supported(pi);
     }
     if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 15)) return QAMW_ERR_INVALID_ARG;
-    if (g_kernel_path.load() == 0) {
+    if (codec_path() == 0) {
         qamw::Problem shared = make_problem(items[0].d_out, items[0].d_in, nullptr, nullptr, nullptr, codebook, bits,
                                             hadamard_block, stream);
         hipError_t e = hipErrorNotSupported;
@@ -385,7 +396,7 @@ static int encode_pruned_impl(const void *W, int dtype, int d_out, int d_in, int
     p.full_scans = full_scans;
     qamw::SearchGridView g;
     g.table = grid;
-    g.variant = g_kernel_path.load();
+    g.variant = codec_path();
     if (qamw_search_grid_size(bits, &g.G, nullptr) != QAMW_OK) return QAMW_ERR_INVALID_ARG;
     // nothing is launched for a shape outside the kernel's range
     if (!qamw::grid_encode_launchable(W, dtype, ldw, p, g)) return QAMW_ERR_UNSUPPORTED;
@@ -441,7 +452,7 @@ static int decode_batch_impl(const qamw_decode_item *items, int n_items, const f
     }
     qamw::Problem shared = make_problem(items[0].d_out, items[0].d_in, nullptr, nullptr, nullptr, codebook, bits,
                                         hadamard_block, stream);
-    if (g_kernel_path.load() != 1 || traffic_only) {
+    if (codec_path() != 1 || traffic_only) {
         hipError_t e = qamw::launch_decode_batch_fast(its, n_items, shared, true, traffic_only);
         if (e == hipSuccess) return QAMW_OK;
         if (e != hipErrorNotSupported) return QAMW_ERR_DEVICE;
@@ -524,7 +535,7 @@ static int matmul_batch_impl(const qamw_matmul_item *items, int n_items, int x_d
                 its[i].Y = items[i].Y + (size_t)t0 * (size_t)items[i].ldy;
             }
         }
-        hipError_t e = qamw::launch_matmul_batch(its, n_items, x_dtype, rows, p, workspace, g_kernel_path.load());
+        hipError_t e = qamw::launch_matmul_batch(its, n_items, x_dtype, rows, p, workspace, codec_path());
         if (e == hipErrorNotSupported) return QAMW_ERR_UNSUPPORTED;
         if (e != hipSuccess) return QAMW_ERR_DEVICE;
     }

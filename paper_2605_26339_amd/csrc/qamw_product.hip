@@ -198,14 +198,21 @@ Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, 
         }
     return best;
 }
-Plan plan(const Product &p) {
-    const int64_t groups = !p.offsets ? 1 : p.m < p.n_experts ? p.m : p.n_experts;
-    return plan(p.m, groups, p.offsets != nullptr, p.d_out, p.d_in, p.gated, p.i8, p.scratch != nullptr);
+Plan plan_of(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, bool i8, bool may_part) {
+    if (const int rows = product_tile_rows()) return {false, rows, 1, 0.0};
+    return plan(m, !grouped ? 1 : m < n_experts ? m : n_experts, grouped, d_out, d_in, gated, i8, may_part);
 }
 
 }  // namespace
 
-// The sums of all parts.
+void product_plan(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, bool i8, bool may_part, int (&out)[3]) {
+    const Plan c = plan_of(m, n_experts, grouped, d_out, d_in, gated, i8, may_part);
+    out[0] = c.few ? 0 : 1;
+    out[1] = c.tile_rows;
+    out[2] = c.parts;
+}
+
+// The sums of all parts, whatever qamw_set_kernel_path() says: a workspace of this size serves the call before and after.
 size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated) {
     if (m == 0) return 0;
     const int parts = plan(m, 1, false, d_out, d_in, gated, true, true).parts;
@@ -215,7 +222,7 @@ size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated) {
 hipError_t launch_product(const Product &p) {
     if (p.m == 0) return hipSuccess;
     if (!product_wide_supported(p)) return p.i8 ? launch_any<true>(p) : launch_any<false>(p);
-    const Plan c = plan(p);
+    const Plan c = plan_of(p.m, p.n_experts, p.offsets != nullptr, p.d_out, p.d_in, p.gated, p.i8, p.scratch != nullptr);
     return c.few ? launch_product_few(p, c.tile_rows) : launch_product_wide(p, c.tile_rows, c.parts);
 }
 

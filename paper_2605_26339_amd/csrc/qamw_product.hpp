@@ -26,6 +26,9 @@ struct Product {
 };
 
 hipError_t launch_product(const Product &p);
+int product_tile_rows();                                                // set by qamw_set_kernel_path(): products of many rows by such tiles; 0: as estimated
+// What launch_product() would take for operands that product_wide_supported(); may_part: with scratch.
+void product_plan(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, bool i8, bool may_part, int (&out)[3]);
 size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated);   // of an int8 product of one group
 // Row of the sums of a part of the columns, in 32-bit words: whole 16 bytes; where the up projection's follow the gate's, four of them
 // are read together from anywhere.

@@ -126,6 +126,17 @@ int qamw_grouped_matmul(const void *X, int dtype, const float *x_scales, int x_r
     return status_of(qamw::launch_product(p));
 }
 
+int qamw_product_plan(int dtype, int m, int n_experts, int d_out, int d_in, int gated, int plan_out[3]) {
+    if (!plan_out || m < 1 || m > QAMW_INT8_MAX_ROWS || n_experts < 0 || n_experts > QAMW_MAX_EXPERTS || d_in < 1 ||
+        d_in > QAMW_INT8_MAX_D_IN || d_out < 1 || d_out > QAMW_PRODUCT_MAX_D_OUT || gated < 0 || gated > 1)
+        return QAMW_ERR_INVALID_ARG;
+    if (dtype != QAMW_DTYPE_I8 && (dtype != QAMW_DTYPE_BF16 || n_experts == 0)) return QAMW_ERR_INVALID_ARG;
+    int plan[3];
+    qamw::product_plan(m, n_experts, n_experts > 0, d_out, d_in, gated != 0, dtype == QAMW_DTYPE_I8, n_experts == 0, plan);
+    for (int i = 0; i < 3; ++i) plan_out[i] = plan[i];
+    return QAMW_OK;
+}
+
 static int route_check(int m, int n_experts, int k) {
     if (m < 0 || m > QAMW_INT8_MAX_ROWS || n_experts < 1 || n_experts > QAMW_MAX_EXPERTS || k < 1 || k > QAMW_MAX_CHOICES || k > n_experts)
         return QAMW_ERR_INVALID_ARG;

@@ -27,7 +27,7 @@ EXPORTS = [
     "qamw_search_grid_size", "qamw_search_grid_build", "qamw_encode_pruned", "qamw_calibrate_sigma_static", "qamw_decode_traffic_probe", "qamw_encode_batch", "qamw_calibrate_sigma_batch",
     "qamw_encode_workspace_bytes", "qamw_encode_ws", "qamw_encode_batch_ws", "qamw_encode_pruned_ws",
     "qamw_int8_quantize", "qamw_int8_matmul_workspace_bytes", "qamw_int8_matmul", "qamw_grouped_matmul",
-    "qamw_route_workspace_bytes", "qamw_route", "qamw_combine",
+    "qamw_product_plan", "qamw_route_workspace_bytes", "qamw_route", "qamw_combine",
 ]
 
 
@@ -121,6 +121,7 @@ def lib() -> C.CDLL:
         L.qamw_int8_matmul_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, C.POINTER(C.c_size_t)]
         L.qamw_int8_matmul.argtypes = [vp, i32, vp, vp, i32, i64, vp, vp, i64, i32, i32, i32, vp, i32, i64, vp, C.c_size_t, vp]
         L.qamw_grouped_matmul.argtypes = [vp, i32, vp, i32, i64, vp, vp, vp, i64, i64, vp, i32, i32, i32, i32, i32, vp, i32, i64, vp]
+        L.qamw_product_plan.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(i32)]
         L.qamw_route_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(C.c_size_t)]
         L.qamw_route.argtypes = [vp, i32, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.qamw_combine.argtypes = [vp, i32, i32, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp]
@@ -769,6 +770,17 @@ def grouped_matmul(X, W, offsets, rows=None, x_scales=None, w_scales=None, gated
                                      W.data_ptr(), _ptr(w_scales), ldw, stride[0], offsets.data_ptr(), n, m, d_out, d_in,
                                      1 if gated else 0, y.data_ptr(), y_code, ldy, _raw_stream(stream, dev)), "qamw_grouped_matmul")
     return y
+
+
+ProductPlan = collections.namedtuple("ProductPlan", "many_rows tile_rows parts")
+
+
+def product_plan(dtype: int, m: int, d_out: int, d_in: int, n_experts: int = 0, gated: bool = False) -> ProductPlan:
+    """Which kernel a product of aligned operands takes: whether the one for many rows, the rows of its tiles, the parts of the columns.
+    n_experts = 0: int8_matmul of codes; otherwise grouped_matmul of m rows (see qamw_product_plan in include/qamw.h)."""
+    out = (C.c_int * 3)()
+    _check(lib().qamw_product_plan(dtype, m, n_experts, d_out, d_in, int(gated), out), "qamw_product_plan")
+    return ProductPlan(bool(out[0]), out[1], out[2])
 
 
 Routing = collections.namedtuple("Routing", "experts weights offsets rows positions")
