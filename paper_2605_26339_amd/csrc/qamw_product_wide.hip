@@ -172,7 +172,7 @@ template <typename S> struct Tile {
 // OUT: what is stored: 0 fp32, 1 bf16, 2 the sums of a part of the columns as they are (int32 or fp32), one array of `part_stride`
 // elements a part.
 template <bool I8, bool GATED, int OUT, typename S>
-__global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, int col_tiles, int group, int whole, int parts, int64_t part_stride) {
+__global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, int most_tiles, int col_tiles, int group, int whole, int parts, int64_t part_stride) {
     constexpr bool YBF16 = OUT == 1, SCALED = I8 && OUT != 2;
     using M = Mfma<I8>;
     extern __shared__ __align__(16) char pw_lds[];
@@ -183,7 +183,9 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     // Workgroups go to the 8 XCDs in turn: an XCD gets tiles that follow one another, and these are ordered such that `group` row
     // tiles share their W while it is in the XCD's cache.  8 of them: gated int8, 8192 rows by 2 x 11008 x 4096, by groups of 1, 2, 4, 8, 16, 32:
     // 651, 636, 622, 618, 643, 654 us; 8002 rows of 8 such experts 807, 735, 703, 695, 681, 689.
-    const uint32_t one = (uint32_t)count_tiles<S::BM>(a) * (uint32_t)col_tiles, all = one * parts, share = (all + 7) / 8;
+    //   Offsets that do not ascend can make more row tiles than rows have room for: no more than the host has counted on are done, or the number of all
+    // tiles could pass 32 bits and a workgroup's turn with it.
+    const uint32_t one = (uint32_t)min(count_tiles<S::BM>(a), most_tiles) * (uint32_t)col_tiles, all = one * parts, share = (all + 7) / 8;
     const uint32_t begin = blockIdx.x % 8 * share, end = min(begin + share, all), step = gridDim.x / 8;
     // fragment f, row r of a tile's W: the output it makes (gated: 16 of the gate, then the same 16 of up)
     auto out_of = [&](int ct, int f, int r) { return GATED ? ct * (S::BN / 2) + (f >> 1) * 16 + r : ct * S::BN + f * 16 + r; };
@@ -452,7 +454,7 @@ __global__ __launch_bounds__(PS_THREADS) void k_product_parts(ProductArgs a, con
 
 template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Product &p, int parts, int64_t part_stride) {
     const int outs = GATED ? S::BN / 2 : S::BN;
-    const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, tiles = most_row_tiles(p, S::BM) * cols * parts;
+    const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, rows = most_row_tiles(p, S::BM), tiles = rows * cols * parts;
     if (tiles > 0x7FFFFFFF / 2) return hipErrorNotSupported;
     const int64_t blocks = tiles < PW_CUS ? (tiles + 7) / 8 * 8 : PW_CUS;       // one a CU, which goes from tile to tile
     const int64_t y_bytes = OUT == 1 ? 2 : 4;
@@ -463,7 +465,7 @@ template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Prod
     static MoreLds more;
     const hipError_t e = more.ask(reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
-    kernel<<<dim3((uint32_t)blocks), PW_THREADS, lds, p.stream>>>(args_of(p), (int)cols, 8, whole, parts, part_stride);
+    kernel<<<dim3((uint32_t)blocks), PW_THREADS, lds, p.stream>>>(args_of(p), (int)rows, (int)cols, 8, whole, parts, part_stride);
     return hipGetLastError();
 }
 

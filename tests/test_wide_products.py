@@ -222,3 +222,21 @@ def test_experts_from_tile_to_tile(by_tiles, i8, gated, gather):
                     r = torch.arange(a, b, device=DEV) if rows is None else rows[a:b].long()
                     ref, slack = _reference(x[r], None if xs is None else xs[r], w[e], None if ws is None else ws[e])
                     expect(y[a:b], ref, gated, slack, (dtype, e))
+
+
+@gpu
+@pytest.mark.parametrize("by_tiles", [64, 128, 256], indirect=True)
+@pytest.mark.parametrize("i8", [False, True])
+def test_offsets_that_do_not_ascend(by_tiles, i8):
+    """Every other expert claims all places, so that there are many times the tiles that rows have room for: the call ends, and nothing is
+    written beside Y.  Where every expert has the same matrix its claims agree, and what is written is right."""
+    n, m, d_out, d_in = 40, 3 * by_tiles + 9, 515, 256
+    say(f"[wide] by {by_tiles}: offsets up and down, {m} rows of {n} experts, int8 {i8}")
+    g = _gen(m)
+    x, w, xs, ws = _operands(g, i8, 1, d_out, m, d_in)
+    off = torch.tensor([0, m] * (n // 2) + [0], dtype=torch.int32, device=DEV)
+    guarded = torch.full((3 * m, d_out), 5.0, device=DEV)
+    qamw.grouped_matmul(x, w.expand(n, -1, -1), off, x_scales=xs, w_scales=None if ws is None else ws.repeat(n, 1), out=guarded[m:2 * m])
+    assert (guarded[:m] == 5).all() and (guarded[2 * m:] == 5).all()
+    ref, slack = _reference(x, xs, w[0], None if ws is None else ws[0])
+    expect(guarded[m:2 * m], ref, False, slack, "all places claimed")
