@@ -319,7 +319,7 @@ __global__ __launch_bounds__(CB_THREADS) void k_combine(const void *Y, int64_t y
     constexpr int AT_ONCE = 8;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     const int64_t s = (int64_t)t * k;
-    if (c + 8 <= d) {
+    if (d - c >= 8) {                                       // c + 8 need not fit
         for (int j0 = 0; j0 < k; j0 += AT_ONCE) {
             int at[AT_ONCE];
             float w[AT_ONCE];
