@@ -87,7 +87,7 @@ __global__ __launch_bounds__(QT) void k_quantize_any(const void *X, int d, int64
     __shared__ uint32_t part[QT / WAVE];
     const int64_t row = blockIdx.x, at = row * ldx;
     uint32_t most = 0;
-    for (int j = threadIdx.x; j < d; j += QT) {
+    for (uint32_t j = threadIdx.x; j < (uint32_t)d; j += QT) {             // unsigned: the last step may pass 2^31
         const float v = Elem<DTYPE>::load(X, at + j) * (col_scale ? col_scale[j] : 1.0f);
         most = max(most, __float_as_uint(v) & 0x7FFFFFFFu);
     }
@@ -96,7 +96,7 @@ __global__ __launch_bounds__(QT) void k_quantize_any(const void *X, int d, int64
     __syncthreads();
     const Quantiser z(wave_max(part[threadIdx.x % (QT / WAVE)]));
     if (threadIdx.x == 0) scales[row] = z.scale;
-    for (int j = threadIdx.x; j < d; j += QT)
+    for (uint32_t j = threadIdx.x; j < (uint32_t)d; j += QT)
         codes[row * ldc + j] = (int8_t)z.code(Elem<DTYPE>::load(X, at + j) * (col_scale ? col_scale[j] : 1.0f));
 }
 

@@ -21,3 +21,18 @@ def test_combine_of_the_longest_rows(d):
     one = torch.ones(1, 1, device=DEV)
     qamw.combine(y[:, :d], torch.zeros(1, 1, dtype=torch.int32, device=DEV), one, out=out[:, :d])
     assert torch.equal(out[:, :d], y[:, :d]) and (out[:, d:] == 7).all()
+
+
+@pytest.mark.parametrize("d", [LONGEST])
+def test_quantise_the_longest_row(d):
+    """By the definition, piece by piece; the largest value is the last one, and nothing is written behind it."""
+    say(f"[quantise] a row of {d}")
+    x = torch.empty(1, d, dtype=torch.bfloat16, device=DEV).uniform_(-1, 1, generator=torch.Generator(DEV).manual_seed(2))
+    x[0, -1] = 2.0
+    codes = torch.full((1, d + 9), 77, dtype=torch.int8, device=DEV)
+    scales = torch.empty(1, device=DEV)
+    qamw.int8_quantize(x, out=(codes[:, :d], scales))
+    assert scales.item() == torch.tensor(2.0).div(127).item() and (codes[:, d:] == 77).all() and codes[0, d - 1] == 127
+    for a in range(0, d, 1 << 28):
+        b = min(a + (1 << 28), d)
+        assert torch.equal(codes[0, a:b], (x[0, a:b].float() * 63.5).round().to(torch.int8))   # 127 / 2 is exact
