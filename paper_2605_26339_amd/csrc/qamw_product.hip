@@ -100,7 +100,7 @@ template <bool I8> hipError_t launch_any(const Product &p) {
     const ProductArgs a = args_of(p);
     const int outs = p.gated ? 32 : 64;
     const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, n = most_row_tiles(p, PA_TILE) * cols;
-    if (n > 0x7FFFFFFF) return hipErrorNotSupported;
+    if (n * PA_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
     const dim3 g((uint32_t)n);
     if (p.gated) {
         if (p.y_bf16) k_product_any<I8, true, true><<<g, PA_THREADS, 0, p.stream>>>(a, (int)cols);
