@@ -22,7 +22,7 @@
 namespace qamw {
 namespace {
 
-constexpr int PW_WAVES = 8, PW_THREADS = PW_WAVES * WAVE, PW_FRAG = 2048, PW_KB = 128, PW_CUS = 256, PW_TURN = 2048;
+constexpr int PW_WAVES = 8, PW_THREADS = PW_WAVES * WAVE, PW_FRAG = 2048, PW_KB = 128, PW_CUS = 256, PW_TURN = 2048, PW_SLOTS = 3;
 constexpr uint32_t PW_NOWHERE = 0x80000000u;       // added to an offset: beyond the end of any buffer here
 
 // Tiles: WN x WM waves, each of FN fragments of W and FM of X.  A stage in LDS: the first halves of the waves' fragments of W, the second
@@ -243,10 +243,12 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         }
         return z;
     };
-    auto request_scales = [&](const Tile<S> &z, uint32_t parity) {
+    // Three slots: a tile of one or two stages asks for the next one's scales before its first barrier, when the second group may still have the
+    // scales of the tile before it to read; in the third are its own.
+    auto request_scales = [&](const Tile<S> &z, uint32_t slot) {
         if (!SCALED) return;
         const float *from = wave < PW_WAVES / 2 ? a.x_scales + (a.rows ? 0 : z.row0) : a.w_scales + (int64_t)z.expert * a.d_out * (GATED ? 2 : 1);
-        request_dword(z.off_scale, resource(from), scales0 + parity * 2048 + wave * 256);
+        request_dword(z.off_scale, resource(from), scales0 + slot + wave * 256);
     };
 
     const int wn = wave % S::WN, wm = wave / S::WN;
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     uint32_t t = begin + blockIdx.x / 8;
     Tile<S> now = tile_at(t);
     if (now.n == 0) return;
-    uint32_t at = 0, parity = 0;                                              // the stage that is read, the scales that are
+    uint32_t at = 0, slot = 0;                                                // the stage that is read, the scales that are
     // which lanes have nothing in stage s of a tile
     auto nothing = [&](const Tile<S> &z, int s) { return s >= z.full || (s == z.full - 1 && z.part == parts - 1 && past) ? PW_NOWHERE : 0; };
     auto offsets = [&](auto &to, const auto &from, uint32_t gone) {
@@ -338,19 +340,18 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         const bool busy = wm * S::FM * 16 < now.n && out_of(now.ct, wn * S::FN, 0) < a.d_out;   // some of the wave's rows and outputs are there
         const int stages = max(now.full, 2);
         for (int s = 0; s < stages - 2; ++s) stage(now, s + 1, now, s + 2, stored && s == 0, busy);
-        // The last two stages ask for the first ones of the next tile.  Its scales go where those of the tile before this one were, which the second
-        // group reads up to the first barrier of this tile's own: they are asked for after a stage of this tile, however few it has.  The last
-        // stage's waits leave nothing older than its own loads on the way, so that they are there when the next tile needs them.
+        // the last two stages ask for the first ones of the next tile
         t += step;
         const Tile<S> next = tile_at(t);
+        const uint32_t slot_next = slot == (PW_SLOTS - 1) * 2048 ? 0 : slot + 2048;
+        request_scales(next, slot_next);
         stage(now, stages - 1, next, 0, stored && stages == 2, busy);
-        request_scales(next, parity ^ 1);
         stage(next, 0, next, 1, false, busy);
 
         const int q0 = (lane >> 4) * 4;
         // four outputs of fragment i (gated: and i + 1) in row j * 16 + lane % 16
         auto four = [&](int i, int j, float (&y)[4]) {
-            const uint32_t sc = scales0 + parity * 2048;
+            const uint32_t sc = scales0 + slot;
             float xs = 1.0f;
             pr_f32x4_t sg = {1, 1, 1, 1}, su = {1, 1, 1, 1};
             if (SCALED) {
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
             }
         if (next.n == 0) break;
         now = next;
-        parity ^= 1;
+        slot = slot_next;
         stored = whole != 0;
     }
     if (wave < PW_WAVES / 2) meet();
@@ -461,7 +462,7 @@ template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Prod
     const bool whole = (reinterpret_cast<uintptr_t>(p.Y) & 15) == 0 && p.ldy * y_bytes % 16 == 0 && (p.d_out * y_bytes % 16 == 0 || OUT == 2) &&
                        p.ldy <= 0x7FFFFFFF / (S::BM * y_bytes);
     const auto kernel = &k_product_wide<I8, GATED, OUT, S>;
-    constexpr int lds = 2 * S::STAGE + PW_WAVES * PW_TURN + 2 * 2048;
+    constexpr int lds = 2 * S::STAGE + PW_WAVES * PW_TURN + PW_SLOTS * 2048;
     static MoreLds more;
     const hipError_t e = more.ask(reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
