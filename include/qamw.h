@@ -427,8 +427,9 @@ int qamw_matmul_batch(const qamw_matmul_item *items, int n_items, int x_dtype, i
  * Layers as they are served: products in 8-bit integers, routed experts.
  * Device entry points with the conventions above.  A call with m = 0 rows is valid and does nothing (qamw_route writes
  * n_experts + 1 zeros).  Pointers need the alignment of their elements only; rows of whole 16 bytes on 16-byte boundaries
- * (pointers, leading dimensions, d_in) are served by the fast kernels.  Index arrays are device data and are not read on the
- * host: an entry out of range makes the rows concerned unspecified, and nothing outside the arrays given is read or written.
+ * (pointers, leading dimensions, d_in) are served by the fast kernels, where a matrix of W, 256 rows of X, and all of an X whose
+ * rows are gathered lie within 2 GiB; other products take up to three to four times as long.  Index arrays are device data and
+ * are not read on the host: an entry out of range makes the rows concerned unspecified, and nothing outside the arrays given is read or written.
  * ------------------------------------------------------------------------------------------ */
 enum {
     QAMW_INT8_MAX_ROWS = 1 << 22,      /* rows of a call                                                          */
@@ -455,6 +456,7 @@ int qamw_int8_quantize(const void *X, int dtype, int m, int d, int64_t ldx, cons
  *      qamw_int8_quantize (with col_scale, nullable), x_scales = NULL
  *   W  device, rows of d_in int8, leading dimension ldw, with w_scales, one float a row.  gated = 0: d_out rows.
  *      gated = 1: the d_out rows of a gate, then the d_out rows of an up projection, and Y = g / (1 + exp(-g)) * u
+ *      in fp32, the first factor with a relative error under 1.1 (|g| + 8) 2^-24, and 0 below g = -87.34
  *   Y  device, m rows of d_out elements of y_dtype (F32 or BF16, rounded to nearest even), leading dimension ldy
  *   workspace  qamw_int8_matmul_workspace_bytes() of device memory, 16-byte aligned (the codes; and where there are too few
  *      tiles for the chip, the sums of parts of the columns); NULL where that is 0, and where the product's own launch quantises
@@ -496,6 +498,7 @@ int qamw_product_plan(int dtype, int m, int n_experts, int d_out, int d_in, int 
  *   rows     [m k]: the token of each place; -1 for the places from offsets[n_experts] on
  *   positions [m][k]: the place of each choice, -1 where there is none
  *   workspace  qamw_route_workspace_bytes() of device memory, 16-byte aligned
+ * From some 30000 tokens on the time grows with the square of m (256 experts: 0.13 ms for 131072, 4.7 ms for 1048576).
  * Errors: m outside [0, QAMW_INT8_MAX_ROWS], n_experts outside [1, QAMW_MAX_EXPERTS], k outside [1, min(n_experts,
  * QAMW_MAX_CHOICES)], NULL or misaligned pointers, workspace too small -> INVALID_ARG; ld < n_experts -> SHAPE. */
 int qamw_route_workspace_bytes(int m, int n_experts, int k, size_t *bytes_out);

@@ -150,8 +150,9 @@ struct Quantiser {
     __device__ __forceinline__ uint32_t code(float v) const { return inv != 0.0f ? (uint32_t)(int)rintf(v * inv) & 255u : 0u; }
 };
 
-// g / (1 + exp(-g)) with the hardware's exponential and reciprocal: a few units in the last place of fp32, below a product's own
-// rounding, for a fifth of the instructions.  exp overflows to infinity, whose reciprocal is 0.
+// g / (1 + exp(-g)) with the hardware's exponential and reciprocal, for a fifth of the instructions.  Relative error, measured from -110 to
+// 110: under 1.1 (|g| + 8) 2^-24 for g < 0, since the exponential's argument is rounded and its size multiplies that, 2.4 * 2^-24 for g >= 0.  From
+// g = -87.34 down the reciprocal would be subnormal and is 0, where silu is under 1.1e-36 in size; exp overflows to infinity, whose reciprocal is 0.
 __device__ __forceinline__ float silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
 // Two values rounded to bf16 (nearest, ties to even).

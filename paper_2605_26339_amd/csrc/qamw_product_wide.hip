@@ -11,8 +11,10 @@
 //   multiplies, then they change places; a barrier is all that they need to keep in step.
 // What is not there (rows past the end, columns past d_in, stages past the last) is loaded as zeros: such a lane asks for an
 // address beyond its buffer's end.
-// What bounds it: power.  8192 x 8192 x 8192 in int8 runs at 2200 TOPS with random operands and at 3185 with zeros, at 1.3 and 1.9 GHz and
-// in the same clocks a stage, bf16 at 1270 and 1747 TFLOP/s; matrix instructions alone reach 3527 and 1981 with random operands.  256 rows of W and
+// What bounds it: power, and what a stage does beside its products.  8192 x 8192 x 8192 in int8 runs at 2200 TOPS with random operands and at
+// 3185 with zeros, at 1.3 and 1.9 GHz and in the same clocks a stage, bf16 at 1270 and 1747 TFLOP/s; matrix instructions alone reach 3527 and 1981
+// with random operands.  Of a wave's 1500 clocks a stage 585 are products, 428 reads, 490 waits and barriers; the matrix cores are busy for three
+// fifths.  The library's product of the same card reaches 2140 to 2175 TOPS and 1435 to 1550 TFLOP/s: for bf16 power is not all.  256 rows of W and
 // 256 of X, the most that accumulators have room for, read least for each product.  Smaller row tiles where there are too few to fill
 // the CUs: 1000 rows by 4096 x 4096 in 30.2 us by 64, 34.2 by 128, 48.4 by 256; 4000 rows 106, 71.9, 62.0.
 // Tried and slower: four waves of 128 x 128, one barrier a stage for all eight waves, five stages of 64 bytes, loads issued among the matrix
@@ -522,7 +524,8 @@ template <typename S> hipError_t launch_either(const Product &p, int parts) {
 
 }  // namespace
 
-// Whole 16 bytes everywhere, and offsets from a tile's or an expert's first row that 31 bits hold (with what a stage goes past a row).
+// Whole 16 bytes everywhere, and offsets from a tile's or an expert's first row that 31 bits hold (with what a stage goes past a row); rows that
+// are gathered come from anywhere, so that all of X has to lie within.
 bool product_wide_supported(const Product &p) {
     const int64_t e = p.i8 ? 1 : 2, most = 0x7FFFFFFF - 2 * PW_KB;
     auto whole = [](int64_t v) { return v % 16 == 0; };

@@ -129,6 +129,9 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 // workgroup within the expert.  A single workgroup knows all counts by itself: up to 64 tokens are one launch (5 tokens, 8 experts 3.4 us),
 // more are two: a workgroup of the second sums the counts of all and of those before it, so none waits for another.  What it reads of
 // them bounds that: 16384 tokens over 256 experts 6.1 us with counts of 8 bits, four experts' to a load, 8.5 with ones of 32 bits.
+//   Every workgroup reads all workgroups' counts, (m / 64)^2 bytes an expert, so that the second launch's time grows with the square of the tokens and
+// is most of a large call: over 256 experts, 8 of them chosen, both launches take 27 us for 32768 tokens, 128 for 131072, 381 for 262144 and 4.7 ms
+// for 1048576.
 
 // Exclusive sums of the counts in `total` (LDS), by one wave; their sum.
 __device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
@@ -289,6 +292,8 @@ constexpr int CB_THREADS = 256;
 // A thread has eight neighbours of a token's row, wherever they lie: the memory instructions take any address.  What it reads of
 // the experts' rows it asks for eight rows at a time.  Memory bounds it: 8192 tokens of 8 rows of 4096 bf16 in 104 us, 5.8 TB/s; one value a
 // thread, one row at a time took 312.  5 tokens of 2 rows 3.4 us, a launch.
+//   The last d % 8 columns are one thread's, which asks for one value at a time and waits for it: 8192 tokens of 8 rows of 4097 take 128 us, of 4095
+// 212 (fp32: 262 and 344, 237 of 4096), 100 tokens of 4095 14.5 against 7.2.
 // Rows that are read once, and a layer's are many: what passes them by is kept in the caches instead (132 us with ordinary loads).
 typedef uint32_t cb_u32x4_t __attribute__((ext_vector_type(4)));
 template <int DTYPE> struct EightOf;
