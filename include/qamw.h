@@ -59,7 +59,7 @@ enum {
     QAMW_ERR_DEVICE = 4       /* HIP reported an error at launch                          */
 };
 
-enum { QAMW_DTYPE_F32 = 0, QAMW_DTYPE_BF16 = 1, QAMW_DTYPE_I8 = 2 };   /* I8: where an entry point says so */
+enum { QAMW_DTYPE_F32 = 0, QAMW_DTYPE_BF16 = 1, QAMW_DTYPE_I8 = 2, QAMW_DTYPE_MX4 = 3 };   /* I8, MX4: where an entry point says so */
 
 enum { QAMW_MAX_BITS = 12, QAMW_MAX_BLOCK = 1024 };
 
@@ -436,7 +436,9 @@ enum {
     QAMW_INT8_MAX_D_IN = 131056,       /* columns: 2^14 each, sums stay within 32 bits                             */
     QAMW_PRODUCT_MAX_D_OUT = 1 << 24,
     QAMW_MAX_EXPERTS = 1024,
-    QAMW_MAX_CHOICES = 32
+    QAMW_MAX_CHOICES = 32,
+    QAMW_MAX_GROUPS = 64,
+    QAMW_MX4_MAX_D = 131072            /* columns of rows in 4 bits                                               */
 };
 
 /* Rows to 8-bit integers with one scale each (a token's activations, or the weights of an output channel):
@@ -481,6 +483,62 @@ int qamw_grouped_matmul(const void *X, int dtype, const float *x_scales, int x_r
                         const float *w_scales, int64_t ldw, int64_t expert_stride, const int32_t *offsets, int n_experts, int m,
                         int d_out, int d_in, int gated, void *Y, int y_dtype, int64_t ldy, void *stream);
 
+/* Rows in 4-bit floating point with a scale for every 32 columns (MX4).  Column j of a row has a code of 4 bits, sign, two bits of exponent and one of
+ * mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives; block b, columns 32 b .. 32 b + 31, has a scale, a byte s for 2^(s - 127), 255 for not a number.
+ *   codes   rows of 16 ceil(d / 32) bytes: column j in byte j / 2, an even column in the low half
+ *   scales  rows of 16 ceil(d / 512) bytes: block b in byte 16 (b / 16) + 4 (b % 4) + (b % 16) / 4
+ * Rows follow one another; both arrays are 16-byte aligned; what no column has is zero.
+ * qamw_mx4_row_bytes: the bytes of a row of both.  Errors: d outside [1, QAMW_MX4_MAX_D], NULL -> INVALID_ARG. */
+int qamw_mx4_row_bytes(int d, size_t *codes_out, size_t *scales_out);
+
+/* v_j = X_ij * col_scale_j (fp32, rounded once);  a = max |v| of the block;  e = max(floor(log2 a) - 2, -127), -127 for a = 0;  s = e + 127;
+ * code_j = v_j 2^-e to the nearest value, ties to the one of even mantissa, and beyond 6 to 6.  A block with an infinity or a NaN: s = 255 and codes 0,
+ * which makes every product with its row NaN.
+ *   X  device, m rows of d elements (F32 or BF16), leading dimension ldx;  col_scale  device, d floats, or NULL (ones)
+ * Errors: m outside [0, QAMW_INT8_MAX_ROWS], d outside [1, QAMW_MX4_MAX_D], NULL or misaligned pointers, dtype -> INVALID_ARG; ldx < d -> SHAPE;
+ * more blocks than a launch has threads for -> UNSUPPORTED. */
+int qamw_mx4_quantize(const void *X, int dtype, int m, int d, int64_t ldx, const float *col_scale, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* What the codes stand for, in out_dtype (F32, exact, or BF16, exact but for values below its normal numbers). */
+int qamw_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int m, int d, void *out, int out_dtype, int64_t ldo, void *stream);
+
+/* Y = X W^T of rows in 4 bits: products exact, sums in fp32 on the matrix cores.
+ *   X  x_dtype MX4: codes, with x_scales (ldx is not looked at).  x_dtype F32 or BF16: quantised in the call as by qamw_mx4_quantize (with col_scale,
+ *      nullable), x_scales = NULL
+ *   W  device, codes and scales.  gated = 0: d_out rows.  gated = 1: the d_out rows of a gate, then the d_out rows of an up projection, and
+ *      Y = g / (1 + exp(-g)) * u in fp32, as qamw_int8_matmul
+ *   Y  device, m rows of d_out elements of y_dtype (F32 or BF16, rounded to nearest even), leading dimension ldy
+ *   workspace  qamw_mx4_matmul_workspace_bytes() with x_rows = m and n_experts = 0, 16-byte aligned; NULL where that is 0
+ * Errors: sizes out of the ranges above, NULL or misaligned pointers, x_scales with floating X or col_scale with codes, a workspace too small ->
+ * INVALID_ARG; leading dimensions smaller than a row -> SHAPE; more tiles than a launch has, or a matrix of W or a gathered X of more than 2 GiB of codes ->
+ * UNSUPPORTED. */
+int qamw_mx4_matmul_workspace_bytes(int x_dtype, int x_rows, int m, int n_experts, int d_out, int d_in, int gated, size_t *bytes_out);
+int qamw_mx4_matmul(const void *X, int x_dtype, const uint8_t *x_scales, const float *col_scale, int m, int64_t ldx, const uint8_t *W,
+                    const uint8_t *w_scales, int d_out, int d_in, int gated, void *Y, int y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes,
+                    void *stream);
+
+/* The experts' products of rows in 4 bits: as qamw_grouped_matmul, with X (x_rows rows, all quantised in the call where they are floating) and the
+ * experts' matrices, one after the other, as qamw_mx4_matmul.  workspace: the same question, with all of the call's numbers.
+ * Errors: as qamw_mx4_matmul; n_experts outside [1, QAMW_MAX_EXPERTS], no offsets -> INVALID_ARG; without rows x_rows < m, with rows x_rows < 1 -> SHAPE. */
+int qamw_mx4_grouped_matmul(const void *X, int x_dtype, const uint8_t *x_scales, const float *col_scale, int x_rows, int64_t ldx, const int32_t *rows,
+                            const uint8_t *W, const uint8_t *w_scales, const int32_t *offsets, int n_experts, int m, int d_out, int d_in, int gated,
+                            void *Y, int y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The norms around a block: its output b, normalised, gated and scaled, goes into the stream h, and the norm of that is what the next block takes.
+ *   b' = b / sqrt(mean(b^2) + eps) * block_weight (block_weight NULL: b' = b);  b'' = gate * b' (gate NULL: b'' = b')
+ *   h_out = h + scale * b'', a fused multiply-add, rounded to dtype;  x = h_out / sqrt(mean(h_out^2) + eps) * weight (weight NULL: ones)
+ * in fp32, the sums of squares too.  block NULL: h_out is h, and x its norm; block_weight, gate and h_out are NULL then.
+ *   h, block, gate, h_out  device, rows of d elements of dtype (F32 or BF16) with leading dimensions ldh, ldb, ldg, ldho; ldg = 0: one row for all.
+ *      h_out may be h or block, with its leading dimension
+ *   weight, block_weight  device, d floats
+ *   x  x_dtype F32 or BF16: m rows of d, leading dimension ldx, x_scales NULL.  I8: rows as by qamw_int8_quantize of the fp32 values, x_scales m
+ *      floats.  MX4: rows as by qamw_mx4_quantize of them (ldx is not looked at), x_scales their scales
+ * Errors: m outside [0, QAMW_INT8_MAX_ROWS], d outside [1, QAMW_MX4_MAX_D], eps < 0 or NaN, types, NULL or misaligned pointers -> INVALID_ARG; leading
+ * dimensions smaller than a row -> SHAPE. */
+int qamw_block_norm(const void *h, int dtype, int m, int d, int64_t ldh, const void *block, int64_t ldb, const float *block_weight, const void *gate,
+                    int64_t ldg, float scale, const float *weight, float eps, void *h_out, int64_t ldho, void *x, int x_dtype, int64_t ldx, void *x_scales,
+                    void *stream);
+
 /* Which kernel a product takes whose operands are whole 16 bytes (a question for tests and measurements: it launches nothing).
  * n_experts = 0: qamw_int8_matmul of codes (I8), with its workspace; otherwise qamw_grouped_matmul (BF16 or I8) of m rows.
  *   plan_out  [0] 0: the kernel for few rows, 1: the one for many; [1] rows of its tiles; [2] parts of the columns
@@ -505,6 +563,20 @@ int qamw_route_workspace_bytes(int m, int n_experts, int k, size_t *bytes_out);
 int qamw_route(const void *logits, int dtype, int m, int n_experts, int64_t ld, int k, int renormalise, int32_t *experts,
                float *weights, int32_t *offsets, int32_t *rows, int32_t *positions, void *workspace, size_t workspace_bytes,
                void *stream);
+
+/* Logits to experts by scores: s_e = 1 / (1 + exp(-x_e)) (QAMW_SCORES_SIGMOID) or exp(x_e) / sum exp(x) (QAMW_SCORES_SOFTMAX), c_e = s_e + bias_e.
+ * The experts are `groups` groups of neighbours; a group's value is the sum of its group_top (1 or 2) largest c; the top_groups groups of largest value
+ * stay (groups = 1: all experts), and of their experts the k of largest c are chosen, in that order; of equal values the lowest group, the lowest expert
+ * first.  The weight is scale * s_e, renormalise = 1: scale * s_e / sum of the chosen s (0 where that is 0).  Scores, c and their sums are in 64 bits.
+ * Never chosen: an expert whose logit is -inf or NaN, or whose bias is; it adds nothing to its group's value, and a group of such experts does not stay.
+ * A softmax of several +inf shares among these equally.
+ *   bias  device, n_experts floats, or NULL (zeros);  everything else as qamw_route, with its workspace
+ * Errors: as qamw_route; scores, groups outside [1, QAMW_MAX_GROUPS], top_groups outside [1, groups], group_top -> INVALID_ARG; n_experts no multiple of
+ * groups -> SHAPE. */
+enum { QAMW_SCORES_SIGMOID = 0, QAMW_SCORES_SOFTMAX = 1 };
+int qamw_route_scored(const void *logits, int dtype, int m, int n_experts, int64_t ld, int k, int scores, const float *bias, int groups, int top_groups,
+                      int group_top, int renormalise, float scale, int32_t *experts, float *weights, int32_t *offsets, int32_t *rows, int32_t *positions,
+                      void *workspace, size_t workspace_bytes, void *stream);
 
 /* The way back: out_t = sum_j weights[t][j] * Y[positions[t][j]], fp32, j ascending, one fused multiply-add each.  A position
  * below 0 (or from y_rows on) adds nothing, whatever its weight.

@@ -1,0 +1,58 @@
+// Rows in 4-bit floating point with a scale for every 32 columns: their layout, their quantisation, their products.
+#pragma once
+#include "qamw_product_tile.hpp"
+
+namespace qamw {
+
+// Where the scale of block b is: the matrix instruction takes the scales of four neighbouring blocks from four groups of lanes, and one of the four bytes
+// of a register, so that a lane's blocks b % 4 of four such instructions are one dword.
+inline __host__ __device__ int mx4_scale_at(int b) { return b / 16 * 16 + b % 4 * 4 + b % 16 / 4; }
+
+// A block's exponent from its largest |v| (the bits; infinities and NaNs are the largest of all): 2^e times 6 is the largest value, so that one of
+// 2^(floor(log2 |v|) + 1) is rounded down to it.
+struct Mx4Scale {
+    uint32_t byte;                       // e + 127; 255: not a number
+    float inv;                           // 2^-e, or 0 where all codes are 0
+    __device__ __forceinline__ explicit Mx4Scale(uint32_t most) {
+        const uint32_t p = most >> 23;                     // floor(log2) + 127, or 0 below the smallest normal number, where e is -127 in any case
+        byte = p >= 255 ? 255 : p > 2 ? p - 2 : 0;
+        inv = p >= 255 ? 0.0f : __uint_as_float((254 - byte) << 23);
+    }
+};
+// Eight neighbours to codes, the first in the lowest bits.  The conversion rounds to nearest, ties to even, and what is beyond 6 to 6.
+__device__ __forceinline__ uint32_t mx4_codes(const float (&v)[8], const Mx4Scale &s) {
+    if (s.byte == 255) return 0;
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0] * s.inv, v[1] * s.inv, 1.0f, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2] * s.inv, v[3] * s.inv, 1.0f, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * s.inv, v[5] * s.inv, 1.0f, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * s.inv, v[7] * s.inv, 1.0f, 3);
+    return c;
+}
+// The largest of four neighbouring lanes' values.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));
+}
+// 2^(byte - 127)
+__device__ __forceinline__ float mx4_power(uint32_t byte) {
+    return __uint_as_float(byte == 255 ? 0x7FC00000u : byte ? byte << 23 : 0x00400000u);
+}
+
+// 16 rows of W times 16 rows of X over 128 columns: lane l holds block l / 16 of row l % 16 of both operands, and the block's scale in byte T of a
+// register; it gets W rows 4 (l / 16) .. + 4 of the column that is X row l % 16.
+typedef int mx4_i32x8_t __attribute__((ext_vector_type(8)));
+template <int T> __device__ __forceinline__ pr_f32x4_t mx4_mul(pr_i32x4_t w, pr_i32x4_t x, pr_f32x4_t c, int w_scale, int x_scale) {
+    const mx4_i32x8_t a = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1), b = __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, T, w_scale, T, x_scale);
+}
+
+// A product: ProductArgs with rows of codes (ldx, ldw, expert_stride in bytes), and the scales.
+struct Mx4Args {
+    ProductArgs p;
+    const uint8_t *xs, *ws;
+    int64_t lds;                         // bytes of a row of scales
+};
+inline Mx4Args mx4_args_of(const Mx4Product &q) { return {args_of(q.p), q.xs, q.ws, mx4_scale_bytes(q.p.d_in)}; }
+
+}  // namespace qamw

@@ -63,6 +63,32 @@ hipError_t launch_product_from_floats(const Product &p, const void *X, int dtype
 hipError_t launch_int8_quantize(const void *X, int dtype, int64_t m, int d, int64_t ldx, const float *col_scale, int8_t *codes,
                                 int64_t ldc, float *scales, hipStream_t stream);
 
+// Rows in 4-bit floating point with a scale for every 32 columns.
+// A row's codes are whole 16 bytes, a block of 32 columns each; its scales whole 16 bytes, 16 blocks each.
+inline __host__ __device__ int64_t mx4_code_bytes(int64_t d) { return (d + 31) / 32 * 16; }
+inline __host__ __device__ int64_t mx4_scale_bytes(int64_t d) { return (d + 511) / 512 * 16; }
+hipError_t launch_mx4_quantize(const void *X, int dtype, int64_t m, int d, int64_t ldx, const float *col_scale, uint8_t *codes, uint8_t *scales,
+                               hipStream_t stream);
+hipError_t launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t m, int d, void *out, int out_dtype, int64_t ldo, hipStream_t stream);
+// A Product of rows in 4 bits: i8 is set, and ldx, ldw and expert_stride are the codes' bytes.
+struct Mx4Product {
+    Product p;
+    const uint8_t *xs = nullptr, *ws = nullptr;   // the scales, as the rows of X and W
+};
+hipError_t launch_mx4_product(const Mx4Product &p);
+
+// Norms around a block.  Null: without block, block_weight, gate, weight.
+struct BlockNorm {
+    const void *h = nullptr, *block = nullptr, *gate = nullptr;
+    const float *block_weight = nullptr, *weight = nullptr;
+    void *h_out = nullptr, *x = nullptr, *x_scales = nullptr;
+    int64_t ldh = 0, ldb = 0, ldg = 0, ldho = 0, ldx = 0;
+    int dtype = 0, x_dtype = 0, m = 0, d = 0;     // x_dtype: 0 fp32, 1 bf16, 2 int8, 3 4 bits
+    float scale = 1.0f, eps = 0.0f;
+    hipStream_t stream = nullptr;
+};
+hipError_t launch_block_norm(const BlockNorm &p);
+
 // Routed experts.
 struct RouteProblem {
     const void *logits = nullptr;
@@ -73,6 +99,11 @@ struct RouteProblem {
     float *weights = nullptr;
     uint8_t *counts = nullptr;           // scratch
     hipStream_t stream = nullptr;
+    // by scores: choices by the logits alone where it is not set
+    bool scored = false, softmax = false;
+    const float *bias = nullptr;
+    int groups = 1, top_groups = 1, group_top = 1;
+    float scale = 1.0f;
 };
 size_t route_workspace_bytes(int m, int n_experts, int k);
 hipError_t launch_route(const RouteProblem &p);

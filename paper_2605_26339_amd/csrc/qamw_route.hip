@@ -1,4 +1,5 @@
 // Routed experts: the choice of experts, the order of the rows, and the way back.
+#include "qamw.h"
 #include "qamw_product_tile.hpp"
 
 namespace qamw {
@@ -16,6 +17,7 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 // instructions, 2 the logits' 8.4 MB, the rest a launch and the steps between (12.4 where a choice was struck out, and values were made of numbers
 // again for the sum).  With 64 lanes for a token the whole routing took 31.6 us, with sixteen 16.4.
 constexpr int RT_LANES = 16, RT_GROUPS = WAVE / RT_LANES;
+constexpr int RT_GROUP_SLOTS = QAMW_MAX_GROUPS / RT_LANES;    // groups of experts that a lane looks after
 // Tokens of a workgroup of the first launch, and so the most that it can count for an expert: 8 bits hold it.  A workgroup's counts lie in
 // sectors of 32 bytes of their own, so that no two write to one.
 constexpr int RT_TOKENS = RT_GROUPS * RT_WAVES;
@@ -120,6 +122,128 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
     for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 ? mine[h] / total : 0.0f;
 }
 
+// ---- choice by scores -----------------------------------------------------------------------------------------------------
+//
+// Scores, the bias and the sums of groups are in 64 bits: a choice is a comparison, and two values that 32 bits cannot tell apart are usual
+// among a few million.  As above sixteen lanes have a token, a lane PER experts that follow one another.
+
+__device__ __forceinline__ double row_max(double v) {
+    auto step = [](double x, auto move) { return __hiloint2double(move(__double2hiint(x)), move(__double2loint(x))); };
+    v = fmax(v, step(v, [](int w) { return dpp_move<DPP_XOR1>(w); }));
+    v = fmax(v, step(v, [](int w) { return dpp_move<DPP_XOR2>(w); }));
+    v = fmax(v, step(v, [](int w) { return dpp_move<DPP_HALF_MIRROR>(w); }));
+    return fmax(v, step(v, [](int w) { return dpp_move<DPP_MIRROR>(w); }));
+}
+__device__ __forceinline__ double row_sum(double v) {
+    auto step = [](double x, auto move) { return __hiloint2double(move(__double2hiint(x)), move(__double2loint(x))); };
+    v += step(v, [](int w) { return dpp_move<DPP_XOR1>(w); });
+    v += step(v, [](int w) { return dpp_move<DPP_XOR2>(w); });
+    v += step(v, [](int w) { return dpp_move<DPP_HALF_MIRROR>(w); });
+    v += step(v, [](int w) { return dpp_move<DPP_MIRROR>(w); });
+    return v;
+}
+__device__ __forceinline__ int first_of_row(bool has) {      // the lowest of the token's sixteen lanes for which it holds; -1: none
+    return __ffs((int)((uint32_t)(__ballot(has) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu)) - 1;
+}
+
+template <int DTYPE, int PER>
+__device__ __forceinline__ void pick_scored(const RouteProblem &q, int64_t t, int (&expert)[2], float (&weight)[2]) {
+    const int lane = threadIdx.x % RT_LANES, n = q.n_experts, e0 = lane * PER;
+    using E = typename Elem<DTYPE>::type;
+    const double none = -__builtin_inf();
+    auto logit = [&](int i) {
+        return t < q.m && e0 + i < n ? clean(Elem<DTYPE>::load(static_cast<const E *>(q.logits) + t * q.ld, e0 + i)) : -__builtin_inff();
+    };
+    double top = none, total = 1.0;
+    if (q.softmax) {
+        for (int i = 0; i < PER; ++i) top = fmax(top, (double)logit(i));
+        top = row_max(top);
+        total = 0.0;
+        for (int i = 0; i < PER; ++i) {
+            const double x = logit(i);
+            total += x > none ? exp(x == top ? 0.0 : x - top) : 0.0;
+        }
+        total = row_sum(total);
+    }
+    auto score = [&](double x) { return q.softmax ? exp(x == top ? 0.0 : x - top) / total : 1.0 / (1.0 + exp(-x)); };
+    double c[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const double x = logit(i);
+        const double b = q.bias && e0 + i < n ? (double)q.bias[e0 + i] : 0.0;
+        c[i] = x > none && b > none ? score(x) + b : none;
+    }
+    if (q.groups > 1) {
+        const int each = n / q.groups;
+        unsigned long long kept = 0;
+        double value[RT_GROUP_SLOTS];                                          // of the groups lane, lane + 16, ...
+#pragma unroll
+        for (int h = 0; h < RT_GROUP_SLOTS; ++h) value[h] = none;
+        for (int g = 0; g < q.groups; ++g) {
+            double first = none, second = none;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if ((e0 + i) / each == g) {
+                    second = fmax(second, fmin(first, c[i]));
+                    first = fmax(first, c[i]);
+                }
+            const double best = row_max(first);
+            const int who = first_of_row(first == best && best > none);
+            const double next = row_max(lane == who ? second : first);
+            const double v = q.group_top > 1 && next > none ? best + next : best;
+#pragma unroll
+            for (int h = 0; h < RT_GROUP_SLOTS; ++h)
+                if (g == h * RT_LANES + lane) value[h] = v;
+        }
+        for (int j = 0; j < q.top_groups; ++j) {
+            double own = none;
+#pragma unroll
+            for (int h = 0; h < RT_GROUP_SLOTS; ++h) own = fmax(own, value[h]);
+            const double best = row_max(own);
+            int found = 64;                                                    // the lowest group with it
+#pragma unroll
+            for (int h = RT_GROUP_SLOTS - 1; h >= 0; --h)
+                if (value[h] == best && best > none) found = h * RT_LANES + lane;
+            for (int d = 1; d < RT_LANES; d <<= 1) found = min(found, __shfl_xor(found, d, RT_LANES));
+            if (found < 64) kept |= 1ull << found;
+#pragma unroll
+            for (int h = 0; h < RT_GROUP_SLOTS; ++h)
+                if (h * RT_LANES + lane == found) value[h] = none;
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (e0 + i >= n || !(kept >> ((e0 + i) / each) & 1)) c[i] = none;
+    }
+    double mine[2] = {0.0, 0.0}, sum = 0.0;
+    expert[0] = expert[1] = -1;
+    for (int j = 0; j < q.k; ++j) {
+        double own = c[0];
+#pragma unroll
+        for (int i = 1; i < PER; ++i) own = fmax(own, c[i]);
+        const double best = row_max(own);
+        const bool some = best > none;                      // a token that has run out of experts stays so
+        if (!__any(some)) break;
+        const int winner = first_of_row(some && own == best);
+        int at = 0;
+#pragma unroll
+        for (int i = PER - 1; i >= 0; --i) at = c[i] == best ? i : at;
+        const int who = __shfl(e0 + at, max(winner, 0), RT_LANES);
+        at = lane == winner ? at : -1;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = i == at ? none : c[i];
+        if (some) {
+            const double p = score((double)clean(Elem<DTYPE>::load(static_cast<const E *>(q.logits) + t * q.ld, who)));
+            sum += p;
+            if (lane == j % RT_LANES) {
+                expert[j / RT_LANES] = who;
+                mine[j / RT_LANES] = p;
+            }
+        }
+    }
+    const double whole = q.renormalise ? sum : 1.0;
+    for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 && whole > 0.0 ? (float)(mine[h] / whole * (double)q.scale) : 0.0f;
+}
+
 // ---- order ----------------------------------------------------------------------------------------------------------------
 //
 // A stable counting sort of the slots (token after token, choice after choice).  A wave has the slots of the tokens that follow one
@@ -151,7 +275,7 @@ __device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
     return before;
 }
 
-template <int DTYPE, int PER, bool ALONE>
+template <int DTYPE, int PER, bool SCORED, bool ALONE>
 __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
     extern __shared__ uint32_t rt_lds[];                    // [RT_WAVES][n_experts]: counts, then what comes before them
     __shared__ uint32_t all;
@@ -166,7 +290,8 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
     if (t0 < t1) {
         int expert[2];
         float weight[2];
-        pick<DTYPE, PER>(q, t0 + lane / RT_LANES, expert, weight);
+        if constexpr (SCORED) pick_scored<DTYPE, PER>(q, t0 + lane / RT_LANES, expert, weight);
+        else pick<DTYPE, PER>(q, t0 + lane / RT_LANES, expert, weight);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int g0 = t0 + h * at_once;
@@ -366,23 +491,23 @@ __global__ __launch_bounds__(CB_THREADS) void k_combine(const void *Y, int64_t y
     }
 }
 
-template <int DTYPE, int PER> hipError_t launch_pick(const RouteProblem &q, int blocks) {
+template <int DTYPE, int PER, bool SCORED> hipError_t launch_pick(const RouteProblem &q, int blocks) {
     const size_t lds = ((size_t)RT_WAVES + 1) * q.n_experts * 4;
     static MoreLds alone, together;
-    const hipError_t e = blocks == 1 ? alone.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, true>), 80 * 1024)
-                                     : together.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, false>), 80 * 1024);
+    const hipError_t e = blocks == 1 ? alone.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, SCORED, true>), 80 * 1024)
+                                     : together.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, SCORED, false>), 80 * 1024);
     if (e != hipSuccess) return e;
-    if (blocks == 1) k_route_pick<DTYPE, PER, true><<<1, RT_THREADS, lds, q.stream>>>(q);
-    else k_route_pick<DTYPE, PER, false><<<blocks, RT_THREADS, lds, q.stream>>>(q);
+    if (blocks == 1) k_route_pick<DTYPE, PER, SCORED, true><<<1, RT_THREADS, lds, q.stream>>>(q);
+    else k_route_pick<DTYPE, PER, SCORED, false><<<blocks, RT_THREADS, lds, q.stream>>>(q);
     return hipGetLastError();
 }
-template <int DTYPE> hipError_t launch_pick(const RouteProblem &q, int blocks) {
-    if (q.n_experts <= 16) return launch_pick<DTYPE, 1>(q, blocks);
-    if (q.n_experts <= 64) return launch_pick<DTYPE, 4>(q, blocks);
-    if (q.n_experts <= 128) return launch_pick<DTYPE, 8>(q, blocks);
-    if (q.n_experts <= 256) return launch_pick<DTYPE, 16>(q, blocks);
-    if (q.n_experts <= 512) return launch_pick<DTYPE, 32>(q, blocks);
-    return launch_pick<DTYPE, 64>(q, blocks);
+template <int DTYPE, bool SCORED> hipError_t launch_pick(const RouteProblem &q, int blocks) {
+    if (q.n_experts <= 16) return launch_pick<DTYPE, 1, SCORED>(q, blocks);
+    if (q.n_experts <= 64) return launch_pick<DTYPE, 4, SCORED>(q, blocks);
+    if (q.n_experts <= 128) return launch_pick<DTYPE, 8, SCORED>(q, blocks);
+    if (q.n_experts <= 256) return launch_pick<DTYPE, 16, SCORED>(q, blocks);
+    if (q.n_experts <= 512) return launch_pick<DTYPE, 32, SCORED>(q, blocks);
+    return launch_pick<DTYPE, 64, SCORED>(q, blocks);
 }
 
 template <int DTYPE, bool OBF16>
@@ -403,7 +528,9 @@ size_t route_workspace_bytes(int m, int n_experts, int) {
 
 hipError_t launch_route(const RouteProblem &q) {
     const int blocks = q.m <= RT_TOKENS ? 1 : (q.m + RT_TOKENS - 1) / RT_TOKENS;
-    const hipError_t e = q.dtype == 0 ? launch_pick<0>(q, blocks) : launch_pick<1>(q, blocks);
+    hipError_t e;
+    if (q.scored) e = q.dtype == 0 ? launch_pick<0, true>(q, blocks) : launch_pick<1, true>(q, blocks);
+    else e = q.dtype == 0 ? launch_pick<0, false>(q, blocks) : launch_pick<1, false>(q, blocks);
     if (e != hipSuccess || blocks == 1) return e;
     int lanes = WAVE;
     while (lanes * 4 < q.n_experts) lanes *= 2;

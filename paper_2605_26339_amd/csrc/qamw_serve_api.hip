@@ -150,9 +150,8 @@ int qamw_route_workspace_bytes(int m, int n_experts, int k, size_t *bytes_out) {
     return rc;
 }
 
-int qamw_route(const void *logits, int dtype, int m, int n_experts, int64_t ld, int k, int renormalise, int32_t *experts,
-               float *weights, int32_t *offsets, int32_t *rows, int32_t *positions, void *workspace, size_t workspace_bytes,
-               void *stream) {
+static int route(qamw::RouteProblem &q, const void *logits, int dtype, int m, int n_experts, int64_t ld, int k, int renormalise, int32_t *experts,
+                 float *weights, int32_t *offsets, int32_t *rows, int32_t *positions, void *workspace, size_t workspace_bytes, void *stream) {
     size_t need = 0;
     const int rc = qamw_route_workspace_bytes(m, n_experts, k, &need);
     if (rc != QAMW_OK) return rc;
@@ -163,7 +162,6 @@ int qamw_route(const void *logits, int dtype, int m, int n_experts, int64_t ld, 
         misaligned(positions, 4))
         return QAMW_ERR_INVALID_ARG;
     if (ld < n_experts) return QAMW_ERR_SHAPE;
-    qamw::RouteProblem q;
     q.logits = logits;
     q.dtype = dtype;
     q.m = m;
@@ -179,6 +177,170 @@ int qamw_route(const void *logits, int dtype, int m, int n_experts, int64_t ld, 
     q.counts = static_cast<uint8_t *>(workspace);
     q.stream = (hipStream_t)stream;
     return status_of(qamw::launch_route(q));
+}
+
+int qamw_route(const void *logits, int dtype, int m, int n_experts, int64_t ld, int k, int renormalise, int32_t *experts,
+               float *weights, int32_t *offsets, int32_t *rows, int32_t *positions, void *workspace, size_t workspace_bytes,
+               void *stream) {
+    qamw::RouteProblem q;
+    return route(q, logits, dtype, m, n_experts, ld, k, renormalise, experts, weights, offsets, rows, positions, workspace, workspace_bytes, stream);
+}
+
+int qamw_route_scored(const void *logits, int dtype, int m, int n_experts, int64_t ld, int k, int scores, const float *bias, int groups, int top_groups,
+                      int group_top, int renormalise, float scale, int32_t *experts, float *weights, int32_t *offsets, int32_t *rows, int32_t *positions,
+                      void *workspace, size_t workspace_bytes, void *stream) {
+    if (scores != QAMW_SCORES_SIGMOID && scores != QAMW_SCORES_SOFTMAX) return QAMW_ERR_INVALID_ARG;
+    if (groups < 1 || groups > QAMW_MAX_GROUPS || top_groups < 1 || top_groups > groups || group_top < 1 || group_top > 2 || misaligned(bias, 4))
+        return QAMW_ERR_INVALID_ARG;
+    if (n_experts >= 1 && n_experts % groups != 0) return QAMW_ERR_SHAPE;
+    qamw::RouteProblem q;
+    q.scored = true;
+    q.softmax = scores == QAMW_SCORES_SOFTMAX;
+    q.bias = bias;
+    q.groups = groups;
+    q.top_groups = top_groups;
+    q.group_top = group_top;
+    q.scale = scale;
+    return route(q, logits, dtype, m, n_experts, ld, k, renormalise, experts, weights, offsets, rows, positions, workspace, workspace_bytes, stream);
+}
+
+// Rows in 4 bits: whole 16 bytes, on 16-byte boundaries.
+static bool mx4_sizes_ok(int m, int d) { return m >= 0 && m <= QAMW_INT8_MAX_ROWS && d >= 1 && d <= QAMW_MX4_MAX_D; }
+
+int qamw_mx4_row_bytes(int d, size_t *codes_out, size_t *scales_out) {
+    if (!codes_out || !scales_out || d < 1 || d > QAMW_MX4_MAX_D) return QAMW_ERR_INVALID_ARG;
+    *codes_out = (size_t)qamw::mx4_code_bytes(d);
+    *scales_out = (size_t)qamw::mx4_scale_bytes(d);
+    return QAMW_OK;
+}
+
+int qamw_mx4_quantize(const void *X, int dtype, int m, int d, int64_t ldx, const float *col_scale, uint8_t *codes, uint8_t *scales, void *stream) {
+    if (!mx4_sizes_ok(m, d) || !float_dtype(dtype)) return QAMW_ERR_INVALID_ARG;
+    if (m > 0 && (!X || !codes || !scales)) return QAMW_ERR_INVALID_ARG;
+    if (off_type(X, dtype) || misaligned(codes, 16) || misaligned(scales, 16) || misaligned(col_scale, 4)) return QAMW_ERR_INVALID_ARG;
+    if (ldx < d) return QAMW_ERR_SHAPE;
+    return status_of(qamw::launch_mx4_quantize(X, dtype, m, d, ldx, col_scale, codes, scales, (hipStream_t)stream));
+}
+
+int qamw_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int m, int d, void *out, int out_dtype, int64_t ldo, void *stream) {
+    if (!mx4_sizes_ok(m, d) || !float_dtype(out_dtype)) return QAMW_ERR_INVALID_ARG;
+    if (m > 0 && (!codes || !scales || !out)) return QAMW_ERR_INVALID_ARG;
+    if (misaligned(codes, 16) || misaligned(scales, 16) || off_type(out, out_dtype)) return QAMW_ERR_INVALID_ARG;
+    if (ldo < d) return QAMW_ERR_SHAPE;
+    return status_of(qamw::launch_mx4_dequantize(codes, scales, m, d, out, out_dtype, ldo, (hipStream_t)stream));
+}
+
+// In the workspace: the codes of X, then its scales.
+static size_t mx4_rows_bytes(int x_dtype, int rows, int d_in) {
+    return x_dtype == QAMW_DTYPE_MX4 ? 0 : (size_t)rows * (size_t)(qamw::mx4_code_bytes(d_in) + qamw::mx4_scale_bytes(d_in));
+}
+
+int qamw_mx4_matmul_workspace_bytes(int x_dtype, int x_rows, int m, int n_experts, int d_out, int d_in, int gated, size_t *bytes_out) {
+    if (!bytes_out || !mx4_sizes_ok(m, d_in) || !mx4_sizes_ok(x_rows, d_in) || n_experts < 0 || n_experts > QAMW_MAX_EXPERTS || d_out < 1 ||
+        d_out > QAMW_PRODUCT_MAX_D_OUT || gated < 0 || gated > 1 || (!float_dtype(x_dtype) && x_dtype != QAMW_DTYPE_MX4))
+        return QAMW_ERR_INVALID_ARG;
+    *bytes_out = mx4_rows_bytes(x_dtype, x_rows, d_in);
+    return QAMW_OK;
+}
+
+static int mx4_product(const void *X, int x_dtype, const uint8_t *x_scales, const float *col_scale, int x_rows, int64_t ldx, const int32_t *rows,
+                       const uint8_t *W, const uint8_t *w_scales, const int32_t *offsets, int n_experts, int m, int d_out, int d_in, int gated, void *Y,
+                       int y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream) {
+    size_t need = 0;
+    const int rc = qamw_mx4_matmul_workspace_bytes(x_dtype, x_rows, m, n_experts, d_out, d_in, gated, &need);
+    if (rc != QAMW_OK) return rc;
+    if (!float_dtype(y_dtype)) return QAMW_ERR_INVALID_ARG;
+    const bool codes = x_dtype == QAMW_DTYPE_MX4;
+    if (m > 0 && (!X || !W || !w_scales || !Y || (codes && !x_scales) || (n_experts && !offsets))) return QAMW_ERR_INVALID_ARG;
+    if (codes ? col_scale != nullptr : x_scales != nullptr) return QAMW_ERR_INVALID_ARG;
+    if ((codes ? misaligned(X, 16) : off_type(X, x_dtype)) || misaligned(x_scales, 16) || misaligned(W, 16) || misaligned(w_scales, 16) ||
+        off_type(Y, y_dtype) || misaligned(col_scale, 4) || misaligned(rows, 4) || misaligned(offsets, 4))
+        return QAMW_ERR_INVALID_ARG;
+    if ((!codes && ldx < d_in) || ldy < d_out) return QAMW_ERR_SHAPE;
+    if (m > 0 && (rows ? x_rows < 1 : x_rows < m)) return QAMW_ERR_SHAPE;
+    if (need && m > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return QAMW_ERR_INVALID_ARG;
+    if (m == 0) return QAMW_OK;
+    qamw::Mx4Product q;
+    qamw::Product &p = q.p;
+    p.i8 = true;                                             // leading dimensions are bytes
+    p.ldx = p.ldw = qamw::mx4_code_bytes(d_in);
+    p.expert_stride = p.ldw * d_out * (gated ? 2 : 1);
+    p.rows = rows;
+    p.x_rows = x_rows;
+    p.W = W;
+    p.offsets = n_experts ? offsets : nullptr;
+    p.n_experts = n_experts ? n_experts : 1;
+    p.Y = Y;
+    p.ldy = ldy;
+    p.m = m;
+    p.d_out = d_out;
+    p.d_in = d_in;
+    p.gated = gated != 0;
+    p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
+    p.stream = (hipStream_t)stream;
+    q.ws = w_scales;
+    if (codes) {
+        p.X = X;
+        q.xs = x_scales;
+    } else {
+        uint8_t *to = static_cast<uint8_t *>(workspace), *scales = to + (size_t)x_rows * (size_t)p.ldx;
+        p.X = to;
+        q.xs = scales;
+        const hipError_t e = qamw::launch_mx4_quantize(X, x_dtype, x_rows, d_in, ldx, col_scale, to, scales, (hipStream_t)stream);
+        if (e != hipSuccess) return status_of(e);
+    }
+    return status_of(qamw::launch_mx4_product(q));
+}
+
+int qamw_mx4_matmul(const void *X, int x_dtype, const uint8_t *x_scales, const float *col_scale, int m, int64_t ldx, const uint8_t *W,
+                    const uint8_t *w_scales, int d_out, int d_in, int gated, void *Y, int y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes,
+                    void *stream) {
+    return mx4_product(X, x_dtype, x_scales, col_scale, m, ldx, nullptr, W, w_scales, nullptr, 0, m, d_out, d_in, gated, Y, y_dtype, ldy, workspace,
+                       workspace_bytes, stream);
+}
+
+int qamw_mx4_grouped_matmul(const void *X, int x_dtype, const uint8_t *x_scales, const float *col_scale, int x_rows, int64_t ldx, const int32_t *rows,
+                            const uint8_t *W, const uint8_t *w_scales, const int32_t *offsets, int n_experts, int m, int d_out, int d_in, int gated,
+                            void *Y, int y_dtype, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream) {
+    if (n_experts < 1) return QAMW_ERR_INVALID_ARG;
+    return mx4_product(X, x_dtype, x_scales, col_scale, x_rows, ldx, rows, W, w_scales, offsets, n_experts, m, d_out, d_in, gated, Y, y_dtype, ldy,
+                       workspace, workspace_bytes, stream);
+}
+
+int qamw_block_norm(const void *h, int dtype, int m, int d, int64_t ldh, const void *block, int64_t ldb, const float *block_weight, const void *gate,
+                    int64_t ldg, float scale, const float *weight, float eps, void *h_out, int64_t ldho, void *x, int x_dtype, int64_t ldx, void *x_scales,
+                    void *stream) {
+    if (!mx4_sizes_ok(m, d) || !float_dtype(dtype) || x_dtype < QAMW_DTYPE_F32 || x_dtype > QAMW_DTYPE_MX4 || !(eps >= 0.0f)) return QAMW_ERR_INVALID_ARG;
+    const bool mx4 = x_dtype == QAMW_DTYPE_MX4, coded = mx4 || x_dtype == QAMW_DTYPE_I8;
+    if (block ? m > 0 && !h_out : block_weight || gate || h_out) return QAMW_ERR_INVALID_ARG;
+    if (m > 0 && (!h || !x || (coded && !x_scales))) return QAMW_ERR_INVALID_ARG;
+    if (!coded && x_scales) return QAMW_ERR_INVALID_ARG;
+    if (off_type(h, dtype) || off_type(block, dtype) || off_type(gate, dtype) || off_type(h_out, dtype) || misaligned(block_weight, 4) ||
+        misaligned(weight, 4) || (mx4 ? misaligned(x, 16) || misaligned(x_scales, 16) : off_type(x, x_dtype) || misaligned(x_scales, 4)))
+        return QAMW_ERR_INVALID_ARG;
+    if (ldh < d || (block && (ldb < d || ldho < d)) || (gate && ldg != 0 && ldg < d) || (!mx4 && ldx < d)) return QAMW_ERR_SHAPE;
+    qamw::BlockNorm q;
+    q.h = h;
+    q.block = block;
+    q.gate = gate;
+    q.block_weight = block_weight;
+    q.weight = weight;
+    q.h_out = h_out;
+    q.x = x;
+    q.x_scales = x_scales;
+    q.ldh = ldh;
+    q.ldb = ldb;
+    q.ldg = ldg;
+    q.ldho = ldho;
+    q.ldx = ldx;
+    q.dtype = dtype;
+    q.x_dtype = x_dtype;
+    q.m = m;
+    q.d = d;
+    q.scale = scale;
+    q.eps = eps;
+    q.stream = (hipStream_t)stream;
+    return status_of(qamw::launch_block_norm(q));
 }
 
 int qamw_combine(const void *Y, int dtype, int y_rows, int64_t ldy, const int32_t *positions, const float *weights, int m, int k, int d,

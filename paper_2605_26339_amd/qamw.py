@@ -16,7 +16,7 @@ import numpy as np
 from . import build as _build
 
 OK, ERR_INVALID_ARG, ERR_SHAPE, ERR_UNSUPPORTED, ERR_DEVICE = 0, 1, 2, 3, 4
-DTYPE_F32, DTYPE_BF16, DTYPE_I8 = 0, 1, 2
+DTYPE_F32, DTYPE_BF16, DTYPE_I8, DTYPE_MX4 = 0, 1, 2, 3
 
 EXPORTS = [
     "qamw_status_string", "qamw_packed_row_bytes", "qamw_paper_block_size", "qamw_bpw", "qamw_sign_mask",
@@ -28,6 +28,8 @@ EXPORTS = [
     "qamw_encode_workspace_bytes", "qamw_encode_ws", "qamw_encode_batch_ws", "qamw_encode_pruned_ws",
     "qamw_int8_quantize", "qamw_int8_matmul_workspace_bytes", "qamw_int8_matmul", "qamw_grouped_matmul",
     "qamw_product_plan", "qamw_route_workspace_bytes", "qamw_route", "qamw_combine",
+    "qamw_mx4_row_bytes", "qamw_mx4_quantize", "qamw_mx4_dequantize", "qamw_mx4_matmul_workspace_bytes", "qamw_mx4_matmul",
+    "qamw_mx4_grouped_matmul", "qamw_block_norm", "qamw_route_scored",
 ]
 
 
@@ -125,6 +127,15 @@ def lib() -> C.CDLL:
         L.qamw_route_workspace_bytes.argtypes = [i32, i32, i32, C.POINTER(C.c_size_t)]
         L.qamw_route.argtypes = [vp, i32, i32, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.qamw_combine.argtypes = [vp, i32, i32, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp]
+        f32, size_p = C.c_float, C.POINTER(C.c_size_t)
+        L.qamw_mx4_row_bytes.argtypes = [i32, size_p, size_p]
+        L.qamw_mx4_quantize.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp]
+        L.qamw_mx4_dequantize.argtypes = [vp, vp, i32, i32, vp, i32, i64, vp]
+        L.qamw_mx4_matmul_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, i32, size_p]
+        L.qamw_mx4_matmul.argtypes = [vp, i32, vp, vp, i32, i64, vp, vp, i32, i32, i32, vp, i32, i64, vp, C.c_size_t, vp]
+        L.qamw_mx4_grouped_matmul.argtypes = [vp, i32, vp, vp, i32, i64, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, i32, i64, vp, C.c_size_t, vp]
+        L.qamw_block_norm.argtypes = [vp, i32, i32, i32, i64, vp, i64, vp, vp, i64, f32, vp, f32, vp, i64, vp, i32, i64, vp, vp]
+        L.qamw_route_scored.argtypes = [vp, i32, i32, i32, i64, i32, i32, vp, i32, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
         for name in EXPORTS:
             if name != "qamw_status_string":
                 getattr(L, name).restype = C.c_int
@@ -793,18 +804,14 @@ def route_workspace_bytes(m: int, n_experts: int, k: int) -> int:
     return int(out.value)
 
 
-def route(logits, k: int, renormalise=True, workspace=None, stream=None):
-    """Every token's k experts by its logits (fp32 or bf16 [m][n_experts]), their softmax weights (over the chosen, or over all
-    where renormalise is false) and the rows sorted by expert.  Returns a Routing: experts [m][k], weights [m][k],
-    offsets [n_experts + 1], rows [m k] and positions [m][k]; -1 where there is none (see qamw_route in include/qamw.h)."""
+def _routing(logits, m, n, k, workspace, stream):
+    """(a Routing to be written, the workspace's address, its bytes, what is kept until the launches)"""
     import torch
 
-    m, n, ld = _rows(logits, "logits")
-    size = route_workspace_bytes(m, n, k)
-    dev = _one_device(logits, workspace)
+    size, work = route_workspace_bytes(m, n, k), None
     i32, on = torch.int32, logits.device
     if workspace is None:
-        work = _new(1, size, torch.uint8, logits, stream) if size else None   # kept until the launches
+        work = _new(1, size, torch.uint8, logits, stream) if size else None
         at = _ptr(work)
     else:
         at, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -816,8 +823,52 @@ def route(logits, k: int, renormalise=True, workspace=None, stream=None):
     else:
         r = Routing(_empty((m, k), i32, on, stream), _empty((m, k), torch.float32, on, stream), _empty((n + 1,), i32, on, stream),
                     _empty((m * k,), i32, on, stream), _empty((m, k), i32, on, stream))
+    return r, at, size, work
+
+
+def route(logits, k: int, renormalise=True, workspace=None, stream=None):
+    """Every token's k experts by its logits (fp32 or bf16 [m][n_experts]), their softmax weights (over the chosen, or over all
+    where renormalise is false) and the rows sorted by expert.  Returns a Routing: experts [m][k], weights [m][k],
+    offsets [n_experts + 1], rows [m k] and positions [m][k]; -1 where there is none (see qamw_route in include/qamw.h)."""
+    m, n, ld = _rows(logits, "logits")
+    dev = _one_device(logits, workspace)
+    r, at, size, _work = _routing(logits, m, n, k, workspace, stream)
     _check(lib().qamw_route(logits.data_ptr(), _dtype_code(logits), m, n, ld, k, 1 if renormalise else 0, r[0].data_ptr(), r[1].data_ptr(),
                             r[2].data_ptr(), r[3].data_ptr(), r[4].data_ptr(), at, size, _raw_stream(stream, dev)), "qamw_route")
+    return r
+
+
+def _launch(dev, name, *args):
+    """A device entry point on the device of its tensors, whichever is the current one."""
+    import torch
+
+    call = getattr(lib(), name)
+    if dev == torch._C._cuda_getDevice():
+        return _check(call(*args), name)
+    with torch.cuda.device(dev):
+        return _check(call(*args), name)
+
+
+_SCORES = {"sigmoid": 0, "softmax": 1}
+
+
+def route_scored(logits, k: int, scores="sigmoid", bias=None, groups: int = 1, top_groups=None, group_top: int = 2, renormalise=True, scale: float = 1.0,
+                 workspace=None, stream=None):
+    """Every token's k experts by scores of its logits (fp32 or bf16 [m][n_experts]): sigmoid or softmax, plus a bias for balance (fp32
+    [n_experts]) that the weights do not have.  Of `groups` groups of neighbouring experts only the top_groups (all where it is None) with the largest
+    sum of their group_top best are chosen from.  Weights are the chosen scores, over their sum where renormalise is true, times scale.
+    Returns a Routing, as route does (see qamw_route_scored in include/qamw.h)."""
+    import torch
+
+    m, n, ld = _rows(logits, "logits")
+    if scores not in _SCORES:
+        raise ValueError(f"scores are 'sigmoid' or 'softmax', not {scores!r}")
+    _vector(bias, "bias", torch.float32, (n,))
+    dev = _one_device(logits, bias, workspace)
+    r, at, size, _work = _routing(logits, m, n, k, workspace, stream)
+    _launch(dev, "qamw_route_scored", logits.data_ptr(), _dtype_code(logits), m, n, ld, k, _SCORES[scores], _ptr(bias), groups,
+            groups if top_groups is None else top_groups, group_top, 1 if renormalise else 0, scale, r[0].data_ptr(), r[1].data_ptr(),
+            r[2].data_ptr(), r[3].data_ptr(), r[4].data_ptr(), at, size, _raw_stream(stream, dev))
     return r
 
 
@@ -837,3 +888,198 @@ def combine(Y, positions, weights, out=None, out_dtype=None, stream=None):
     _check(lib().qamw_combine(Y.data_ptr(), _dtype_code(Y), y_rows, ldy, positions.data_ptr(), weights.data_ptr(), shape[0], shape[1], d,
                               y.data_ptr(), y_code, ldo, _raw_stream(stream, dev)), "qamw_combine")
     return y
+
+
+# ------------------------------------------------------------------ served layers: rows in 4-bit floating point, norms
+Mx4 = collections.namedtuple("Mx4", "codes scales columns")
+Mx4.__doc__ = """Rows in 4-bit floating point with a scale for every 32 columns: codes uint8 [rows][16 ceil(columns / 32)], scales uint8
+[rows][16 ceil(columns / 512)] (experts: [n_experts][rows][...]), and the number of columns; their layout is in include/qamw.h."""
+
+
+@functools.lru_cache(maxsize=256, typed=True)
+def mx4_row_bytes(d: int):
+    """(bytes of a row of codes, of its scales)"""
+    codes, scales = C.c_size_t(), C.c_size_t()
+    _check(lib().qamw_mx4_row_bytes(d, C.byref(codes), C.byref(scales)), "qamw_mx4_row_bytes")
+    return int(codes.value), int(scales.value)
+
+
+def _mx4(q, name, dims=2):
+    """The rows and columns of an Mx4 that is whole, for experts their number too."""
+    import torch
+
+    codes, scales, d = q
+    shape = codes.shape
+    if len(shape) != dims:
+        raise ValueError(f"{name} must have codes of {dims} dimensions")
+    code_bytes, scale_bytes = mx4_row_bytes(d)
+    _vector(codes, f"{name}.codes", torch.uint8, (*shape[:-1], code_bytes))
+    _vector(scales, f"{name}.scales", torch.uint8, (*shape[:-1], scale_bytes))
+    return (*shape[:-1], d)
+
+
+def mx4_quantize(X, col_scale=None, out=None, stream=None):
+    """Rows of X (fp32 or bf16 [m][d]) to 4-bit floating point with a scale for every 32 columns: an Mx4 (out: one to write to).
+    col_scale (fp32 [d]) multiplies the columns first.  For weights a row is an output channel, for activations a token."""
+    import torch
+
+    m, d, ldx = _rows(X, "X")
+    _vector(col_scale, "col_scale", torch.float32, (d,))
+    if out is None:
+        code_bytes, scale_bytes = mx4_row_bytes(d)
+        out = Mx4(_new(m, code_bytes, torch.uint8, X, stream), _new(m, scale_bytes, torch.uint8, X, stream), d)
+    elif _mx4(out, "out") != (m, d):
+        raise ValueError(f"out must be {m} rows of {d} columns")
+    dev = _one_device(X, col_scale, out[0], out[1])
+    _launch(dev, "qamw_mx4_quantize", X.data_ptr(), _dtype_code(X), m, d, ldx, _ptr(col_scale), out[0].data_ptr(), out[1].data_ptr(),
+            _raw_stream(stream, dev))
+    return out
+
+
+def mx4_dequantize(Q, out=None, out_dtype=None, stream=None):
+    """What the rows of an Mx4 stand for: [m][d] of out_dtype (bf16 where neither it nor out is given)."""
+    m, d = _mx4(Q, "Q")
+    dev = _one_device(Q[0], Q[1], out)
+    y, y_code, ldo = _result(out, m, d, out_dtype, Q[0], stream)
+    _launch(dev, "qamw_mx4_dequantize", Q[0].data_ptr(), Q[1].data_ptr(), m, d, y.data_ptr(), y_code, ldo, _raw_stream(stream, dev))
+    return y
+
+
+@functools.lru_cache(maxsize=256, typed=True)
+def mx4_matmul_workspace_bytes(x_dtype: int, x_rows: int, m: int, n_experts: int, d_out: int, d_in: int, gated: bool = False) -> int:
+    out = C.c_size_t()
+    _check(lib().qamw_mx4_matmul_workspace_bytes(x_dtype, x_rows, m, n_experts, d_out, d_in, int(gated), C.byref(out)),
+           "qamw_mx4_matmul_workspace_bytes")
+    return int(out.value)
+
+
+def _mx4_operand(X, d_in, col_scale):
+    """(address, type, address of the scales, rows, leading dimension, tensors) of the left operand, an Mx4 or floating."""
+    import torch
+
+    _vector(col_scale, "col_scale", torch.float32, (d_in,))
+    if isinstance(X, Mx4):
+        m, d = _mx4(X, "X")
+        at = (X[0].data_ptr(), DTYPE_MX4, X[1].data_ptr(), m, 0, X[0])
+    else:
+        m, d, ldx = _rows(X, "X")
+        at = (X.data_ptr(), _dtype_code(X), None, m, ldx, X)
+    if d != d_in:
+        raise ValueError(f"X and W must have as many columns, got {d} and {d_in}")
+    return at
+
+
+def _mx4_work(need, like, workspace, stream):
+    """(address, bytes, what is kept until the launches)"""
+    import torch
+
+    if workspace is not None:
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+    work = _new(1, need, torch.uint8, like, stream) if need else None
+    return _ptr(work), need, work
+
+
+def mx4_matmul(X, W, col_scale=None, gated=False, out=None, out_dtype=None, workspace=None, stream=None):
+    """Y = X W^T in 4-bit floating point: W an Mx4 of d_out rows; X an Mx4, or fp32 or bf16 [m][d_in], quantised by row in the call
+    (col_scale [d_in] multiplies its columns first).  gated: W has the gate's rows, then the up projection's, and Y = silu(gate) * up.
+    Returns [m][d_out] of out_dtype (bf16 where neither it nor out is given)."""
+    outs, d_in = _mx4(W, "W")
+    x_at, code, xs_at, m, ldx, x = _mx4_operand(X, d_in, col_scale)
+    if outs < 1 or (gated and outs % 2):
+        raise ValueError(f"W must have {'2 d_out' if gated else 'd_out'} rows, got {outs}")
+    dev = _one_device(x, X[1] if code == DTYPE_MX4 else None, W[0], W[1], col_scale, out, workspace)
+    d_out = outs // 2 if gated else outs
+    y, y_code, ldy = _result(out, m, d_out, out_dtype, x, stream)
+    at, size, _work = _mx4_work(mx4_matmul_workspace_bytes(code, m, m, 0, d_out, d_in, bool(gated)), x, workspace, stream)
+    _launch(dev, "qamw_mx4_matmul", x_at, code, xs_at, _ptr(col_scale), m, ldx, W[0].data_ptr(), W[1].data_ptr(), d_out, d_in, 1 if gated else 0,
+            y.data_ptr(), y_code, ldy, at, size, _raw_stream(stream, dev))
+    return y
+
+
+def mx4_grouped_matmul(X, W, offsets, rows=None, col_scale=None, gated=False, out=None, out_dtype=None, workspace=None, stream=None):
+    """The experts' products in 4-bit floating point: places offsets[e] .. offsets[e + 1] (int32 [n_experts + 1], on the device) are
+    expert e's, and Y[i] = X[rows[i]] W[e]^T (rows int32 [m]; without it Y[i] = X[i] W[e]^T).  W is an Mx4 of [n_experts][d_out] rows, X as
+    mx4_matmul takes it.  gated: W has [n_experts][2 d_out] rows and Y = silu(gate) * up.  Returns [m][d_out] of out_dtype (bf16
+    where neither it nor out is given); rows that no expert has are left as they are."""
+    import torch
+
+    n, outs, d_in = _mx4(W, "W", 3)
+    x_at, code, xs_at, x_rows, ldx, x = _mx4_operand(X, d_in, col_scale)
+    if n < 1 or outs < 1 or (gated and outs % 2):
+        raise ValueError(f"W must be [n_experts][{'2 d_out' if gated else 'd_out'}] rows, got {(n, outs)}")
+    m = x_rows if rows is None else rows.numel()
+    _vector(offsets, "offsets", torch.int32, (n + 1,))
+    _vector(rows, "rows", torch.int32, (m,))
+    dev = _one_device(x, X[1] if code == DTYPE_MX4 else None, W[0], W[1], col_scale, offsets, rows, out, workspace)
+    d_out = outs // 2 if gated else outs
+    y, y_code, ldy = _result(out, m, d_out, out_dtype, x, stream)
+    at, size, _work = _mx4_work(mx4_matmul_workspace_bytes(code, x_rows, m, n, d_out, d_in, bool(gated)), x, workspace, stream)
+    _launch(dev, "qamw_mx4_grouped_matmul", x_at, code, xs_at, _ptr(col_scale), x_rows, ldx, _ptr(rows), W[0].data_ptr(), W[1].data_ptr(),
+            offsets.data_ptr(), n, m, d_out, d_in, 1 if gated else 0, y.data_ptr(), y_code, ldy, at, size,
+            _raw_stream(stream, dev))
+    return y
+
+
+def block_norm(h, weight=None, block=None, block_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6, quantize=None, out=None, out_dtype=None,
+               h_out=None, stream=None):
+    """The norms around a block.  h is the stream (fp32 or bf16 [m][d]), block the block's output, which is normalised where block_weight
+    (fp32 [d]) is given, multiplied by gate ([d] or [m][d]) where that is, and added to the stream times scale; then the norm of
+    the stream, times weight (fp32 [d]), is what the next block takes.  Without block: the norm of h alone.  block, gate and h_out are of h's type.
+    Returns (the stream, its norm): a new stream, or h_out (which may be h), and the norm in out_dtype (h's type where neither it nor out
+    is given), for quantize = 'int8' as (codes, scales) of int8_quantize, for 'mx4' as an Mx4 (see qamw_block_norm in include/qamw.h)."""
+    import torch
+
+    m, d, ldh = _rows(h, "h")
+    code = _dtype_code(h)
+    _vector(weight, "weight", torch.float32, (d,))
+    _vector(block_weight, "block_weight", torch.float32, (d,))
+    ldb = ldg = ldho = 0
+    if block is None:
+        if block_weight is not None or gate is not None or h_out is not None:
+            raise ValueError("block_weight, gate and h_out come with a block")
+    else:
+        if block.dtype != h.dtype or block.shape != (m, d):
+            raise ValueError(f"block must be {h.dtype} of shape {(m, d)}, got {block.dtype} {tuple(block.shape)}")
+        ldb = _rows(block, "block")[2]
+        if gate is not None:
+            if gate.dtype != h.dtype or gate.shape not in ((d,), (m, d)):
+                raise ValueError(f"gate must be {h.dtype} of shape {(d,)} or {(m, d)}, got {gate.dtype} {tuple(gate.shape)}")
+            if gate.dim() == 1:
+                _vector(gate, "gate", h.dtype, (d,))
+            else:
+                ldg = _rows(gate, "gate")[2]
+        if h_out is None:
+            h_out, ldho = _new(m, d, h.dtype, h, stream), d
+        else:
+            if h_out.dtype != h.dtype or h_out.shape != (m, d):
+                raise ValueError(f"h_out must be {h.dtype} of shape {(m, d)}, got {h_out.dtype} {tuple(h_out.shape)}")
+            ldho = _rows(h_out, "h_out")[2]
+    scales, ldx = None, 0
+    if quantize is None:
+        x, x_code, ldx = _result(out, m, d, out_dtype or (h.dtype if out is None else None), h, stream)
+        result = x
+    elif out_dtype is not None:
+        raise ValueError("out_dtype is for a norm that is not quantised")
+    elif quantize == "int8":
+        x_code = DTYPE_I8
+        if out is None:
+            out = _new(m, d, torch.int8, h, stream), _empty((m,), torch.float32, h.device, stream)
+        x, scales = result = out
+        _vector(scales, "scales", torch.float32, (m,))
+        if x.dtype != torch.int8 or x.shape != (m, d):
+            raise ValueError("codes must be int8, of the shape of h")
+        ldx = _rows(x, "codes")[2]
+    elif quantize == "mx4":
+        x_code = DTYPE_MX4
+        if out is None:
+            code_bytes, scale_bytes = mx4_row_bytes(d)
+            out = Mx4(_new(m, code_bytes, torch.uint8, h, stream), _new(m, scale_bytes, torch.uint8, h, stream), d)
+        elif _mx4(out, "out") != (m, d):
+            raise ValueError(f"out must be {m} rows of {d} columns")
+        result, x, scales = out, out[0], out[1]
+    else:
+        raise ValueError(f"quantize is None, 'int8' or 'mx4', not {quantize!r}")
+    dev = _one_device(h, weight, block, block_weight, gate, h_out, x, scales)
+    _launch(dev, "qamw_block_norm", h.data_ptr(), code, m, d, ldh, _ptr(block), ldb, _ptr(block_weight), _ptr(gate), ldg, scale, _ptr(weight), eps,
+            _ptr(h_out), ldho, x.data_ptr(), x_code, ldx, _ptr(scales), _raw_stream(stream, dev))
+    return h if block is None else h_out, result

@@ -1,0 +1,224 @@
+"""Experts chosen by scores, a bias and groups: refusals (on the CPU), and choices and order, which have to be equal, against the
+definition in 64 bits, token by token."""
+import ctypes as C
+import math
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_26339_amd import qamw
+
+gpu = pytest.mark.gpu
+DEV = "cuda"
+INF = math.inf
+
+
+def say(*a):
+    print(*a, flush=True)
+    sys.stdout.flush()
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def test_refusals():
+    L, I, S = qamw.lib(), qamw.ERR_INVALID_ARG, qamw.ERR_SHAPE
+    p = 1 << 20
+
+    def route(x=p, t=0, m=4, n=8, ld=8, k=2, sc=0, bias=None, groups=2, top=1, each=2, re=1, scale=1.0, e=p, w=p, off=p, rows=p, pos=p, work=p, size=1 << 20):
+        return L.qamw_route_scored(x, t, m, n, ld, k, sc, bias, groups, top, each, re, scale, e, w, off, rows, pos, work, size, None)
+
+    assert route(t=2) == I and route(k=0) == I and route(k=9) == I and route(n=64, ld=64, k=33) == I and route(n=1025, ld=1025, groups=1) == I
+    assert route(sc=2) == I and route(sc=-1) == I and route(groups=0) == I and route(groups=65, n=130, ld=130) == I and route(top=0) == I and route(top=3) == I
+    assert route(each=0) == I and route(each=3) == I and route(bias=p + 2) == I and route(re=2) == I and route(n=9, ld=9) == S
+    assert route(x=None) == I and route(e=None) == I and route(w=None) == I and route(off=None) == I and route(rows=None) == I and route(pos=None) == I
+    assert route(m=100, work=None) == I and route(m=100, size=63) == I and route(m=100, work=p + 4) == I
+    assert route(ld=7) == S and route(m=-1) == I and route(off=p + 2) == I
+
+
+def test_refusals_of_the_binding(monkeypatch):
+    monkeypatch.setattr(qamw, "_one_device", lambda *t: 0)
+    x = torch.zeros(3, 8)
+    with pytest.raises(ValueError):
+        qamw.route_scored(x, 2, scores="tanh")
+    with pytest.raises(ValueError):
+        qamw.route_scored(x, 2, bias=torch.zeros(7))
+    with pytest.raises(ValueError):
+        qamw.route_scored(x, 2, bias=torch.zeros(8, dtype=torch.float64))
+    with pytest.raises(ValueError):
+        qamw.route_scored(x[0], 2)
+    with pytest.raises(qamw.QamwError):
+        qamw.route_scored(x, 9)
+
+
+def reference(logits, k, scores, bias, groups, top_groups, group_top, renormalise, scale):
+    """The definition: (experts [m][k], weights [m][k] in 64 bits)."""
+    m, n = logits.shape
+    x = logits.double().numpy()
+    x = np.where(np.isnan(x), -INF, x)
+    b = np.zeros(n) if bias is None else bias.double().numpy()
+    experts, weights = np.full((m, k), -1), np.zeros((m, k))
+    each = n // groups
+    for t in range(m):
+        row = x[t]
+        with np.errstate(all="ignore"):
+            if scores == "sigmoid":
+                s = 1 / (1 + np.exp(-row))
+            else:
+                top = row.max()
+                p = np.where(row > -INF, np.exp(np.where(row == top, 0, row - top)), 0)
+                s = p / p.sum() if top > -INF else p
+            c = np.where((row > -INF) & (b > -INF), s + b, -INF)
+        if groups > 1:
+            best = []
+            for g in range(groups):
+                own = sorted((v for v in c[g * each:(g + 1) * each] if v > -INF), reverse=True)[:group_top]
+                best.append(sum(own) if own else -INF)
+            stay = sorted((g for g in range(groups) if best[g] > -INF), key=lambda g: (-best[g], g))[:top_groups]
+            c = np.where(np.isin(np.arange(n) // each, stay), c, -INF)
+        chosen = sorted((e for e in range(n) if c[e] > -INF), key=lambda e: (-c[e], e))[:k]
+        total = math.fsum(s[e] for e in chosen) if renormalise else 1.0
+        experts[t, :len(chosen)] = chosen
+        weights[t, :len(chosen)] = [scale * s[e] / total if total > 0 else 0.0 for e in chosen]
+    return experts, weights
+
+
+def check(r, logits, k, n, want):
+    """Choices, weights (64-bit steps, then one rounding to fp32 and a scale that is given in fp32: within 2^-23), and the sorted order of the choices."""
+    experts, weights = want
+    m = logits.shape[0]
+    assert np.array_equal(r.experts.cpu().numpy(), experts)
+    got = r.weights.cpu().double().numpy()
+    assert (np.abs(got - weights) <= np.abs(weights) * 2.0**-23 + 1e-44).all()
+    flat = np.where(experts < 0, n, experts).reshape(-1)
+    order = np.argsort(flat, kind="stable")
+    offsets = np.searchsorted(flat[order], np.arange(n + 1))
+    used = offsets[n]
+    rows = np.where(np.arange(m * k) < used, order // k, -1)
+    positions = np.empty(m * k, np.int64)
+    positions[order] = np.arange(m * k)
+    assert np.array_equal(r.offsets.cpu().numpy(), offsets) and np.array_equal(r.rows.cpu().numpy(), rows)
+    assert np.array_equal(r.positions.cpu().numpy().reshape(-1), np.where(flat < n, positions, -1))
+
+
+CASES = [
+    # m, experts, k, groups, top groups, best of a group
+    (1, 1, 1, 1, 1, 2), (1, 8, 2, 2, 1, 2), (5, 64, 6, 8, 3, 2), (64, 64, 8, 8, 4, 1), (65, 256, 8, 8, 4, 2), (200, 256, 8, 16, 4, 2), (130, 160, 6, 8, 3, 1), (70, 12, 4, 4, 2, 2),
+    (33, 123, 5, 3, 2, 2), (9, 1024, 32, 64, 9, 2), (100, 512, 17, 32, 5, 2), (40, 384, 8, 1, 1, 2), (7, 90, 9, 45, 6, 2), (300, 16, 16, 1, 1, 1), (66, 4, 4, 4, 4, 2), (20, 1024, 9, 2, 1, 2),
+    (31, 640, 10, 64, 64, 2), (3, 64, 3, 64, 3, 2), (129, 255, 7, 5, 5, 1),
+]
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k,groups,top,each", CASES)
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_choices(m, n, k, groups, top, each, scores, dtype):
+    say(f"[scored] {m} tokens, {n} experts, {k}, {groups} groups {top} {each} {scores} {dtype}")
+    g = _gen(m + n + k + groups)
+    x = (2 * torch.randn(m, n, generator=g)).to(dtype)
+    for bias in (None, 0.2 * torch.randn(n, generator=g)):
+        for renormalise, scale in ((True, 2.5), (False, 1.0)):
+            want = reference(x, k, scores, bias, groups, top, each, renormalise, scale)
+            r = qamw.route_scored(x.to(DEV), k, scores=scores, bias=None if bias is None else bias.to(DEV), groups=groups, top_groups=top, group_top=each,
+                                  renormalise=renormalise, scale=scale)
+            check(r, x, k, n, want)
+
+
+@gpu
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("groups,top", [(1, 1), (4, 2), (16, 3)])
+def test_values_next_to_each_other(scores, groups, top):
+    """Logits and biases whose sums differ by less than 32 bits hold, in another order than the experts'; and equal ones, which go to the lowest."""
+    say(f"[scored] near ties {scores} {groups}")
+    n, m = 64, 80
+    g = _gen(4)
+    x = torch.full((m, n), 0.5)
+    step = torch.arange(n).double()
+    for t in range(m):
+        order = torch.randperm(n, generator=g)
+        if t % 2:
+            x[t] = torch.nextafter(x[t], torch.ones(n)) if t % 4 == 1 else x[t]
+            x[t, order[:n // 2]] = 0.5 + 2.0**-24
+        else:
+            x[t] = (0.5 + (step[order] - 20) * 2.0**-23).float()
+    bias = (torch.randperm(n, generator=g).double() * 2.0**-33 + 2.0**-12).float()
+    for b in (None, bias, bias * 0 + 0.25):
+        want = reference(x, 6, scores, b, groups, top, 2, True, 1.0)
+        check(qamw.route_scored(x.to(DEV), 6, scores=scores, bias=None if b is None else b.to(DEV), groups=groups, top_groups=top), x, 6, n, want)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("n,groups", [(32, 8), (32, 1), (200, 8), (12, 4)])
+def test_closed_experts_and_special_values(dtype, scores, n, groups):
+    say(f"[scored] closed experts {n} {groups} {scores} {dtype}")
+    g = _gen(n + groups)
+    x = torch.randn(70, n, generator=g)
+    each = n // groups
+    x[0] = -INF                                               # padding
+    x[1] = math.nan
+    x[2, 1:] = -INF                                           # one expert only
+    x[3, ::2] = math.nan
+    x[4] = 0                                                  # all alike
+    x[5, :each] = -INF                                        # a whole group closed
+    x[6, each - 1] = INF
+    x[7, [0, n - 1]] = INF
+    x[8] = -100.0
+    x[9] = 100.0
+    x[10] = -0.0
+    x[11, :] = -800.0                                         # below all sigmoids of 64 bits
+    x[12, 3:] = -INF
+    x[40:50] = -INF
+    x = x.to(dtype)
+    bias = 0.3 * torch.randn(n, generator=g)
+    closed = bias.clone()
+    closed[2], closed[n - 1], closed[0] = -INF, math.nan, INF
+    k, top = min(5, n), max(1, groups // 2)
+    for b in (None, bias, closed, -5 - bias.abs()):           # the last: values below zero
+        for each_top in (1, 2):
+            want = reference(x, k, scores, b, groups, top, each_top, True, 1.5)
+            r = qamw.route_scored(x.to(DEV), k, scores=scores, bias=None if b is None else b.to(DEV), groups=groups, top_groups=top, group_top=each_top, scale=1.5)
+            check(r, x, k, n, want)
+
+
+@gpu
+def test_strided_logits_other_streams_and_graphs():
+    say("[scored] strides, stream, graph")
+    g = _gen(6)
+    whole = torch.randn(300, 131, generator=g).to(DEV)
+    x = whole[:, 1:129]
+    kw = dict(scores="sigmoid", bias=(0.1 * torch.randn(128, generator=g)).to(DEV), groups=8, top_groups=3)
+    want = reference(x.cpu(), 6, "sigmoid", kw["bias"].cpu(), 8, 3, 2, True, 1.0)
+    check(qamw.route_scored(x, 6, **kw), x, 6, 128, want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    r = qamw.route_scored(x, 6, stream=side, **kw)
+    torch.cuda.synchronize()
+    check(r, x, 6, 128, want)
+    held = x.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r = qamw.route_scored(held, 6, **kw)
+    for i in range(3):
+        held.copy_(x.roll(i, 0))
+        graph.replay()
+        torch.cuda.synchronize()
+        check(r, x, 6, 128, (np.roll(want[0], i, 0), np.roll(want[1], i, 0)))
+        check(qamw.route_scored(x, 6, **kw), x, 6, 128, want)
+    assert qamw.route_scored(x[:0], 6, **kw).offsets.tolist() == [0] * 129
+
+
+@gpu
+def test_many_tokens_as_a_plain_sort():
+    """4000 tokens over 256 experts by torch in 64 bits."""
+    say("[scored] 4000 tokens")
+    g = _gen(2)
+    x, bias = torch.randn(4000, 256, generator=g), 0.1 * torch.randn(256, generator=g)
+    c = torch.sigmoid(x.double()) + bias.double()
+    r = qamw.route_scored(x.to(DEV), 8, bias=bias.to(DEV))
+    assert torch.equal(r.experts.cpu().long(), torch.sort(c, dim=1, descending=True, stable=True).indices[:, :8])
