@@ -1,4 +1,4 @@
-// Rows in 4-bit floating point with a scale for every 32 columns: their layout, their quantisation, their products.
+// Rows in 4-bit floating point with a scale for every 32 columns: their layout and their quantisation.
 #pragma once
 #include "qamw_product_tile.hpp"
 
@@ -38,21 +38,5 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
 __device__ __forceinline__ float mx4_power(uint32_t byte) {
     return __uint_as_float(byte == 255 ? 0x7FC00000u : byte ? byte << 23 : 0x00400000u);
 }
-
-// 16 rows of W times 16 rows of X over 128 columns: lane l holds block l / 16 of row l % 16 of both operands, and the block's scale in byte T of a
-// register; it gets W rows 4 (l / 16) .. + 4 of the column that is X row l % 16.
-typedef int mx4_i32x8_t __attribute__((ext_vector_type(8)));
-template <int T> __device__ __forceinline__ pr_f32x4_t mx4_mul(pr_i32x4_t w, pr_i32x4_t x, pr_f32x4_t c, int w_scale, int x_scale) {
-    const mx4_i32x8_t a = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1), b = __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, T, w_scale, T, x_scale);
-}
-
-// A product: ProductArgs with rows of codes (ldx, ldw, expert_stride in bytes), and the scales.
-struct Mx4Args {
-    ProductArgs p;
-    const uint8_t *xs, *ws;
-    int64_t lds;                         // bytes of a row of scales
-};
-inline Mx4Args mx4_args_of(const Mx4Product &q) { return {args_of(q.p), q.xs, q.ws, mx4_scale_bytes(q.p.d_in)}; }
 
 }  // namespace qamw

@@ -10,8 +10,7 @@ namespace {
 constexpr int MP_TILE = 64, MP_THREADS = 256;
 
 template <bool GATED, bool YBF16>
-__global__ __launch_bounds__(MP_THREADS) void k_mx4_product(Mx4Args q, int col_tiles) {
-    const ProductArgs &a = q.p;
+__global__ __launch_bounds__(MP_THREADS) void k_mx4_product(ProductArgs a, int col_tiles) {
     const int t = (int)(blockIdx.x / (uint32_t)col_tiles), ct = (int)(blockIdx.x % (uint32_t)col_tiles);
     const RowTile rt = find_tile<MP_TILE>(a, t);
     if (rt.n <= 0) return;
@@ -26,16 +25,16 @@ __global__ __launch_bounds__(MP_THREADS) void k_mx4_product(Mx4Args q, int col_t
         has_w[i] = o < a.d_out;
         const int64_t row = has_w[i] ? (GATED && i ? a.d_out + (int64_t)o : o) : 0;
         w[i] = a.W + rt.expert * a.expert_stride + row * a.ldw + block * 16;
-        ws[i] = q.ws + (rt.expert * (int64_t)a.d_out * (GATED ? 2 : 1) + row) * q.lds + block * 4;
+        ws[i] = a.w_blocks + (rt.expert * (int64_t)a.d_out * (GATED ? 2 : 1) + row) * a.block_bytes + block * 4;
         const int n = wm * 32 + i * 16 + fr;
         has_x[i] = n < rt.n;
         int64_t from = has_x[i] ? rt.row0 + n : 0;
         if (a.rows && has_x[i]) from = min(max(a.rows[from], 0), a.x_rows - 1);
         x[i] = a.X + from * a.ldx + block * 16;
-        xs[i] = q.xs + from * q.lds + block * 4;
+        xs[i] = a.x_blocks + from * a.block_bytes + block * 4;
     }
     pr_f32x4_t acc[2][2] = {};
-    const int blocks = (a.d_in + 31) / 32;
+    const int blocks = a.d_in / 16;
     auto some = [](bool has, const void *from) { return has ? *static_cast<const pr_i32x4_t *>(from) : pr_i32x4_t{0, 0, 0, 0}; };
     for (int b0 = 0; b0 < blocks; b0 += 16) {
         int sw[2], sx[2];
@@ -73,20 +72,18 @@ __global__ __launch_bounds__(MP_THREADS) void k_mx4_product(Mx4Args q, int col_t
 
 }  // namespace
 
-hipError_t launch_mx4_product(const Mx4Product &given) {
-    const Product &p = given.p;
-    if (p.m == 0) return hipSuccess;
-    const Mx4Args q = mx4_args_of(given);
+hipError_t launch_mx4_product(const Product &p) {
+    const ProductArgs a = args_of(p);
     const int outs = p.gated ? 32 : 64;
     const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, n = most_row_tiles(p, MP_TILE) * cols;
     if (n * MP_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
     const dim3 g((uint32_t)n);
     if (p.gated) {
-        if (p.y_bf16) k_mx4_product<true, true><<<g, MP_THREADS, 0, p.stream>>>(q, (int)cols);
-        else k_mx4_product<true, false><<<g, MP_THREADS, 0, p.stream>>>(q, (int)cols);
+        if (p.y_bf16) k_mx4_product<true, true><<<g, MP_THREADS, 0, p.stream>>>(a, (int)cols);
+        else k_mx4_product<true, false><<<g, MP_THREADS, 0, p.stream>>>(a, (int)cols);
     } else {
-        if (p.y_bf16) k_mx4_product<false, true><<<g, MP_THREADS, 0, p.stream>>>(q, (int)cols);
-        else k_mx4_product<false, false><<<g, MP_THREADS, 0, p.stream>>>(q, (int)cols);
+        if (p.y_bf16) k_mx4_product<false, true><<<g, MP_THREADS, 0, p.stream>>>(a, (int)cols);
+        else k_mx4_product<false, false><<<g, MP_THREADS, 0, p.stream>>>(a, (int)cols);
     }
     return hipGetLastError();
 }

@@ -17,7 +17,7 @@ constexpr int PA_TILE = 64, PA_THREADS = 256, PA_K = 128, PA_PITCH = PA_K + 16; 
 
 template <bool I8, bool GATED, bool YBF16>
 __global__ __launch_bounds__(PA_THREADS) void k_product_any(ProductArgs a, int col_tiles) {
-    using M = Mfma<I8>;
+    using M = Mfma<I8 ? PRODUCT_I8 : PRODUCT_BF16>;
     using Piece = Unaligned<typename M::elem_t, 16 / M::ELEM>;
     __shared__ __align__(16) char lds[2][2][PA_TILE * PA_PITCH];
     const int t = (int)(blockIdx.x / (uint32_t)col_tiles), ct = (int)(blockIdx.x % (uint32_t)col_tiles);
@@ -158,8 +158,8 @@ constexpr Cost FEW[3] = {{16, 0.4, 9.4e4}, {32, 0.4, 9.9e4}, {64, 0.4, 8.0e4}}, 
 constexpr double FEW_GATED_64 = 0.75;                      // of the rate: the ring is two units then
 
 // groups: how many have rows, at most; row tiles are expected to be half a tile short.
-Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, bool gated, bool i8, bool may_part) {
-    const int64_t outs = d_out * (gated ? 2 : 1), bytes = d_in * (i8 ? 1 : 2), units = (bytes + 127) / 128;
+Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, bool gated, int kind, bool may_part) {
+    const int64_t outs = d_out * (gated ? 2 : 1), bytes = d_in * (kind == PRODUCT_BF16 ? 2 : 1), units = (bytes + 127) / 128;
     const double each = (double)m / groups, w_bytes = (double)groups * outs * bytes, x_bytes = (double)m * bytes;
     auto time = [&](double work, double memory, const Off &off) {
         if (bytes % 128) {
@@ -198,31 +198,35 @@ Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, 
         }
     return best;
 }
-Plan plan_of(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, bool i8, bool may_part) {
+Plan plan_of(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, int kind, bool may_part) {
     if (const int rows = product_tile_rows()) return {false, rows, 1, 0.0};
-    return plan(m, !grouped ? 1 : m < n_experts ? m : n_experts, grouped, d_out, d_in, gated, i8, may_part);
+    return plan(m, !grouped ? 1 : m < n_experts ? m : n_experts, grouped, d_out, d_in, gated, kind, may_part);
 }
 
 }  // namespace
 
-void product_plan(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, bool i8, bool may_part, int (&out)[3]) {
-    const Plan c = plan_of(m, n_experts, grouped, d_out, d_in, gated, i8, may_part);
+void product_plan(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, int kind, bool may_part, int (&out)[3]) {
+    const Plan c = plan_of(m, n_experts, grouped, d_out, d_in, gated, kind, may_part);
     out[0] = c.few ? 0 : 1;
     out[1] = c.tile_rows;
     out[2] = c.parts;
 }
 
 // The sums of all parts, whatever qamw_set_kernel_path() says: a workspace of this size serves the call before and after.
-size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated) {
+size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated, int kind) {
     if (m == 0) return 0;
-    const int parts = plan(m, 1, false, d_out, d_in, gated, true, true).parts;
+    const int parts = plan(m, 1, false, d_out, d_in, gated, kind, true).parts;
     return parts == 1 ? 0 : (size_t)parts * m * (size_t)parts_row(d_out, gated) * 4;
 }
 
 hipError_t launch_product(const Product &p) {
     if (p.m == 0) return hipSuccess;
-    if (!product_wide_supported(p)) return p.i8 ? launch_any<true>(p) : launch_any<false>(p);
-    const Plan c = plan_of(p.m, p.n_experts, p.offsets != nullptr, p.d_out, p.d_in, p.gated, p.i8, p.scratch != nullptr);
+    if (!product_wide_supported(p)) {
+        if (p.kind == PRODUCT_MX4) return hipErrorNotSupported;            // codes beyond 2 GiB: their rows are whole 16 bytes always
+        return p.kind == PRODUCT_I8 ? launch_any<true>(p) : launch_any<false>(p);
+    }
+    const Plan c = plan_of(p.m, p.n_experts, p.offsets != nullptr, p.d_out, p.d_in, p.gated, p.kind, p.scratch != nullptr);
+    if (c.few && p.kind == PRODUCT_MX4) return launch_mx4_product(p);
     return c.few ? launch_product_few(p, c.tile_rows) : launch_product_wide(p, c.tile_rows, c.parts);
 }
 

@@ -9,9 +9,12 @@
 
 namespace qamw {
 
+// What the operands are.  Rows in 4 bits are rows of bytes: their d_in and leading dimensions are those of their codes.
+enum { PRODUCT_BF16 = 0, PRODUCT_I8 = 1, PRODUCT_MX4 = 2 };
+
 // One call.  Without offsets: one group of m rows.  With offsets: rows offsets[e] .. offsets[e + 1] belong to expert e.
 struct Product {
-    const void *X = nullptr;             // int8 codes or bf16
+    const void *X = nullptr;             // int8 codes, bf16 or codes of 4 bits
     const float *x_scales = nullptr;     // int8: one for each row of X
     const int32_t *rows = nullptr;       // row of X for each row of the product, nullable
     const void *W = nullptr;             // gated: the gate's d_out rows, then the up projection's
@@ -20,7 +23,11 @@ struct Product {
     void *Y = nullptr;
     int64_t ldx = 0, ldw = 0, expert_stride = 0, ldy = 0;
     int m = 0, x_rows = 0, n_experts = 1, d_out = 0, d_in = 0;
-    bool i8 = false, gated = false, y_bf16 = false;
+    int kind = PRODUCT_BF16;
+    bool gated = false, y_bf16 = false;
+    const uint8_t *x_blocks = nullptr, *w_blocks = nullptr;   // 4 bits: the scales of blocks, as the rows of X and W
+    int block_bytes = 0;                 // of a row
+    int64_t elem() const { return kind == PRODUCT_BF16 ? 2 : 1; }
     void *scratch = nullptr;             // product_scratch_bytes(), nullable: the product is not parted then
     hipStream_t stream = nullptr;
 };
@@ -28,8 +35,8 @@ struct Product {
 hipError_t launch_product(const Product &p);
 int product_tile_rows();                                                // set by qamw_set_kernel_path(): products of many rows by such tiles; 0: as estimated
 // What launch_product() would take for operands that product_wide_supported(); may_part: with scratch.
-void product_plan(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, bool i8, bool may_part, int (&out)[3]);
-size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated);   // of an int8 product of one group
+void product_plan(int m, int n_experts, bool grouped, int d_out, int d_in, bool gated, int kind, bool may_part, int (&out)[3]);
+size_t product_scratch_bytes(int m, int d_out, int d_in, bool gated, int kind);   // of an int8 product of one group, or one in 4 bits
 // Row of the sums of a part of the columns, in 32-bit words: whole 16 bytes; where the up projection's follow the gate's, four of them
 // are read together from anywhere.
 inline int64_t parts_row(int64_t d_out, bool gated) { return (d_out * (gated ? 2 : 1) + 3 + (gated ? 3 : 0)) / 4 * 4; }
@@ -49,6 +56,7 @@ struct MoreLds {
 };
 // The kernels by what they are for.  wide and few: products that product_wide_supported(), tile_rows of 16 / 32 / 64 and 64 / 128 / 256.
 bool product_wide_supported(const Product &p);
+hipError_t launch_mx4_product(const Product &p);
 hipError_t launch_product_wide(const Product &p, int tile_rows, int parts);
 hipError_t launch_product_few(const Product &p, int tile_rows);
 // Waves that share a tile of outputs: enough for all of memory's bandwidth, about 8 on every CU, while a share has four units.
@@ -70,13 +78,6 @@ inline __host__ __device__ int64_t mx4_scale_bytes(int64_t d) { return (d + 511)
 hipError_t launch_mx4_quantize(const void *X, int dtype, int64_t m, int d, int64_t ldx, const float *col_scale, uint8_t *codes, uint8_t *scales,
                                hipStream_t stream);
 hipError_t launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t m, int d, void *out, int out_dtype, int64_t ldo, hipStream_t stream);
-// A Product of rows in 4 bits: i8 is set, and ldx, ldw and expert_stride are the codes' bytes.
-struct Mx4Product {
-    Product p;
-    const uint8_t *xs = nullptr, *ws = nullptr;   // the scales, as the rows of X and W
-};
-hipError_t launch_mx4_product(const Mx4Product &p);
-
 // Norms around a block.  Null: without block, block_weight, gate, weight.
 struct BlockNorm {
     const void *h = nullptr, *block = nullptr, *gate = nullptr;

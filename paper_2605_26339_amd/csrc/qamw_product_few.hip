@@ -76,7 +76,7 @@ template <int N> __device__ __forceinline__ void read_unit(uint32_t at, pr_i32x4
 
 template <bool I8, bool GATED, bool YBF16, bool ONCE, typename S>
 __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
-    using M = Mfma<I8>;
+    using M = Mfma<I8 ? PRODUCT_I8 : PRODUCT_BF16>;
     const ProductArgs &a = q.p;
     extern __shared__ __align__(16) char pf_lds[];
     const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
@@ -319,7 +319,7 @@ template <bool I8> hipError_t launch_type(const Product &p, int tile_rows) {
 
 }  // namespace
 
-hipError_t launch_product_few(const Product &p, int tile_rows) { return p.i8 ? launch_type<true>(p, tile_rows) : launch_type<false>(p, tile_rows); }
+hipError_t launch_product_few(const Product &p, int tile_rows) { return p.kind == PRODUCT_I8 ? launch_type<true>(p, tile_rows) : launch_type<false>(p, tile_rows); }
 
 // As many values as the threads of a workgroup hold, and rows that are read in whole 16 bytes, with offsets that 31 bits hold.
 constexpr int PF_MOST_EIGHTS = 4, PF_SPAN = 8 * 8 * WAVE;

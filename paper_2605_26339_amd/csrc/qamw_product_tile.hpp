@@ -10,8 +10,8 @@ typedef __bf16 pr_bf16x8_t __attribute__((ext_vector_type(8)));
 
 // 16 rows of W times 16 rows of X over 64 bytes of each: lane l holds bytes 16 (l / 16) .. + 16 of row l % 16 of both operands,
 // and gets W rows 4 (l / 16) .. + 4 of the column that is X row l % 16.  int8 and bf16 lay their bytes out alike.
-template <bool I8> struct Mfma;
-template <> struct Mfma<true> {
+template <int KIND> struct Mfma;
+template <> struct Mfma<PRODUCT_I8> {
     using acc_t = pr_i32x4_t;
     using elem_t = int8_t;
     static constexpr int ELEM = 1;
@@ -19,7 +19,7 @@ template <> struct Mfma<true> {
         return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, c, 0, 0, 0);
     }
 };
-template <> struct Mfma<false> {
+template <> struct Mfma<PRODUCT_BF16> {
     using acc_t = pr_f32x4_t;
     using elem_t = uint16_t;
     static constexpr int ELEM = 2;
@@ -27,6 +27,16 @@ template <> struct Mfma<false> {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(pr_bf16x8_t, w), __builtin_bit_cast(pr_bf16x8_t, x), c, 0, 0, 0);
     }
 };
+// In 4 bits the 64 bytes are 128 columns, a lane's 16 bytes a block of 32, whose scales are in byte T of a register.
+template <> struct Mfma<PRODUCT_MX4> {
+    using acc_t = pr_f32x4_t;
+    static constexpr int ELEM = 1;
+};
+typedef int pr_i32x8_t __attribute__((ext_vector_type(8)));
+template <int T> __device__ __forceinline__ pr_f32x4_t mx4_mul(pr_i32x4_t w, pr_i32x4_t x, pr_f32x4_t c, int w_scale, int x_scale) {
+    const pr_i32x8_t a = __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1), b = __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, T, w_scale, T, x_scale);   // 4: e2m1
+}
 
 // The device side of a Product.
 struct ProductArgs {
@@ -37,12 +47,15 @@ struct ProductArgs {
     int64_t ldx, ldw, expert_stride;     // in bytes
     int64_t ldy;                         // in elements
     int m, x_rows, n_experts, d_out, d_in;
+    int block_bytes;                     // 4 bits: the scales of blocks
+    const uint8_t *x_blocks, *w_blocks;
 };
 
 inline ProductArgs args_of(const Product &p) {
-    const int64_t e = p.i8 ? 1 : 2;
+    const int64_t e = p.elem();
     return {static_cast<const char *>(p.X), static_cast<const char *>(p.W), p.x_scales, p.w_scales, p.rows, p.offsets, p.Y,
-            p.ldx * e, p.ldw * e, p.expert_stride * e, p.ldy, p.m, p.x_rows, p.n_experts, p.d_out, p.d_in};
+            p.ldx * e, p.ldw * e, p.expert_stride * e, p.ldy, p.m, p.x_rows, p.n_experts, p.d_out, p.d_in,
+            p.block_bytes, p.x_blocks, p.w_blocks};
 }
 
 // Rows row0 .. row0 + n of the product, which are expert `expert`'s; n = 0: nothing to do.

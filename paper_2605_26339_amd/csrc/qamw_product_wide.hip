@@ -169,14 +169,15 @@ template <typename S> struct Tile {
     int part, full;                                  // the part of the columns, its stages
     const char *w, *x;
     uint32_t off_w[2][S::LW], off_x[S::LX], off_scale;
+    const uint8_t *ws, *xs;                          // 4 bits: the scales of its rows
 };
 
 // OUT: what is stored: 0 fp32, 1 bf16, 2 the sums of a part of the columns as they are (int32 or fp32), one array of `part_stride`
 // elements a part.
-template <bool I8, bool GATED, int OUT, typename S>
+template <int KIND, bool GATED, int OUT, typename S>
 __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, int most_tiles, int col_tiles, int group, int whole, int parts, int64_t part_stride) {
-    constexpr bool YBF16 = OUT == 1, SCALED = I8 && OUT != 2;
-    using M = Mfma<I8>;
+    constexpr bool YBF16 = OUT == 1, MX4 = KIND == PRODUCT_MX4, SCALED = KIND == PRODUCT_I8 && OUT != 2;
+    using M = Mfma<KIND>;
     extern __shared__ __align__(16) char pw_lds[];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)pw_lds;
@@ -203,6 +204,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         z.w = z.x = nullptr;
         z.expert = z.row0 = z.ct = z.part = z.full = 0;
         z.off_scale = PW_NOWHERE;
+        z.ws = z.xs = nullptr;
         for (int i = 0; i < S::LW; ++i) z.off_w[0][i] = z.off_w[1][i] = PW_NOWHERE;
         for (int i = 0; i < S::LX; ++i) z.off_x[i] = PW_NOWHERE;
         if (t >= end) return z;
@@ -217,8 +219,9 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         z.ct = in / rows_in;
         z.row0 = et.start + (g0 + in % rows_in) * S::BM;
         z.n = min(S::BM, et.end - z.row0);
-        const int s0 = (int)((int64_t)every * z.part / parts);
-        z.full = (int)((int64_t)every * (z.part + 1) / parts) - s0;
+        const int unit = MX4 ? 2 : 1, units = (every + unit - 1) / unit;       // in 4 bits two stages share the scales' dwords
+        const int s0 = (int)((int64_t)units * z.part / parts) * unit;
+        z.full = min((int)((int64_t)units * (z.part + 1) / parts) * unit, every) - s0;
         z.w = a.W + (int64_t)et.expert * a.expert_stride + s0 * PW_KB;
         z.x = (a.rows ? a.X : a.X + (int64_t)z.row0 * a.ldx) + s0 * PW_KB;
 #pragma unroll
@@ -234,6 +237,16 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
             int row = is ? r : 0;
             if (a.rows && is) row = min(max(a.rows[z.row0 + r], 0), a.x_rows - 1);
             z.off_x[i] = is ? (uint32_t)((int64_t)row * a.ldx) + piece : PW_NOWHERE;
+        }
+        if constexpr (MX4) {                                                  // 16 bytes of scales a thread: 256 rows of W, 256 of X
+            const int r = threadIdx.x % 256;
+            z.ws = a.w_blocks + (int64_t)z.expert * a.d_out * (GATED ? 2 : 1) * a.block_bytes + s0 * 8;
+            z.xs = a.x_blocks + (a.rows ? 0 : (int64_t)z.row0 * a.block_bytes) + s0 * 8;
+            if (threadIdx.x >= 256) {
+                if (r < z.n) z.off_scale = (uint32_t)((a.rows ? min(max(a.rows[z.row0 + r], 0), a.x_rows - 1) : r) * (int64_t)a.block_bytes);
+            } else if (out_of(z.ct, r >> 4, r & 15) < a.d_out) {
+                z.off_scale = (uint32_t)(w_row(z.ct, r >> 4, r & 15) * a.block_bytes);
+            }
         }
         if (SCALED) {                                                         // one scale a thread: 256 of rows, 256 of outputs
             const int r = threadIdx.x % 256;
@@ -251,6 +264,13 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         if (!SCALED) return;
         const float *from = wave < PW_WAVES / 2 ? a.x_scales + (a.rows ? 0 : z.row0) : a.w_scales + (int64_t)z.expert * a.d_out * (GATED ? 2 : 1);
         request_dword(z.off_scale, resource(from), scales0 + slot + wave * 256);
+    };
+
+    // In 4 bits: those of two stages, 16 bytes a row, to one of two slots.  A pair's are asked for when the pair before it is begun: then both
+    // groups have read what was in the slot, two stages before.
+    auto request_blocks = [&](const Tile<S> &z, int pair, uint32_t to) {
+        const uint8_t *from = wave < PW_WAVES / 2 ? z.ws : z.xs;
+        request(pair * 2 < z.full ? z.off_scale : PW_NOWHERE, resource(from), (uint32_t)pair * 16, scales0 + to + wave * 1024);
     };
 
     const int wn = wave % S::WN, wm = wave / S::WN;
@@ -272,6 +292,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         for (int i = 0; i < (int)(sizeof(to) / sizeof(to[0])); ++i) to[i] = from[i] | gone;
     };
     request_scales(now, 0);
+    if constexpr (MX4) request_blocks(now, 0, 0);
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const uint32_t gone = nothing(now, s), to = lds0 + s * S::STAGE + wave * 1024;
@@ -289,7 +310,16 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 
     typename M::acc_t acc[S::FN][S::FM];
     pr_i32x4_t fw[2][S::HN], fx[2][S::FM];                                    // [halves of a row]
-    auto multiply = [&](auto second, bool busy) {
+    int bw[MX4 ? S::FN : 1], bx[MX4 ? S::FM : 1];                             // 4 bits: the scales of both stages' halves, a byte each
+    uint32_t pair_slot = 0;
+    auto read_blocks = [&] {
+        const uint32_t from = scales0 + pair_slot + (lane & 15) * 16 + (lane >> 4) * 4;
+#pragma unroll
+        for (int i = 0; i < S::FN; ++i) bw[i] = lds_read<int>(from + (wn * S::FN + i) * 256);
+#pragma unroll
+        for (int j = 0; j < S::FM; ++j) bx[j] = lds_read<int>(from + 4096 + (wm * S::FM + j) * 256);
+    };
+    auto multiply = [&](auto second, auto odd, bool busy) {
         constexpr int I0 = decltype(second)::value * S::HN;
         __builtin_amdgcn_s_setprio(1);
         if (busy)
@@ -300,7 +330,12 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 #pragma unroll
                     for (int n = 0; n < S::HN; ++n) {
                         const int i = j & 1 ? S::HN - 1 - n : n;              // to and fro: one operand changes at a time, 1 % less time for random ones
-                        acc[I0 + i][j] = M::mul(fw[h][i], fx[h][j], acc[I0 + i][j]);
+                        if constexpr (MX4) {
+                            if (h == 0) acc[I0 + i][j] = mx4_mul<decltype(odd)::value * 2>(fw[h][i], fx[h][j], acc[I0 + i][j], bw[I0 + i], bx[j]);
+                            else acc[I0 + i][j] = mx4_mul<decltype(odd)::value * 2 + 1>(fw[h][i], fx[h][j], acc[I0 + i][j], bw[I0 + i], bx[j]);
+                        } else {
+                            acc[I0 + i][j] = M::mul(fw[h][i], fx[h][j], acc[I0 + i][j]);
+                        }
                     }
         __builtin_amdgcn_s_setprio(0);
     };
@@ -308,18 +343,25 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     // second half of W; X and the first half of W of stage s2 of tile z2, the one after, are asked for.  Either goes over what
     // both groups have read a step before, and is waited for a stage later.  `stored`: the stores of the tile before may still be on
     // their way, between the loads that are waited for and the newer ones.
-    auto stage = [&](const Tile<S> &z1, int s1, const Tile<S> &z2, int s2, bool stored, bool busy) {
+    // In 4 bits the even one of two stages reads the scales of both, and asks for those of stages s2 and s2 + 1 of tile z2.
+    auto stage = [&](auto odd, const Tile<S> &z1, int s1, const Tile<S> &z2, int s2, bool stored, bool busy) {
+        constexpr bool FIRST = MX4 && decltype(odd)::value == 0;
         const uint32_t other = S::STAGE - at;
         auto wait = [&] {
-            if (stored) wait_loads<L + STORES>();
-            else wait_loads<L>();
+            if (stored) wait_loads<L + FIRST + STORES>();
+            else wait_loads<L + FIRST>();
         };
         uint32_t ow[S::LW], ox[S::LX];
+        if constexpr (FIRST) {
+            read_blocks();
+            pair_slot ^= 8192;
+            request_blocks(z2, s2 / 2, pair_slot);
+        }
         offsets(ow, z1.off_w[1], nothing(z1, s1));
         read_first<S::HN, S::FM, S::LW>(read_w + at, read_x + at, fw, fx, ow, resource(z1.w), (uint32_t)s1 * PW_KB, lds0 + other + S::SECOND + wave * 1024);
         wait();                                                               // the second half of this stage's W is there
         meet();
-        multiply(First{}, busy);
+        multiply(First{}, odd, busy);
         meet();
         const uint32_t gone = nothing(z2, s2);
         offsets(ow, z2.off_w[0], gone);
@@ -328,7 +370,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
                                          lds0 + at + wave * 1024, lds0 + at + S::X + wave * 1024);
         wait();                                                               // the rest of the next stage is there
         meet();
-        multiply(Second{}, busy);
+        multiply(Second{}, odd, busy);
         meet();
         at = other;
     };
@@ -340,15 +382,21 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 #pragma unroll
             for (int j = 0; j < S::FM; ++j) acc[i][j] = typename M::acc_t{};
         const bool busy = wm * S::FM * 16 < now.n && out_of(now.ct, wn * S::FN, 0) < a.d_out;   // some of the wave's rows and outputs are there
-        const int stages = max(now.full, 2);
-        for (int s = 0; s < stages - 2; ++s) stage(now, s + 1, now, s + 2, stored && s == 0, busy);
+        const int stages = MX4 ? (now.full + 1) / 2 * 2 : max(now.full, 2);
+        if constexpr (MX4)
+            for (int s = 0; s < stages - 2; s += 2) {
+                stage(First{}, now, s + 1, now, s + 2, stored && s == 0, busy);
+                stage(Second{}, now, s + 2, now, s + 3, false, busy);
+            }
+        else
+            for (int s = 0; s < stages - 2; ++s) stage(First{}, now, s + 1, now, s + 2, stored && s == 0, busy);
         // the last two stages ask for the first ones of the next tile
         t += step;
         const Tile<S> next = tile_at(t);
         const uint32_t slot_next = slot == (PW_SLOTS - 1) * 2048 ? 0 : slot + 2048;
         request_scales(next, slot_next);
-        stage(now, stages - 1, next, 0, stored && stages == 2, busy);
-        stage(next, 0, next, 1, false, busy);
+        stage(First{}, now, stages - 1, next, 0, stored && stages == 2, busy);
+        stage(Second{}, next, 0, next, 1, false, busy);
 
         const int q0 = (lane >> 4) * 4;
         // four outputs of fragment i (gated: and i + 1) in row j * 16 + lane % 16
@@ -431,18 +479,26 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 //   Parts pay where the tiles of whole columns leave CUs without one: 300 rows by 5120 x 13824 take 40.0 us in 4 parts of tiles of 128
 // rows, sums included, and 88 in one.  int8 only: its sums are whole numbers, and in any order the same.
 constexpr int PS_THREADS = 256;
-template <bool GATED, bool YBF16, int PARTS>
+template <bool MX4, bool GATED, bool YBF16, int PARTS>
 __global__ __launch_bounds__(PS_THREADS) void k_product_parts(ProductArgs a, const char *sums, int64_t part_stride, int64_t ld, int fours) {
     const uint32_t id = blockIdx.x * PS_THREADS + threadIdx.x;
     const int64_t row = id / (uint32_t)fours;
     const int o = (int)(id % (uint32_t)fours) * 4;
     if (row >= a.m) return;
     const char *at = sums + (row * ld + o) * 4, *up = at + (int64_t)a.d_out * 4;
-    pr_i32x4_t g = {0, 0, 0, 0}, u = {0, 0, 0, 0};
+    using Sums = typename Mfma<MX4 ? PRODUCT_MX4 : PRODUCT_I8>::acc_t;
+    Sums g = {0, 0, 0, 0}, u = {0, 0, 0, 0};
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-        g += *reinterpret_cast<const pr_i32x4_t *>(at + p * part_stride * 4);
-        if (GATED) u += __builtin_bit_cast(pr_i32x4_t, *reinterpret_cast<const Unaligned<int, 4> *>(up + p * part_stride * 4));
+        g += *reinterpret_cast<const Sums *>(at + p * part_stride * 4);
+        if (GATED) u += __builtin_bit_cast(Sums, *reinterpret_cast<const Unaligned<int, 4> *>(up + p * part_stride * 4));
+    }
+    if constexpr (MX4) {
+        float y[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) y[q] = GATED ? silu(g[q]) * u[q] : g[q];
+        store_y4<YBF16>(a.Y, row * a.ldy + o, y, a.d_out - o);
+        return;
     }
     const float xs = a.x_scales[row];
     float y[4];
@@ -455,7 +511,7 @@ __global__ __launch_bounds__(PS_THREADS) void k_product_parts(ProductArgs a, con
     store_y4<YBF16>(a.Y, row * a.ldy + o, y, a.d_out - o);
 }
 
-template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Product &p, int parts, int64_t part_stride) {
+template <int KIND, bool GATED, int OUT, typename S> hipError_t launch(const Product &p, int parts, int64_t part_stride) {
     const int outs = GATED ? S::BN / 2 : S::BN;
     const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, rows = most_row_tiles(p, S::BM), tiles = rows * cols * parts;
     if (tiles > 0x7FFFFFFF / 2) return hipErrorNotSupported;
@@ -463,8 +519,8 @@ template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Prod
     const int64_t y_bytes = OUT == 1 ? 2 : 4;
     const bool whole = (reinterpret_cast<uintptr_t>(p.Y) & 15) == 0 && p.ldy * y_bytes % 16 == 0 && (p.d_out * y_bytes % 16 == 0 || OUT == 2) &&
                        p.ldy <= 0x7FFFFFFF / (S::BM * y_bytes);
-    const auto kernel = &k_product_wide<I8, GATED, OUT, S>;
-    constexpr int lds = 2 * S::STAGE + PW_WAVES * PW_TURN + PW_SLOTS * 2048;
+    const auto kernel = &k_product_wide<KIND, GATED, OUT, S>;
+    constexpr int lds = 2 * S::STAGE + PW_WAVES * PW_TURN + (KIND == PRODUCT_MX4 ? 2 * 8192 : PW_SLOTS * 2048);
     static MoreLds more;
     const hipError_t e = more.ask(reinterpret_cast<const void *>(kernel), lds);
     if (e != hipSuccess) return e;
@@ -472,23 +528,27 @@ template <bool I8, bool GATED, int OUT, typename S> hipError_t launch(const Prod
     return hipGetLastError();
 }
 
-template <bool I8, typename S> hipError_t launch_shape(const Product &p) {
-    if (p.gated) return p.y_bf16 ? launch<I8, true, 1, S>(p, 1, 0) : launch<I8, true, 0, S>(p, 1, 0);
-    return p.y_bf16 ? launch<I8, false, 1, S>(p, 1, 0) : launch<I8, false, 0, S>(p, 1, 0);
+template <int KIND, typename S> hipError_t launch_shape(const Product &p) {
+    if (p.gated) return p.y_bf16 ? launch<KIND, true, 1, S>(p, 1, 0) : launch<KIND, true, 0, S>(p, 1, 0);
+    return p.y_bf16 ? launch<KIND, false, 1, S>(p, 1, 0) : launch<KIND, false, 0, S>(p, 1, 0);
 }
 
-template <int PARTS> void launch_sums(const Product &p, int64_t stride, int64_t ld) {
+template <bool MX4, int PARTS> void launch_sums(const Product &p, int64_t stride, int64_t ld) {
     const int64_t fours = ((int64_t)p.d_out + 3) / 4;
     const dim3 g((uint32_t)((fours * p.m + PS_THREADS - 1) / PS_THREADS));
     const ProductArgs a = args_of(p);
     const char *sums = static_cast<const char *>(p.scratch);
     if (p.gated) {
-        if (p.y_bf16) k_product_parts<true, true, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
-        else k_product_parts<true, false, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
+        if (p.y_bf16) k_product_parts<MX4, true, true, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
+        else k_product_parts<MX4, true, false, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
     } else {
-        if (p.y_bf16) k_product_parts<false, true, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
-        else k_product_parts<false, false, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
+        if (p.y_bf16) k_product_parts<MX4, false, true, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
+        else k_product_parts<MX4, false, false, PARTS><<<g, PS_THREADS, 0, p.stream>>>(a, sums, stride, ld, (int)fours);
     }
+}
+template <int PARTS> void launch_sums(const Product &p, int64_t stride, int64_t ld) {
+    if (p.kind == PRODUCT_MX4) launch_sums<true, PARTS>(p, stride, ld);
+    else launch_sums<false, PARTS>(p, stride, ld);
 }
 
 // In `parts` parts of the columns (2, 3, 4, 6 or 8), whose sums lie in p.scratch.
@@ -500,7 +560,7 @@ template <typename S> hipError_t launch_parts(const Product &p, int parts) {
     q.ldy = parts_row(p.d_out, p.gated);
     const int64_t stride = q.ldy * p.m;
     if (((int64_t)p.d_out + 3) / 4 * p.m + PS_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
-    const hipError_t e = launch<true, false, 2, S>(q, parts, stride);
+    const hipError_t e = p.kind == PRODUCT_MX4 ? launch<PRODUCT_MX4, false, 2, S>(q, parts, stride) : launch<PRODUCT_I8, false, 2, S>(q, parts, stride);
     if (e != hipSuccess) return e;
     switch (parts) {
     case 2: launch_sums<2>(p, stride, q.ldy); break;
@@ -519,7 +579,8 @@ using Shape64 = Shape<8, 2, 1, 4>;
 
 template <typename S> hipError_t launch_either(const Product &p, int parts) {
     if (parts > 1) return launch_parts<S>(p, parts);
-    return p.i8 ? launch_shape<true, S>(p) : launch_shape<false, S>(p);
+    if (p.kind == PRODUCT_MX4) return launch_shape<PRODUCT_MX4, S>(p);
+    return p.kind == PRODUCT_I8 ? launch_shape<PRODUCT_I8, S>(p) : launch_shape<PRODUCT_BF16, S>(p);
 }
 
 }  // namespace
@@ -527,7 +588,7 @@ template <typename S> hipError_t launch_either(const Product &p, int parts) {
 // Whole 16 bytes everywhere, and offsets from a tile's or an expert's first row that 31 bits hold (with what a stage goes past a row); rows that
 // are gathered come from anywhere, so that all of X has to lie within.
 bool product_wide_supported(const Product &p) {
-    const int64_t e = p.i8 ? 1 : 2, most = 0x7FFFFFFF - 2 * PW_KB;
+    const int64_t e = p.elem(), most = 0x7FFFFFFF - 2 * PW_KB;
     auto whole = [](int64_t v) { return v % 16 == 0; };
     if (!whole(p.d_in * e) || !whole(p.ldx * e) || !whole(p.ldw * e) || !whole(p.expert_stride * e) || (reinterpret_cast<uintptr_t>(p.X) & 15) ||
         (reinterpret_cast<uintptr_t>(p.W) & 15))

@@ -35,7 +35,7 @@ int qamw_int8_matmul_workspace_bytes(int x_dtype, int m, int d_out, int d_in, in
         d_out > QAMW_PRODUCT_MAX_D_OUT || gated < 0 || gated > 1)
         return QAMW_ERR_INVALID_ARG;
     if (!float_dtype(x_dtype) && x_dtype != QAMW_DTYPE_I8) return QAMW_ERR_INVALID_ARG;
-    *bytes_out = codes_bytes(x_dtype, m, d_in) + qamw::product_scratch_bytes(m, d_out, d_in, gated != 0);
+    *bytes_out = codes_bytes(x_dtype, m, d_in) + qamw::product_scratch_bytes(m, d_out, d_in, gated != 0, qamw::PRODUCT_I8);
     return QAMW_OK;
 }
 
@@ -62,7 +62,7 @@ int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const fl
     p.m = p.x_rows = m;
     p.d_out = d_out;
     p.d_in = d_in;
-    p.i8 = true;
+    p.kind = qamw::PRODUCT_I8;
     p.gated = gated != 0;
     p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
     p.stream = (hipStream_t)stream;
@@ -119,7 +119,7 @@ int qamw_grouped_matmul(const void *X, int dtype, const float *x_scales, int x_r
     p.m = m;
     p.d_out = d_out;
     p.d_in = d_in;
-    p.i8 = codes;
+    p.kind = codes ? qamw::PRODUCT_I8 : qamw::PRODUCT_BF16;
     p.gated = gated != 0;
     p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
     p.stream = (hipStream_t)stream;
@@ -132,7 +132,7 @@ int qamw_product_plan(int dtype, int m, int n_experts, int d_out, int d_in, int 
         return QAMW_ERR_INVALID_ARG;
     if (dtype != QAMW_DTYPE_I8 && (dtype != QAMW_DTYPE_BF16 || n_experts == 0)) return QAMW_ERR_INVALID_ARG;
     int plan[3];
-    qamw::product_plan(m, n_experts, n_experts > 0, d_out, d_in, gated != 0, dtype == QAMW_DTYPE_I8, n_experts == 0, plan);
+    qamw::product_plan(m, n_experts, n_experts > 0, d_out, d_in, gated != 0, dtype == QAMW_DTYPE_I8 ? qamw::PRODUCT_I8 : qamw::PRODUCT_BF16, n_experts == 0, plan);
     for (int i = 0; i < 3; ++i) plan_out[i] = plan[i];
     return QAMW_OK;
 }
@@ -240,6 +240,7 @@ int qamw_mx4_matmul_workspace_bytes(int x_dtype, int x_rows, int m, int n_expert
         d_out > QAMW_PRODUCT_MAX_D_OUT || gated < 0 || gated > 1 || (!float_dtype(x_dtype) && x_dtype != QAMW_DTYPE_MX4))
         return QAMW_ERR_INVALID_ARG;
     *bytes_out = mx4_rows_bytes(x_dtype, x_rows, d_in);
+    if (n_experts == 0) *bytes_out += qamw::product_scratch_bytes(m, d_out, (int)qamw::mx4_code_bytes(d_in), gated != 0, qamw::PRODUCT_MX4);
     return QAMW_OK;
 }
 
@@ -260,36 +261,39 @@ static int mx4_product(const void *X, int x_dtype, const uint8_t *x_scales, cons
     if (m > 0 && (rows ? x_rows < 1 : x_rows < m)) return QAMW_ERR_SHAPE;
     if (need && m > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return QAMW_ERR_INVALID_ARG;
     if (m == 0) return QAMW_OK;
-    qamw::Mx4Product q;
-    qamw::Product &p = q.p;
-    p.i8 = true;                                             // leading dimensions are bytes
-    p.ldx = p.ldw = qamw::mx4_code_bytes(d_in);
+    qamw::Product p;
+    p.kind = qamw::PRODUCT_MX4;
+    p.d_in = (int)qamw::mx4_code_bytes(d_in);
+    p.ldx = p.ldw = p.d_in;
     p.expert_stride = p.ldw * d_out * (gated ? 2 : 1);
+    p.block_bytes = (int)qamw::mx4_scale_bytes(d_in);
     p.rows = rows;
     p.x_rows = x_rows;
     p.W = W;
+    p.w_blocks = w_scales;
     p.offsets = n_experts ? offsets : nullptr;
     p.n_experts = n_experts ? n_experts : 1;
     p.Y = Y;
     p.ldy = ldy;
     p.m = m;
     p.d_out = d_out;
-    p.d_in = d_in;
     p.gated = gated != 0;
     p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
     p.stream = (hipStream_t)stream;
-    q.ws = w_scales;
+    const size_t before = mx4_rows_bytes(x_dtype, x_rows, d_in);
+    if (need > before) p.scratch = static_cast<char *>(workspace) + before;
     if (codes) {
         p.X = X;
-        q.xs = x_scales;
+        p.x_blocks = x_scales;
     } else {
         uint8_t *to = static_cast<uint8_t *>(workspace), *scales = to + (size_t)x_rows * (size_t)p.ldx;
         p.X = to;
-        q.xs = scales;
+        p.x_blocks = scales;
+        if (!qamw::product_wide_supported(p)) return QAMW_ERR_UNSUPPORTED;
         const hipError_t e = qamw::launch_mx4_quantize(X, x_dtype, x_rows, d_in, ldx, col_scale, to, scales, (hipStream_t)stream);
         if (e != hipSuccess) return status_of(e);
     }
-    return status_of(qamw::launch_mx4_product(q));
+    return status_of(qamw::launch_product(p));
 }
 
 int qamw_mx4_matmul(const void *X, int x_dtype, const uint8_t *x_scales, const float *col_scale, int m, int64_t ldx, const uint8_t *W,

@@ -314,6 +314,34 @@ def test_matmul_of_codes(m, d_out, d_in, gated):
 
 
 @gpu
+@pytest.mark.parametrize("m,d_out,d_in", [(1, 5, 7), (300, 700, 100), (77, 260, 4100), (513, 513, 513), (256, 512, 1024), (600, 300, 769), (2000, 300, 256)])
+@pytest.mark.parametrize("tile", [64, 128, 256])
+@pytest.mark.parametrize("gated", [False, True])
+def test_matmul_by_tiles(m, d_out, d_in, tile, gated):
+    """The kernel for many rows by every size of tile, whatever the estimate would choose: the same exact sums."""
+    say(f"[mx4] tiles of {tile}: {m} x {d_out} x {d_in} gated {gated}")
+    g = _gen(m + d_out * 5 + d_in)
+    (xc, xs), (wc, ws) = _rows(g, m, d_in, 2), _rows(g, d_out * (2 if gated else 1), d_in, 4)
+    x, w = to_device(xc, xs, d_in), to_device(wc, ws, d_in)
+    before = qamw.set_kernel_path(tile)
+    try:
+        y = qamw.mx4_matmul(x, w, gated=gated, out_dtype=torch.float32)
+        b = qamw.mx4_matmul(x, w, gated=gated)
+        e = qamw.Mx4(w.codes.view(1, *w.codes.shape), w.scales.view(1, *w.scales.shape), d_in)
+        rows = torch.randint(0, m, (m,), generator=g).to(torch.int32)
+        grouped = qamw.mx4_grouped_matmul(x, e, torch.tensor([0, m], dtype=torch.int32, device=DEV), rows=rows.to(DEV), gated=gated, out_dtype=torch.float32)
+    finally:
+        qamw.set_kernel_path(before)
+    ref = product_ref(xc, xs, wc, ws, d_in)
+    if gated:
+        want, slack = gate_ref(ref[:, :d_out], ref[:, d_out:])
+        check(y, want, slack)
+    else:
+        assert torch.equal(y.cpu(), ref.float())
+    assert torch.equal(b, y.bfloat16()) and torch.equal(grouped, y[rows.long().to(DEV)])
+
+
+@gpu
 @pytest.mark.parametrize("m,d_out,d_in", [(1, 300, 4096), (12, 64, 5632), (100, 333, 2048), (600, 300, 4100)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("smooth", [False, True])
