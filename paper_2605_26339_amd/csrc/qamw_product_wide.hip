@@ -150,6 +150,14 @@ __device__ __forceinline__ pw_u32x4_t resource(const void *p, uint32_t records =
     return {(uint32_t)(uintptr_t)p, (uint32_t)((uintptr_t)p >> 32) & 0xFFFFu, records, 0x00020000u};
 }
 
+// The same value, which the compiler does not know to be so: what is made from it is made where it is used.  Held in registers through the stages instead
+// it left too few of them, and the loads that brought it back from scratch memory had to wait for a tile's stores, which memory operations' order
+// demands: of a tile of 256 rows in 4 bits the last step took 15500 clocks that way.
+__device__ __forceinline__ int fresh(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 template <bool BF16> struct Store {
     using type = float;
 };
@@ -194,11 +202,11 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
     auto out_of = [&](int ct, int f, int r) { return GATED ? ct * (S::BN / 2) + (f >> 1) * 16 + r : ct * S::BN + f * 16 + r; };
     auto w_row = [&](int ct, int f, int r) { return (int64_t)(GATED && (f & 1) ? a.d_out : 0) + out_of(ct, f, r); };
     const int bytes = a.d_in * M::ELEM, every = (bytes + PW_KB - 1) / PW_KB;
-    const int lr = lane >> 3, piece = ((lane & 7) ^ lr) * 16;
-    const bool past = (every - 1) * PW_KB + piece >= bytes;                   // nothing there in the last stage of all
+    const bool past = (every - 1) * PW_KB + ((lane & 7) ^ (lane >> 3)) * 16 >= bytes;   // nothing there in the last stage of all
 
     ExpertTiles et = {0, 0, 0, 0, 0};
     auto tile_at = [&](uint32_t t) {
+        const int lane = fresh((int)threadIdx.x % WAVE), lr = lane >> 3, piece = ((lane & 7) ^ lr) * 16;
         Tile<S> z;
         z.n = 0;
         z.w = z.x = nullptr;
@@ -398,14 +406,14 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
         stage(First{}, now, stages - 1, next, 0, stored && stages == 2, busy);
         stage(Second{}, next, 0, next, 1, false, busy);
 
-        const int q0 = (lane >> 4) * 4;
+        const int elane = fresh(lane), q0 = (elane >> 4) * 4;
         // four outputs of fragment i (gated: and i + 1) in row j * 16 + lane % 16
         auto four = [&](int i, int j, float (&y)[4]) {
             const uint32_t sc = scales0 + slot;
             float xs = 1.0f;
             pr_f32x4_t sg = {1, 1, 1, 1}, su = {1, 1, 1, 1};
             if (SCALED) {
-                xs = lds_read<float>(sc + ((wm * S::FM + j) * 16 + (lane & 15)) * 4);
+                xs = lds_read<float>(sc + ((wm * S::FM + j) * 16 + (elane & 15)) * 4);
                 sg = lds_read<pr_f32x4_t>(sc + 1024 + ((wn * S::FN + i) * 16 + q0) * 4);
                 if (GATED) su = lds_read<pr_f32x4_t>(sc + 1024 + ((wn * S::FN + i + 1) * 16 + q0) * 4);
             }
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
                 for (int f = 0; f < FRAGS; ++f) {
                     float y[4];
                     if constexpr (OUT != 2) four((h * FRAGS + f) * STEP, j, y);
-                    const int r = lane & 15, b = (f * 16 + q0) * YB;
+                    const int r = elane & 15, b = (f * 16 + q0) * YB;
                     const uint32_t to = turn + r * 128 + (((b >> 4) ^ (r & 7)) << 4) + (b & 15);
                     if constexpr (YBF16) lds_write<uint64_t>(to, (uint64_t)pack_bf16(y[2], y[3]) << 32 | pack_bf16(y[0], y[1]));
                     else if constexpr (OUT == 2) lds_write<pr_i32x4_t>(to, __builtin_bit_cast(pr_i32x4_t, acc[h * FRAGS + f][j]));
@@ -444,7 +452,7 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int k = 0; k < TIMES; ++k) {
-                    const int nth = k * AT_ONCE + lane / PIECES, r = nth & 15, p = lane % PIECES;
+                    const int nth = k * AT_ONCE + elane / PIECES, r = nth & 15, p = elane % PIECES;
                     const pr_i32x4_t v = lds_read<pr_i32x4_t>(turn + r * 128 + ((p ^ (r & 7)) << 4));
                     const int row = (wm * S::FM + j) * 16 + r, col = col0 + h * PASS + p * EACH;
                     const bool is = nth < 16 && row < now.n && col < a.d_out;
