@@ -508,7 +508,9 @@ int qamw_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int m, int 
  *   W  device, codes and scales.  gated = 0: d_out rows.  gated = 1: the d_out rows of a gate, then the d_out rows of an up projection, and
  *      Y = g / (1 + exp(-g)) * u in fp32, as qamw_int8_matmul
  *   Y  device, m rows of d_out elements of y_dtype (F32 or BF16, rounded to nearest even), leading dimension ldy
- *   workspace  qamw_mx4_matmul_workspace_bytes() with x_rows = m and n_experts = 0, 16-byte aligned; NULL where that is 0
+ *   workspace  qamw_mx4_matmul_workspace_bytes() with x_rows = m and n_experts = 0, 16-byte aligned; NULL where that is 0, and where the product's own
+ *      launch quantises the rows: m * ceil(d_in / 4096) <= 4, d_in a multiple of 8, X and col_scale on 16-byte boundaries, rows of X of whole 16 bytes
+ *      and at most 2^24 elements apart
  * Errors: sizes out of the ranges above, NULL or misaligned pointers, x_scales with floating X or col_scale with codes, a workspace too small ->
  * INVALID_ARG; leading dimensions smaller than a row -> SHAPE; more tiles than a launch has, or a matrix of W or a gathered X of more than 2 GiB of codes ->
  * UNSUPPORTED. */

@@ -226,7 +226,6 @@ hipError_t launch_product(const Product &p) {
         return p.kind == PRODUCT_I8 ? launch_any<true>(p) : launch_any<false>(p);
     }
     const Plan c = plan_of(p.m, p.n_experts, p.offsets != nullptr, p.d_out, p.d_in, p.gated, p.kind, p.scratch != nullptr);
-    if (c.few && p.kind == PRODUCT_MX4) return launch_mx4_product(p);
     return c.few ? launch_product_few(p, c.tile_rows) : launch_product_wide(p, c.tile_rows, c.parts);
 }
 

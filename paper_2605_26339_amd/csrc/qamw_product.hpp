@@ -56,7 +56,6 @@ struct MoreLds {
 };
 // The kernels by what they are for.  wide and few: products that product_wide_supported(), tile_rows of 16 / 32 / 64 and 64 / 128 / 256.
 bool product_wide_supported(const Product &p);
-hipError_t launch_mx4_product(const Product &p);
 hipError_t launch_product_wide(const Product &p, int tile_rows, int parts);
 hipError_t launch_product_few(const Product &p, int tile_rows);
 // Waves that share a tile of outputs: enough for all of memory's bandwidth, about 8 on every CU, while a share has four units.
@@ -66,8 +65,8 @@ inline int few_split(int64_t tiles, int units, int waves) {
     return split;
 }
 // The product of rows that are quantised in the same launch; W as launch_product_few() needs it.
-bool product_from_floats_supported(const Product &p, const void *X, int dtype, int64_t ldx, const float *col_scale);
-hipError_t launch_product_from_floats(const Product &p, const void *X, int dtype, int64_t ldx, const float *col_scale);
+bool product_from_floats_supported(const Product &p, const void *X, int dtype, int columns, int64_t ldx, const float *col_scale);
+hipError_t launch_product_from_floats(const Product &p, const void *X, int dtype, int columns, int64_t ldx, const float *col_scale);
 hipError_t launch_int8_quantize(const void *X, int dtype, int64_t m, int d, int64_t ldx, const float *col_scale, int8_t *codes,
                                 int64_t ldc, float *scales, hipStream_t stream);
 

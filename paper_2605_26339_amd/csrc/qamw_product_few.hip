@@ -14,7 +14,7 @@
 // workgroup does so again.  Against a launch for it, in a graph: one row by 4096 x 4096 6.9 us (8.1), of 11008 columns 13.1 (15.2), 4 rows
 // of 4096 columns 9.9 (8.3); called one by one, a launch less is 4 us less of the host's time.  13 rows of 5632 took 18.6 us, in two launches
 // 8.5: so no more values than the threads hold in four groups of 8.
-#include "qamw_product_tile.hpp"
+#include "qamw_mx4.hpp"
 
 namespace qamw {
 namespace {
@@ -24,15 +24,18 @@ constexpr int PF_ONCE = 2;                                     // cache policy o
 constexpr uint32_t PF_NOWHERE = 0x80000000u;                    // added to an offset: beyond the end of any buffer here
 // FROM: where X comes from: -1 as the product takes it, from memory; 0 fp32 and 1 bf16 to be quantised here, EIGHTS groups of 8
 // values by a thread.
-template <int T_, int FN_, int FROM_ = -1, int EIGHTS_ = 1> struct FewShape {
+// MX4: rows in 4 bits, whose scales come by units in pairs, 16 bytes a row, to a ring of their own.
+template <int T_, int FN_, int FROM_ = -1, int EIGHTS_ = 1, bool MX4_ = false> struct FewShape {
     static constexpr int T = T_, FN = FN_, FROM = FROM_, EIGHTS = EIGHTS_, XT = FROM >= 0 ? 0 : T;   // XT: fragments of X in the ring
     static constexpr int SLOT = (FN + XT) * PF_SLOT;
     // Workgroups of 4 waves, two or more on a CU, share the CUs more evenly than ones of 8 (288 rows routed to those 64 experts 58 us a call
     // and 10 to the 8 21 us, 71 and 27 with ones of 8); one that quantises has 8 for it.
     static constexpr int WAVES = FROM >= 0 ? 8 : 4;
-    static constexpr int FIT = 80 * 1024 / (WAVES * SLOT), RING = FROM >= 0 || FIT > 4 ? 4 : FIT < 2 ? 2 : FIT;   // units on their way or being read
+    static constexpr int FIT = 80 * 1024 / (WAVES * SLOT), MOST = FROM >= 0 || FIT > 4 ? 4 : FIT < 2 ? 2 : FIT;
+    static constexpr int RING = MX4_ ? MOST / 2 * 2 : MOST;                                           // units on their way or being read
+    static constexpr int BLOCKS = MX4_ ? (FN + XT) * 256 : 0, PAIRS = RING / 2;                       // a pair's scales, and pairs of the ring
     static constexpr int THREADS = WAVES * WAVE, BM = T * 16;
-    static constexpr int LDS = WAVES * RING * SLOT;
+    static constexpr int CODES = RING * SLOT, OWN = CODES + PAIRS * BLOCKS, LDS = WAVES * OWN;        // of a wave, of the workgroup
 };
 
 struct FewArgs {
@@ -41,6 +44,7 @@ struct FewArgs {
     const void *xf;                                             // rows to be quantised here
     const float *col_scale;
     int64_t ldxf;
+    int columns;                                                // of these rows: d_in where it is not the bytes of codes
 };
 
 // N fragments from `at` on, complete when this returns: rows are 128 bytes apart, `piece` is where the lane's 16 bytes are.
@@ -74,9 +78,10 @@ template <int N> __device__ __forceinline__ void read_unit(uint32_t at, pr_i32x4
                      : "memory");
 }
 
-template <bool I8, bool GATED, bool YBF16, bool ONCE, typename S>
+template <int KIND, bool GATED, bool YBF16, bool ONCE, typename S>
 __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
-    using M = Mfma<I8 ? PRODUCT_I8 : PRODUCT_BF16>;
+    constexpr bool I8 = KIND == PRODUCT_I8, MX4 = KIND == PRODUCT_MX4;
+    using M = Mfma<KIND>;
     const ProductArgs &a = q.p;
     extern __shared__ __align__(16) char pf_lds[];
     const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
@@ -86,7 +91,9 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     if (rt.n <= 0) return;
     const int ct = (int)(blockIdx.x % (uint32_t)groups) * per + wave / q.split, part = wave % q.split;
     const int bytes = a.d_in * M::ELEM, units = (bytes + PF_UNIT - 1) / PF_UNIT;
-    const int u0 = (int)((int64_t)units * part / q.split), u1 = ct < q.col_tiles ? (int)((int64_t)units * (part + 1) / q.split) : u0;
+    constexpr int STEP = MX4 ? 2 : 1;                                          // shares of whole pairs
+    const int steps = (units + STEP - 1) / STEP;
+    const int u0 = (int)((int64_t)steps * part / q.split) * STEP, u1 = ct < q.col_tiles ? min((int)((int64_t)steps * (part + 1) / q.split) * STEP, units) : u0;
 
     // fragment f, row r of W: its output (gated: fragments in pairs, 16 of the gate and the same 16 of up)
     auto out_of = [&](int f, int r) { return (GATED ? ct * (S::FN / 2) + f / 2 : ct * S::FN + f) * 16 + r; };
@@ -113,9 +120,40 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
             if (a.rows && is) row = min(max(a.rows[rt.row0 + r], 0), a.x_rows - 1);
             off_x[t][h] = is ? (uint32_t)((int64_t)row * a.ldx) + piece : PF_NOWHERE;
         }
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)pf_lds, ring = lds0 + wave * (S::RING * S::SLOT);
-    constexpr int L = 2 * (S::FN + S::XT);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)pf_lds, ring = lds0 + wave * S::OWN;
+    constexpr int L = 2 * (S::FN + S::XT), LB = MX4 ? S::FN + S::XT : 0;
+    // In 4 bits: the scales of units u and u + 1, a dword a lane; 16 bytes a row
+    uint32_t off_b[S::FN + S::XT];
+    if constexpr (MX4) {
+        const int br = lane >> 2;
+#pragma unroll
+        for (int f = 0; f < S::FN; ++f) {
+            const int o = out_of(f, br);
+            const int64_t row = GATED && (f & 1) ? a.d_out + (int64_t)o : o;
+            off_b[f] = o < a.d_out ? (uint32_t)(row * a.block_bytes) + (lane & 3) * 4 : PF_NOWHERE;
+        }
+#pragma unroll
+        for (int t = 0; t < S::XT; ++t) {
+            const int r = t * 16 + br;
+            const bool is = r < rt.n;
+            int64_t row = is ? rt.row0 + r : 0;
+            if (a.rows && is) row = min(max(a.rows[row], 0), a.x_rows - 1);
+            off_b[S::FN + t] = is ? (uint32_t)((row - (a.rows ? 0 : rt.row0)) * a.block_bytes) + (lane & 3) * 4 : PF_NOWHERE;
+        }
+    }
+    const uint8_t *wb = a.w_blocks + (int64_t)rt.expert * a.d_out * (GATED ? 2 : 1) * a.block_bytes, *xb = a.x_blocks + (a.rows ? 0 : (int64_t)rt.row0 * a.block_bytes);
+    auto request_blocks = [&](int u) {
+        const int records = u < u1 ? 0x7FFFFFFF : 0, pair = (u - u0) / 2;
+        const auto wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(wb), 0, records, 0x00020000);
+        const auto xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(xb), 0, records, 0x00020000);
+        const uint32_t to = ring + S::CODES + (uint32_t)(pair % S::PAIRS) * S::BLOCKS;
+#pragma unroll
+        for (int f = 0; f < S::FN + S::XT; ++f)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(f < S::FN ? wr : xr, (__attribute__((address_space(3))) void *)(uintptr_t)(to + f * 256), 4, (int)off_b[f], u * 8, 0, 0);
+    };
     auto request = [&](int u) {
+        if constexpr (MX4)
+            if (((u - u0) & 1) == 0) request_blocks(u);
         const int records = u < u1 ? 0x7FFFFFFF : 0;
         const auto wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(wp), 0, records, 0x00020000);
         const auto xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(xp), 0, records, 0x00020000);
@@ -150,7 +188,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     }
     // the rows to be quantised are asked for before the weights, or they would be waited for together
     constexpr int SPAN = S::THREADS * 8;
-    const int spans = (a.d_in + SPAN - 1) / SPAN;                              // m * spans <= EIGHTS
+    const int spans = (q.columns + SPAN - 1) / SPAN;                           // m * spans <= EIGHTS
     Eight<(S::FROM == 1)> raw[S::EIGHTS];
     Eight<0> col[S::EIGHTS];
     if constexpr (S::FROM >= 0) {
@@ -159,7 +197,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
 #pragma unroll
         for (int i = 0; i < S::EIGHTS; ++i) {
             const int r = i / spans, j = (i % spans) * SPAN + tid * 8;
-            const uint32_t gone = r < a.m && j < a.d_in ? 0 : PF_NOWHERE;
+            const uint32_t gone = r < a.m && j < q.columns ? 0 : PF_NOWHERE;
             raw[i].load(xf, (uint32_t)((r * (uint32_t)q.ldxf + j) * (S::FROM ? 2 : 4)) | gone);
             col[i].load(cs, (uint32_t)(j * 4) | gone);
         }
@@ -168,8 +206,27 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     for (int i = 0; i < S::RING; ++i) request(u0 + i);
 
     // the rows of X as codes, a pitch of units * 128 + 16 bytes apart, behind the rings
-    const uint32_t x_pitch = units * PF_UNIT + 16, x_at = lds0 + S::LDS;
-    if constexpr (S::FROM >= 0) {
+    const uint32_t x_pitch = units * PF_UNIT + 16, x_at = lds0 + S::LDS, x_blocks = x_at + a.m * x_pitch;
+    if constexpr (S::FROM >= 0 && MX4) {                                       // a block is four lanes': no lane waits for another wave's
+#pragma unroll
+        for (int i = 0; i < S::EIGHTS; ++i) {
+            const int r = i / spans, j = (i % spans) * SPAN + tid * 8;
+            float v[8];
+            uint32_t most = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = raw[i].value(k);
+                if (q.col_scale) v[k] *= col[i].value(k);
+                most = max(most, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+            }
+            const Mx4Scale z(quad_max(most));
+            if (r >= a.m) continue;
+            if (j / 2 < units * PF_UNIT) lds_write<uint32_t>(x_at + r * x_pitch + j / 2, mx4_codes(v, z));
+            if (lane % 4 == 0 && j / 32 < a.block_bytes) lds_write<uint8_t>(x_blocks + r * a.block_bytes + mx4_scale_at(j / 32), (uint8_t)z.byte);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    if constexpr (S::FROM >= 0 && !MX4) {
         const uint32_t most_of = x_at + a.m * x_pitch;                        // [EIGHTS][WAVES], behind the codes
         float v[S::EIGHTS][8];
 #pragma unroll
@@ -207,11 +264,23 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     const uint32_t mine = (uint32_t)(fr * PF_UNIT);
     const uint32_t x_mine = x_at + min(fr, a.m - 1) * x_pitch + (lane >> 4) * 16;
     typename M::acc_t acc[S::FN][S::T] = {};
-    for (int u = u0; u < u1; ++u) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S::RING - 1) * L) : "memory");
+    int bw[S::FN], bx[S::T];
+    // Unit u.  In 4 bits the even one of two reads the scales of both; those of later pairs are on their way between its loads and the next ones'.
+    auto unit = [&](int u, auto odd) {
+        constexpr int ODD = decltype(odd)::value;
+        constexpr int PAIRS_AHEAD = MX4 ? (ODD ? S::RING / 2 : (S::RING - 1) / 2) : 0;
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S::RING - 1) * L + PAIRS_AHEAD * LB) : "memory");
         const uint32_t slot = ring + (uint32_t)((u - u0) % S::RING) * S::SLOT + mine;
         pr_i32x4_t f0[S::FN + S::XT], f1[S::FN + S::XT], x0[1], x1[1];
-        read_unit<S::FN + S::XT>(slot + (((lane >> 4) ^ (fr & 7)) * 16), f0);
+        if constexpr (MX4 && ODD == 0) {
+            const uint32_t from = ring + S::CODES + (uint32_t)((u - u0) / 2 % S::PAIRS) * S::BLOCKS + fr * 16 + (lane >> 4) * 4;
+#pragma unroll
+            for (int f = 0; f < S::FN; ++f) bw[f] = lds_read<int>(from + f * 256);
+#pragma unroll
+            for (int t = 0; t < S::XT; ++t) bx[t] = lds_read<int>(from + (S::FN + t) * 256);
+            if constexpr (S::FROM >= 0) bx[0] = lds_read<int>(x_blocks + min(fr, a.m - 1) * a.block_bytes + u * 8 + (lane >> 4) * 4);
+        }
+        read_unit<S::FN + S::XT>(slot + (((lane >> 4) ^ (fr & 7)) * 16), f0);  // complete with what was read before it
         read_unit<S::FN + S::XT>(slot + (((4 + (lane >> 4)) ^ (fr & 7)) * 16), f1);
         if constexpr (S::FROM >= 0) {
             read_unit<1>(x_mine + u * PF_UNIT, x0);
@@ -222,9 +291,23 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
         for (int f = 0; f < S::FN; ++f)
 #pragma unroll
             for (int t = 0; t < S::T; ++t) {
-                acc[f][t] = M::mul(f0[f], S::FROM >= 0 ? x0[0] : f0[S::FROM >= 0 ? 0 : S::FN + t], acc[f][t]);
-                acc[f][t] = M::mul(f1[f], S::FROM >= 0 ? x1[0] : f1[S::FROM >= 0 ? 0 : S::FN + t], acc[f][t]);
+                const pr_i32x4_t &xa = S::FROM >= 0 ? x0[0] : f0[S::FROM >= 0 ? 0 : S::FN + t], &xb = S::FROM >= 0 ? x1[0] : f1[S::FROM >= 0 ? 0 : S::FN + t];
+                if constexpr (MX4) {
+                    acc[f][t] = mx4_mul<2 * ODD>(f0[f], xa, acc[f][t], bw[f], bx[t]);
+                    acc[f][t] = mx4_mul<2 * ODD + 1>(f1[f], xb, acc[f][t], bw[f], bx[t]);
+                } else {
+                    acc[f][t] = M::mul(f0[f], xa, acc[f][t]);
+                    acc[f][t] = M::mul(f1[f], xb, acc[f][t]);
+                }
             }
+    };
+    if constexpr (MX4) {
+        for (int u = u0; u < u1; u += 2) {                                     // an odd number's last one is nothing: zeros
+            unit(u, std::integral_constant<int, 0>{});
+            unit(u + 1, std::integral_constant<int, 1>{});
+        }
+    } else {
+        for (int u = u0; u < u1; ++u) unit(u, std::integral_constant<int, 0>{});
     }
 
     // the shares of the columns are added in their order, in LDS, where the ring was
@@ -244,7 +327,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
             for (int t = 0; t < S::T; ++t)
                 for (int s = 1; s < q.split; ++s)
                     acc[f][t] += __builtin_bit_cast(typename M::acc_t, *reinterpret_cast<__attribute__((address_space(3))) pr_i32x4_t *>(
-                                                                           (uintptr_t)(ring + s * (S::RING * S::SLOT) + (f * S::T + t) * 1024 + lane * 16)));
+                                                                           (uintptr_t)(ring + s * S::OWN + (f * S::T + t) * 1024 + lane * 16)));
     }
 
 #pragma unroll
@@ -271,11 +354,11 @@ __global__ __launch_bounds__(S::THREADS) void k_product_few(FewArgs q) {
     }
 }
 
-template <bool I8, bool GATED, bool YBF16, bool ONCE, typename S> hipError_t launch_once(const Product &p, const FewArgs &given, size_t more_lds) {
+template <int KIND, bool GATED, bool YBF16, bool ONCE, typename S> hipError_t launch_once(const Product &p, const FewArgs &given, size_t more_lds) {
     FewArgs q = given;
     const int outs = (GATED ? S::FN / 2 : S::FN) * 16;
     const int64_t cols = ((int64_t)p.d_out + outs - 1) / outs, rows = most_row_tiles(p, S::BM);
-    const int units = (int)((p.d_in * (I8 ? 1 : 2) + PF_UNIT - 1) / PF_UNIT);
+    const int units = (int)((p.d_in * p.elem() + PF_UNIT - 1) / PF_UNIT);
     const int split = few_split((p.offsets && p.m < p.n_experts ? p.m : rows) * cols, units, S::WAVES);
     const int per = S::WAVES / split;
     const int64_t blocks = rows * ((cols + per - 1) / per);
@@ -283,7 +366,7 @@ template <bool I8, bool GATED, bool YBF16, bool ONCE, typename S> hipError_t lau
     q.p = args_of(p);
     q.col_tiles = (int)cols;
     q.split = split;
-    const auto kernel = &k_product_few<I8, GATED, YBF16, ONCE, S>;
+    const auto kernel = &k_product_few<KIND, GATED, YBF16, ONCE, S>;
     static MoreLds more;
     const hipError_t e = more.ask(reinterpret_cast<const void *>(kernel), 160 * 1024);
     if (e != hipSuccess) return e;
@@ -296,51 +379,59 @@ template <bool I8, bool GATED, bool YBF16, bool ONCE, typename S> hipError_t lau
 // 40 99.6 and 96.3.  Not where rows are off the 128-byte lines, whose other part the next unit asks for: 64 of 1408 x 2064 92.9 and 85.9, 8 of
 // 11008 x 4112 197 and 180.  Smaller weights may be found there again: 13824 x 5120 int8, over and over, 24.1 and 19.4.
 constexpr int64_t PF_KEPT = 128ll << 20;
-template <bool I8, bool GATED, bool YBF16, typename S> hipError_t launch(const Product &p, const FewArgs &q, size_t more_lds) {
-    const int64_t bytes = (int64_t)p.n_experts * p.d_out * (p.gated ? 2 : 1) * p.d_in * (I8 ? 1 : 2);
+template <int KIND, bool GATED, bool YBF16, typename S> hipError_t launch(const Product &p, const FewArgs &q, size_t more_lds) {
+    const int64_t bytes = (int64_t)p.n_experts * p.d_out * (p.gated ? 2 : 1) * p.d_in * p.elem();
     constexpr bool MAY = S::FROM < 0 && S::T == 1;
-    const bool on_lines = (p.ldw * (I8 ? 1 : 2) % 128 | p.expert_stride * (I8 ? 1 : 2) % 128 | (int64_t)(reinterpret_cast<uintptr_t>(p.W) % 128)) == 0;
-    return MAY && on_lines && bytes > PF_KEPT ? launch_once<I8, GATED, YBF16, MAY, S>(p, q, more_lds) : launch_once<I8, GATED, YBF16, false, S>(p, q, more_lds);
+    const bool on_lines = (p.ldw * p.elem() % 128 | p.expert_stride * p.elem() % 128 | (int64_t)(reinterpret_cast<uintptr_t>(p.W) % 128)) == 0;
+    return MAY && on_lines && bytes > PF_KEPT ? launch_once<KIND, GATED, YBF16, MAY, S>(p, q, more_lds) : launch_once<KIND, GATED, YBF16, false, S>(p, q, more_lds);
 }
 
-template <bool I8, int T, int FROM, int EIGHTS> hipError_t launch_shape(const Product &p, const FewArgs &q, size_t more_lds) {
-    using Gated = FewShape<T, 2, FROM, EIGHTS>;
-    using Plain = FewShape<T, 1, FROM, EIGHTS>;
-    if (p.gated) return p.y_bf16 ? launch<I8, true, true, Gated>(p, q, more_lds) : launch<I8, true, false, Gated>(p, q, more_lds);
-    return p.y_bf16 ? launch<I8, false, true, Plain>(p, q, more_lds) : launch<I8, false, false, Plain>(p, q, more_lds);
+template <int KIND, int T, int FROM, int EIGHTS> hipError_t launch_shape(const Product &p, const FewArgs &q, size_t more_lds) {
+    using Gated = FewShape<T, 2, FROM, EIGHTS, KIND == PRODUCT_MX4>;
+    using Plain = FewShape<T, 1, FROM, EIGHTS, KIND == PRODUCT_MX4>;
+    if (p.gated) return p.y_bf16 ? launch<KIND, true, true, Gated>(p, q, more_lds) : launch<KIND, true, false, Gated>(p, q, more_lds);
+    return p.y_bf16 ? launch<KIND, false, true, Plain>(p, q, more_lds) : launch<KIND, false, false, Plain>(p, q, more_lds);
 }
 
-template <bool I8> hipError_t launch_type(const Product &p, int tile_rows) {
+template <int KIND> hipError_t launch_type(const Product &p, int tile_rows) {
     const FewArgs q = {};
-    if (tile_rows <= 16) return launch_shape<I8, 1, -1, 1>(p, q, 0);
-    if (tile_rows <= 32) return launch_shape<I8, 2, -1, 1>(p, q, 0);
-    return launch_shape<I8, 4, -1, 1>(p, q, 0);
+    if (tile_rows <= 16) return launch_shape<KIND, 1, -1, 1>(p, q, 0);
+    if (tile_rows <= 32) return launch_shape<KIND, 2, -1, 1>(p, q, 0);
+    return launch_shape<KIND, 4, -1, 1>(p, q, 0);
 }
 
 }  // namespace
 
-hipError_t launch_product_few(const Product &p, int tile_rows) { return p.kind == PRODUCT_I8 ? launch_type<true>(p, tile_rows) : launch_type<false>(p, tile_rows); }
+hipError_t launch_product_few(const Product &p, int tile_rows) {
+    if (p.kind == PRODUCT_MX4) return launch_type<PRODUCT_MX4>(p, tile_rows);
+    return p.kind == PRODUCT_I8 ? launch_type<PRODUCT_I8>(p, tile_rows) : launch_type<PRODUCT_BF16>(p, tile_rows);
+}
 
 // As many values as the threads of a workgroup hold, and rows that are read in whole 16 bytes, with offsets that 31 bits hold.
 constexpr int PF_MOST_EIGHTS = 4, PF_SPAN = 8 * 8 * WAVE;
 
-bool product_from_floats_supported(const Product &p, const void *X, int dtype, int64_t ldx, const float *col_scale) {
-    const int64_t spans = ((int64_t)p.d_in + PF_SPAN - 1) / PF_SPAN, e = dtype == 0 ? 4 : 2;
-    return p.m * spans <= PF_MOST_EIGHTS && (reinterpret_cast<uintptr_t>(X) & 15) == 0 && (reinterpret_cast<uintptr_t>(col_scale) & 15) == 0 &&
-           ldx * e % 16 == 0 && ldx * e <= 0x7FFFFFFF / PF_MOST_EIGHTS;
+bool product_from_floats_supported(const Product &p, const void *X, int dtype, int columns, int64_t ldx, const float *col_scale) {
+    const int64_t spans = ((int64_t)columns + PF_SPAN - 1) / PF_SPAN, e = dtype == 0 ? 4 : 2;
+    return p.m * spans <= PF_MOST_EIGHTS && columns % 8 == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0 &&
+           (reinterpret_cast<uintptr_t>(col_scale) & 15) == 0 && ldx * e % 16 == 0 && ldx * e <= 0x7FFFFFFF / PF_MOST_EIGHTS;
 }
 
-template <int EIGHTS> static hipError_t from_floats(const Product &p, const FewArgs &q, int dtype, size_t codes) {
-    return dtype == 0 ? launch_shape<true, 1, 0, EIGHTS>(p, q, codes) : launch_shape<true, 1, 1, EIGHTS>(p, q, codes);
+template <int KIND, int EIGHTS> static hipError_t from_floats(const Product &p, const FewArgs &q, int dtype, size_t codes) {
+    return dtype == 0 ? launch_shape<KIND, 1, 0, EIGHTS>(p, q, codes) : launch_shape<KIND, 1, 1, EIGHTS>(p, q, codes);
 }
 
-hipError_t launch_product_from_floats(const Product &p, const void *X, int dtype, int64_t ldx, const float *col_scale) {
+hipError_t launch_product_from_floats(const Product &p, const void *X, int dtype, int columns, int64_t ldx, const float *col_scale) {
     FewArgs q = {};
     q.xf = X;
     q.ldxf = ldx;
+    q.columns = columns;
     q.col_scale = col_scale;
-    const size_t codes = (size_t)p.m * (((size_t)p.d_in + PF_UNIT - 1) / PF_UNIT * PF_UNIT + 16) + PF_MOST_EIGHTS * 8 * 4;   // and the waves' maxima
-    return p.m == 1 && p.d_in <= PF_SPAN ? from_floats<1>(p, q, dtype, codes) : from_floats<PF_MOST_EIGHTS>(p, q, dtype, codes);
+    // and the waves' maxima; in 4 bits the scales, and what the second of two units reads past the last row
+    const size_t row = ((size_t)p.d_in + PF_UNIT - 1) / PF_UNIT * PF_UNIT + 16;
+    const bool mx4 = p.kind == PRODUCT_MX4, one = p.m == 1 && columns <= PF_SPAN;
+    const size_t codes = mx4 ? p.m * (row + p.block_bytes) + PF_UNIT : p.m * row + PF_MOST_EIGHTS * 8 * 4;
+    if (mx4) return one ? from_floats<PRODUCT_MX4, 1>(p, q, dtype, codes) : from_floats<PRODUCT_MX4, PF_MOST_EIGHTS>(p, q, dtype, codes);
+    return one ? from_floats<PRODUCT_I8, 1>(p, q, dtype, codes) : from_floats<PRODUCT_I8, PF_MOST_EIGHTS>(p, q, dtype, codes);
 }
 
 }  // namespace qamw

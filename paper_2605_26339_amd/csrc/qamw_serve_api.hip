@@ -67,8 +67,8 @@ int qamw_int8_matmul(const void *X, int x_dtype, const float *x_scales, const fl
     p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
     p.stream = (hipStream_t)stream;
     p.ldx = codes ? ldx : (int64_t)round16((size_t)d_in);
-    if (!codes && qamw::product_wide_supported(p) && qamw::product_from_floats_supported(p, X, x_dtype, ldx, col_scale))
-        return status_of(qamw::launch_product_from_floats(p, X, x_dtype, ldx, col_scale));
+    if (!codes && qamw::product_wide_supported(p) && qamw::product_from_floats_supported(p, X, x_dtype, d_in, ldx, col_scale))
+        return status_of(qamw::launch_product_from_floats(p, X, x_dtype, d_in, ldx, col_scale));
     if (need && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return QAMW_ERR_INVALID_ARG;
     const size_t before = codes_bytes(x_dtype, m, d_in);
     if (need > before) p.scratch = static_cast<char *>(workspace) + before;
@@ -259,7 +259,6 @@ static int mx4_product(const void *X, int x_dtype, const uint8_t *x_scales, cons
         return QAMW_ERR_INVALID_ARG;
     if ((!codes && ldx < d_in) || ldy < d_out) return QAMW_ERR_SHAPE;
     if (m > 0 && (rows ? x_rows < 1 : x_rows < m)) return QAMW_ERR_SHAPE;
-    if (need && m > 0 && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return QAMW_ERR_INVALID_ARG;
     if (m == 0) return QAMW_OK;
     qamw::Product p;
     p.kind = qamw::PRODUCT_MX4;
@@ -280,6 +279,9 @@ static int mx4_product(const void *X, int x_dtype, const uint8_t *x_scales, cons
     p.gated = gated != 0;
     p.y_bf16 = y_dtype == QAMW_DTYPE_BF16;
     p.stream = (hipStream_t)stream;
+    if (!codes && !n_experts && qamw::product_wide_supported(p) && qamw::product_from_floats_supported(p, X, x_dtype, d_in, ldx, col_scale))
+        return status_of(qamw::launch_product_from_floats(p, X, x_dtype, d_in, ldx, col_scale));
+    if (need && (!workspace || workspace_bytes < need || misaligned(workspace, 16))) return QAMW_ERR_INVALID_ARG;
     const size_t before = mx4_rows_bytes(x_dtype, x_rows, d_in);
     if (need > before) p.scratch = static_cast<char *>(workspace) + before;
     if (codes) {

@@ -990,9 +990,14 @@ def mx4_matmul(X, W, col_scale=None, gated=False, out=None, out_dtype=None, work
     dev = _one_device(x, X[1] if code == DTYPE_MX4 else None, W[0], W[1], col_scale, out, workspace)
     d_out = outs // 2 if gated else outs
     y, y_code, ldy = _result(out, m, d_out, out_dtype, x, stream)
-    at, size, _work = _mx4_work(mx4_matmul_workspace_bytes(code, m, m, 0, d_out, d_in, bool(gated)), x, workspace, stream)
-    _launch(dev, "qamw_mx4_matmul", x_at, code, xs_at, _ptr(col_scale), m, ldx, W[0].data_ptr(), W[1].data_ptr(), d_out, d_in, 1 if gated else 0,
-            y.data_ptr(), y_code, ldy, at, size, _raw_stream(stream, dev))
+    w_at, c_at = W[0].data_ptr(), _ptr(col_scale)
+    if (workspace is None and code != DTYPE_MX4 and m * -(-d_in // 4096) <= 4 and not (x_at | (c_at or 0) | d_in * 2 | ldx * x.element_size()) & 15
+            and W[0].numel() < 0x7FFFFE00 and ldx <= 1 << 24):
+        at = size = _work = None                                  # the product's own launch quantises the rows
+    else:
+        at, size, _work = _mx4_work(mx4_matmul_workspace_bytes(code, m, m, 0, d_out, d_in, bool(gated)), x, workspace, stream)
+    _launch(dev, "qamw_mx4_matmul", x_at, code, xs_at, c_at, m, ldx, w_at, W[1].data_ptr(), d_out, d_in, 1 if gated else 0,
+            y.data_ptr(), y_code, ldy, at, size or 0, _raw_stream(stream, dev))
     return y
 
 
