@@ -39,4 +39,24 @@ __device__ __forceinline__ float mx4_power(uint32_t byte) {
     return __uint_as_float(byte == 255 ? 0x7FC00000u : byte ? byte << 23 : 0x00400000u);
 }
 
+// Eight neighbours of a row of d >= 8, as they are read, wherever they begin: of a row's last ones, or where none are left, the eight that end with the row.
+// Loads under a condition would be waited for one after the other.
+template <int DTYPE> struct Raw {
+    using E = typename Elem<DTYPE>::type;
+    Unaligned<E, 8> e;
+    __device__ __forceinline__ void load(const void *row, int j, int d) { e = *reinterpret_cast<const Unaligned<E, 8> *>(static_cast<const E *>(row) + min(j, d - 8)); }
+    __device__ __forceinline__ float value(int k) const { return DTYPE == 1 ? __uint_as_float((uint32_t)e.v[k] << 16) : (float)e.v[k]; }
+};
+// As values: the first `there` of them, after the last 8 - there of what was read; zeros behind.
+template <int DTYPE, bool RAGGED> __device__ __forceinline__ void values_of(const Raw<DTYPE> &raw, int there, float (&v)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = there > 0 ? raw.value(k) : 0.0f;
+    if (!RAGGED) return;                                                       // rows of whole eights
+    const int by = there >= 8 || there <= 0 ? 0 : 8 - there;
+#pragma unroll
+    for (int bit = 1; bit < 8; bit <<= 1)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = by & bit ? (k + bit < 8 ? v[(k + bit) & 7] : 0.0f) : v[k];
+}
+
 }  // namespace qamw

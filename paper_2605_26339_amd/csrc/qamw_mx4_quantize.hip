@@ -8,58 +8,98 @@ namespace {
 
 constexpr int MQ_THREADS = 256, MQ_WAVES = MQ_THREADS / WAVE, MQ_SPAN = WAVE * 8;
 
-template <int DTYPE, bool SCALED>
-__global__ __launch_bounds__(MQ_THREADS) void k_mx4_quantize(const void *X, int64_t waves, int groups, int d, int64_t ldx, const float *col_scale,
+// Group `id` of 512 columns: its row, and the column where the lane's eight begin.
+struct Group {
+    int64_t row;
+    int g, j;
+    __device__ __forceinline__ Group(uint32_t id, uint32_t groups) : row(id / groups), g((int)(id % groups)), j(g * MQ_SPAN + (int)(threadIdx.x % WAVE) * 8) {}
+};
+
+// EACH groups a wave, all asked for together.  ROWS: 0 of whole eights, 1 of eight columns and more, 2 of fewer.
+template <int DTYPE, bool SCALED, int EACH, int ROWS>
+__global__ __launch_bounds__(MQ_THREADS) void k_mx4_quantize(const void *X, uint32_t all, uint32_t groups, int d, int64_t ldx, const float *col_scale,
                                                              uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds) {
     using E = typename Elem<DTYPE>::type;
     const int lane = threadIdx.x % WAVE;
-    const int64_t id = (int64_t)blockIdx.x * MQ_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    if (id >= waves) return;
-    const int64_t row = id / groups;
-    const int g = (int)(id % groups);
-    const int64_t j = (int64_t)g * MQ_SPAN + lane * 8;
-    const E *x = static_cast<const E *>(X) + row * ldx + j;
-    float v[8];
-    if (j + 8 <= d) {                                       // wherever they lie: the memory instructions take any address
-        const auto e = *reinterpret_cast<const Unaligned<E, 8> *>(x);
+    const uint32_t id0 = (blockIdx.x * MQ_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE)) * EACH;
+    Raw<DTYPE> raw[EACH];
+    Raw<0> col[EACH];
+    if (ROWS != 2)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = DTYPE == 1 ? __uint_as_float((uint32_t)e.v[i] << 16) : (float)e.v[i];
-        if (SCALED) {
-            const auto c = *reinterpret_cast<const Unaligned<float, 8> *>(col_scale + j);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= c.v[i];
+        for (int n = 0; n < EACH; ++n) {
+            const Group a(min(id0 + n, all - 1), groups);
+            raw[n].load(static_cast<const E *>(X) + a.row * ldx, a.j, d);
+            if (SCALED) col[n].load(col_scale, a.j, d);
         }
-    } else
-        for (int i = 0; i < 8; ++i) v[i] = j + i < d ? Elem<DTYPE>::load(x, i) * (SCALED ? col_scale[j + i] : 1.0f) : 0.0f;
-    uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    const Mx4Scale s(quad_max(most));
-    const int64_t block = j / 32;
-    if (block * 32 < d) *reinterpret_cast<uint32_t *>(codes + row * ldc + j / 2) = mx4_codes(v, s);
-    if (lane % 4 == 0) scales[row * lds + g * 16 + mx4_scale_at(lane / 4)] = block * 32 < d ? (uint8_t)s.byte : 0;
+    for (int n = 0; n < EACH; ++n) {
+        if (id0 + n >= all) return;
+        const Group a(id0 + n, groups);
+        float v[8], c[8];
+        if (ROWS == 2) {
+            for (int i = 0; i < 8; ++i) {
+                const bool is = a.j + i < d;
+                v[i] = is ? Elem<DTYPE>::load(X, a.row * ldx + a.j + i) : 0.0f;
+                if (SCALED) c[i] = is ? col_scale[a.j + i] : 0.0f;
+            }
+        } else {
+            values_of<DTYPE, ROWS == 1>(raw[n], d - a.j, v);
+            if (SCALED) values_of<0, ROWS == 1>(col[n], d - a.j, c);
+        }
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (SCALED) v[i] *= c[i];
+            most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        }
+        const Mx4Scale s(quad_max(most));
+        const bool is = a.j / 32 * 32 < d;
+        if (is) *reinterpret_cast<uint32_t *>(codes + a.row * ldc + a.j / 2) = mx4_codes(v, s);
+        if (lane % 4 == 0) scales[a.row * lds + a.g * 16 + mx4_scale_at(lane / 4)] = is ? (uint8_t)s.byte : 0;
+    }
 }
 
-template <bool OBF16>
-__global__ __launch_bounds__(MQ_THREADS) void k_mx4_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t lds, int64_t waves,
-                                                               int groups, int d, void *out, int64_t ldo) {
+template <bool OBF16, int EACH>
+__global__ __launch_bounds__(MQ_THREADS) void k_mx4_dequantize(const uint8_t *codes, int64_t ldc, const uint8_t *scales, int64_t lds, uint32_t all,
+                                                               uint32_t groups, int d, void *out, int64_t ldo) {
     typedef float f2 __attribute__((ext_vector_type(2)));
     const int lane = threadIdx.x % WAVE;
-    const int64_t id = (int64_t)blockIdx.x * MQ_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
-    if (id >= waves) return;
-    const int64_t row = id / groups;
-    const int g = (int)(id % groups);
-    const int64_t j = (int64_t)g * MQ_SPAN + lane * 8;
-    if (j >= d) return;
-    const uint32_t c = *reinterpret_cast<const uint32_t *>(codes + row * ldc + j / 2);
-    const float p = mx4_power(scales[row * lds + g * 16 + mx4_scale_at(lane / 4)]);
-    const f2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1);
-    const f2 e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3);
-    const float lo[4] = {a[0] * p, a[1] * p, b[0] * p, b[1] * p}, hi[4] = {e[0] * p, e[1] * p, f[0] * p, f[1] * p};
-    const int64_t at = row * ldo + j;
-    const int there = (int)min((int64_t)8, d - j);
-    store_y4<OBF16>(out, at, lo, there);
-    if (there > 4) store_y4<OBF16>(out, at + 4, hi, there - 4);
+    const uint32_t id0 = (blockIdx.x * MQ_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE)) * EACH;
+    uint32_t c[EACH], byte[EACH];
+#pragma unroll
+    for (int n = 0; n < EACH; ++n) {
+        const Group a(min(id0 + n, all - 1), groups);
+        c[n] = *reinterpret_cast<const uint32_t *>(codes + a.row * ldc + min((int64_t)a.j / 2, ldc - 4));   // past the end: the row's last ones
+        byte[n] = scales[a.row * lds + a.g * 16 + mx4_scale_at(lane / 4)];
+    }
+#pragma unroll
+    for (int n = 0; n < EACH; ++n) {
+        if (id0 + n >= all) return;
+        const Group a(id0 + n, groups);
+        const float p = mx4_power(byte[n]);
+        const f2 v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[n], 1.0f, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[n], 1.0f, 1);
+        const f2 v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[n], 1.0f, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[n], 1.0f, 3);
+        const float lo[4] = {v0[0] * p, v0[1] * p, v1[0] * p, v1[1] * p}, hi[4] = {v2[0] * p, v2[1] * p, v3[0] * p, v3[1] * p};
+        const int64_t at = a.row * ldo + a.j;
+        const int there = d - a.j;
+        if (OBF16 && there >= 8) {
+            const uint4 eight = {pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
+            *reinterpret_cast<Unaligned<uint16_t, 8> *>(static_cast<uint16_t *>(out) + at) = __builtin_bit_cast(Unaligned<uint16_t, 8>, eight);
+        } else if (there > 0) {
+            store_y4<OBF16>(out, at, lo, there);
+            if (there > 4) store_y4<OBF16>(out, at + 4, hi, there - 4);
+        }
+    }
+}
+
+// Four groups a wave where that leaves enough waves to fill the chip.
+constexpr int64_t MQ_MANY = 4 * 8192;
+template <typename Launch> hipError_t launch_groups(int64_t m, int d, Launch launch) {
+    const int64_t groups = ((int64_t)d + MQ_SPAN - 1) / MQ_SPAN, all = m * groups, each = all >= MQ_MANY ? 4 : 1;
+    const int64_t blocks = (all + MQ_WAVES * each - 1) / (MQ_WAVES * each);
+    if (all > 0x7FFFFFFF || blocks * MQ_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
+    launch((uint32_t)blocks, (uint32_t)all, (uint32_t)groups, each == 4);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -67,30 +107,30 @@ __global__ __launch_bounds__(MQ_THREADS) void k_mx4_dequantize(const uint8_t *co
 hipError_t launch_mx4_quantize(const void *X, int dtype, int64_t m, int d, int64_t ldx, const float *col_scale, uint8_t *codes, uint8_t *scales,
                                hipStream_t stream) {
     if (m == 0) return hipSuccess;
-    const int64_t groups = ((int64_t)d + MQ_SPAN - 1) / MQ_SPAN, waves = m * groups, blocks = (waves + MQ_WAVES - 1) / MQ_WAVES;
-    if (blocks * MQ_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
     const int64_t ldc = mx4_code_bytes(d), lds = mx4_scale_bytes(d);
-    const dim3 g((uint32_t)blocks);
-    if (dtype == 0) {
-        if (col_scale) k_mx4_quantize<0, true><<<g, MQ_THREADS, 0, stream>>>(X, waves, (int)groups, d, ldx, col_scale, codes, ldc, scales, lds);
-        else k_mx4_quantize<0, false><<<g, MQ_THREADS, 0, stream>>>(X, waves, (int)groups, d, ldx, col_scale, codes, ldc, scales, lds);
-    } else {
-        if (col_scale) k_mx4_quantize<1, true><<<g, MQ_THREADS, 0, stream>>>(X, waves, (int)groups, d, ldx, col_scale, codes, ldc, scales, lds);
-        else k_mx4_quantize<1, false><<<g, MQ_THREADS, 0, stream>>>(X, waves, (int)groups, d, ldx, col_scale, codes, ldc, scales, lds);
-    }
-    return hipGetLastError();
+    return launch_groups(m, d, [&](uint32_t blocks, uint32_t all, uint32_t groups, bool four) {
+        auto go = [&](auto kernel) { kernel<<<blocks, MQ_THREADS, 0, stream>>>(X, all, groups, d, ldx, col_scale, codes, ldc, scales, lds); };
+        auto by_rows = [&](auto type, auto scaled) {
+            constexpr int T = decltype(type)::value;
+            constexpr bool S = decltype(scaled)::value;
+            if (d < 8) four ? go(k_mx4_quantize<T, S, 4, 2>) : go(k_mx4_quantize<T, S, 1, 2>);
+            else if (d % 8) four ? go(k_mx4_quantize<T, S, 4, 1>) : go(k_mx4_quantize<T, S, 1, 1>);
+            else four ? go(k_mx4_quantize<T, S, 4, 0>) : go(k_mx4_quantize<T, S, 1, 0>);
+        };
+        auto by_scale = [&](auto type) { col_scale ? by_rows(type, std::true_type{}) : by_rows(type, std::false_type{}); };
+        dtype == 0 ? by_scale(std::integral_constant<int, 0>{}) : by_scale(std::integral_constant<int, 1>{});
+    });
 }
 
 hipError_t launch_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int64_t m, int d, void *out, int out_dtype, int64_t ldo,
                                  hipStream_t stream) {
     if (m == 0) return hipSuccess;
-    const int64_t groups = ((int64_t)d + MQ_SPAN - 1) / MQ_SPAN, waves = m * groups, blocks = (waves + MQ_WAVES - 1) / MQ_WAVES;
-    if (blocks * MQ_THREADS > 0xFFFFFFFFll) return hipErrorNotSupported;
     const int64_t ldc = mx4_code_bytes(d), lds = mx4_scale_bytes(d);
-    const dim3 g((uint32_t)blocks);
-    if (out_dtype == 1) k_mx4_dequantize<true><<<g, MQ_THREADS, 0, stream>>>(codes, ldc, scales, lds, waves, (int)groups, d, out, ldo);
-    else k_mx4_dequantize<false><<<g, MQ_THREADS, 0, stream>>>(codes, ldc, scales, lds, waves, (int)groups, d, out, ldo);
-    return hipGetLastError();
+    return launch_groups(m, d, [&](uint32_t blocks, uint32_t all, uint32_t groups, bool four) {
+        auto go = [&](auto kernel) { kernel<<<blocks, MQ_THREADS, 0, stream>>>(codes, ldc, scales, lds, all, groups, d, out, ldo); };
+        if (out_dtype == 1) four ? go(k_mx4_dequantize<true, 4>) : go(k_mx4_dequantize<true, 1>);
+        else four ? go(k_mx4_dequantize<false, 4>) : go(k_mx4_dequantize<false, 1>);
+    });
 }
 
 }  // namespace qamw

@@ -7,6 +7,7 @@ namespace qamw {
 namespace {
 
 constexpr int BN_THREADS = 256, BN_WAVES = BN_THREADS / WAVE, BN_SPAN = BN_THREADS * 8;
+constexpr int BN_HELD = 2;                                 // groups of 512 columns that a wave holds, at most
 
 // The sum over the workgroup in a fixed order, the same in every lane.
 __device__ __forceinline__ float sum_of_all(float v, float *part) {
@@ -39,7 +40,190 @@ template <int DTYPE> __device__ __forceinline__ float rounded(float v) {
     return DTYPE == 1 ? __uint_as_float(bf16_rne_bits(v) << 16) : v;
 }
 
-// A workgroup has a row, a thread 8 neighbours of every BN_SPAN.
+// What is done with a row's eight columns from j on, of which `there` are: stored as they are, or in 4 bits, by whole waves.
+template <int OUT> __device__ __forceinline__ void put_8(const BlockNorm &q, int64_t row, int64_t j, int there, float (&v)[8]) {
+    if constexpr (OUT <= 1) {
+        if (there > 0) store_8<OUT>(q.x, row * q.ldx + j, there, v);
+    } else {
+        static_assert(OUT == 3, "");
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = i < there ? v[i] : 0.0f;                                    // a row that is not a number stays zero past its end
+            most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+        }
+        const Mx4Scale s(quad_max(most));
+        const bool is = j / 32 * 32 < q.d;
+        if (is) *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(q.x) + row * mx4_code_bytes(q.d) + j / 2) = mx4_codes(v, s);
+        if (threadIdx.x % 4 == 0)
+            static_cast<uint8_t *>(q.x_scales)[row * mx4_scale_bytes(q.d) + j / 512 * 16 + mx4_scale_at((int)(j % 512 / 32))] = is ? (uint8_t)s.byte : 0;
+    }
+}
+template <int DTYPE> __device__ __forceinline__ void codes_8(const BlockNorm &q, int64_t row, int64_t j, int there, const float (&v)[8], const Quantiser &z) {
+    uint8_t *to = static_cast<uint8_t *>(q.x) + row * q.ldx + j;
+    Unaligned<uint8_t, 8> c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c.v[i] = (uint8_t)z.code(v[i]);
+    if (there >= 8) *reinterpret_cast<Unaligned<uint8_t, 8> *>(to) = c;
+    else
+        for (int i = 0; i < 7; ++i)
+            if (i < there) to[i] = c.v[i];
+}
+
+// ---- rows that a workgroup's registers hold --------------------------------------------------------------------------------
+//
+// `waves` waves have a row, EIGHTS groups of 8 neighbours a lane, between the sums and the result: one read of h and the block.  A workgroup goes from row to
+// row, with the weights in registers; the next row is asked for before this one's sums are known.
+//   Every lane loads eight values (Raw): loads under a condition had to be waited for one after the other.
+
+// The sum and the largest over each LANES neighbouring lanes, the same in all of them.
+template <int LANES> __device__ __forceinline__ float lanes_add(float v) {
+    if (LANES == 64) return wave_add(v);
+    v += dpp_move<DPP_XOR1>(v);
+    v += dpp_move<DPP_XOR2>(v);
+    v += dpp_move<DPP_HALF_MIRROR>(v);
+    v += dpp_move<DPP_MIRROR>(v);
+    if (LANES == 16) return v;
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+    if (LANES == 64) return wave_max(v);
+    v = quad_max(v);
+    v = max(v, (uint32_t)dpp_move<DPP_HALF_MIRROR>((int)v));
+    v = max(v, (uint32_t)dpp_move<DPP_MIRROR>((int)v));
+    if (LANES == 16) return v;
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return max(a[0], a[1]);
+}
+
+// LANES: of a row that has fewer than a wave's 512 columns; 64 otherwise.
+template <int DTYPE, int OUT, int EIGHTS, bool RAGGED, int LANES>
+__global__ __launch_bounds__(1024) void k_block_norm_held(BlockNorm q, int waves) {
+    static_assert(LANES == 64 || (EIGHTS == 1 && OUT != 3), "");               // 4 bits: a wave writes a group of scales
+    __shared__ float part[3][16];
+    using E = typename Elem<DTYPE>::type;
+    const int lane = threadIdx.x % LANES, all = blockDim.x / WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), mine = wave % waves;
+    const int at_once = LANES < 64 ? (int)blockDim.x / LANES : all / waves;    // rows of a workgroup
+    auto column = [&](int i) { return (i * waves + mine) * 512 + lane * 8; };
+    auto there = [&](int i) { return min(8, q.d - column(i)); };
+    // over the waves of a row; the workgroup has one row where there are several
+    auto whole = [&](float v, int which) {
+        v = lanes_add<LANES>(v);
+        if (waves == 1) return v;
+        if (lane == 0) part[which][wave] = v;
+        __syncthreads();
+        return wave_add(lane < waves ? part[which][lane] : 0.0f);
+    };
+    auto ask = [&](const void *from, int64_t at, Raw<DTYPE> (&to)[EIGHTS]) {
+#pragma unroll
+        for (int i = 0; i < EIGHTS; ++i) to[i].load(static_cast<const E *>(from) + at, column(i), q.d);
+    };
+    Raw<DTYPE> h[EIGHTS], b[EIGHTS], g[EIGHTS];
+    auto ask_row = [&](int64_t r) {
+        if (r >= q.m) return;                                                  // whole rows; with several waves to one, the workgroup
+        ask(q.h, r * q.ldh, h);
+        if (q.block) ask(q.block, r * q.ldb, b);
+        if (q.gate && q.ldg != 0) ask(q.gate, r * q.ldg, g);
+    };
+    int64_t row = (int64_t)blockIdx.x * at_once + (LANES < 64 ? (int)threadIdx.x / LANES : wave / waves);
+    const int64_t step = (int64_t)gridDim.x * at_once;
+    ask_row(row);
+    if (q.gate && q.ldg == 0) ask(q.gate, 0, g);
+    float w[EIGHTS][8], bw[EIGHTS][8];
+    auto weights = [&](const float *from, float (&to)[EIGHTS][8]) {
+        Raw<0> raw[EIGHTS];
+#pragma unroll
+        for (int i = 0; i < EIGHTS; ++i)
+            if (from) raw[i].load(from, column(i), q.d);
+#pragma unroll
+        for (int i = 0; i < EIGHTS; ++i) {
+            if (from) values_of<0, RAGGED>(raw[i], there(i), to[i]);
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k) to[i][k] = 1.0f;
+        }
+    };
+    weights(q.block_weight, bw);
+    weights(q.weight, w);
+    for (; row < q.m; row += step) {
+        float v[EIGHTS][8], s = 0.0f;
+        if (q.block) {
+            float r_block = 1.0f;
+            if (q.block_weight) {
+#pragma unroll
+                for (int i = 0; i < EIGHTS; ++i) {
+                    float y[8];
+                    values_of<DTYPE, RAGGED>(b[i], there(i), y);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) s = fmaf(y[k], y[k], s);
+                }
+                r_block = 1.0f / sqrtf(whole(s, 0) / (float)q.d + q.eps);
+                s = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < EIGHTS; ++i) {
+                float y[8], x[8];
+                values_of<DTYPE, RAGGED>(b[i], there(i), y);
+                if (q.block_weight)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = y[k] * r_block * bw[i][k];
+                if (q.gate) {
+                    values_of<DTYPE, RAGGED>(g[i], there(i), x);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] *= x[k];
+                }
+                values_of<DTYPE, RAGGED>(h[i], there(i), x);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[i][k] = k < there(i) ? rounded<DTYPE>(fmaf(q.scale, y[k], x[k])) : 0.0f;   // a sum that is not a number makes no others
+                    s = fmaf(v[i][k], v[i][k], s);
+                }
+                if (there(i) > 0) store_8<DTYPE>(q.h_out, row * q.ldho + column(i), there(i), v[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < EIGHTS; ++i) {
+                values_of<DTYPE, RAGGED>(h[i], there(i), v[i]);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s = fmaf(v[i][k], v[i][k], s);
+            }
+        }
+        ask_row(row + step);
+        const float r = 1.0f / sqrtf(whole(s, 1) / (float)q.d + q.eps);
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < EIGHTS; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[i][k] = v[i][k] * r;
+                if (q.weight) v[i][k] *= w[i][k];
+                if (OUT == 2) most = max(most, k < there(i) ? __float_as_uint(v[i][k]) & 0x7FFFFFFFu : 0);
+            }
+        if constexpr (OUT == 2) {
+            most = lanes_max<LANES>(most);
+            if (waves > 1) {
+                if (lane == 0) part[2][wave] = __uint_as_float(most);
+                __syncthreads();
+                most = wave_max(lane < waves ? __float_as_uint(part[2][lane]) : 0);
+            }
+            const Quantiser z(most);
+            if (lane == 0 && mine == 0) static_cast<float *>(q.x_scales)[row] = z.scale;
+#pragma unroll
+            for (int i = 0; i < EIGHTS; ++i)
+                if (there(i) > 0) codes_8<DTYPE>(q, row, column(i), there(i), v[i], z);
+        } else {
+#pragma unroll
+            for (int i = 0; i < EIGHTS; ++i)
+                if (OUT != 3 || column(i) / 512 * 512 < q.d) put_8<OUT>(q, row, column(i), there(i), v[i]);
+        }
+        if (waves > 1) __syncthreads();                                        // the sums are read before the next row's are written
+    }
+}
+
+// ---- longer rows, and ones below 8 -----------------------------------------------------------------------------------------------------------
+//
+// A workgroup has a row, a thread 8 neighbours of every BN_SPAN, in a sweep for each sum and one for the result; the caches have the row by then.
 template <int DTYPE, int OUT>
 __global__ __launch_bounds__(BN_THREADS) void k_block_norm(BlockNorm q) {
     __shared__ float part[BN_WAVES];
@@ -109,33 +293,41 @@ __global__ __launch_bounds__(BN_THREADS) void k_block_norm(BlockNorm q) {
         float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         const int there = (int)min((int64_t)8, q.d - j);
         if (there > 0) normed(j, there, v);
-        if (OUT <= 1) store_8<OUT>(q.x, row * q.ldx + j, there, v);
-        if (OUT == 2) {
-            uint8_t *to = static_cast<uint8_t *>(q.x) + row * q.ldx + j;
-            for (int i = 0; i < there && i < 8; ++i) to[i] = (uint8_t)z.code(v[i]);
-        }
-        if (OUT == 3) {
-            uint32_t largest = 0;
-            for (int i = 0; i < 8; ++i) largest = max(largest, i < there ? __float_as_uint(v[i]) & 0x7FFFFFFFu : 0);
-            const Mx4Scale sc(quad_max(largest));
-            for (int i = 0; i < 8; ++i) v[i] = i < there ? v[i] : 0.0f;
-            const bool is = j / 32 * 32 < q.d;
-            if (is) *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(q.x) + row * mx4_code_bytes(q.d) + j / 2) = mx4_codes(v, sc);
-            if (threadIdx.x % 4 == 0)
-                static_cast<uint8_t *>(q.x_scales)[row * mx4_scale_bytes(q.d) + j / 512 * 16 + mx4_scale_at((int)(j % 512 / 32))] = is ? (uint8_t)sc.byte : 0;
-        }
+        if constexpr (OUT == 2) codes_8<DTYPE>(q, row, j, there, v, z);
+        else put_8<OUT>(q, row, j, there, v);
     }
 }
 
-template <int DTYPE> hipError_t launch_type(const BlockNorm &q) {
-    const dim3 g((uint32_t)q.m);
-    switch (q.x_dtype) {
-    case 0: k_block_norm<DTYPE, 0><<<g, BN_THREADS, 0, q.stream>>>(q); break;
-    case 1: k_block_norm<DTYPE, 1><<<g, BN_THREADS, 0, q.stream>>>(q); break;
-    case 2: k_block_norm<DTYPE, 2><<<g, BN_THREADS, 0, q.stream>>>(q); break;
-    default: k_block_norm<DTYPE, 3><<<g, BN_THREADS, 0, q.stream>>>(q); break;
-    }
+template <int DTYPE, int OUT, int EIGHTS, int LANES> hipError_t launch_held(const BlockNorm &q, int groups) {
+    const int waves = (groups + EIGHTS - 1) / EIGHTS, rows = waves == 1 ? 4 * (WAVE / LANES) : 1, threads = rows * waves * LANES;
+    const int64_t most = (int64_t)256 * (2048 / threads), need = ((int64_t)q.m + rows - 1) / rows;
+    const dim3 g((uint32_t)(need < most ? need : most));
+    if (q.d % 8) k_block_norm_held<DTYPE, OUT, EIGHTS, true, LANES><<<g, threads, 0, q.stream>>>(q, waves);
+    else k_block_norm_held<DTYPE, OUT, EIGHTS, false, LANES><<<g, threads, 0, q.stream>>>(q, waves);
     return hipGetLastError();
+}
+// Two groups a lane are two rows' loads for the same waits, but more registers, and longer for a row alone: bf16 8192 x 4096 53.0 us (62.6 with one),
+// 5 x 4096 5.6 (4.8); fp32 4001 x 5120 83.5 (71.7).
+template <int DTYPE, int OUT> hipError_t launch_out(const BlockNorm &q) {
+    const int groups = (q.d + 511) / 512;                                      // of a wave
+    if (groups > BN_HELD * 16 || q.d < 8) {
+        k_block_norm<DTYPE, OUT><<<dim3((uint32_t)q.m), BN_THREADS, 0, q.stream>>>(q);
+        return hipGetLastError();
+    }
+    if constexpr (OUT != 3) {
+        if (q.d <= 128) return launch_held<DTYPE, OUT, 1, 16>(q, groups);
+        if (q.d <= 256) return launch_held<DTYPE, OUT, 1, 32>(q, groups);
+    }
+    if (groups == 1 || (groups <= 16 && (DTYPE == 0 || q.m <= 512))) return launch_held<DTYPE, OUT, 1, 64>(q, groups);
+    return launch_held<DTYPE, OUT, BN_HELD, 64>(q, groups);
+}
+template <int DTYPE> hipError_t launch_type(const BlockNorm &q) {
+    switch (q.x_dtype) {
+    case 0: return launch_out<DTYPE, 0>(q);
+    case 1: return launch_out<DTYPE, 1>(q);
+    case 2: return launch_out<DTYPE, 2>(q);
+    default: return launch_out<DTYPE, 3>(q);
+    }
 }
 
 }  // namespace

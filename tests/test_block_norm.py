@@ -92,7 +92,8 @@ def _strided(t, pad, skip):
 
 
 SHAPES = [(1, 1, 0, 0), (3, 5, 0, 0), (1, 4096, 0, 0), (5, 257, 3, 1), (4, 512, 0, 0), (2, 2047, 1, 0), (7, 2048, 8, 8), (300, 1024, 0, 0), (3, 5632, 0, 0), (2, 8200, 0, 0),
-          (2, 13824, 16, 8), (2, 16385, 0, 0), (1, 131072, 0, 0), (2, 131071, 0, 1), (70, 33, 0, 0), (9, 7168, 0, 0), (5, 4100, 0, 0)]
+          (2, 13824, 16, 8), (2, 16385, 0, 0), (1, 131072, 0, 0), (2, 131071, 0, 1), (70, 33, 0, 0), (9, 7168, 0, 0), (5, 4100, 0, 0), (4, 8, 0, 0),
+          (5, 9, 2, 1), (1000, 100, 0, 0), (33, 250, 6, 0), (40, 256, 0, 0), (70000, 16, 0, 0), (5000, 1100, 0, 0), (600, 4096, 0, 0)]
 
 
 @gpu
