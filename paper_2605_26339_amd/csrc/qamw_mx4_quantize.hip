@@ -31,10 +31,10 @@ __global__ __launch_bounds__(MQ_THREADS) void k_mx4_quantize(const void *X, uint
             raw[n].load(static_cast<const E *>(X) + a.row * ldx, a.j, d);
             if (SCALED) col[n].load(col_scale, a.j, d);
         }
+    uint32_t code[EACH], byte[EACH];
 #pragma unroll
     for (int n = 0; n < EACH; ++n) {
-        if (id0 + n >= all) return;
-        const Group a(id0 + n, groups);
+        const Group a(min(id0 + n, all - 1), groups);
         float v[8], c[8];
         if (ROWS == 2) {
             for (int i = 0; i < 8; ++i) {
@@ -53,9 +53,35 @@ __global__ __launch_bounds__(MQ_THREADS) void k_mx4_quantize(const void *X, uint
             most = max(most, __float_as_uint(v[i]) & 0x7FFFFFFFu);
         }
         const Mx4Scale s(quad_max(most));
-        const bool is = a.j / 32 * 32 < d;
-        if (is) *reinterpret_cast<uint32_t *>(codes + a.row * ldc + a.j / 2) = mx4_codes(v, s);
-        if (lane % 4 == 0) scales[a.row * lds + a.g * 16 + mx4_scale_at(lane / 4)] = is ? (uint8_t)s.byte : 0;
+        code[n] = mx4_codes(v, s);
+        byte[n] = s.byte;                                   // 0 where no column is
+    }
+    if constexpr (EACH == 4) {
+        // Four lanes have a block of each of four groups, and exchange them: each gets a whole block of one, which is a store of 16 bytes for four of 4.
+        auto swap = [](uint32_t &lo, uint32_t &hi, bool up, auto move) {
+            const uint32_t got = (uint32_t)move((int)(up ? lo : hi));
+            lo = up ? got : lo;
+            hi = up ? hi : got;
+        };
+        const int q = lane % 4;
+        auto one = [](int v) { return dpp_move<DPP_XOR1>(v); };
+        auto two = [](int v) { return dpp_move<DPP_XOR2>(v); };
+        swap(code[0], code[1], q & 1, one);
+        swap(code[2], code[3], q & 1, one);
+        swap(code[0], code[2], q & 2, two);
+        swap(code[1], code[3], q & 2, two);
+        const uint32_t mine = q & 2 ? (q & 1 ? byte[3] : byte[2]) : q & 1 ? byte[1] : byte[0];
+        const uint32_t id = id0 + q;
+        if (id >= all) return;
+        const int64_t row = id / groups;
+        const int g = (int)(id % groups), block = g * 16 + lane / 4;
+        if (block * 32 < d) *reinterpret_cast<uint4 *>(codes + row * ldc + block * 16) = {code[0], code[1], code[2], code[3]};
+        scales[row * lds + g * 16 + mx4_scale_at(lane / 4)] = (uint8_t)mine;
+    } else {
+        const Group a(min(id0, all - 1), groups);
+        if (id0 >= all) return;
+        if (a.j / 32 * 32 < d) *reinterpret_cast<uint32_t *>(codes + a.row * ldc + a.j / 2) = code[0];
+        if (lane % 4 == 0) scales[a.row * lds + a.g * 16 + mx4_scale_at(lane / 4)] = (uint8_t)byte[0];
     }
 }
 
