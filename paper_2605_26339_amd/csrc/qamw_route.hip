@@ -17,7 +17,6 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 // instructions, 2 the logits' 8.4 MB, the rest a launch and the steps between (12.4 where a choice was struck out, and values were made of numbers
 // again for the sum).  With 64 lanes for a token the whole routing took 31.6 us, with sixteen 16.4.
 constexpr int RT_LANES = 16, RT_GROUPS = WAVE / RT_LANES;
-constexpr int RT_GROUP_SLOTS = QAMW_MAX_GROUPS / RT_LANES;    // groups of experts that a lane looks after
 // Tokens of a workgroup of the first launch, and so the most that it can count for an expert: 8 bits hold it.  A workgroup's counts lie in
 // sectors of 32 bytes of their own, so that no two write to one.
 constexpr int RT_TOKENS = RT_GROUPS * RT_WAVES;
@@ -124,124 +123,329 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 
 // ---- choice by scores -----------------------------------------------------------------------------------------------------
 //
-// Scores, the bias and the sums of groups are in 64 bits: a choice is a comparison, and two values that 32 bits cannot tell apart are usual
-// among a few million.  As above sixteen lanes have a token, a lane PER experts that follow one another.
+// A choice is a comparison, and among a few million values there are always two that 32 bits of floating point cannot tell apart.  So scores are made in 64
+// bits, and compared as whole numbers, their distance from the token's smallest value in units of some 2^-28 of the distance to its largest; where all that is
+// compared for a token is more than a unit apart, 64 bits would choose alike (choose_fast).  A token in doubt is done again in 64 bits, by its whole
+// wave (choose_exact).  That code is cold when a wave comes to it and takes it 10 us, which the whole launch waits for: with comparisons in fp32, sure to 2^-19, one
+// in a thousand tokens was in doubt, and every large call took 30 us where it takes TIME now.  Without a bias and groups the logits order as the scores do.
+//   The weights, k a token, are in 64 bits too.
 
-__device__ __forceinline__ double row_max(double v) {
+// How the groups lie on `all` lanes, a power of two for each group: 2^shift lanes of a group, none if there are more groups than lanes, and experts of a lane.
+struct GroupLanes {
+    int shift, lanes, per, each;
+    __host__ __device__ GroupLanes(int all, int n_experts, int groups) : shift(0), lanes(all), per(0), each(n_experts / groups) {
+        for (int g = 1; g < groups; g <<= 1) lanes >>= 1;
+        while (lanes >> (shift + 1)) ++shift;
+        if (lanes) per = (each + lanes - 1) >> shift;
+    }
+    __device__ __forceinline__ int group(int lane) const { return lane >> shift; }
+    __device__ __forceinline__ int first_lane(int lane) const { return lane >> shift << shift; }   // of its group
+    __device__ __forceinline__ int first_expert(int lane) const { return group(lane) * each + (lane & (lanes - 1)) * per; }
+    // experts of the lane; not above 0 where there are none
+    __device__ __forceinline__ int count(int lane, int groups) const { return group(lane) < groups ? min(per, each - (lane & (lanes - 1)) * per) : 0; }
+};
+
+// PER neighbours from `e0` on of a token's logits or of the bias, with others of the row in place of those past the end of it: all are asked for at once.
+template <int DTYPE, int PER> __device__ __forceinline__ void neighbours(const void *row, int e0, int n, float (&v)[PER]) {
+    using E = typename Elem<DTYPE>::type;
+    const E *from = static_cast<const E *>(row);
+    if (e0 + PER <= n) {
+        const auto w = *reinterpret_cast<const Unaligned<E, PER> *>(from + e0);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = DTYPE == 1 ? __uint_as_float((uint32_t)w.v[i] << 16) : (float)w.v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = Elem<DTYPE>::load(from, min(e0 + i, n - 1));
+    }
+}
+// Logits so: NaN as -inf, and what another lane has, too.
+template <int DTYPE, int PER> __device__ __forceinline__ void own_logits(const RouteProblem &q, int64_t t, int e0, int count, float (&v)[PER]) {
+    neighbours<DTYPE, PER>(static_cast<const typename Elem<DTYPE>::type *>(q.logits) + min(t, (int64_t)q.m - 1) * q.ld, e0, q.n_experts, v);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = i < count ? clean(v[i]) : -__builtin_inff();
+}
+
+__device__ __forceinline__ double row_sum(double v) { return wave_sum_of_16(v); }
+__device__ __forceinline__ bool all_of_row(bool b) { return ((uint32_t)(__ballot(b) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu) == 0xFFFFu; }
+
+// exp(x) for |x| <= 690: 2^n times the series of the rest, of at most ln 2 / 2, up to its eighth power: off by at most 3e-10 of it.  The sum with 1.5 * 2^52
+// rounds to a whole number, which its lower half is; conversions, minima and maxima in 64 bits take four times as long as sums and products.
+__device__ __forceinline__ double exp_near(double x) {
+    constexpr double WHOLE = 0x1.8p52;
+    const double t = fma(x, 1.4426950408889634, WHOLE), r = fma(t - WHOLE, -0.6931471805599453, x);
+    double p = 1.0 / 40320;
+    p = fma(p, r, 1.0 / 5040);
+    p = fma(p, r, 1.0 / 720);
+    p = fma(p, r, 1.0 / 120);
+    p = fma(p, r, 1.0 / 24);
+    p = fma(p, r, 1.0 / 6);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(t) << 20), __double2loint(p));
+}
+// 1 / x of a normal number, after a step of Newton's: off by at most 1e-14 of it.
+__device__ __forceinline__ double inverse_near(double x) {
+    const double y = __builtin_amdgcn_rcp(x);
+    return fma(fma(-x, y, 1.0), y, y);
+}
+
+// Sixteen lanes a token.  A number, below 2^31, is a value in units, above which one of its lane's PER experts it is, the lowest as the largest; 0: closed.  The
+// next choice is the largest number below the last one, found as with packed logits above; if two lanes have it, the token is in doubt.
+// Lane j gets the choices j and j + 16.  Returns, for each token, whether 64 bits are sure to choose alike.  A score is off by 6e-10 at most, an exponential's
+// 3e-10 twice for a softmax, and by a rounding of its sum with the bias.  The range is 8 and the bias', a unit PER 2^-31 of it and so 3.7e-9 or more: where
+// two numbers' units differ by more than one, the values are more than a unit apart, which is more than both are off.  Half the sum of two is known to a unit
+// less.
+template <int DTYPE, int PER>
+__device__ __forceinline__ bool choose_fast(const RouteProblem &q, int64_t t, int (&expert)[2]) {
+    const int lane = threadIdx.x % RT_LANES, n = q.n_experts;
+    const GroupLanes g(RT_LANES, n, q.groups);
+    const int e0 = g.first_expert(lane), count = t < q.m ? g.count(lane, q.groups) : 0;
+    float x[PER], bias[PER] = {};
+    own_logits<DTYPE, PER>(q, t, e0, count, x);
+    if (q.bias) neighbours<0, PER>(q.bias, e0, n, bias);
+    double c[PER], share = 1.0;
+    if (q.softmax) {
+        float top = -__builtin_inff();
+        double total = 0.0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) top = fmaxf(top, x[i]);
+        top = value_of(row_max(key_of(top)));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            // infinities of one sign: 0; the difference is rounded by 2^-24 of its size, times e to that: below 2^-25, and so in 64 bits
+            const double e = exp_near(x[i] - top > -689.0f ? (double)x[i] - (double)top : x[i] == top ? 0.0 : -689.0);
+            c[i] = e;
+            total += x[i] > -__builtin_inff() ? e : 0.0;
+        }
+        total = row_sum(total);
+        share = inverse_near(total >= 1.0 ? total : 1.0);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] *= share;
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) c[i] = inverse_near(1.0 + exp_near(-(double)fminf(fmaxf(x[i], -690.0f), 690.0f)));
+    }
+    // the bias' range, and 1 for the scores'; of no expert 0
+    float low = __builtin_inff(), high = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (!(bias[i] > -__builtin_inff())) x[i] = -__builtin_inff();
+        const bool open = x[i] > -__builtin_inff();
+        low = fminf(low, open ? bias[i] : low);
+        high = fmaxf(high, open ? bias[i] : high);
+    }
+    high = value_of(row_max(key_of(high)));
+    low = -value_of(row_max(key_of(-low)));
+    const double units = 0x1.fffffep30 / ((double)high - (double)low + 8.0), from = fma(-((double)low - 1.0), units, 0x1p52);
+    constexpr uint32_t INDEX = PER - 1;
+    uint32_t v[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const uint32_t u = (uint32_t)__double2loint(fma(c[i] + (double)bias[i], units, from));   // as a whole number
+        v[i] = x[i] > -__builtin_inff() ? (u & ~INDEX) | (INDEX - i) : 0;
+    }
+    bool certain = high < __builtin_inff();
+    auto apart = [&](uint32_t a, uint32_t b, uint32_t by) { certain = certain && (b == 0 || a / PER - b / PER > by); };
+    if (q.groups > 1) {
+        uint32_t first = 0, second = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            second = max(second, min(first, v[i]));
+            first = max(first, v[i]);
+        }
+        for (int d = 1; d < g.lanes; d <<= 1) {
+            const uint32_t f = (uint32_t)__shfl_xor((int)first, d, RT_LANES), z = (uint32_t)__shfl_xor((int)second, d, RT_LANES);
+            second = max(min(first, f), max(second, z));
+            first = max(first, f);
+        }
+        // a group's value, in its first lane; as a number that is not 0.  One expert alone has no number for the other.
+        const bool two = q.group_top > 1 && g.each > 1;
+        certain = certain && !(two && first != 0 && second == 0);
+        uint32_t value = g.first_lane(lane) == lane && first != 0 ? (two ? first / 2 + second / 2 : first) | 1 : 0, last = 0, kept = 0;
+        for (int j = 0; j <= q.top_groups; ++j) {           // the order of those that stay matters to nobody, so that only the next one has to be apart
+            const uint32_t best = row_max(value);
+            if (j == q.top_groups) {
+                apart(last, best, 3);
+                break;
+            }
+            const uint32_t has = (uint32_t)(__ballot(value == best && best != 0) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu, one = has & (0u - has);
+            kept |= one;
+            value = one >> lane & 1 ? 0 : value;
+            last = best;
+        }
+        const bool stays = kept >> g.first_lane(lane) & 1;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = stays ? v[i] : 0;
+    }
+    expert[0] = expert[1] = -1;
+    uint32_t last = 0;
+    bool some = true;
+    for (int j = 0; j <= q.k; ++j) {                         // one more than are chosen: it has to be apart, too
+        uint32_t own = v[0] - last;
+#pragma unroll
+        for (int i = 1; i < PER; ++i) own = max(own, v[i] - last);
+        const uint32_t best = last + row_max(own);
+        if (j > 0 && some) apart(last, best, 1);
+        some = some && best != 0;                            // a token that has run out of experts stays so
+        if (j == q.k || !__any(some)) break;
+        const uint32_t has = (uint32_t)(__ballot(last + own == best) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu;
+        certain = certain && ((has & (has - 1)) == 0 || !some);
+        const int who = g.first_expert(__ffs((int)has) - 1) + (int)(INDEX - (best & INDEX));
+        if (some && lane == j) expert[0] = who;
+        if (some && lane + RT_LANES == j) expert[1] = who;
+        last = best;
+    }
+    return all_of_row(certain);                             // a group alone is in doubt in its own lanes
+}
+
+__device__ __forceinline__ double whole_max(double v) {
     auto step = [](double x, auto move) { return __hiloint2double(move(__double2hiint(x)), move(__double2loint(x))); };
     v = fmax(v, step(v, [](int w) { return dpp_move<DPP_XOR1>(w); }));
     v = fmax(v, step(v, [](int w) { return dpp_move<DPP_XOR2>(w); }));
     v = fmax(v, step(v, [](int w) { return dpp_move<DPP_HALF_MIRROR>(w); }));
-    return fmax(v, step(v, [](int w) { return dpp_move<DPP_MIRROR>(w); }));
-}
-__device__ __forceinline__ double row_sum(double v) {
-    auto step = [](double x, auto move) { return __hiloint2double(move(__double2hiint(x)), move(__double2loint(x))); };
-    v += step(v, [](int w) { return dpp_move<DPP_XOR1>(w); });
-    v += step(v, [](int w) { return dpp_move<DPP_XOR2>(w); });
-    v += step(v, [](int w) { return dpp_move<DPP_HALF_MIRROR>(w); });
-    v += step(v, [](int w) { return dpp_move<DPP_MIRROR>(w); });
-    return v;
-}
-__device__ __forceinline__ int first_of_row(bool has) {      // the lowest of the token's sixteen lanes for which it holds; -1: none
-    return __ffs((int)((uint32_t)(__ballot(has) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu)) - 1;
+    v = fmax(v, step(v, [](int w) { return dpp_move<DPP_MIRROR>(w); }));
+    auto row = [&](int l) { return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l)); };
+    return fmax(fmax(row(0), row(16)), fmax(row(32), row(48)));
 }
 
+// In 64 bits, one token of the wave's four by all of its lanes, of equal values the lowest group and the lowest expert.  The token's lanes get the choices.
 template <int DTYPE, int PER>
-__device__ __forceinline__ void pick_scored(const RouteProblem &q, int64_t t, int (&expert)[2], float (&weight)[2]) {
-    const int lane = threadIdx.x % RT_LANES, n = q.n_experts, e0 = lane * PER;
-    using E = typename Elem<DTYPE>::type;
+__device__ __forceinline__ void choose_exact(const RouteProblem &q, int64_t t, int token, int (&expert)[2]) {
+    const int lane = threadIdx.x % WAVE, n = q.n_experts;
+    const GroupLanes g(WAVE, n, q.groups);
+    const int e0 = g.first_expert(lane), count = g.count(lane, q.groups);
+    float x[PER], bias[PER] = {};
+    own_logits<DTYPE, PER>(q, t, e0, count, x);
+    if (q.bias) neighbours<0, PER>(q.bias, e0, n, bias);
     const double none = -__builtin_inf();
-    auto logit = [&](int i) {
-        return t < q.m && e0 + i < n ? clean(Elem<DTYPE>::load(static_cast<const E *>(q.logits) + t * q.ld, e0 + i)) : -__builtin_inff();
-    };
-    double top = none, total = 1.0;
+    double top = none, total = 0.0, c[PER];
     if (q.softmax) {
-        for (int i = 0; i < PER; ++i) top = fmax(top, (double)logit(i));
-        top = row_max(top);
-        total = 0.0;
-        for (int i = 0; i < PER; ++i) {
-            const double x = logit(i);
-            total += x > none ? exp(x == top ? 0.0 : x - top) : 0.0;
-        }
-        total = row_sum(total);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) top = fmax(top, (double)x[i]);
+        top = whole_max(top);
     }
-    auto score = [&](double x) { return q.softmax ? exp(x == top ? 0.0 : x - top) / total : 1.0 / (1.0 + exp(-x)); };
-    double c[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const double x = logit(i);
-        const double b = q.bias && e0 + i < n ? (double)q.bias[e0 + i] : 0.0;
-        c[i] = x > none && b > none ? score(x) + b : none;
+        c[i] = exp(q.softmax ? (x[i] == top ? 0.0 : x[i] - top) : -(double)x[i]);   // of -inf: 0, and infinity
+        total += c[i];
     }
+    if (q.softmax) total = wave_sum(total);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const double s = (q.softmax ? c[i] : 1.0) / (q.softmax ? total : 1.0 + c[i]);
+        c[i] = x[i] > none && bias[i] > -__builtin_inff() ? s + (double)bias[i] : none;
+    }
+    auto first_lane = [](bool has) { return __ffsll((long long)__ballot(has)) - 1; };
     if (q.groups > 1) {
-        const int each = n / q.groups;
+        double first = none, second = none;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            second = fmax(second, fmin(first, c[i]));
+            first = fmax(first, c[i]);
+        }
+        for (int d = 1; d < g.lanes; d <<= 1) {
+            const double f = __shfl_xor(first, d), z = __shfl_xor(second, d);
+            second = fmax(fmin(first, f), fmax(second, z));
+            first = fmax(first, f);
+        }
+        double value = g.first_lane(lane) != lane ? none : q.group_top > 1 && second > none ? first + second : first;
         unsigned long long kept = 0;
-        double value[RT_GROUP_SLOTS];                                          // of the groups lane, lane + 16, ...
-#pragma unroll
-        for (int h = 0; h < RT_GROUP_SLOTS; ++h) value[h] = none;
-        for (int g = 0; g < q.groups; ++g) {
-            double first = none, second = none;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if ((e0 + i) / each == g) {
-                    second = fmax(second, fmin(first, c[i]));
-                    first = fmax(first, c[i]);
-                }
-            const double best = row_max(first);
-            const int who = first_of_row(first == best && best > none);
-            const double next = row_max(lane == who ? second : first);
-            const double v = q.group_top > 1 && next > none ? best + next : best;
-#pragma unroll
-            for (int h = 0; h < RT_GROUP_SLOTS; ++h)
-                if (g == h * RT_LANES + lane) value[h] = v;
-        }
         for (int j = 0; j < q.top_groups; ++j) {
-            double own = none;
-#pragma unroll
-            for (int h = 0; h < RT_GROUP_SLOTS; ++h) own = fmax(own, value[h]);
-            const double best = row_max(own);
-            int found = 64;                                                    // the lowest group with it
-#pragma unroll
-            for (int h = RT_GROUP_SLOTS - 1; h >= 0; --h)
-                if (value[h] == best && best > none) found = h * RT_LANES + lane;
-            for (int d = 1; d < RT_LANES; d <<= 1) found = min(found, __shfl_xor(found, d, RT_LANES));
-            if (found < 64) kept |= 1ull << found;
-#pragma unroll
-            for (int h = 0; h < RT_GROUP_SLOTS; ++h)
-                if (h * RT_LANES + lane == found) value[h] = none;
+            const double best = whole_max(value);
+            if (!(best > none)) break;
+            const int who = first_lane(value == best);
+            kept |= 1ull << who;
+            if (lane == who) value = none;
         }
+        const bool stays = kept >> g.first_lane(lane) & 1;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (e0 + i >= n || !(kept >> ((e0 + i) / each) & 1)) c[i] = none;
+        for (int i = 0; i < PER; ++i) c[i] = stays ? c[i] : none;
     }
-    double mine[2] = {0.0, 0.0}, sum = 0.0;
-    expert[0] = expert[1] = -1;
+    const bool mine = lane / RT_LANES == token;
+    if (mine) expert[0] = expert[1] = -1;
     for (int j = 0; j < q.k; ++j) {
         double own = c[0];
 #pragma unroll
         for (int i = 1; i < PER; ++i) own = fmax(own, c[i]);
-        const double best = row_max(own);
-        const bool some = best > none;                      // a token that has run out of experts stays so
-        if (!__any(some)) break;
-        const int winner = first_of_row(some && own == best);
+        const double best = whole_max(own);
+        if (!(best > none)) break;
+        const int winner = first_lane(own == best);
         int at = 0;
 #pragma unroll
         for (int i = PER - 1; i >= 0; --i) at = c[i] == best ? i : at;
-        const int who = __shfl(e0 + at, max(winner, 0), RT_LANES);
+        const int who = g.first_expert(winner) + __builtin_amdgcn_readlane(at, winner);
         at = lane == winner ? at : -1;
 #pragma unroll
         for (int i = 0; i < PER; ++i) c[i] = i == at ? none : c[i];
-        if (some) {
-            const double p = score((double)clean(Elem<DTYPE>::load(static_cast<const E *>(q.logits) + t * q.ld, who)));
-            sum += p;
-            if (lane == j % RT_LANES) {
-                expert[j / RT_LANES] = who;
-                mine[j / RT_LANES] = p;
+        if (mine && lane % RT_LANES == j) expert[0] = who;
+        if (mine && lane % RT_LANES + RT_LANES == j) expert[1] = who;
+    }
+}
+
+// The weights of the lane's choices, in 64 bits, off by 1e-9 at most before they are rounded.
+template <int DTYPE>
+__device__ __forceinline__ void weigh(const RouteProblem &q, int64_t t, const int (&expert)[2], float (&weight)[2]) {
+    using E = typename Elem<DTYPE>::type;
+    const E *from = static_cast<const E *>(q.logits) + min(t, (int64_t)q.m - 1) * q.ld;
+    const int lane = threadIdx.x % RT_LANES;
+    double top = 0.0, total = 1.0;
+    if (q.softmax) {
+        float most = -__builtin_inff();
+        for (int e = lane; e < q.n_experts; e += RT_LANES) most = fmaxf(most, clean(Elem<DTYPE>::load(from, e)));
+        top = value_of(row_max(key_of(most)));
+        if (!q.renormalise) {
+            total = 0.0;
+            for (int e = lane; e < q.n_experts; e += RT_LANES) {
+                const double x = clean(Elem<DTYPE>::load(from, e));
+                total += x > -__builtin_inf() ? exp(x == top ? 0.0 : x - top) : 0.0;
             }
+            total = row_sum(total);
         }
     }
-    const double whole = q.renormalise ? sum : 1.0;
-    for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 && whole > 0.0 ? (float)(mine[h] / whole * (double)q.scale) : 0.0f;
+    double s[2] = {0.0, 0.0};
+    for (int h = 0; h < (q.k > RT_LANES ? 2 : 1); ++h)
+        if (expert[h] >= 0) {
+            const double x = clean(Elem<DTYPE>::load(from, expert[h])), e = q.softmax ? (x == top ? 0.0 : x - top) : -x;
+            if (__any(fabs(e) > 600.0)) {                   // what 64 bits no longer hold
+                const double p = exp(e);
+                s[h] = (q.softmax ? p : 1.0) / (q.softmax ? total : 1.0 + p);
+            } else {
+                const double p = exp_near(e);
+                s[h] = (q.softmax ? p : 1.0) * inverse_near(q.softmax ? total : 1.0 + p);
+            }
+        }
+    const double sum = q.renormalise ? row_sum(s[0] + s[1]) : 1.0;
+    const double factor = (double)q.scale / sum;
+    for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 && sum > 0.0 ? (float)(s[h] * factor) : 0.0f;
+}
+
+// FAST: groups that sixteen lanes have room for, PER experts a lane; otherwise every token in 64 bits.
+template <int DTYPE, int PER, bool FAST>
+__device__ __forceinline__ void pick_scored(const RouteProblem &q, int64_t t, int (&expert)[2], float (&weight)[2]) {
+    bool certain = false;
+    float first = 0.0f;                                     // the token's largest logit
+    expert[0] = expert[1] = -1;
+    if (FAST && !q.bias && q.groups == 1) {                 // the scores order as the logits do
+        pick<DTYPE, PER>(q, t, expert, weight);
+        // but where 64 bits no longer tell them apart: e^-16 times the last place of an fp32 number below 16 is 1e-13, and beyond 700 there is nothing
+        bool plain = true;
+        for (int h = 0; h < (q.k > RT_LANES ? 2 : 1); ++h) {
+            const int e = max(expert[h], 0);
+            const float x = clean(Elem<DTYPE>::load(static_cast<const typename Elem<DTYPE>::type *>(q.logits) + min(t, (int64_t)q.m - 1) * q.ld, e));
+            const float top = __shfl(h == 0 ? x : 0.0f, 0, RT_LANES), from = h == 0 ? top : first;
+            first = from;
+            plain = plain && (expert[h] < 0 || (q.softmax ? x - from > -700.0f : x > -700.0f && x < 16.0f));
+        }
+        certain = all_of_row(plain);
+    } else if (FAST) {
+        certain = choose_fast<DTYPE, PER>(q, t, expert);
+    }
+    const unsigned long long doubt = __ballot(!certain && t < q.m);
+    const int64_t t0 = t - threadIdx.x % WAVE / RT_LANES;
+    for (int token = 0; token < RT_GROUPS; ++token)
+        if (doubt >> (token * RT_LANES) & 1) choose_exact<DTYPE, (PER + 3) / 4>(q, t0 + token, token, expert);
+    weigh<DTYPE>(q, t, expert, weight);
 }
 
 // ---- order ----------------------------------------------------------------------------------------------------------------
@@ -275,7 +479,8 @@ __device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
     return before;
 }
 
-template <int DTYPE, int PER, bool SCORED, bool ALONE>
+// SCORED: 0 by the logits, 1 by scores, 2 by scores, in 64 bits at once.
+template <int DTYPE, int PER, int SCORED, bool ALONE>
 __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
     extern __shared__ uint32_t rt_lds[];                    // [RT_WAVES][n_experts]: counts, then what comes before them
     __shared__ uint32_t all;
@@ -290,7 +495,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
     if (t0 < t1) {
         int expert[2];
         float weight[2];
-        if constexpr (SCORED) pick_scored<DTYPE, PER>(q, t0 + lane / RT_LANES, expert, weight);
+        if constexpr (SCORED != 0) pick_scored<DTYPE, PER, SCORED == 1>(q, t0 + lane / RT_LANES, expert, weight);
         else pick<DTYPE, PER>(q, t0 + lane / RT_LANES, expert, weight);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -491,7 +696,7 @@ __global__ __launch_bounds__(CB_THREADS) void k_combine(const void *Y, int64_t y
     }
 }
 
-template <int DTYPE, int PER, bool SCORED> hipError_t launch_pick(const RouteProblem &q, int blocks) {
+template <int DTYPE, int PER, int SCORED> hipError_t launch_pick(const RouteProblem &q, int blocks) {
     const size_t lds = ((size_t)RT_WAVES + 1) * q.n_experts * 4;
     static MoreLds alone, together;
     const hipError_t e = blocks == 1 ? alone.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, SCORED, true>), 80 * 1024)
@@ -501,12 +706,14 @@ template <int DTYPE, int PER, bool SCORED> hipError_t launch_pick(const RoutePro
     else k_route_pick<DTYPE, PER, SCORED, false><<<blocks, RT_THREADS, lds, q.stream>>>(q);
     return hipGetLastError();
 }
-template <int DTYPE, bool SCORED> hipError_t launch_pick(const RouteProblem &q, int blocks) {
-    if (q.n_experts <= 16) return launch_pick<DTYPE, 1, SCORED>(q, blocks);
-    if (q.n_experts <= 64) return launch_pick<DTYPE, 4, SCORED>(q, blocks);
-    if (q.n_experts <= 128) return launch_pick<DTYPE, 8, SCORED>(q, blocks);
-    if (q.n_experts <= 256) return launch_pick<DTYPE, 16, SCORED>(q, blocks);
-    if (q.n_experts <= 512) return launch_pick<DTYPE, 32, SCORED>(q, blocks);
+template <int DTYPE, int SCORED> hipError_t launch_pick(const RouteProblem &q, int blocks) {
+    const int per = SCORED == 0 ? (q.n_experts + RT_LANES - 1) / RT_LANES : SCORED == 1 ? GroupLanes(RT_LANES, q.n_experts, q.groups).per : 4 * GroupLanes(WAVE, q.n_experts, q.groups).per;
+    if (per <= 1) return launch_pick<DTYPE, 1, SCORED>(q, blocks);
+    if (per <= 4) return launch_pick<DTYPE, 4, SCORED>(q, blocks);
+    if (per <= 8) return launch_pick<DTYPE, 8, SCORED>(q, blocks);
+    if (per <= 16) return launch_pick<DTYPE, 16, SCORED>(q, blocks);
+    if (per <= 32) return launch_pick<DTYPE, 32, SCORED>(q, blocks);
+    if (SCORED == 2 && per > 64) return launch_pick<DTYPE, SCORED == 2 ? 128 : 64, SCORED>(q, blocks);
     return launch_pick<DTYPE, 64, SCORED>(q, blocks);
 }
 
@@ -529,8 +736,10 @@ size_t route_workspace_bytes(int m, int n_experts, int) {
 hipError_t launch_route(const RouteProblem &q) {
     const int blocks = q.m <= RT_TOKENS ? 1 : (q.m + RT_TOKENS - 1) / RT_TOKENS;
     hipError_t e;
-    if (q.scored) e = q.dtype == 0 ? launch_pick<0, true>(q, blocks) : launch_pick<1, true>(q, blocks);
-    else e = q.dtype == 0 ? launch_pick<0, false>(q, blocks) : launch_pick<1, false>(q, blocks);
+    const GroupLanes g(RT_LANES, q.n_experts, q.groups);
+    if (!q.scored) e = q.dtype == 0 ? launch_pick<0, 0>(q, blocks) : launch_pick<1, 0>(q, blocks);
+    else if (g.lanes >= 1 && g.per <= 32) e = q.dtype == 0 ? launch_pick<0, 1>(q, blocks) : launch_pick<1, 1>(q, blocks);
+    else e = q.dtype == 0 ? launch_pick<0, 2>(q, blocks) : launch_pick<1, 2>(q, blocks);
     if (e != hipSuccess || blocks == 1) return e;
     int lanes = WAVE;
     while (lanes * 4 < q.n_experts) lanes *= 2;

@@ -173,6 +173,10 @@ def test_closed_experts_and_special_values(dtype, scores, n, groups):
     x[10] = -0.0
     x[11, :] = -800.0                                         # below all sigmoids of 64 bits
     x[12, 3:] = -INF
+    x[13] = 30 + torch.rand(n, generator=g) * 10              # sigmoids that 64 bits cannot tell apart: the lowest expert
+    x[14] = -760 + torch.rand(n, generator=g) * 30
+    x[15] = torch.linspace(-900, 0, n)
+    x[16] = 15 + torch.rand(n, generator=g) * 2
     x[40:50] = -INF
     x = x.to(dtype)
     bias = 0.3 * torch.randn(n, generator=g)
