@@ -594,12 +594,12 @@ int qamw_combine(const void *Y, int dtype, int y_rows, int64_t ldy, const int32_
  * 2 = the central cells in LDS whatever the size.  qamw_matmul / qamw_matmul_batch with one or two
  * activation rows: 0 = chosen by the size of the launch, 1 = activations rotated by a launch of their
  * own, 2 = rotated inside the product kernel; the results are the same, bit for bit.
- * qamw_int8_matmul of codes / qamw_grouped_matmul: 0, 1 and 2 = chosen by an estimate of the time (qamw_product_plan),
+ * qamw_int8_matmul of codes / qamw_grouped_matmul / the products in 4 bits: 0, 1 and 2 = chosen by an estimate of the time (qamw_product_plan),
  * 64, 128 and 256 = the kernel for many rows by tiles of so many, where the operands are whole 16 bytes: in int8 the
- * same bits, in bf16 sums in another order.  All other entry points take 64, 128 and 256 as 0.
+ * same bits, in bf16 and in 4 bits sums in another order.  All other entry points take 64, 128 and 256 as 0.
  * This is the library's ONE piece of process-wide state: an atomic integer, safe to set from any thread, but it
  * affects every call of every thread made afterwards -- a switch for tests and measurements, not for production code
- * (all settings give the same results, but for the order of those bf16 sums).  Returns the previous value (also
+ * (all settings give the same results, but for the order of those sums).  Returns the previous value (also
  * for a value out of range, which changes nothing). */
 int qamw_set_kernel_path(int path);
 

@@ -152,10 +152,16 @@ struct Cost {
     int rows;
     double tile, stage;                                    // us, and bytes a us / us for 128 bytes of columns
 };
-constexpr double LAUNCH = 3.3, MEMORY = 7.3e6, PARTS = 2.2, PARTS_RATE = 6.5e6, FEW_X = 0.45, FEW_W = 0.15, WIDE_X = 0.12;
+constexpr double LAUNCH = 3.3, MEMORY = 7.3e6, PARTS = 2.2, PARTS_RATE = 6.5e6, FEW_W = 0.15, WIDE_X = 0.12;
 constexpr Off FEW_OFF = {1.3, 1.45}, WIDE_OFF = {1.23, 1.23};
-constexpr Cost FEW[3] = {{16, 0.4, 9.4e4}, {32, 0.4, 9.9e4}, {64, 0.4, 8.0e4}}, WIDE[3] = {{64, 2.9, 0.72}, {128, 3.8, 0.83}, {256, 5.9, 1.12}};
-constexpr double FEW_GATED_64 = 0.75;                      // of the rate: the ring is two units then
+struct Costs {
+    Cost few[3], wide[3];
+    double few_gated_64, few_x;                            // the first of the rate: the ring is two units then
+};
+constexpr Costs BYTES = {{{16, 0.4, 9.4e4}, {32, 0.4, 9.9e4}, {64, 0.4, 8.0e4}}, {{64, 2.9, 0.72}, {128, 3.8, 0.83}, {256, 5.9, 1.12}}, 0.75, 0.45};
+// In 4 bits, with the scales beside them, of 163 shapes of 1 to 32768 rows, 1 to 128 experts, 700 to 27648 outputs and 333 to 13824 columns: the choice 1 % slower
+// than the fastest in the mean (2 % by the figures above), a fifth at worst.
+constexpr Costs MX4 = {{{16, 0.4, 8.5e4}, {32, 0.4, 9.9e4}, {64, 0.47, 5.9e4}}, {{64, 3.1, 0.63}, {128, 3.0, 0.96}, {256, 4.1, 1.12}}, 0.9, 0.6};
 
 // groups: how many have rows, at most; row tiles are expected to be half a tile short.
 Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, bool gated, int kind, bool may_part) {
@@ -176,19 +182,20 @@ Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, 
     };
     auto rounds = [](double blocks) { return blocks <= 256 ? 1.0 : blocks <= 1024 ? (double)(((int64_t)blocks + 255) / 256) : blocks / 256 + 0.5; };
     auto xcds = [](double readers) { return readers < 1 ? 1 : readers > 8 ? 8 : readers; };
+    const Costs &costs = kind == PRODUCT_MX4 ? MX4 : BYTES;
     Plan best = {true, 64, 1, 1e30};
     auto offer = [&](bool few, int rows, int parts, double us) {
         if (us < best.us) best = {few, rows, parts, us};
     };
-    for (const Cost &c : FEW) {
+    for (const Cost &c : costs.few) {
         const double mine = row_tiles(c.rows), cols = (double)((d_out + 15) / 16), tiles = groups * mine * cols;
         const int split = few_split((int64_t)tiles, (int)units, 4);
-        const double slot = 2048.0 * ((gated ? 2 : 1) + c.rows / 16), rate = gated && c.rows == 64 ? c.stage * FEW_GATED_64 : c.stage;
+        const double slot = 2048.0 * ((gated ? 2 : 1) + c.rows / 16), rate = gated && c.rows == 64 ? c.stage * costs.few_gated_64 : c.stage;
         const double work = rounds(tiles * split / 4) * (c.tile + units * 4 / split * slot / rate);
-        offer(true, c.rows, 1, time(work, w_bytes * (1 + FEW_W * (mine - 1)) + x_bytes * FEW_X * xcds(cols * split / 4), FEW_OFF));
+        offer(true, c.rows, 1, time(work, w_bytes * (1 + FEW_W * (mine - 1)) + x_bytes * costs.few_x * xcds(cols * split / 4), FEW_OFF));
     }
     const double cols = (double)((outs + 255) / 256);
-    for (const Cost &c : WIDE)
+    for (const Cost &c : costs.wide)
         for (int parts : {1, 2, 3, 4, 6, 8}) {
             if (parts > 1 && (!may_part || units < parts * 4)) break;
             const double work = rounds(groups * row_tiles(c.rows) * cols * parts) * (c.tile + (double)units / parts * c.stage);

@@ -132,7 +132,8 @@ int qamw_product_plan(int dtype, int m, int n_experts, int d_out, int d_in, int 
         return QAMW_ERR_INVALID_ARG;
     if (dtype != QAMW_DTYPE_I8 && (dtype != QAMW_DTYPE_BF16 || n_experts == 0)) return QAMW_ERR_INVALID_ARG;
     int plan[3];
-    qamw::product_plan(m, n_experts, n_experts > 0, d_out, d_in, gated != 0, dtype == QAMW_DTYPE_I8 ? qamw::PRODUCT_I8 : qamw::PRODUCT_BF16, n_experts == 0, plan);
+    qamw::product_plan(m, n_experts, n_experts > 0, d_out, d_in, gated != 0, dtype == QAMW_DTYPE_I8 ? qamw::PRODUCT_I8 : qamw::PRODUCT_BF16, n_experts == 0,
+                       plan);
     for (int i = 0; i < 3; ++i) plan_out[i] = plan[i];
     return QAMW_OK;
 }
