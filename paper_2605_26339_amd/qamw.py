@@ -842,11 +842,14 @@ def _launch(dev, name, *args):
     """A device entry point on the device of its tensors, whichever is the current one."""
     import torch
 
-    call = getattr(lib(), name)
+    call = getattr(_lib or lib(), name)
     if dev == torch._C._cuda_getDevice():
-        return _check(call(*args), name)
-    with torch.cuda.device(dev):
-        return _check(call(*args), name)
+        status = call(*args)
+    else:
+        with torch.cuda.device(dev):
+            status = call(*args)
+    if status != OK:
+        raise QamwError(status, name)
 
 
 _SCORES = {"sigmoid": 0, "softmax": 1}
@@ -905,17 +908,17 @@ def mx4_row_bytes(d: int):
 
 
 def _mx4(q, name, dims=2):
-    """The rows and columns of an Mx4 that is whole, for experts their number too."""
+    """(rows, columns) of an Mx4 that is whole; with three dimensions (experts, rows, columns)."""
     import torch
 
     codes, scales, d = q
-    shape = codes.shape
-    if len(shape) != dims:
-        raise ValueError(f"{name} must have codes of {dims} dimensions")
-    code_bytes, scale_bytes = mx4_row_bytes(d)
-    _vector(codes, f"{name}.codes", torch.uint8, (*shape[:-1], code_bytes))
-    _vector(scales, f"{name}.scales", torch.uint8, (*shape[:-1], scale_bytes))
-    return (*shape[:-1], d)
+    shape, of_scales, u8 = codes.shape, scales.shape, torch.uint8
+    if len(shape) == dims and len(of_scales) == dims and codes.dtype == u8 and scales.dtype == u8 and codes.is_contiguous() and scales.is_contiguous():
+        code_bytes, scale_bytes = mx4_row_bytes(d)
+        if shape[-1] == code_bytes and of_scales[-1] == scale_bytes and shape[0] == of_scales[0] and (dims == 2 or shape[1] == of_scales[1]):
+            return (shape[0], d) if dims == 2 else (shape[0], shape[1], d)
+    raise ValueError(f"{name} must be contiguous uint8 codes and scales of {dims} dimensions, for rows of {d} columns, got {codes.dtype} {tuple(shape)} and "
+                     f"{scales.dtype} {tuple(of_scales)}")
 
 
 def mx4_quantize(X, col_scale=None, out=None, stream=None):
@@ -954,16 +957,18 @@ def mx4_matmul_workspace_bytes(x_dtype: int, x_rows: int, m: int, n_experts: int
 
 
 def _mx4_operand(X, d_in, col_scale):
-    """(address, type, address of the scales, rows, leading dimension, tensors) of the left operand, an Mx4 or floating."""
+    """(address, type, address of the scales, rows, leading dimension, a tensor, the scales) of the left operand, an Mx4 or floating."""
     import torch
 
-    _vector(col_scale, "col_scale", torch.float32, (d_in,))
+    if col_scale is not None:
+        _vector(col_scale, "col_scale", torch.float32, (d_in,))
     if isinstance(X, Mx4):
         m, d = _mx4(X, "X")
-        at = (X[0].data_ptr(), DTYPE_MX4, X[1].data_ptr(), m, 0, X[0])
+        x, scales = X[0], X[1]
+        at = (x.data_ptr(), DTYPE_MX4, scales.data_ptr(), m, 0, x, scales)
     else:
         m, d, ldx = _rows(X, "X")
-        at = (X.data_ptr(), _dtype_code(X), None, m, ldx, X)
+        at = (X.data_ptr(), _dtype_code(X), None, m, ldx, X, None)
     if d != d_in:
         raise ValueError(f"X and W must have as many columns, got {d} and {d_in}")
     return at
@@ -975,8 +980,10 @@ def _mx4_work(need, like, workspace, stream):
 
     if workspace is not None:
         return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
-    work = _new(1, need, torch.uint8, like, stream) if need else None
-    return _ptr(work), need, work
+    if not need:
+        return None, 0, None
+    work = _new(1, need, torch.uint8, like, stream)
+    return work.data_ptr(), need, work
 
 
 def mx4_matmul(X, W, col_scale=None, gated=False, out=None, out_dtype=None, workspace=None, stream=None):
@@ -984,20 +991,20 @@ def mx4_matmul(X, W, col_scale=None, gated=False, out=None, out_dtype=None, work
     (col_scale [d_in] multiplies its columns first).  gated: W has the gate's rows, then the up projection's, and Y = silu(gate) * up.
     Returns [m][d_out] of out_dtype (bf16 where neither it nor out is given)."""
     outs, d_in = _mx4(W, "W")
-    x_at, code, xs_at, m, ldx, x = _mx4_operand(X, d_in, col_scale)
+    x_at, code, xs_at, m, ldx, x, xs = _mx4_operand(X, d_in, col_scale)
     if outs < 1 or (gated and outs % 2):
         raise ValueError(f"W must have {'2 d_out' if gated else 'd_out'} rows, got {outs}")
-    dev = _one_device(x, X[1] if code == DTYPE_MX4 else None, W[0], W[1], col_scale, out, workspace)
+    w, ws = W[0], W[1]
+    dev = _one_device(x, xs, w, ws, col_scale, out, workspace)
     d_out = outs // 2 if gated else outs
     y, y_code, ldy = _result(out, m, d_out, out_dtype, x, stream)
-    w_at, c_at = W[0].data_ptr(), _ptr(col_scale)
-    if (workspace is None and code != DTYPE_MX4 and m * -(-d_in // 4096) <= 4 and not (x_at | (c_at or 0) | d_in * 2 | ldx * x.element_size()) & 15
-            and W[0].numel() < 0x7FFFFE00 and ldx <= 1 << 24):
-        at = size = _work = None                                  # the product's own launch quantises the rows
-    else:
+    c_at, at, size, _work = None if col_scale is None else col_scale.data_ptr(), None, 0, None
+    # not where the product's own launch quantises the rows
+    if (workspace is not None or code == DTYPE_MX4 or m * -(-d_in // 4096) > 4 or (x_at | (c_at or 0) | d_in * 2 | ldx * x.element_size()) & 15
+            or w.numel() >= 0x7FFFFE00 or ldx > 1 << 24):
         at, size, _work = _mx4_work(mx4_matmul_workspace_bytes(code, m, m, 0, d_out, d_in, bool(gated)), x, workspace, stream)
-    _launch(dev, "qamw_mx4_matmul", x_at, code, xs_at, c_at, m, ldx, w_at, W[1].data_ptr(), d_out, d_in, 1 if gated else 0,
-            y.data_ptr(), y_code, ldy, at, size or 0, _raw_stream(stream, dev))
+    _launch(dev, "qamw_mx4_matmul", x_at, code, xs_at, c_at, m, ldx, w.data_ptr(), ws.data_ptr(), d_out, d_in, 1 if gated else 0,
+            y.data_ptr(), y_code, ldy, at, size, _raw_stream(stream, dev))
     return y
 
 
@@ -1009,13 +1016,13 @@ def mx4_grouped_matmul(X, W, offsets, rows=None, col_scale=None, gated=False, ou
     import torch
 
     n, outs, d_in = _mx4(W, "W", 3)
-    x_at, code, xs_at, x_rows, ldx, x = _mx4_operand(X, d_in, col_scale)
+    x_at, code, xs_at, x_rows, ldx, x, xs = _mx4_operand(X, d_in, col_scale)
     if n < 1 or outs < 1 or (gated and outs % 2):
         raise ValueError(f"W must be [n_experts][{'2 d_out' if gated else 'd_out'}] rows, got {(n, outs)}")
     m = x_rows if rows is None else rows.numel()
     _vector(offsets, "offsets", torch.int32, (n + 1,))
     _vector(rows, "rows", torch.int32, (m,))
-    dev = _one_device(x, X[1] if code == DTYPE_MX4 else None, W[0], W[1], col_scale, offsets, rows, out, workspace)
+    dev = _one_device(x, xs, W[0], W[1], col_scale, offsets, rows, out, workspace)
     d_out = outs // 2 if gated else outs
     y, y_code, ldy = _result(out, m, d_out, out_dtype, x, stream)
     at, size, _work = _mx4_work(mx4_matmul_workspace_bytes(code, x_rows, m, n, d_out, d_in, bool(gated)), x, workspace, stream)
@@ -1035,26 +1042,26 @@ def block_norm(h, weight=None, block=None, block_weight=None, gate=None, scale: 
     import torch
 
     m, d, ldh = _rows(h, "h")
-    code = _dtype_code(h)
-    _vector(weight, "weight", torch.float32, (d,))
-    _vector(block_weight, "block_weight", torch.float32, (d,))
+    code, dtype, f32, shape, of_columns = _dtype_code(h), h.dtype, torch.float32, (m, d), (d,)
+    _vector(weight, "weight", f32, of_columns)
+    _vector(block_weight, "block_weight", f32, of_columns)
     ldb = ldg = ldho = 0
     if block is None:
         if block_weight is not None or gate is not None or h_out is not None:
             raise ValueError("block_weight, gate and h_out come with a block")
     else:
-        if block.dtype != h.dtype or block.shape != (m, d):
+        if block.dtype != dtype or block.shape != shape:
             raise ValueError(f"block must be {h.dtype} of shape {(m, d)}, got {block.dtype} {tuple(block.shape)}")
         ldb = _rows(block, "block")[2]
         if gate is not None:
-            if gate.dtype != h.dtype or gate.shape not in ((d,), (m, d)):
-                raise ValueError(f"gate must be {h.dtype} of shape {(d,)} or {(m, d)}, got {gate.dtype} {tuple(gate.shape)}")
             if gate.dim() == 1:
-                _vector(gate, "gate", h.dtype, (d,))
+                _vector(gate, "gate", dtype, of_columns)
+            elif gate.dtype != dtype or gate.shape != shape:
+                raise ValueError(f"gate must be {dtype} of shape {of_columns} or {shape}, got {gate.dtype} {tuple(gate.shape)}")
             else:
                 ldg = _rows(gate, "gate")[2]
         if h_out is None:
-            h_out, ldho = _new(m, d, h.dtype, h, stream), d
+            h_out, ldho = _new(m, d, dtype, h, stream), d
         else:
             if h_out.dtype != h.dtype or h_out.shape != (m, d):
                 raise ValueError(f"h_out must be {h.dtype} of shape {(m, d)}, got {h_out.dtype} {tuple(h_out.shape)}")
