@@ -1,9 +1,10 @@
 """A routed feed-forward layer served from packed experts.
 
 Every expert's matrices are coded by the codec, as they would be stored; to serve them they are decoded to bf16 and, for the 8-bit
-layer, quantised once more to 8-bit integers with a scale for each output channel.  A pass is: logits to experts, tokens to 8
-bits, the gate and up projections of the chosen experts with silu(gate) * up, that to 8 bits, the down projections, and the weighted
-sum back to the tokens.
+layer, quantised once more to 8-bit integers with a scale for each output channel, or for the 4-bit one to 4-bit floats with a
+scale for every 32 columns.  A pass is: logits to experts, tokens to 8 or 4 bits, the gate and up projections of the chosen experts with
+silu(gate) * up, that to 8 or 4 bits, the down projections, and the weighted sum back to the tokens.  `routed_block` has the norms around it,
+too, and chooses experts by sigmoid scores with a bias, from the best groups.
 
     python examples/routed_layer.py [--tokens 256] [--experts 16] [--choices 2] [--width 2048] [--hidden 1024]
 """
@@ -41,10 +42,33 @@ def in_8_bits(experts):
     return Experts(codes.view(n, outs, ins), scales.view(n, outs))
 
 
+def in_4_bits(experts):
+    """The same experts in 4-bit floating point."""
+    n, outs, ins = experts.weights.shape
+    q = qamw.mx4_quantize(experts.weights.view(n * outs, ins))
+    return qamw.Mx4(q.codes.view(n, outs, -1), q.scales.view(n, outs, -1), ins)
+
+
+def routed_block(h, norm_weight, router, bias, up, down, choices, groups, top_groups, next_weight, gate=None):
+    """A block in 4 bits with the norms around it: h [tokens][width] bf16 is the stream, router [experts][width], bias [experts] fp32, up
+    and down as routed_layer takes them.  Returns the stream after the block and, in 4 bits, the norm of it that the next block takes."""
+    _, x = qamw.block_norm(h, norm_weight)
+    r = qamw.route_scored(x @ router.t(), choices, bias=bias, groups=groups, top_groups=top_groups)
+    y = experts_in_4_bits(x, r, up, down)
+    return qamw.block_norm(h, next_weight, block=y, gate=gate, quantize="mx4")
+
+
+def experts_in_4_bits(x, r, up, down):
+    h = qamw.mx4_grouped_matmul(x, up, r.offsets, rows=r.rows, gated=True)      # the tokens once, however many experts they have
+    return qamw.combine(qamw.mx4_grouped_matmul(h, down, r.offsets), r.positions, r.weights)
+
+
 def routed_layer(x, logits, up, down, choices):
     """x [tokens][width] bf16, logits [tokens][experts]; up [n][2 hidden][width] (gates, then up projections), down [n][width][hidden],
-    both in 8 bits or both in bf16.  Returns [tokens][width] bf16."""
+    both in 4 bits, in 8 bits or in bf16.  Returns [tokens][width] bf16."""
     r = qamw.route(logits, choices)
+    if isinstance(up, qamw.Mx4):
+        return experts_in_4_bits(x, r, up, down)
     if up.scales is None:
         h = qamw.grouped_matmul(x, up.weights, r.offsets, rows=r.rows, gated=True)
         y = qamw.grouped_matmul(h, down.weights, r.offsets)
@@ -74,11 +98,11 @@ def main():
     ap.add_argument("--hidden", type=int, default=1024)
     a = ap.parse_args()
     router, up, down = build(a.experts, a.width, a.hidden)
-    up8, down8 = in_8_bits(up), in_8_bits(down)
+    up8, down8, up4, down4 = in_8_bits(up), in_8_bits(down), in_4_bits(up), in_4_bits(down)
     x = torch.randn(a.tokens, a.width, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").bfloat16()
     logits = x @ router.t()
     results = {}
-    for name, u, d in (("bf16", up, down), ("8 bits", up8, down8)):
+    for name, u, d in (("bf16", up, down), ("8 bits", up8, down8), ("4 bits", up4, down4)):
         for _ in range(3):
             results[name] = routed_layer(x, logits, u, d, a.choices)
         torch.cuda.synchronize()
@@ -92,11 +116,13 @@ def main():
         for _ in range(20):
             graph.replay()
         torch.cuda.synchronize()
-        size = sum(e.weights.numel() * e.weights.element_size() for e in (u, d))
+        size = sum(e[0].numel() * e[0].element_size() for e in (u, d))
         print(f"{name}: {(time.perf_counter() - t) / 20 * 1e6:.0f} us a pass, {size / 1e6:.0f} MB of weights")
-    off = (results["8 bits"].float() - results["bf16"].float()).norm() / results["bf16"].float().norm()
-    print(f"8 bits against bf16: relative difference {off:.4f}")
-    return float(off)
+    off = {}
+    for name in ("4 bits", "8 bits"):
+        off[name] = float((results[name].float() - results["bf16"].float()).norm() / results["bf16"].float().norm())
+        print(f"{name} against bf16: relative difference {off[name]:.4f}")
+    return off["8 bits"]
 
 
 if __name__ == "__main__":
