@@ -68,6 +68,8 @@ def test_refusals_of_the_entry_points():
     assert mm(**five, work=None, n=0) == I and mm(**five, n=64) == I and mm(**five, work=p + 8) == I
     assert mm(xt=1, xs=None, ldx=7) == S and mm(ldy=7) == S
     assert mm(m=1 << 22, d_out=1 << 24, ldy=1 << 24) == U                  # more tiles than a launch has
+    assert mm(d_out=1 << 16, d_in=131072, ldy=1 << 16) == U                # more than 2 GiB of codes
+    assert mm(**five, d_out=1 << 16, d_in=131072, ldx=131072, ldy=1 << 16) == U
     assert mm(m=0, X=None, xs=None, W=None, ws=None, Y=None, work=None, n=0) == qamw.OK
 
     def grouped(X=p, t=3, xs=p, cs=None, xr=4, ldx=8, rows=None, W=p, ws=p, off=p, n=2, m=4, d_out=8, d_in=8, gated=0, Y=p, yt=1, ldy=8, work=p, size=1 << 30):
@@ -75,6 +77,7 @@ def test_refusals_of_the_entry_points():
 
     assert grouped(n=0) == I and grouped(n=-1) == I and grouped(n=1025) == I and grouped(off=None) == I and grouped(off=p + 2) == I and grouped(rows=p + 1) == I
     assert grouped(xr=3) == S and grouped(rows=p, xr=0) == S and grouped(ldy=7) == S and grouped(t=0) == I and grouped(t=0, xs=None, size=0) == I
+    assert grouped(rows=p, xr=1 << 20, d_in=131072) == U                   # gathered from more than 2 GiB
     assert grouped(m=0, X=None, xs=None, W=None, ws=None, off=None, Y=None, work=None, size=0) == qamw.OK
 
 

@@ -146,6 +146,9 @@ def test_values_next_to_each_other(scores, groups, top):
         else:
             x[t] = (0.5 + (step[order] - 20) * 2.0**-23).float()
     bias = (torch.randperm(n, generator=g).double() * 2.0**-33 + 2.0**-12).float()
+    x[70] = 1e-20 * (1 + torch.randperm(n, generator=g))      # equal in 64 bits: the lowest experts, whatever the logits' order
+    x[71, 10:] = -1e-25 * (1 + torch.arange(n - 10))
+    x[72] = 20 + torch.randperm(n, generator=g) * 2.0**-19
     for b in (None, bias, bias * 0 + 0.25):
         want = reference(x, 6, scores, b, groups, top, 2, True, 1.0)
         check(qamw.route_scored(x.to(DEV), 6, scores=scores, bias=None if b is None else b.to(DEV), groups=groups, top_groups=top), x, 6, n, want)
