@@ -531,7 +531,7 @@ int qamw_mx4_grouped_matmul(const void *X, int x_dtype, const uint8_t *x_scales,
  *   h_out = h + scale * b'', a fused multiply-add, rounded to dtype;  x = h_out / sqrt(mean(h_out^2) + eps) * weight (weight NULL: ones)
  * in fp32, the sums of squares too.  block NULL: h_out is h, and x its norm; block_weight, gate and h_out are NULL then.
  *   h, block, gate, h_out  device, rows of d elements of dtype (F32 or BF16) with leading dimensions ldh, ldb, ldg, ldho; ldg = 0: one row for all.
- *      h_out may be h or block, with its leading dimension
+ *      h_out may be h or block, and x may be block, or h where block is NULL, with its type and leading dimension
  *   weight, block_weight  device, d floats
  *   x  x_dtype F32 or BF16: m rows of d, leading dimension ldx, x_scales NULL.  I8: rows as by qamw_int8_quantize of the fp32 values, x_scales m
  *      floats.  MX4: rows as by qamw_mx4_quantize of them (ldx is not looked at), x_scales their scales

@@ -248,7 +248,8 @@ __device__ __forceinline__ bool choose_fast(const RouteProblem &q, int64_t t, in
         const uint32_t u = (uint32_t)__double2loint(fma(c[i] + (double)bias[i], units, from));   // as a whole number
         v[i] = x[i] > -__builtin_inff() ? (u & ~INDEX) | (INDEX - i) : 0;
     }
-    bool certain = high < __builtin_inff();
+    // sums of a bias 2^17 times the range are rounded by a sixteenth of a unit, and those of a larger one might be to either side of it
+    bool certain = high < low || (high < __builtin_inff() && fmaxf(fabsf(low), fabsf(high)) * 0x1p-17f <= high - low + 8.0f);
     auto apart = [&](uint32_t a, uint32_t b, uint32_t by) { certain = certain && (b == 0 || a / PER - b / PER > by); };
     if (q.groups > 1) {
         uint32_t first = 0, second = 0;

@@ -201,3 +201,42 @@ def test_stream_and_graph():
         torch.cuda.synchronize()
         assert torch.equal(h_out, e) and torch.equal(q.codes, y.codes) and torch.equal(q.scales, y.scales)
         assert torch.equal(qamw.block_norm(hs[1], w, block=b, block_weight=w)[0], want[1][0])
+
+
+@gpu
+@pytest.mark.parametrize("m,d", [(3, 5), (70, 33), (40, 256), (9, 4100), (5, 8200), (2, 16385)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_norm_in_place(m, d, dtype):
+    """The norm over the stream that it is of, and over the block's output."""
+    say(f"[norm] in place {m}x{d} {dtype}")
+    g = _gen(d)
+    h, b, w = torch.randn(m, d, generator=g).to(dtype).to(DEV), torch.randn(m, d, generator=g).to(dtype).to(DEV), torch.rand(d, generator=g).to(DEV)
+    want = qamw.block_norm(h, w)[1]
+    hs, x = qamw.block_norm(h, w, block=b, block_weight=w, scale=0.5)
+    into = b.clone()
+    h2, x2 = qamw.block_norm(h, w, block=into, block_weight=w, scale=0.5, out=into)
+    assert x2 is into and torch.equal(h2, hs) and torch.equal(x2, x)
+    assert torch.equal(qamw.block_norm(h, w, out=h)[1], want) and torch.equal(h, want)
+
+
+@gpu
+def test_rows_far_apart():
+    """Rows that begin more than 2^31 values apart."""
+    say("[norm] rows far apart")
+    g, d, apart = _gen(2), 4100, 2**30 + 2**29 + 8
+    want = torch.randn(3, d, generator=g).bfloat16().to(DEV)
+    far = torch.as_strided(torch.empty(2 * apart + d, dtype=torch.bfloat16, device=DEV), (3, d), (apart, 1))
+    far.copy_(want)
+    assert torch.equal(qamw.block_norm(far)[1], qamw.block_norm(want)[1])
+    a, b = qamw.mx4_quantize(far), qamw.mx4_quantize(want)
+    assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales)
+    near_by = qamw.block_norm(want, block=want, gate=want, quantize="mx4")
+    for h_out in (None, far):
+        h, q = qamw.block_norm(far, block=far, gate=far, quantize="mx4", h_out=h_out)
+        assert torch.equal(h, near_by[0]) and torch.equal(q.codes, near_by[1].codes) and torch.equal(q.scales, near_by[1].scales)
+    qamw.mx4_dequantize(a, out=far)
+    assert torch.equal(far, qamw.mx4_dequantize(b))
+    w = qamw.mx4_quantize(want.repeat(7, 1))
+    far.copy_(want)
+    y = torch.as_strided(torch.empty(2 * apart + 21, dtype=torch.bfloat16, device=DEV), (3, 21), (apart, 1))
+    assert torch.equal(qamw.mx4_matmul(far, w, out=y), qamw.mx4_matmul(want, w))

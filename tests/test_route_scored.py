@@ -155,6 +155,18 @@ def test_values_next_to_each_other(scores, groups, top):
 
 
 @gpu
+@pytest.mark.parametrize("bias", [2.0**30, -(2.0**22), -(2.0**27), 3e38])
+@pytest.mark.parametrize("groups,top", [(1, 1), (4, 2)])
+def test_large_biases(bias, groups, top):
+    """Sums of which 64 bits hold a few digits: equal ones go to the lowest expert."""
+    say(f"[scored] bias {bias} {groups}")
+    n, m = 64, 1500
+    x = torch.randn(m, n, generator=_gen(7)) * 2.0**-16
+    for b in (torch.full((n,), bias), torch.full((n,), bias) * (1 + (torch.arange(n) % 3) * 2.0**-23)):
+        check(qamw.route_scored(x.to(DEV), 6, bias=b.to(DEV), groups=groups, top_groups=top), x, 6, n, reference(x, 6, "sigmoid", b, groups, top, 2, True, 1.0))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
 @pytest.mark.parametrize("n,groups", [(32, 8), (32, 1), (200, 8), (12, 4)])
