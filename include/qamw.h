@@ -499,7 +499,8 @@ int qamw_mx4_row_bytes(int d, size_t *codes_out, size_t *scales_out);
  * more blocks than a launch has threads for -> UNSUPPORTED. */
 int qamw_mx4_quantize(const void *X, int dtype, int m, int d, int64_t ldx, const float *col_scale, uint8_t *codes, uint8_t *scales, void *stream);
 
-/* What the codes stand for, in out_dtype (F32, exact, or BF16, exact but for values below its normal numbers). */
+/* What the codes stand for, in out_dtype (F32, exact, or BF16, exact but for values below its normal numbers).  Errors: as qamw_mx4_quantize, ldo < d ->
+ * SHAPE; of any number of blocks. */
 int qamw_mx4_dequantize(const uint8_t *codes, const uint8_t *scales, int m, int d, void *out, int out_dtype, int64_t ldo, void *stream);
 
 /* Y = X W^T of rows in 4 bits: products exact, sums in fp32 on the matrix cores.

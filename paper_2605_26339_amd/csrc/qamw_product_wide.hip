@@ -1,7 +1,7 @@
-// Y = X W^T on the matrix cores for many rows: 8-bit integers with scales or bf16, one matrix or one for each expert.
+// Y = X W^T on the matrix cores for many rows: 8-bit integers with scales, bf16, or 4 bits with scales of blocks, one matrix or one for each expert.
 //
 // A workgroup of eight waves has a tile of BN rows of W and BM of X and steps over 128 bytes of both at a time (a stage: 128
-// columns of int8, 64 of bf16).  16 rows of a stage are a fragment, 2 KB in LDS, filled by two buffer loads of a wave that go
+// columns of int8, 64 of bf16, 256 in 4 bits).  16 rows of a stage are a fragment, 2 KB in LDS, filled by two buffer loads of a wave that go
 // to LDS directly, eight whole lines each, and read by two 16-byte LDS reads of a wave: the operands of 16x16 matrix instructions.
 //   In LDS the eight 16-byte pieces of a row are exchanged by row mod 8, or the lanes of a read would meet in some of the
 //   banks; the loading lanes ask for their piece accordingly, from the same 128 bytes.
@@ -11,12 +11,17 @@
 //   multiplies, then they change places; a barrier is all that they need to keep in step.
 // What is not there (rows past the end, columns past d_in, stages past the last) is loaded as zeros: such a lane asks for an
 // address beyond its buffer's end.
-// What bounds it: power, and what a stage does beside its products.  8192 x 8192 x 8192 in int8 runs at 2200 TOPS with random operands and at
+// What bounds it: power, and what a stage does beside its products.  8192 x 8192 x 8192 in int8 runs at 2200 TOPS with random operands, sustained, and at
 // 3185 with zeros, at 1.3 and 1.9 GHz and in the same clocks a stage, bf16 at 1270 and 1747 TFLOP/s; matrix instructions alone reach 3527 and 1981
-// with random operands.  Of a wave's 1500 clocks a stage 585 are products, 428 reads, 490 waits and barriers; the matrix cores are busy for three
+// with random operands.  A call alone takes 405 us in int8 and 726 in bf16.  Of a wave's 1500 clocks a stage 585 are products, 428 reads, 490 waits and barriers; the matrix cores are busy for three
 // fifths.  The library's product of the same card reaches 2140 to 2175 TOPS and 1435 to 1550 TFLOP/s: for bf16 power is not all.  256 rows of W and
 // 256 of X, the most that accumulators have room for, read least for each product.  Smaller row tiles where there are too few to fill
-// the CUs: 1000 rows by 4096 x 4096 in 30.2 us by 64, 34.2 by 128, 48.4 by 256; 4000 rows 106, 71.9, 62.0.
+// the CUs: 1000 rows by 4096 x 4096 in 30.8 us by 64, 34.2 by 128, 45.6 by 256; 4000 rows 105, 70.7, 56.6.
+//   In 4 bits a matrix instruction takes 64 bytes of each operand as in int8, which are twice the columns, and for every 16 bytes a scale.  16 bytes of a
+// row's scales serve two stages and come as one load more for each wave; a lane reads a dword for a fragment, whose bytes are the four instructions'.
+// 8192 x 8192 x 8192 takes 250 us, 4400 TFLOP/s (4090 sustained, 5850 with zeros; instructions alone 7250 and 9500): again power and what lies beside the
+// products, for the matrix cores are busy for 54 % of the clocks.  8192 rows by 2 x 11008 x 4096, gated, 366 us by 256 rows, 453 by 128, 618 by 64; 1000 by
+// 4096 x 4096 30.3, 22.1 and 18.2.  Tried, with the same time in 2 to 6 % other clocks: the columns' halves as the two steps, and the scales read a step earlier.
 // Tried and slower: four waves of 128 x 128, one barrier a stage for all eight waves, five stages of 64 bytes, loads issued among the matrix
 // instructions, and the barrier before the last of a step's products (3 to 12 %).
 #include "qamw_product_tile.hpp"
@@ -484,8 +489,9 @@ __global__ __launch_bounds__(PW_THREADS, 2) void k_product_wide(ProductArgs a, i
 // The sums of the parts, in their order, and what is done with them: four outputs a thread.  Memory bounds it: 4 bytes a part and output
 // are read, and all parts' are asked for together, which is why their number is known here: 509 rows of 5120 outputs in 3 parts 7.1 us, 5.2 TB/s
 // with what is written (10.4 with a loop over any number).
-//   Parts pay where the tiles of whole columns leave CUs without one: 300 rows by 5120 x 13824 take 40.0 us in 4 parts of tiles of 128
-// rows, sums included, and 88 in one.  int8 only: its sums are whole numbers, and in any order the same.
+//   Parts pay where the tiles of whole columns leave CUs without one: 300 rows by 5120 x 13824 take 36.5 us in 4 parts of tiles of 128
+// rows, sums included, and 87 in one (int8); in 4 bits 29.0 and 53.  Not for bf16, whose sums would depend on the parts; int8's are whole numbers, and in any
+// order the same.  In 4 bits they are added in the order of the parts.
 constexpr int PS_THREADS = 256;
 template <bool MX4, bool GATED, bool YBF16, int PARTS>
 __global__ __launch_bounds__(PS_THREADS) void k_product_parts(ProductArgs a, const char *sums, int64_t part_stride, int64_t ld, int fours) {
