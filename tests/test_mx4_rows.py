@@ -189,7 +189,7 @@ def _strided(t, pad, skip):
     (5, 512, torch.bfloat16, 8, 0, True), (5, 513, torch.bfloat16, 3, 1, False), (300, 1024, torch.float32, 4, 4, True), (9, 31, torch.bfloat16, 0, 0, True),
     (9, 32, torch.float32, 1, 0, False), (9, 33, torch.bfloat16, 0, 1, False), (4, 5632, torch.float32, 0, 0, False), (3, 13824, torch.bfloat16, 16, 8, False),
     (2, 4095, torch.float32, 1, 1, True), (1, 131072, torch.float32, 0, 0, False), (2, 131071, torch.bfloat16, 0, 0, True), (70000, 16, torch.bfloat16, 0, 0, False),
-    (33, 11008, torch.bfloat16, 0, 0, True),
+    (33, 11008, torch.bfloat16, 0, 0, True), (16400, 5, torch.bfloat16, 2, 1, True), (17001, 33, torch.float32, 0, 0, False), (5601, 1029, torch.bfloat16, 3, 1, True),
 ])
 def test_quantise(m, d, dtype, pad, skip, smooth):
     say(f"[mx4] quantise {m}x{d} {dtype} pad {pad} skip {skip} smooth {smooth}")
