@@ -1,4 +1,5 @@
-// Y = X W^T for few rows: what is read of W is what it costs.  8-bit integers with scales or bf16, one matrix or one for each expert.
+// Y = X W^T for few rows: what is read of W is what it costs.  8-bit integers with scales, bf16, or 4 bits with scales of blocks, one matrix or one for
+// each expert.
 //
 // A wave has 16 rows of W (gated: 16 of the gate and the same 16 of the up projection), up to 64 rows of X and a share of the columns, in
 // units of 128 bytes.  Units come to the wave's own ring in LDS by buffer loads that go there directly, whole 128-byte lines of
@@ -8,12 +9,16 @@
 // columns among waves until there are about 8 on every CU; with enough of them, memory.  Launches included: 4096 x 4096 int8 for 8 rows 6.4 us,
 // 11008 x 4096 12.1, 5120 x 13824 19.1 (3.7 TB/s); gated int8 of 8 experts of 2 x 5632 x 2048 for 10 rows 27 us; bf16 of 64 experts of
 // 1408 x 2048 with 8 rows each 70.6 us (5.2 TB/s).
+//   In 4 bits: 4096 x 4096 for 8 rows 3.8 us, 5120 x 13824 9.5 (3.7 TB/s), for 64 rows 18.5; gated, 2 x 11008 x 4096 for 16 rows 9.8 (4.6 TB/s of codes);
+// 8 experts of 2 x 5632 x 2048 for 10 rows 15.4, 64 of 1408 x 2048 with 4 or 5 rows each 21.2.  The weights are half of int8's, so that a launch's beginning
+// and end are more of it; the scales, a byte for 16 of codes, are one load of 4 bytes a lane for two units of a fragment.
 //   Rows of X are read again for every 16 outputs, from the caches, so that many rows are dearer here than in tiles of 256 outputs; the
 // estimate that chooses has both sides.
 // Few values, quantised in the call: the workgroup's waves quantise the rows while their first weights are on their way.  Every
 // workgroup does so again.  Against a launch for it, in a graph: one row by 4096 x 4096 6.9 us (8.1), of 11008 columns 13.1 (15.2), 4 rows
 // of 4096 columns 9.9 (8.3); called one by one, a launch less is 4 us less of the host's time.  13 rows of 5632 took 18.6 us, in two launches
-// 8.5: so no more values than the threads hold in four groups of 8.
+// 8.5: so no more values than the threads hold in four groups of 8.  In 4 bits a block's largest is found among four lanes, with no barrier for it: one row
+// by 4096 x 4096 4.2 us in one launch, 13 rows of 5632, fp32, by 2047 6.4 in two.
 #include "qamw_mx4.hpp"
 
 namespace qamw {

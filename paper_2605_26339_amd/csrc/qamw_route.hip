@@ -127,11 +127,11 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 // bits, and compared as whole numbers, their distance from the token's smallest value in units of some 2^-28 of the distance to its largest; where all that is
 // compared for a token is more than a unit apart, 64 bits would choose alike (choose_fast).  A token in doubt is done again in 64 bits, by its whole
 // wave (choose_exact).  That code is cold when a wave comes to it and takes it 10 us, which the whole launch waits for: with comparisons in fp32, sure to 2^-19, one
-// in a thousand tokens was in doubt, and every large call took 30 us where it takes 27 now.  Without a bias and groups the logits order as the scores do (choose_by_logits).
+// in a thousand tokens was in doubt, and every large call took 30 us where it takes 26 now.  Without a bias and groups the logits order as the scores do (choose_by_logits).
 //   The weights, k a token, are in 64 bits too.
-//   Arithmetic bounds it: 16384 tokens over 256 experts in 16 groups, 8 chosen, bf16, 27 us, of which 21 are this launch, some 1800 instructions a wave, a
-// third of them in 64 bits.  Without a bias and groups 17; every token in 64 bits 68.  More than 16 groups, or more than 32 experts a lane, are done in 64 bits
-// at once: 160 experts in 20 groups 42 us, 4096 tokens over 1024 experts 99.
+//   Arithmetic bounds it: 16384 tokens over 256 experts in 16 groups, 8 chosen, bf16, 26 us, of which 20 are this launch: 14 the values, a third of whose
+// instructions are in 64 bits, and the comparisons, 1 the weights, 1.5 the tokens in doubt.  Without a bias and groups 17; every token in 64 bits 68.  More than
+// 16 groups, or more than 32 experts a lane, are done in 64 bits at once: 160 experts in 20 groups 41 us, 4096 tokens over 1024 experts 98.
 
 // How the groups lie on `all` lanes, a power of two for each group: 2^shift lanes of a group, none if there are more groups than lanes, and experts of a lane.
 struct GroupLanes {
@@ -196,8 +196,8 @@ __device__ __forceinline__ double inverse_near(double x) {
 // Sixteen lanes a token.  A number, below 2^31, is a value in units, above which one of its lane's PER experts it is, the lowest as the largest; 0: closed.  The
 // next choice is the largest number below the last one, found as with packed logits above; if two lanes have it, the token is in doubt.
 // Lane j gets the choices j and j + 16.  Returns, for each token, whether 64 bits are sure to choose alike.  A score is off by 6e-10 at most, an exponential's
-// 3e-10 twice for a softmax, and by a rounding of its sum with the bias.  The range is 8 and the bias', a unit PER 2^-31 of it and so 3.7e-9 or more: where
-// two numbers' units differ by more than one, the values are more than a unit apart, which is more than both are off.  Half the sum of two is known to a unit
+// 3e-10 twice for a softmax, and by a rounding of its sum with the bias.  The range is the bias' and 2, or 8, a unit PER 2^-31 of it and so 3.7e-9 or more: where
+// two numbers are more than two units apart, the values are more than a unit apart, which is more than both are off.  Half the sum of two is known to a unit
 // less.
 template <int DTYPE, int PER>
 __device__ __forceinline__ bool choose_fast(const RouteProblem &q, int64_t t, int (&expert)[2]) {
@@ -229,18 +229,19 @@ __device__ __forceinline__ bool choose_fast(const RouteProblem &q, int64_t t, in
 #pragma unroll
         for (int i = 0; i < PER; ++i) c[i] = inverse_near(1.0 + exp_near(-(double)fminf(fmaxf(x[i], -690.0f), 690.0f)));
     }
-    // the bias' range, and 1 for the scores'; of no expert 0
+    // the bias' range, and what is beside it: 1 for the scores', and more where a unit would be too small
+    constexpr double BESIDE = PER >= 4 ? 2.0 : 8.0;
     float low = __builtin_inff(), high = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        if (!(bias[i] > -__builtin_inff())) x[i] = -__builtin_inff();
-        const bool open = x[i] > -__builtin_inff();
-        low = fminf(low, open ? bias[i] : low);
-        high = fmaxf(high, open ? bias[i] : high);
+        const bool open = bias[i] > -__builtin_inff();
+        x[i] = open ? x[i] : -__builtin_inff();
+        low = __builtin_fminf(low, open ? bias[i] : __builtin_inff());
+        high = __builtin_fmaxf(high, open ? bias[i] : -__builtin_inff());
     }
     high = value_of(row_max(key_of(high)));
     low = -value_of(row_max(key_of(-low)));
-    const double units = 0x1.fffffep30 / ((double)high - (double)low + 8.0), from = fma(-((double)low - 1.0), units, 0x1p52);
+    const double units = 0x1.fffffep30 / ((double)high - (double)low + BESIDE), from = fma(-((double)low - 1.0), units, 0x1p52 + PER);   // PER: no open one is 0
     constexpr uint32_t INDEX = PER - 1;
     uint32_t v[PER];
 #pragma unroll
@@ -249,7 +250,7 @@ __device__ __forceinline__ bool choose_fast(const RouteProblem &q, int64_t t, in
         v[i] = x[i] > -__builtin_inff() ? (u & ~INDEX) | (INDEX - i) : 0;
     }
     // sums of a bias 2^17 times the range are rounded by a sixteenth of a unit, and those of a larger one might be to either side of it
-    bool certain = high < low || (high < __builtin_inff() && fmaxf(fabsf(low), fabsf(high)) * 0x1p-17f <= high - low + 8.0f);
+    bool certain = high < low || (high < __builtin_inff() && fmaxf(fabsf(low), fabsf(high)) * 0x1p-17f <= high - low + 2.0f);
     auto apart = [&](uint32_t a, uint32_t b, uint32_t by) { certain = certain && (b == 0 || a / PER - b / PER > by); };
     if (q.groups > 1) {
         uint32_t first = 0, second = 0;
@@ -282,24 +283,29 @@ __device__ __forceinline__ bool choose_fast(const RouteProblem &q, int64_t t, in
 #pragma unroll
         for (int i = 0; i < PER; ++i) v[i] = stays ? v[i] : 0;
     }
-    expert[0] = expert[1] = -1;
-    uint32_t last = 0;
+    uint32_t last = 0, winners[2] = {0, 0}, numbers[2] = {0, 0};   // the lane that has a choice, as one bit, and the choice's number; 0: none
     bool some = true;
     for (int j = 0; j <= q.k; ++j) {                         // one more than are chosen: it has to be apart, too
         uint32_t own = v[0] - last;
 #pragma unroll
         for (int i = 1; i < PER; ++i) own = max(own, v[i] - last);
-        const uint32_t best = last + row_max(own);
-        if (j > 0 && some) apart(last, best, 1);
+        const uint32_t most = row_max(own), best = last + most;
+        if (j > 0) certain = certain && (!some || best == 0 || most < 0u - 2 * PER);   // more than two units below the last one
         some = some && best != 0;                            // a token that has run out of experts stays so
         if (j == q.k || !__any(some)) break;
-        const uint32_t has = (uint32_t)(__ballot(last + own == best) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu;
+        const uint32_t has = (uint32_t)(__ballot(own == most) >> (threadIdx.x % WAVE / RT_LANES * RT_LANES)) & 0xFFFFu;
         certain = certain && ((has & (has - 1)) == 0 || !some);
-        const int who = g.first_expert(__ffs((int)has) - 1) + (int)(INDEX - (best & INDEX));
-        if (some && lane == j) expert[0] = who;
-        if (some && lane + RT_LANES == j) expert[1] = who;
+        const bool is = some && lane == j % RT_LANES;
+        if (j < RT_LANES) {
+            winners[0] = is ? has : winners[0];
+            numbers[0] = is ? best : numbers[0];
+        } else {
+            winners[1] = is ? has : winners[1];
+            numbers[1] = is ? best : numbers[1];
+        }
         last = best;
     }
+    for (int h = 0; h < 2; ++h) expert[h] = numbers[h] ? g.first_expert(__ffs((int)winners[h]) - 1) + (int)(INDEX - (numbers[h] & INDEX)) : -1;
     return all_of_row(certain);                             // a group alone is in doubt in its own lanes
 }
 

@@ -164,6 +164,10 @@ def test_large_biases(bias, groups, top):
     x = torch.randn(m, n, generator=_gen(7)) * 2.0**-16
     for b in (torch.full((n,), bias), torch.full((n,), bias) * (1 + (torch.arange(n) % 3) * 2.0**-23)):
         check(qamw.route_scored(x.to(DEV), 6, bias=b.to(DEV), groups=groups, top_groups=top), x, 6, n, reference(x, 6, "sigmoid", b, groups, top, 2, True, 1.0))
+    for e in (2, 3):                                          # two experts alone, far apart
+        b = torch.full((n,), -INF)
+        b[5], b[e] = 0.0, -abs(bias)
+        check(qamw.route_scored(x.to(DEV), 2, bias=b.to(DEV), groups=groups, top_groups=top), x, 2, n, reference(x, 2, "sigmoid", b, groups, top, 2, True, 1.0))
 
 
 @gpu
