@@ -11,9 +11,9 @@
 //   multiplies, then they change places; a barrier is all that they need to keep in step.
 // What is not there (rows past the end, columns past d_in, stages past the last) is loaded as zeros: such a lane asks for an
 // address beyond its buffer's end.
-// What bounds it: power, and what a stage does beside its products.  8192 x 8192 x 8192 in int8 runs at 2200 TOPS with random operands, sustained, and at
-// 3185 with zeros, at 1.3 and 1.9 GHz and in the same clocks a stage, bf16 at 1270 and 1747 TFLOP/s; matrix instructions alone reach 3527 and 1981
-// with random operands.  A call alone takes 405 us in int8 and 726 in bf16.  Of a wave's 1500 clocks a stage 585 are products, 428 reads, 490 waits and barriers; the matrix cores are busy for three
+// What bounds it: power, and what a stage does beside its products.  8192 x 8192 x 8192 in int8 runs at 2560 to 2810 TOPS with random operands and at 3580
+// with zeros, bf16 at 1430 to 1510 and 1780 TFLOP/s; matrix instructions alone reach 3527 and 1981 with random operands.  Random operands and zeros
+// take the same clocks a stage, at 1.3 and 1.9 GHz.  Of a wave's 1500 clocks a stage 585 are products, 428 reads, 490 waits and barriers; the matrix cores are busy for three
 // fifths.  The library's product of the same card reaches 2140 to 2175 TOPS and 1435 to 1550 TFLOP/s: for bf16 power is not all.  256 rows of W and
 // 256 of X, the most that accumulators have room for, read least for each product.  Smaller row tiles where there are too few to fill
 // the CUs: 1000 rows by 4096 x 4096 in 30.8 us by 64, 34.2 by 128, 45.6 by 256; 4000 rows 105, 70.7, 56.6.
