@@ -507,3 +507,29 @@ def test_two_products_at_once_and_in_a_graph():
             torch.cuda.synchronize()
             assert torch.equal(y, e)
             assert torch.equal(qamw.mx4_matmul(xs[1], w), want[1])
+
+
+@gpu
+@pytest.mark.parametrize("m", [3, 300])
+def test_experts_beyond_4_gib(m):
+    """The last of many experts, whose matrix begins beyond 2^32 bytes of codes, and no rows for the others."""
+    say(f"[mx4] {m} rows of the last of 104 experts")
+    n, outs, d = 104, 22016, 4096
+    cb, sb = qamw.mx4_row_bytes(d)
+    W = qamw.Mx4(torch.zeros(n, outs, cb, dtype=torch.uint8, device=DEV), torch.zeros(n, outs, sb, dtype=torch.uint8, device=DEV), d)
+    assert (n - 1) * outs * cb > 2**32
+    last = qamw.Mx4(W.codes[-1], W.scales[-1], d)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    qamw.mx4_quantize(torch.randn(outs, d, generator=g, device=DEV, dtype=torch.bfloat16), out=last)
+    x = qamw.mx4_quantize(torch.randn(m, d, generator=g, device=DEV))
+    offsets = torch.zeros(n + 1, dtype=torch.int32, device=DEV)
+    offsets[-1] = m
+    for gated in (False, True):
+        try:
+            qamw.set_kernel_path(0 if m == 3 else 128)        # the same tiles, and so the same sums
+            got, want = qamw.mx4_grouped_matmul(x, W, offsets, gated=gated), qamw.mx4_matmul(x, last, gated=gated)
+        finally:
+            qamw.set_kernel_path(0)
+        assert torch.isfinite(want).all() and want.abs().max() > 10
+        err = (got.double() - want.double()).abs().max() / want.double().abs().max()
+        assert err <= 2.0**-8 if m == 3 else torch.equal(got, want)
