@@ -1,11 +1,13 @@
 // Routed experts: the choice of experts, the order of the rows, and the way back.
+#include <algorithm>
+
 #include "qamw.h"
 #include "qamw_product_tile.hpp"
 
 namespace qamw {
 namespace {
 
-constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
+constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;   // of a workgroup, at most
 
 // ---- choice ---------------------------------------------------------------------------------------------------------------
 //
@@ -19,7 +21,7 @@ constexpr int RT_WAVES = 16, RT_THREADS = RT_WAVES * WAVE;
 constexpr int RT_LANES = 16, RT_GROUPS = WAVE / RT_LANES;
 // Tokens of a workgroup of the first launch, and so the most that it can count for an expert: 8 bits hold it.  A workgroup's counts lie in
 // sectors of 32 bytes of their own, so that no two write to one.
-constexpr int RT_TOKENS = RT_GROUPS * RT_WAVES;
+constexpr int RT_TOKENS = RT_GROUPS * RT_WAVES, RT_CUS = 256;
 __host__ __device__ constexpr int counts_row(int n_experts) { return (n_experts + 31) / 32 * 32; }
 
 __device__ __forceinline__ uint32_t row_max(uint32_t v) {
@@ -49,32 +51,24 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 // exp(x - top), x <= top; infinities of one sign are equal: their difference is no number, and 0 the smaller of the two
 __device__ __forceinline__ float share_of(float x, float top) { return __expf(fminf(x - top, 0.0f)); }
 
-// Lane j of a token's sixteen gets its choices j and j + 16: the experts (-1: none) and weights.  t >= m: none.
-template <int DTYPE, int PER>
-__device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&expert)[2], float (&weight)[2]) {
-    constexpr bool PACKED = DTYPE == 1;
-    const int lane = threadIdx.x % RT_LANES, n = q.n_experts, e0 = lane * PER;
-    using E = typename Elem<DTYPE>::type;
-    uint32_t key[PER];
-    Unaligned<E, PER> row;                                  // wherever it lies: the memory instructions take any address
-    const bool whole = t < q.m && e0 + PER <= n;
-    if (whole) row = *reinterpret_cast<const Unaligned<E, PER> *>(static_cast<const E *>(q.logits) + t * q.ld + e0);
-    else
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (DTYPE == 1) row.v[i] = (E)0xFF80u;          // -inf
-            else row.v[i] = (E)-__builtin_inff();
-            if (t < q.m && e0 + i < n) row.v[i] = static_cast<const E *>(q.logits)[t * q.ld + e0 + i];
-        }
-    auto logit = [&](int i) { return clean(DTYPE == 1 ? __uint_as_float((uint32_t)row.v[i] << 16) : (float)row.v[i]); };
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        key[i] = key_of(logit(i));
-        if (PACKED) key[i] = (key[i] >> 16 << 10 | (1023u - (uint32_t)e0)) - i;   // e0 + i <= 1023: no borrow
+// Logits as numbers, of expert e0 + i; bf16 with the expert below it.
+template <int DTYPE> struct Key {
+    static constexpr bool PACKED = DTYPE == 1;
+    static constexpr uint32_t LEAST = PACKED ? RT_LEAST >> 16 << 10 : RT_LEAST;
+    static __device__ __forceinline__ uint32_t of(float logit, int e0, int i) {
+        const uint32_t k = key_of(logit);
+        return PACKED ? (k >> 16 << 10 | (1023u - (uint32_t)e0)) - i : k;      // e0 + i <= 1023: no borrow
     }
-    constexpr uint32_t LEAST = PACKED ? RT_LEAST >> 16 << 10 : RT_LEAST;
     // of a packed key all that a negative value lacks are ones
-    auto value = [](uint32_t k) { return value_of(PACKED ? (k >> 10 << 16) | (k & 0x2000000u ? 0u : 0xFFFFu) : k); };
+    static __device__ __forceinline__ float value(uint32_t k) { return value_of(PACKED ? (k >> 10 << 16) | (k & 0x2000000u ? 0u : 0xFFFFu) : k); }
+};
+
+// Lane j of a token's sixteen gets its choices j and j + 16 of all lanes' experts, e0 + i with key[i]: the experts (-1: none) and weights.
+template <int DTYPE, int PER, typename Logit>
+__device__ __forceinline__ void pick_keys(const RouteProblem &q, int e0, uint32_t (&key)[PER], Logit logit, int (&expert)[2], float (&weight)[2]) {
+    constexpr bool PACKED = Key<DTYPE>::PACKED;
+    const int lane = threadIdx.x % RT_LANES;
+    auto value = [](uint32_t k) { return Key<DTYPE>::value(k); };
     float total = 0.0f, top = 0.0f, mine[2] = {0.0f, 0.0f};
     expert[0] = expert[1] = -1;
     uint32_t best = 0;
@@ -85,7 +79,7 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 #pragma unroll
         for (int i = 1; i < PER; ++i) own = max(own, key[i] - last);
         best = last + row_max(own);
-        some = some && best >= LEAST;                       // a token that has run out of experts stays so
+        some = some && best >= Key<DTYPE>::LEAST;                       // a token that has run out of experts stays so
         if (!__any(some)) break;
         const float v = value(best);
         if (j == 0) {
@@ -121,16 +115,38 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
     for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 ? mine[h] / total : 0.0f;
 }
 
+// Of token t, PER neighbours a lane.  t >= m: none.
+template <int DTYPE, int PER>
+__device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&expert)[2], float (&weight)[2]) {
+    const int n = q.n_experts, e0 = threadIdx.x % RT_LANES * PER;
+    using E = typename Elem<DTYPE>::type;
+    uint32_t key[PER];
+    Unaligned<E, PER> row;                                  // wherever it lies: the memory instructions take any address
+    const bool whole = t < q.m && e0 + PER <= n;
+    if (whole) row = *reinterpret_cast<const Unaligned<E, PER> *>(static_cast<const E *>(q.logits) + t * q.ld + e0);
+    else
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (DTYPE == 1) row.v[i] = (E)0xFF80u;          // -inf
+            else row.v[i] = (E)-__builtin_inff();
+            if (t < q.m && e0 + i < n) row.v[i] = static_cast<const E *>(q.logits)[t * q.ld + e0 + i];
+        }
+    auto logit = [&](int i) { return clean(DTYPE == 1 ? __uint_as_float((uint32_t)row.v[i] << 16) : (float)row.v[i]); };
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = Key<DTYPE>::of(logit(i), e0, i);
+    pick_keys<DTYPE, PER>(q, e0, key, logit, expert, weight);
+}
+
 // ---- choice by scores -----------------------------------------------------------------------------------------------------
 //
 // A choice is a comparison, and among a few million values there are always two that 32 bits of floating point cannot tell apart.  So scores are made in 64
 // bits, and compared as whole numbers, their distance from the token's smallest value in units of some 2^-28 of the distance to its largest; where all that is
 // compared for a token is more than a unit apart, 64 bits would choose alike (choose_fast).  A token in doubt is done again in 64 bits, by its whole
 // wave (choose_exact).  That code is cold when a wave comes to it and takes it 10 us, which the whole launch waits for: with comparisons in fp32, sure to 2^-19, one
-// in a thousand tokens was in doubt, and every large call took 30 us where it takes 26 now.  Without a bias and groups the logits order as the scores do (choose_by_logits).
+// in a thousand tokens was in doubt, and every large call took 30 us where it takes 26 now.  Without a bias the logits order as the scores do (choose_by_logits).
 //   The weights, k a token, are in 64 bits too.
 //   Arithmetic bounds it: 16384 tokens over 256 experts in 16 groups, 8 chosen, bf16, 26 us, of which 20 are this launch: 14 the values, a third of whose
-// instructions are in 64 bits, and the comparisons, 1 the weights, 1.5 the tokens in doubt.  Without a bias and groups 17; every token in 64 bits 68.  More than
+// instructions are in 64 bits, and the comparisons, 1 the weights, 1.5 the tokens in doubt.  Without a bias 17, with 8 or 16 groups 24; every token in 64 bits 68.  More than
 // 16 groups, or more than 32 experts a lane, are done in 64 bits at once: 160 experts in 20 groups 41 us, 4096 tokens over 1024 experts 98.
 
 // How the groups lie on `all` lanes, a power of two for each group: 2^shift lanes of a group, none if there are more groups than lanes, and experts of a lane.
@@ -430,7 +446,51 @@ __device__ __forceinline__ void weigh(const RouteProblem &q, int64_t t, const in
     for (int h = 0; h < 2; ++h) weight[h] = expert[h] >= 0 && sum > 0.0 ? (float)(s[h] * factor) : 0.0f;
 }
 
-// Without a bias and groups: by the logits, which order as the scores do.  Sure to be so in 64 bits where of two neighbours in that order, the next one after the
+template <typename F, int... T> __device__ __forceinline__ void each_turn(F f, std::integer_sequence<int, T...>) { (f(std::integral_constant<int, T + 1>{}), ...); }
+
+// Without a bias, the values of groups: one expert's score or two's, of a softmax times what all have.  Keys of groups that do not stay become 0.  A group's rank
+// is the number of groups above it, found by turning the values around the sixteen lanes.  Returns whether 64 bits are sure to order alike: of two groups
+// either the logits are the same, or the values, which are off by 3e-10, are 2^-29 of their size apart.
+template <int DTYPE, int PER>
+__device__ __forceinline__ bool groups_by_logits(const RouteProblem &q, const GroupLanes &g, uint32_t (&key)[PER]) {
+    const int lane = threadIdx.x % RT_LANES;
+    uint32_t first = 0, second = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        second = max(second, min(first, key[i]));
+        first = max(first, key[i]);
+    }
+    for (int d = 1; d < g.lanes; d <<= 1) {
+        const uint32_t f = (uint32_t)__shfl_xor((int)first, d, RT_LANES), z = (uint32_t)__shfl_xor((int)second, d, RT_LANES);
+        second = max(min(first, f), max(second, z));
+        first = max(first, f);
+    }
+    constexpr uint32_t LEAST = Key<DTYPE>::LEAST;
+    const bool open = first >= LEAST, two = q.group_top > 1 && second >= LEAST;
+    const float x1 = open ? Key<DTYPE>::value(first) : -__builtin_inff(), x2 = two ? Key<DTYPE>::value(second) : -__builtin_inff();
+    const float top = q.softmax ? value_of(row_max(key_of(x1))) : 0.0f;
+    auto score = [&](float x) {
+        if (q.softmax) return exp_near(x - top > -689.0f ? (double)x - (double)top : x == top ? 0.0 : -689.0);
+        return inverse_near(1.0 + exp_near(-(double)fminf(fmaxf(x, -690.0f), 690.0f)));
+    };
+    const double value = !open || g.first_lane(lane) != lane ? -1.0 : score(x1) + (two ? score(x2) : 0.0);
+    int above = 0;
+    bool certain = true;
+    auto compare = [&](auto turn) {
+        auto from = [&](int v) { return dpp_move<DPP_ROW_ROTATE_8 - 8 + decltype(turn)::value>(v); };
+        const double v = __hiloint2double(from(__double2hiint(value)), from(__double2loint(value)));
+        const bool same = __int_as_float(from(__float_as_int(x1))) == x1 && __int_as_float(from(__float_as_int(x2))) == x2, lower = from(lane) < lane;
+        above += v > value || (v == value && lower);
+        certain = certain && (same || fabs(v - value) > value * 0x1p-29);      // where either is -1: sure
+    };
+    each_turn(compare, std::make_integer_sequence<int, RT_LANES - 1>{});
+    const bool stays = __shfl((int)(open && above < q.top_groups), g.first_lane(lane), RT_LANES) != 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = stays ? key[i] : 0;
+    return certain || value < 0.0;
+}
+
+// Without a bias: by the logits, which order as the scores do.  Sure to be so in 64 bits where of two neighbours in that order, the next one after the
 // last choice among them, either is the other or they are 2^-23 apart: times e^-16, the slope of a sigmoid at 16, and more of a softmax, 1e-14.
 template <int DTYPE, int PER>
 __device__ __forceinline__ bool choose_by_logits(const RouteProblem &q, int64_t t, int (&expert)[2]) {
@@ -438,13 +498,26 @@ __device__ __forceinline__ bool choose_by_logits(const RouteProblem &q, int64_t 
     const int lane = threadIdx.x % RT_LANES;
     RouteProblem more = q;                                  // one more than are chosen
     more.k = min(q.k + 1, q.n_experts);
+    more.renormalise = true;
     if (more.k > 2 * RT_LANES) return false;
     float weight[2], x[2];
-    pick<DTYPE, PER>(more, t, expert, weight);
+    bool plain = true;
+    if (q.groups > 1) {
+        const GroupLanes g(RT_LANES, q.n_experts, q.groups);
+        const int e0 = g.first_expert(lane);
+        float own[PER];
+        uint32_t key[PER];
+        own_logits<DTYPE, PER>(q, t, e0, t < q.m ? g.count(lane, q.groups) : 0, own);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) key[i] = Key<DTYPE>::of(own[i], e0, i);
+        plain = groups_by_logits<DTYPE, PER>(q, g, key);
+        pick_keys<DTYPE, PER>(more, e0, key, [](int) { return 0.0f; }, expert, weight);
+    } else {
+        pick<DTYPE, PER>(more, t, expert, weight);
+    }
     const E *from = static_cast<const E *>(q.logits) + min(t, (int64_t)q.m - 1) * q.ld;
     for (int h = 0; h < 2; ++h) x[h] = expert[h] >= 0 ? clean(Elem<DTYPE>::load(from, expert[h])) : -__builtin_inff();
     const float top = __shfl(x[0], 0, RT_LANES), middle = __shfl(x[1], 0, RT_LANES);
-    bool plain = true;
     for (int h = 0; h < 2; ++h) {
         const float after = __shfl_down(x[h], 1, RT_LANES), next = lane < RT_LANES - 1 ? after : h == 0 ? middle : -__builtin_inff();
         plain = plain && (next == -__builtin_inff() || x[h] == next || x[h] - next > 0x1p-23f);
@@ -460,7 +533,7 @@ template <int DTYPE, int PER, bool FAST>
 __device__ __forceinline__ void pick_scored(const RouteProblem &q, int64_t t, int (&expert)[2], float (&weight)[2]) {
     bool certain = false;
     expert[0] = expert[1] = -1;
-    if (FAST) certain = !q.bias && q.groups == 1 ? choose_by_logits<DTYPE, PER>(q, t, expert) : choose_fast<DTYPE, PER>(q, t, expert);
+    if (FAST) certain = !q.bias ? choose_by_logits<DTYPE, PER>(q, t, expert) : choose_fast<DTYPE, PER>(q, t, expert);
     const unsigned long long doubt = __ballot(!certain && t < q.m);
     const int64_t t0 = t - threadIdx.x % WAVE / RT_LANES;
     for (int token = 0; token < RT_GROUPS; ++token)
@@ -476,10 +549,10 @@ __device__ __forceinline__ void pick_scored(const RouteProblem &q, int64_t t, in
 // expert in the workgroup; when all counts are known, what comes before is added: what comes before an expert, and before the
 // workgroup within the expert.  A single workgroup knows all counts by itself: up to 64 tokens are one launch (5 tokens, 8 experts 3.4 us),
 // more are two: a workgroup of the second sums the counts of all and of those before it, so none waits for another.  What it reads of
-// them bounds that: 16384 tokens over 256 experts 6.1 us with counts of 8 bits, four experts' to a load, 8.5 with ones of 32 bits.
+// them bounds that: 16384 tokens over 256 experts 6 us with counts of 8 bits, four experts' to a load, 8.5 with ones of 32 bits.  Eight loads are on their way
+// together, the last ones too, and as many threads read as there are experts for: both launches over 8 experts 34 us for 131072 tokens (95 before), over 64 54 (105).
 //   Every workgroup reads all workgroups' counts, (m / 64)^2 bytes an expert, so that the second launch's time grows with the square of the tokens and
-// is most of a large call: over 256 experts, 8 of them chosen, both launches take 27 us for 32768 tokens, 128 for 131072, 381 for 262144 and 4.7 ms
-// for 1048576.
+// is most of a large call: over 256 experts, 8 of them chosen, both launches take 25 us for 32768 tokens, 124 for 131072, and 4.7 ms for 1048576.
 
 // Exclusive sums of the counts in `total` (LDS), by one wave; their sum.
 __device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
@@ -500,15 +573,16 @@ __device__ __forceinline__ uint32_t exclusive(uint32_t *total, int n) {
 }
 
 // SCORED: 0 by the logits, 1 by scores, 2 by scores, in 64 bits at once.
-template <int DTYPE, int PER, int SCORED, bool ALONE>
+// WAVES: of a workgroup, or 0 for as many as it has been given: 0.4 us more of each.
+template <int DTYPE, int PER, int SCORED, bool ALONE, int WAVES>
 __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
-    extern __shared__ uint32_t rt_lds[];                    // [RT_WAVES][n_experts]: counts, then what comes before them
+    extern __shared__ uint32_t rt_lds[];                    // [waves][n_experts]: counts, then what comes before them
     __shared__ uint32_t all;
-    const int n = q.n_experts, k = q.k, lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
-    uint32_t *mine = rt_lds + wave * n, *total = rt_lds + RT_WAVES * n;
-    for (int i = threadIdx.x; i < RT_WAVES * n; i += RT_THREADS) rt_lds[i] = 0;
+    const int n = q.n_experts, k = q.k, lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, waves = WAVES ? WAVES : (int)blockDim.x / WAVE, threads = waves * WAVE;
+    uint32_t *mine = rt_lds + wave * n, *total = rt_lds + waves * n;
+    for (int i = threadIdx.x; i < waves * n; i += threads) rt_lds[i] = 0;
     __syncthreads();
-    const int t0 = (blockIdx.x * RT_WAVES + wave) * RT_GROUPS, t1 = min(t0 + RT_GROUPS, q.m);
+    const int t0 = (blockIdx.x * waves + wave) * RT_GROUPS, t1 = min(t0 + RT_GROUPS, q.m);
     // lane's slots, of the tokens that are ranked together: token g0 + lane / k, choice lane % k
     const int at_once = k <= RT_LANES ? RT_GROUPS : 2, token = lane / k, choice = lane % k;
     int slot_expert[2] = {-1, -1}, slot_rank[2] = {-1, -1};
@@ -548,9 +622,9 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
         }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < n; e += RT_THREADS) {
+    for (int e = threadIdx.x; e < n; e += threads) {
         uint32_t before = 0;
-        for (int w = 0; w < RT_WAVES; ++w) {
+        for (int w = 0; w < waves; ++w) {
             const uint32_t c = rt_lds[w * n + e];
             rt_lds[w * n + e] = before;
             before += c;
@@ -565,7 +639,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
             if (lane == 0) all = sum;
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < n; e += RT_THREADS) q.offsets[e] = (int32_t)total[e];
+        for (int e = threadIdx.x; e < n; e += threads) q.offsets[e] = (int32_t)total[e];
         if (threadIdx.x == 0) q.offsets[n] = (int32_t)all;
     }
 #pragma unroll
@@ -577,32 +651,46 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_pick(RouteProblem q) {
         if (ALONE) q.rows[place] = t0 + h * at_once + token;
     }
     if (ALONE)
-        for (int p = (int)all + threadIdx.x; p < q.m * k; p += RT_THREADS) q.rows[p] = -1;
+        for (int p = (int)all + threadIdx.x; p < q.m * k; p += threads) q.rows[p] = -1;
 }
 
-// `lanes` threads, a power of two, have four experts each; RT_THREADS / lanes of them share the sums of the experts' counts.
+// `lanes` threads, a power of two, have four experts each; the workgroup's rest of them share the sums of the experts' counts.
 __global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int tokens, int blocks, int lanes) {
     extern __shared__ uint32_t rt_lds[];
     uint32_t *before = rt_lds, *total = rt_lds + q.n_experts;   // [n_experts] each: of the workgroups before, of all
     __shared__ uint32_t all;
     const int n = q.n_experts, k = q.k;
-    for (int i = threadIdx.x; i < 2 * n; i += RT_THREADS) rt_lds[i] = 0;
+    for (int i = threadIdx.x; i < 2 * n; i += blockDim.x) rt_lds[i] = 0;
     __syncthreads();
-    const int e0 = threadIdx.x % lanes * 4, segment = threadIdx.x / lanes, segments = RT_THREADS / lanes, row = counts_row(n);
+    const int e0 = threadIdx.x % lanes * 4, segment = threadIdx.x / lanes, segments = blockDim.x / lanes, row = counts_row(n);
     if (e0 < n) {
         constexpr int MOST = 0xFFFF / RT_TOKENS;            // counts that 16 bits hold the sum of
         for (int i0 = segment; i0 < blocks; i0 += segments * MOST) {
             uint32_t b[2] = {0, 0}, t[2] = {0, 0};          // experts e0 and e0 + 2, e0 + 1 and e0 + 3
             const int i1 = min((int64_t)blocks, i0 + (int64_t)segments * MOST);
-#pragma unroll 8
-            for (int i = i0; i < i1; i += segments) {
-                const uint32_t c = *reinterpret_cast<const uint32_t *>(q.counts + (int64_t)i * row + e0), even = c & 0xFF00FF, odd = c >> 8 & 0xFF00FF;
-                const bool is = i < (int)blockIdx.x;
-                t[0] += even;
-                t[1] += odd;
-                b[0] += is ? even : 0;
-                b[1] += is ? odd : 0;
-            }
+            auto eight = [&](int from, auto some) {         // all asked for together; where only some are there, the last one for the others
+                constexpr bool SOME = decltype(some)::value;
+                uint32_t c[8];
+                const uint8_t *at = q.counts + (int64_t)from * row + e0;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    c[u] = *reinterpret_cast<const uint32_t *>(at);
+                    at += !SOME || from + (u + 1) * segments < i1 ? (int64_t)segments * row : 0;
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int i = from + u * segments;
+                    const uint32_t own = !SOME || i < i1 ? c[u] : 0, even = own & 0xFF00FF, odd = own >> 8 & 0xFF00FF;
+                    const bool is = i < (int)blockIdx.x;
+                    t[0] += even;
+                    t[1] += odd;
+                    b[0] += is ? even : 0;
+                    b[1] += is ? odd : 0;
+                }
+            };
+            int from = i0;
+            for (; from + 7 * segments < i1; from += 8 * segments) eight(from, std::false_type{});
+            if (from < i1) eight(from, std::true_type{});
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 if (e0 + j < n) {                           // whole numbers: their order changes nothing
@@ -618,11 +706,11 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int 
     }
     __syncthreads();
     if (blockIdx.x == 0) {
-        for (int e = threadIdx.x; e < n; e += RT_THREADS) q.offsets[e] = (int32_t)total[e];
+        for (int e = threadIdx.x; e < n; e += blockDim.x) q.offsets[e] = (int32_t)total[e];
         if (threadIdx.x == 0) q.offsets[n] = (int32_t)all;
     }
     const int64_t slots = (int64_t)q.m * k, s0 = (int64_t)blockIdx.x * tokens * k, s1 = min(s0 + (int64_t)tokens * k, slots);
-    for (int64_t s = s0 + threadIdx.x; s < s1; s += RT_THREADS) {
+    for (int64_t s = s0 + threadIdx.x; s < s1; s += blockDim.x) {
         const int e = q.experts[s];
         if (e >= 0) {
             const uint32_t place = total[e] + before[e] + (uint32_t)q.positions[s];
@@ -631,7 +719,7 @@ __global__ __launch_bounds__(RT_THREADS) void k_route_order(RouteProblem q, int 
         }
     }
     // places that no slot has
-    for (int64_t p = (int64_t)all + (int64_t)blockIdx.x * RT_THREADS + threadIdx.x; p < slots; p += (int64_t)blocks * RT_THREADS)
+    for (int64_t p = (int64_t)all + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; p < slots; p += (int64_t)blocks * blockDim.x)
         q.rows[p] = -1;
 }
 
@@ -716,27 +804,30 @@ __global__ __launch_bounds__(CB_THREADS) void k_combine(const void *Y, int64_t y
     }
 }
 
-template <int DTYPE, int PER, int SCORED> hipError_t launch_pick(const RouteProblem &q, int blocks) {
-    const size_t lds = ((size_t)RT_WAVES + 1) * q.n_experts * 4;
-    static MoreLds alone, together;
-    const hipError_t e = blocks == 1 ? alone.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, SCORED, true>), 80 * 1024)
-                                     : together.ask(reinterpret_cast<const void *>(&k_route_pick<DTYPE, PER, SCORED, false>), 80 * 1024);
+template <int DTYPE, int PER, int SCORED> hipError_t launch_pick(const RouteProblem &q, int waves, int blocks) {
+    const size_t lds = ((size_t)waves + 1) * q.n_experts * 4;
+    auto go = [&](auto kernel, MoreLds &more) {
+        const hipError_t e = more.ask(reinterpret_cast<const void *>(kernel), 80 * 1024);
+        if (e == hipSuccess) kernel<<<blocks, waves * WAVE, lds, q.stream>>>(q);
+        return e;
+    };
+    static MoreLds alone, many, some;
+    const hipError_t e = blocks == 1 ? go(&k_route_pick<DTYPE, PER, SCORED, true, RT_WAVES>, alone)
+                         : waves == RT_WAVES ? go(&k_route_pick<DTYPE, PER, SCORED, false, RT_WAVES>, many) : go(&k_route_pick<DTYPE, PER, SCORED, false, 0>, some);
     if (e != hipSuccess) return e;
-    if (blocks == 1) k_route_pick<DTYPE, PER, SCORED, true><<<1, RT_THREADS, lds, q.stream>>>(q);
-    else k_route_pick<DTYPE, PER, SCORED, false><<<blocks, RT_THREADS, lds, q.stream>>>(q);
     return hipGetLastError();
 }
-template <int DTYPE, int SCORED> hipError_t launch_pick(const RouteProblem &q, int blocks) {
+template <int DTYPE, int SCORED> hipError_t launch_pick(const RouteProblem &q, int waves, int blocks) {
     const int per = SCORED == 0 ? (q.n_experts + RT_LANES - 1) / RT_LANES : SCORED == 1 ? GroupLanes(RT_LANES, q.n_experts, q.groups).per : 4 * GroupLanes(WAVE, q.n_experts, q.groups).per;
     if constexpr (SCORED != 2)
-        if (per <= 1) return launch_pick<DTYPE, 1, SCORED>(q, blocks);
-    if (per <= 4) return launch_pick<DTYPE, 4, SCORED>(q, blocks);
-    if (per <= 8) return launch_pick<DTYPE, 8, SCORED>(q, blocks);
-    if (per <= 16) return launch_pick<DTYPE, 16, SCORED>(q, blocks);
-    if (SCORED == 1 || per <= 32) return launch_pick<DTYPE, 32, SCORED>(q, blocks);
+        if (per <= 1) return launch_pick<DTYPE, 1, SCORED>(q, waves, blocks);
+    if (per <= 4) return launch_pick<DTYPE, 4, SCORED>(q, waves, blocks);
+    if (per <= 8) return launch_pick<DTYPE, 8, SCORED>(q, waves, blocks);
+    if (per <= 16) return launch_pick<DTYPE, 16, SCORED>(q, waves, blocks);
+    if (SCORED == 1 || per <= 32) return launch_pick<DTYPE, 32, SCORED>(q, waves, blocks);
     if constexpr (SCORED == 2)
-        if (per > 64) return launch_pick<DTYPE, 128, SCORED>(q, blocks);
-    if constexpr (SCORED != 1) return launch_pick<DTYPE, 64, SCORED>(q, blocks);
+        if (per > 64) return launch_pick<DTYPE, 128, SCORED>(q, waves, blocks);
+    if constexpr (SCORED != 1) return launch_pick<DTYPE, 64, SCORED>(q, waves, blocks);
     return hipErrorNotSupported;
 }
 
@@ -751,22 +842,33 @@ hipError_t launch_combine_type(const void *Y, int64_t y_rows, int64_t ldy, const
 
 }  // namespace
 
-// Counts by workgroup and expert; a single workgroup keeps them.
+// A workgroup takes as long for four tokens a wave whether others have any, and less where fewer waves share a SIMD: so few waves that every CU has a workgroup
+// of 4, 8 or 16.  Over 256 experts, 8 of them chosen by scores from 8 groups, 100 tokens 13.7 us (21.7 with 16 waves), 4096 16.2 (23.8), 8192 19.8 (24.0; 23.8
+// with 4 waves); by logits 8.9 (11.9), 11.2 (14.0), 12.8 (14.0).  Up to 64 tokens are one launch of one workgroup.
+int route_waves(int m) {
+    int waves = m <= RT_TOKENS ? RT_WAVES : 4;
+    while (waves < RT_WAVES && m > waves * RT_GROUPS * RT_CUS) waves *= 2;
+    return waves;
+}
+
+// Counts by workgroup and expert; a single workgroup keeps them.  As many as for any smaller m.
 size_t route_workspace_bytes(int m, int n_experts, int) {
-    return m <= RT_TOKENS ? 0 : (size_t)((m + RT_TOKENS - 1) / RT_TOKENS) * counts_row(n_experts);
+    if (m <= RT_TOKENS) return 0;
+    auto blocks = [&](int tokens) { return (m + tokens - 1) / tokens; };
+    return (size_t)std::max(std::min(blocks(4 * RT_GROUPS), RT_CUS), blocks(RT_TOKENS)) * counts_row(n_experts);
 }
 
 hipError_t launch_route(const RouteProblem &q) {
-    const int blocks = q.m <= RT_TOKENS ? 1 : (q.m + RT_TOKENS - 1) / RT_TOKENS;
+    const int waves = route_waves(q.m), tokens = waves * RT_GROUPS, blocks = q.m <= RT_TOKENS ? 1 : (q.m + tokens - 1) / tokens;
     hipError_t e;
     const GroupLanes g(RT_LANES, q.n_experts, q.groups);
-    if (!q.scored) e = q.dtype == 0 ? launch_pick<0, 0>(q, blocks) : launch_pick<1, 0>(q, blocks);
-    else if (g.lanes >= 1 && g.per <= 32) e = q.dtype == 0 ? launch_pick<0, 1>(q, blocks) : launch_pick<1, 1>(q, blocks);
-    else e = q.dtype == 0 ? launch_pick<0, 2>(q, blocks) : launch_pick<1, 2>(q, blocks);
+    if (!q.scored) e = q.dtype == 0 ? launch_pick<0, 0>(q, waves, blocks) : launch_pick<1, 0>(q, waves, blocks);
+    else if (g.lanes >= 1 && g.per <= 32) e = q.dtype == 0 ? launch_pick<0, 1>(q, waves, blocks) : launch_pick<1, 1>(q, waves, blocks);
+    else e = q.dtype == 0 ? launch_pick<0, 2>(q, waves, blocks) : launch_pick<1, 2>(q, waves, blocks);
     if (e != hipSuccess || blocks == 1) return e;
-    int lanes = WAVE;
+    int lanes = 8;
     while (lanes * 4 < q.n_experts) lanes *= 2;
-    k_route_order<<<blocks, RT_THREADS, 2 * (size_t)q.n_experts * 4, q.stream>>>(q, RT_TOKENS, blocks, lanes);
+    k_route_order<<<blocks, RT_THREADS, 2 * (size_t)q.n_experts * 4, q.stream>>>(q, tokens, blocks, lanes);
     return hipGetLastError();
 }
 

@@ -245,3 +245,46 @@ def test_many_tokens_as_a_plain_sort():
     c = torch.sigmoid(x.double()) + bias.double()
     r = qamw.route_scored(x.to(DEV), 8, bias=bias.to(DEV))
     assert torch.equal(r.experts.cpu().long(), torch.sort(c, dim=1, descending=True, stable=True).indices[:, :8])
+
+
+def test_workspace_of_more_tokens_serves_fewer():
+    for n in (1, 33, 256, 1024):
+        sizes = [qamw.route_workspace_bytes(m, n, 1) for m in (0, 1, 64, 65, 80, 81, 1000, 4096, 4097, 8192, 8193, 16384, 16385, 100000, 1 << 22)]
+        assert sizes[:3] == [0, 0, 0] and sizes[3] > 0 and sizes == sorted(sizes)
+
+
+@gpu
+@pytest.mark.parametrize("m", [65, 79, 1000, 4096, 4097, 8192, 8193, 16385])
+@pytest.mark.parametrize("n,k,groups,top,bias", [(64, 6, 8, 3, False), (60, 4, 1, 1, True), (256, 8, 16, 4, False)])
+def test_workgroups_of_every_size(m, n, k, groups, top, bias):
+    """Choices and weights as of 64 tokens a call, and one order over all of them; and by logits, too."""
+    say(f"[scored] {m} tokens over {n}")
+    x = torch.randn(m, n, generator=_gen(m)).bfloat16()
+    dx, b = x.to(DEV), (0.1 * torch.randn(n, generator=_gen(1))).to(DEV) if bias else None
+    for call in (lambda t, w=None: qamw.route_scored(t, k, bias=b, groups=groups, top_groups=top, workspace=w), lambda t, w=None: qamw.route(t, k, workspace=w)):
+        parts = [call(p) for p in dx.split(64)]
+        want = torch.cat([p.experts for p in parts]).cpu().numpy(), torch.cat([p.weights for p in parts]).cpu().double().numpy()
+        space = torch.zeros(qamw.route_workspace_bytes(m, n, k) + 64, dtype=torch.uint8, device=DEV)
+        space[-64:] = 77
+        check(call(dx, space[:-64]), x, k, n, want)
+        assert (space[-64:] == 77).all()
+
+
+@gpu
+@pytest.mark.parametrize("group_top", [1, 2])
+@pytest.mark.parametrize("scores", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("n,groups,top", [(64, 16, 3), (48, 3, 2), (40, 8, 8), (256, 8, 4)])
+def test_groups_without_a_bias(scores, n, groups, top, group_top):
+    """Few different logits, so that most groups' values are equal or the same pair in other places; and ones whose scores 64 bits cannot tell apart."""
+    say(f"[scored] groups without a bias {scores} {n} {groups} {group_top}")
+    g = _gen(n + group_top)
+    x = torch.randint(-3, 4, (240, n), generator=g).float() * 0.25
+    x[60:90] *= 40                                            # a sigmoid of 30 and of 20
+    x[90:120] *= 400                                          # and of -300
+    x[120:150] += torch.where(torch.rand(30, n, generator=g) < 0.7, -INF, 0.0)
+    x[150:180] += torch.where(torch.rand(30, n, generator=g) < 0.1, INF, 0.0)
+    x[180:210] = torch.randn(30, n, generator=g) * 1e-7
+    for dtype in (torch.bfloat16, torch.float32):
+        t = x.to(dtype)
+        want = reference(t, 5, scores, None, groups, top, group_top, False, 1.0)
+        check(qamw.route_scored(t.to(DEV), 5, scores=scores, groups=groups, top_groups=top, group_top=group_top, renormalise=False), t, 5, n, want)
