@@ -146,7 +146,7 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 // in a thousand tokens was in doubt, and every large call took 30 us where it takes 26 now.  Without a bias the logits order as the scores do (choose_by_logits).
 //   The weights, k a token, are in 64 bits too.
 //   Arithmetic bounds it: 16384 tokens over 256 experts in 16 groups, 8 chosen, bf16, 26 us, of which 20 are this launch: 14 the values, a third of whose
-// instructions are in 64 bits, and the comparisons, 1 the weights, 1.5 the tokens in doubt.  Without a bias 17, with 8 or 16 groups 24; every token in 64 bits 68.  More than
+// instructions are in 64 bits, and the comparisons, 1 the weights, 1.5 the tokens in doubt.  Without a bias 17, with 8 groups 23, with 16 24.5; every token in 64 bits 68.  More than
 // 16 groups, or more than 32 experts a lane, are done in 64 bits at once: 160 experts in 20 groups 41 us, 4096 tokens over 1024 experts 98.
 
 // How the groups lie on `all` lanes, a power of two for each group: 2^shift lanes of a group, none if there are more groups than lanes, and experts of a lane.
@@ -477,6 +477,7 @@ __device__ __forceinline__ bool groups_by_logits(const RouteProblem &q, const Gr
     int above = 0;
     bool certain = true;
     auto compare = [&](auto turn) {
+        if (decltype(turn)::value & (g.lanes - 1)) return;                     // no group's first lane
         auto from = [&](int v) { return dpp_move<DPP_ROW_ROTATE_8 - 8 + decltype(turn)::value>(v); };
         const double v = __hiloint2double(from(__double2hiint(value)), from(__double2loint(value)));
         const bool same = __int_as_float(from(__float_as_int(x1))) == x1 && __int_as_float(from(__float_as_int(x2))) == x2, lower = from(lane) < lane;
