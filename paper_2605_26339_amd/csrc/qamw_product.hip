@@ -144,6 +144,7 @@ struct Plan {
     bool few;
     int tile_rows, parts;
     double us;
+    bool pair;                                             // few rows: of the kernel's two forms the one with 32 outputs a wave
 };
 struct Off {
     double work, memory;                                   // times as much for rows off the 128-byte lines
@@ -157,11 +158,12 @@ constexpr Off FEW_OFF = {1.3, 1.45}, WIDE_OFF = {1.23, 1.23};
 struct Costs {
     Cost few[3], wide[3];
     double few_gated_64, few_x;                            // the first of the rate: the ring is two units then
+    double few_pair[2];                                    // more a tile of 16 and 32 rows with 32 outputs a wave
 };
-constexpr Costs BYTES = {{{16, 0.4, 9.4e4}, {32, 0.4, 9.9e4}, {64, 0.4, 8.0e4}}, {{64, 2.9, 0.72}, {128, 3.8, 0.83}, {256, 5.9, 1.12}}, 0.75, 0.45};
-// In 4 bits, with the scales beside them, of 163 shapes of 1 to 32768 rows, 1 to 128 experts, 700 to 27648 outputs and 333 to 13824 columns: the choice 1 % slower
-// than the fastest in the mean (2 % by the figures above), a fifth at worst.
-constexpr Costs MX4 = {{{16, 0.4, 8.5e4}, {32, 0.4, 9.9e4}, {64, 0.47, 5.9e4}}, {{64, 3.1, 0.63}, {128, 3.0, 0.96}, {256, 4.1, 1.12}}, 0.9, 0.6};
+constexpr Costs BYTES = {{{16, 0.4, 9.4e4}, {32, 0.4, 9.9e4}, {64, 0.4, 8.0e4}}, {{64, 2.9, 0.72}, {128, 3.8, 0.83}, {256, 5.9, 1.12}}, 0.75, 0.45, {}};
+// In 4 bits, with the scales beside them, of 163 shapes of 1 to 32768 rows, 1 to 128 experts, 700 to 27648 outputs and 333 to 13824 columns, and 218 of up to
+// 1800 rows for the pairs: the choice 1 % slower than the fastest in the mean, a fifth to a quarter at worst.
+constexpr Costs MX4 = {{{16, 0.4, 8.5e4}, {32, 0.4, 9.9e4}, {64, 0.47, 5.9e4}}, {{64, 3.1, 0.63}, {128, 3.0, 0.96}, {256, 4.1, 1.12}}, 0.9, 0.6, {0.0, 0.6}};
 
 // groups: how many have rows, at most; row tiles are expected to be half a tile short.
 Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, bool gated, int kind, bool may_part) {
@@ -184,16 +186,18 @@ Plan plan(int64_t m, int64_t groups, bool grouped, int64_t d_out, int64_t d_in, 
     auto xcds = [](double readers) { return readers < 1 ? 1 : readers > 8 ? 8 : readers; };
     const Costs &costs = kind == PRODUCT_MX4 ? MX4 : BYTES;
     Plan best = {true, 64, 1, 1e30};
-    auto offer = [&](bool few, int rows, int parts, double us) {
-        if (us < best.us) best = {few, rows, parts, us};
+    auto offer = [&](bool few, int rows, int parts, double us, bool pair = false) {
+        if (us < best.us) best = {few, rows, parts, us, pair};
     };
-    for (const Cost &c : costs.few) {
-        const double mine = row_tiles(c.rows), cols = (double)((d_out + 15) / 16), tiles = groups * mine * cols;
-        const int split = few_split((int64_t)tiles, (int)units, 4);
-        const double slot = 2048.0 * ((gated ? 2 : 1) + c.rows / 16), rate = gated && c.rows == 64 ? c.stage * costs.few_gated_64 : c.stage;
-        const double work = rounds(tiles * split / 4) * (c.tile + units * 4 / split * slot / rate);
-        offer(true, c.rows, 1, time(work, w_bytes * (1 + FEW_W * (mine - 1)) + x_bytes * costs.few_x * xcds(cols * split / 4), FEW_OFF));
-    }
+    for (const Cost &c : costs.few)
+        for (bool pair : {false, true}) {
+            if (pair && (kind != PRODUCT_MX4 || gated || c.rows == 64)) break;
+            const double mine = row_tiles(c.rows), cols = (double)(((d_out + 15) / 16 + pair) / (1 + pair)), tiles = groups * mine * cols;
+            const int split = few_split((int64_t)tiles, (int)units, 4);
+            const double slot = 2048.0 * ((gated || pair ? 2 : 1) + c.rows / 16), rate = gated && c.rows == 64 ? c.stage * costs.few_gated_64 : c.stage;
+            const double work = rounds(tiles * split / 4) * (c.tile + (pair ? costs.few_pair[c.rows / 32] : 0.0) + units * 4 / split * slot / rate);
+            offer(true, c.rows, 1, time(work, w_bytes * (1 + FEW_W * (mine - 1)) + x_bytes * costs.few_x * xcds(cols * split / 4), FEW_OFF), pair);
+        }
     const double cols = (double)((outs + 255) / 256);
     for (const Cost &c : costs.wide)
         for (int parts : {1, 2, 3, 4, 6, 8}) {
@@ -233,7 +237,7 @@ hipError_t launch_product(const Product &p) {
         return p.kind == PRODUCT_I8 ? launch_any<true>(p) : launch_any<false>(p);
     }
     const Plan c = plan_of(p.m, p.n_experts, p.offsets != nullptr, p.d_out, p.d_in, p.gated, p.kind, p.scratch != nullptr);
-    return c.few ? launch_product_few(p, c.tile_rows) : launch_product_wide(p, c.tile_rows, c.parts);
+    return c.few ? launch_product_few(p, c.tile_rows, c.pair) : launch_product_wide(p, c.tile_rows, c.parts);
 }
 
 }  // namespace qamw

@@ -57,7 +57,7 @@ struct MoreLds {
 // The kernels by what they are for.  wide and few: products that product_wide_supported(), tile_rows of 16 / 32 / 64 and 64 / 128 / 256.
 bool product_wide_supported(const Product &p);
 hipError_t launch_product_wide(const Product &p, int tile_rows, int parts);
-hipError_t launch_product_few(const Product &p, int tile_rows);
+hipError_t launch_product_few(const Product &p, int tile_rows, bool pair);   // pair: 4 bits, tiles of 16 or 32 rows, not gated: 32 rows of W a wave
 // Waves that share a tile of outputs: enough for all of memory's bandwidth, about 8 on every CU, while a share has four units.
 inline int few_split(int64_t tiles, int units, int waves) {
     int split = 1;

@@ -1,7 +1,7 @@
 // Y = X W^T for few rows: what is read of W is what it costs.  8-bit integers with scales, bf16, or 4 bits with scales of blocks, one matrix or one for
 // each expert.
 //
-// A wave has 16 rows of W (gated: 16 of the gate and the same 16 of the up projection), up to 64 rows of X and a share of the columns, in
+// A wave has 16 rows of W (gated: 16 of the gate and the same 16 of the up projection; in 4 bits 32 where there are many), up to 64 rows of X and a share of the columns, in
 // units of 128 bytes.  Units come to the wave's own ring in LDS by buffer loads that go there directly, whole 128-byte lines of
 // eight rows at a time; no barrier is needed until the waves that share rows of W add up what they have.
 //   In LDS the eight 16-byte pieces of a row are exchanged by row mod 8, against bank conflicts of the 16 lanes that read a column.
@@ -391,10 +391,14 @@ template <int KIND, bool GATED, bool YBF16, typename S> hipError_t launch(const 
     return MAY && on_lines && bytes > PF_KEPT ? launch_once<KIND, GATED, YBF16, MAY, S>(p, q, more_lds) : launch_once<KIND, GATED, YBF16, false, S>(p, q, more_lds);
 }
 
-template <int KIND, int T, int FROM, int EIGHTS> hipError_t launch_shape(const Product &p, const FewArgs &q, size_t more_lds) {
+// PAIR: 32 rows of W a wave where they are not gated: rows of X are read half as often, by half as many waves.  13824 x 5120 for 8 rows 8.6 us (11.3), 5120 x 13824
+// for 8 8.9 (10.5) and for 32 11.3 (13.6), 64 experts of 5632 x 2048 with 4 or 5 rows each 64 (83); but 4096 x 4096 for 8 rows 5.0 (4.7).  With 64 rows of X never the
+// fastest.
+template <int KIND, int T, int FROM, int EIGHTS, bool PAIR = false> hipError_t launch_shape(const Product &p, const FewArgs &q, size_t more_lds) {
     using Gated = FewShape<T, 2, FROM, EIGHTS, KIND == PRODUCT_MX4>;
-    using Plain = FewShape<T, 1, FROM, EIGHTS, KIND == PRODUCT_MX4>;
-    if (p.gated) return p.y_bf16 ? launch<KIND, true, true, Gated>(p, q, more_lds) : launch<KIND, true, false, Gated>(p, q, more_lds);
+    using Plain = FewShape<T, PAIR ? 2 : 1, FROM, EIGHTS, KIND == PRODUCT_MX4>;
+    if constexpr (!PAIR)
+        if (p.gated) return p.y_bf16 ? launch<KIND, true, true, Gated>(p, q, more_lds) : launch<KIND, true, false, Gated>(p, q, more_lds);
     return p.y_bf16 ? launch<KIND, false, true, Plain>(p, q, more_lds) : launch<KIND, false, false, Plain>(p, q, more_lds);
 }
 
@@ -407,7 +411,8 @@ template <int KIND> hipError_t launch_type(const Product &p, int tile_rows) {
 
 }  // namespace
 
-hipError_t launch_product_few(const Product &p, int tile_rows) {
+hipError_t launch_product_few(const Product &p, int tile_rows, bool pair) {
+    if (p.kind == PRODUCT_MX4 && pair) return tile_rows <= 16 ? launch_shape<PRODUCT_MX4, 1, -1, 1, true>(p, {}, 0) : launch_shape<PRODUCT_MX4, 2, -1, 1, true>(p, {}, 0);
     if (p.kind == PRODUCT_MX4) return launch_type<PRODUCT_MX4>(p, tile_rows);
     return p.kind == PRODUCT_I8 ? launch_type<PRODUCT_I8>(p, tile_rows) : launch_type<PRODUCT_BF16>(p, tile_rows);
 }

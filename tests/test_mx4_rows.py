@@ -291,6 +291,7 @@ SHAPES = [
     (1, 1, 1), (1, 17, 32), (2, 64, 100), (1, 4096, 4096), (3, 130, 1040), (8, 257, 2048), (13, 2047, 5632), (15, 33, 511), (16, 100, 512), (17, 31, 513),
     (31, 500, 272), (40, 2048, 1008), (64, 65, 4112), (65, 128, 64), (100, 700, 336), (129, 300, 1024), (200, 63, 15), (257, 513, 2065), (300, 260, 176),
     (513, 1030, 656), (700, 384, 128), (1000, 1600, 512), (33, 5, 13824), (5, 1000, 767), (300, 520, 769), (260, 256, 1280),
+    (1, 13837, 300), (8, 9001, 1100), (16, 8193, 2048), (20, 9001, 1100), (32, 5120, 3333), (45, 5130, 3333), (128, 2047, 5632),   # many outputs of few rows
 ]
 
 
@@ -420,7 +421,7 @@ def _offsets(sizes, m, g):
 @gpu
 @pytest.mark.parametrize("sizes,tokens,d_out,d_in", [
     ([1, 0, 3, 0], 5, 33, 96), ([0, 0, 0, 7], 7, 130, 512), ([2, 2, 2, 2, 2], 3, 5632, 2048), ([70, 0, 1, 64, 65], 100, 100, 333), ([300, 17, 0, 257, 1], 200, 270, 1024),
-    ([16] * 40, 64, 48, 640), ([1] * 100, 30, 64, 100), ([1000, 24], 600, 300, 1500),
+    ([16] * 40, 64, 48, 640), ([1] * 100, 30, 64, 100), ([1000, 24], 600, 300, 1500), ([5] * 16, 30, 5643, 300), ([20, 31, 32, 33, 0, 1], 40, 5650, 640),
 ])
 @pytest.mark.parametrize("gated", [False, True])
 @pytest.mark.parametrize("gather", [False, True])
