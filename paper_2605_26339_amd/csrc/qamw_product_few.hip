@@ -9,8 +9,8 @@
 // columns among waves until there are about 8 on every CU; with enough of them, memory.  Launches included: 4096 x 4096 int8 for 8 rows 6.4 us,
 // 11008 x 4096 12.1, 5120 x 13824 19.1 (3.7 TB/s); gated int8 of 8 experts of 2 x 5632 x 2048 for 10 rows 27 us; bf16 of 64 experts of
 // 1408 x 2048 with 8 rows each 70.6 us (5.2 TB/s).
-//   In 4 bits: 4096 x 4096 for 8 rows 3.8 us, 5120 x 13824 9.5 (3.7 TB/s), for 64 rows 18.5; gated, 2 x 11008 x 4096 for 16 rows 9.8 (4.6 TB/s of codes);
-// 8 experts of 2 x 5632 x 2048 for 10 rows 15.4, 64 of 1408 x 2048 with 4 or 5 rows each 21.2.  The weights are half of int8's, so that a launch's beginning
+//   In 4 bits: 4096 x 4096 for 8 rows 3.8 us, 5120 x 13824 8.1 (4.4 TB/s), for 64 rows 16.1; gated, 2 x 11008 x 4096 for 16 rows 9.9 (4.6 TB/s of codes);
+// 8 experts of 2 x 5632 x 2048 for 10 rows 15.4, 64 of 1408 x 2048 with 4 or 5 rows each 17.8.  The weights are half of int8's, so that a launch's beginning
 // and end are more of it; the scales, a byte for 16 of codes, are one load of 4 bytes a lane for two units of a fragment.
 //   Rows of X are read again for every 16 outputs, from the caches, so that many rows are dearer here than in tiles of 256 outputs; the
 // estimate that chooses has both sides.
@@ -393,7 +393,7 @@ template <int KIND, bool GATED, bool YBF16, typename S> hipError_t launch(const 
 
 // PAIR: 32 rows of W a wave where they are not gated: rows of X are read half as often, by half as many waves.  13824 x 5120 for 8 rows 8.6 us (11.3), 5120 x 13824
 // for 8 8.9 (10.5) and for 32 11.3 (13.6), 64 experts of 5632 x 2048 with 4 or 5 rows each 64 (83); but 4096 x 4096 for 8 rows 5.0 (4.7).  With 64 rows of X never the
-// fastest.
+// fastest, and gated, 32 of the gate and 32 of up, nowhere; where the launch quantises the rows 5.1 for 4.2 and 13.1 for 8.8.
 template <int KIND, int T, int FROM, int EIGHTS, bool PAIR = false> hipError_t launch_shape(const Product &p, const FewArgs &q, size_t more_lds) {
     using Gated = FewShape<T, 2, FROM, EIGHTS, KIND == PRODUCT_MX4>;
     using Plain = FewShape<T, PAIR ? 2 : 1, FROM, EIGHTS, KIND == PRODUCT_MX4>;
