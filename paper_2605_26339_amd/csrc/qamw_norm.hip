@@ -1,7 +1,7 @@
 // The norms around a block, with its gate and the scale of the stream:
 //   b' = b / sqrt(mean b^2 + eps) w_b;  h' = h + scale (gate b');  x = h' / sqrt(mean h'^2 + eps) w, of h' as it is stored.
 // Memory bounds it: h, b and a gate of every value are read once, h' and x written once.  With a norm of the block, bf16 8192 x 4096 53 us, 5.1 TB/s (83 by a
-// sweep for each sum); fp32 4001 x 5120 with a gate of every value, to 4 bits, 71.7 us, 5.4 TB/s (97); 5 x 4096 4.8 us, a launch and a row's latency; 100000 x 96
+// sweep for each sum); fp32 4001 x 5120 with a gate of every value, to 4 bits, 72.7 us, 5.3 TB/s (97); 5 x 4096 4.8 us, a launch and a row's latency; 100000 x 96
 // 22.7.  Rows that are no whole eights 72 for 8192 x 4095.
 #include "qamw_mx4.hpp"
 
@@ -11,15 +11,37 @@ namespace {
 constexpr int BN_THREADS = 256, BN_WAVES = BN_THREADS / WAVE, BN_SPAN = BN_THREADS * 8;
 constexpr int BN_HELD = 2;                                 // groups of 512 columns that a wave holds, at most
 
+// A row's sum is held in 64 bits beyond a wave, and beyond a lane where the norm is stored in more than bf16; its root and the norm's two products are
+// rounded once there.  All of a row's values take part in an error of the root, and one of 2^-24 puts some of a million values to the other side of a border of
+// their 4 bits.
+
 // The sum over the workgroup in a fixed order, the same in every lane.
-__device__ __forceinline__ float sum_of_all(float v, float *part) {
-    v = wave_add(v);
+template <bool FINE> __device__ __forceinline__ double sum_of_all(float v, double *part) {
+    const double mine = FINE ? wave_sum((double)v) : (double)wave_add(v);
     __syncthreads();
-    if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = v;
+    if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = mine;
     __syncthreads();
-    float s = 0.0f;
+    double s = 0.0;
     for (int w = 0; w < BN_WAVES; ++w) s += part[w];
     return s;
+}
+
+// 1 / sqrt(sum / d + eps) and what its first 24 bits leave: a step of Newton's from the instruction's 2^-24 or so.
+struct Root {
+    float hi, lo;
+    __device__ __forceinline__ Root(double sum, double share, float eps) {   // share: 1 / d
+        const double x = sum * share + (double)eps, y = __builtin_amdgcn_rsq(x);
+        const double r = x > 0.0 && x < (double)__builtin_inff() ? y * fma(-0.5 * x * y, y, 1.5) : y;
+        hi = (float)r;
+        lo = fabsf(hi) < __builtin_inff() ? (float)(r - (double)hi) : 0.0f;
+    }
+};
+// v r w, rounded once, or in bf16's way as it comes.
+template <bool FINE> __device__ __forceinline__ float normed_by(float v, const Root &r, float w) {
+    const float p = v * r.hi, q = p * w;
+    if (!FINE) return q;
+    const float left = fmaf(p, w, -q) + (fmaf(v, r.hi, -p) + v * r.lo) * w;
+    return fabsf(q) < __builtin_inff() ? q + left : q;
 }
 
 template <int DTYPE> __device__ __forceinline__ void load_8(const void *from, int64_t at, int there, float (&v)[8]) {
@@ -89,6 +111,11 @@ template <int LANES> __device__ __forceinline__ float lanes_add(float v) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
+template <int LANES> __device__ __forceinline__ double lanes_sum(double v) {
+    if (LANES == 64) return wave_sum(v);
+    v = wave_sum_of_16(v);
+    return LANES == 16 ? v : wave_add_16(v, v);
+}
 template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
     if (LANES == 64) return wave_max(v);
     v = quad_max(v);
@@ -103,19 +130,22 @@ template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
 template <int DTYPE, int OUT, int EIGHTS, bool RAGGED, int LANES>
 __global__ __launch_bounds__(1024) void k_block_norm_held(BlockNorm q, int waves) {
     static_assert(LANES == 64 || (EIGHTS == 1 && OUT != 3), "");               // 4 bits: a wave writes a group of scales
-    __shared__ float part[3][16];
+    constexpr bool FINE = OUT != 1;
+    __shared__ double part[2][16];
+    __shared__ uint32_t parts[16];
     using E = typename Elem<DTYPE>::type;
+    const double share = 1.0 / q.d;
     const int lane = threadIdx.x % LANES, all = blockDim.x / WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), mine = wave % waves;
     const int at_once = LANES < 64 ? (int)blockDim.x / LANES : all / waves;    // rows of a workgroup
     auto column = [&](int i) { return (i * waves + mine) * 512 + lane * 8; };
     auto there = [&](int i) { return min(8, q.d - column(i)); };
     // over the waves of a row; the workgroup has one row where there are several
     auto whole = [&](float v, int which) {
-        v = lanes_add<LANES>(v);
-        if (waves == 1) return v;
-        if (lane == 0) part[which][wave] = v;
+        const double sum = FINE && which == 1 ? lanes_sum<LANES>((double)v) : (double)lanes_add<LANES>(v);
+        if (waves == 1) return sum;
+        if (lane == 0) part[which][wave] = sum;
         __syncthreads();
-        return wave_add(lane < waves ? part[which][lane] : 0.0f);
+        return wave_sum_of_16(lane % 16 < waves ? part[which][lane % 16] : 0.0);
     };
     auto ask = [&](const void *from, int64_t at, Raw<DTYPE> (&to)[EIGHTS]) {
 #pragma unroll
@@ -160,7 +190,7 @@ __global__ __launch_bounds__(1024) void k_block_norm_held(BlockNorm q, int waves
 #pragma unroll
                     for (int k = 0; k < 8; ++k) s = fmaf(y[k], y[k], s);
                 }
-                r_block = 1.0f / sqrtf(whole(s, 0) / (float)q.d + q.eps);
+                r_block = Root(whole(s, 0), share, q.eps).hi;
                 s = 0.0f;
             }
 #pragma unroll
@@ -192,22 +222,21 @@ __global__ __launch_bounds__(1024) void k_block_norm_held(BlockNorm q, int waves
             }
         }
         ask_row(row + step);
-        const float r = 1.0f / sqrtf(whole(s, 1) / (float)q.d + q.eps);
+        const Root r(whole(s, 1), share, q.eps);
         uint32_t most = 0;
 #pragma unroll
         for (int i = 0; i < EIGHTS; ++i)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                v[i][k] = v[i][k] * r;
-                if (q.weight) v[i][k] *= w[i][k];
+                v[i][k] = normed_by<FINE>(v[i][k], r, w[i][k]);
                 if (OUT == 2) most = max(most, k < there(i) ? __float_as_uint(v[i][k]) & 0x7FFFFFFFu : 0);
             }
         if constexpr (OUT == 2) {
             most = lanes_max<LANES>(most);
             if (waves > 1) {
-                if (lane == 0) part[2][wave] = __uint_as_float(most);
+                if (lane == 0) parts[wave] = most;
                 __syncthreads();
-                most = wave_max(lane < waves ? __float_as_uint(part[2][lane]) : 0);
+                most = wave_max(lane < waves ? parts[lane] : 0);
             }
             const Quantiser z(most);
             if (lane == 0 && mine == 0) static_cast<float *>(q.x_scales)[row] = z.scale;
@@ -228,8 +257,10 @@ __global__ __launch_bounds__(1024) void k_block_norm_held(BlockNorm q, int waves
 // A workgroup has a row, a thread 8 neighbours of every BN_SPAN, in a sweep for each sum and one for the result; the caches have the row by then.
 template <int DTYPE, int OUT>
 __global__ __launch_bounds__(BN_THREADS) void k_block_norm(BlockNorm q) {
-    __shared__ float part[BN_WAVES];
+    constexpr bool FINE = OUT != 1;
+    __shared__ double part[BN_WAVES];
     __shared__ uint32_t parts[BN_WAVES];
+    const double share = 1.0 / q.d;
     const int64_t row = blockIdx.x;
     const int64_t at_h = row * q.ldh, at_b = row * q.ldb, at_g = row * q.ldg, at_o = row * q.ldho;
     float r_block = 1.0f;
@@ -239,7 +270,7 @@ __global__ __launch_bounds__(BN_THREADS) void k_block_norm(BlockNorm q) {
             load_8<DTYPE>(q.block, at_b + j, (int)min((int64_t)8, q.d - j), v);
             for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
         }
-        r_block = 1.0f / sqrtf(sum_of_all(s, part) / (float)q.d + q.eps);
+        r_block = Root(sum_of_all<false>(s, part), share, q.eps).hi;
     }
     // h' of eight columns, as it is stored
     auto stream = [&](int64_t j, int there, float (&v)[8]) {
@@ -265,16 +296,13 @@ __global__ __launch_bounds__(BN_THREADS) void k_block_norm(BlockNorm q) {
         if (q.block) store_8<DTYPE>(q.h_out, at_o + j, there, v);
         for (int i = 0; i < 8; ++i) s = fmaf(v[i], v[i], s);
     }
-    const float r = 1.0f / sqrtf(sum_of_all(s, part) / (float)q.d + q.eps);
+    const Root r(sum_of_all<FINE>(s, part), share, q.eps);
     auto normed = [&](int64_t j, int there, float (&v)[8]) {
         float w[8];
         if (q.block) load_8<DTYPE>(q.h_out, at_o + j, there, v);   // this thread's own stores
         else load_8<DTYPE>(q.h, at_h + j, there, v);
         if (q.weight) load_8<0>(q.weight, j, there, w);
-        for (int i = 0; i < 8; ++i) {
-            v[i] = v[i] * r;
-            if (q.weight) v[i] *= w[i];
-        }
+        for (int i = 0; i < 8; ++i) v[i] = normed_by<FINE>(v[i], r, q.weight ? w[i] : 1.0f);
     };
     uint32_t most = 0;
     if (OUT == 2) {
