@@ -12,8 +12,8 @@ constexpr int BN_THREADS = 256, BN_WAVES = BN_THREADS / WAVE, BN_SPAN = BN_THREA
 constexpr int BN_HELD = 2;                                 // groups of 512 columns that a wave holds, at most
 
 // A row's sum is held in 64 bits beyond a wave, and beyond a lane where the norm is stored in more than bf16; its root and the norm's two products are
-// rounded once there.  All of a row's values take part in an error of the root, and one of 2^-24 puts some of a million values to the other side of a border of
-// their 4 bits.
+// rounded once there.  All of a row's values take part in an error of the root, and one of 2^-24 puts one of some ten million
+// values to the other side of a border of its 4 bits.
 
 // The sum over the workgroup in a fixed order, the same in every lane.
 template <bool FINE> __device__ __forceinline__ double sum_of_all(float v, double *part) {
