@@ -147,7 +147,7 @@ __device__ __forceinline__ void pick(const RouteProblem &q, int64_t t, int (&exp
 //   The weights, k a token, are in 64 bits too.
 //   Arithmetic bounds it: 16384 tokens over 256 experts in 16 groups, 8 chosen, bf16, 26 us, of which 20 are this launch: 14 the values, a third of whose
 // instructions are in 64 bits, and the comparisons, 1 the weights, 1.5 the tokens in doubt.  Without a bias 17, with 8 groups 23, with 16 24.5; every token in 64 bits 68.  More than
-// 16 groups, or more than 32 experts a lane, are done in 64 bits at once: 160 experts in 20 groups 41 us, 4096 tokens over 1024 experts 98.
+// 16 groups, or more than 32 experts a lane, are done in 64 bits at once: 160 experts in 20 groups 41 us, 4096 tokens over 1024 experts 59.
 
 // How the groups lie on `all` lanes, a power of two for each group: 2^shift lanes of a group, none if there are more groups than lanes, and experts of a lane.
 struct GroupLanes {
